@@ -231,6 +231,89 @@ int mosaic_bsa_rope(const mosaic_bsa_params *p, const void *q, const void *k, co
 int mosaic_bsa_select_static(const mosaic_bsa_params *p, const void *q, const void *k, int32_t *block_idx,
                              void *cuda_stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------
+ * Operators on token sequences: positions are token indices instead of points of a grid.
+ *
+ * Rules beyond the common ones above
+ *   - A tensor [B, heads, tokens, d] comes as a mosaic_view: base pointer and the strides, in elements, between batch
+ *     members, heads and tokens; the d channels of a row are contiguous.  [B, heads, tokens, d] and [B, tokens, heads, d]
+ *     in memory are both views, slices of a larger tensor too.  Base and strides are multiples of 16 bytes (the stride
+ *     of an extent of one is not looked at); strides are not negative; rows of an output do not overlap.
+ *   - Tensors are bf16, binary16 with MOSAIC_FLAG_FP16, or (rotation and norms only) fp32 with MOSAIC_FLAG_FP32.
+ *   - H % Hkv == 0; query head h belongs to key/value head h / (H / Hkv).
+ */
+typedef struct mosaic_view {
+  void *data;
+  int64_t sb, sh, sn; /* strides in elements between batch members, heads, tokens */
+} mosaic_view;
+
+#define MOSAIC_FLAG_FP32 4u       /* tensors are fp32 */
+#define MOSAIC_FLAG_HALF_PAIRS 8u /* rotation turns the pairs (i, i + rot_dim/2) instead of (2i, 2i+1) */
+#define MOSAIC_FLAG_INVERSE 16u   /* rotation by the negated angles: the transpose, what a backward applies */
+
+/*
+ * Rotary position embedding of queries and keys by token index, and root-mean-square norms of their heads.
+ *   rotation   channels c < rot_dim of a row turn in rot_dim/2 pairs; pair i of the token at position p by the angle
+ *              p * freqs[i]: (x, y) -> amplitude * (x cos - y sin, x sin + y cos); channels from rot_dim on pass through
+ *   norm       y_c = x_c * w_c / sqrt(mean(x^2) + eps) over the d channels of a row, before the rotation
+ * Angles are taken and reduced in fp64, cosines, sums and products in fp32, one rounding to the storage type at the end.
+ * Any position whose angle fp64 holds; negative ones too.
+ */
+typedef struct mosaic_rotary_params {
+  int32_t B, H, Hkv, N; /* batch, query heads, key heads, tokens                                           */
+  int32_t d;            /* channels of a head: a multiple of 16, at most 256                               */
+  int32_t rot_dim;      /* channels that turn: even, at most d; a multiple of 16 with MOSAIC_FLAG_HALF_PAIRS;
+                           0: none (norms alone)                                                          */
+  uint32_t flags;       /* MOSAIC_FLAG_FP16 or _FP32, _HALF_PAIRS, _INVERSE (rotation alone)               */
+  float amplitude;      /* factor of the turned channels (long-context scalings use one); 0 means 1        */
+  float eps;            /* of the norm, >= 0                                                               */
+} mosaic_rotary_params;
+
+/* Frequencies of the turned pairs, radians per position, on the HOST (a program makes them once and copies them over):
+ * kind MOSAIC_ROTARY_PLAIN   f_i = theta^(-2i/rot_dim)
+ *      MOSAIC_ROTARY_LINEAR  f_i / factor (positions interpolated)
+ *      MOSAIC_ROTARY_BASE    theta * factor^(rot_dim/(rot_dim-2)) in theta's place: the slowest pair is slowed by the factor
+ *      MOSAIC_ROTARY_PARTS   f_i (1 - t) + f_i/factor t, t a ramp over the pair index from the pair that turns `fast` times
+ *                            in `length` positions (rounded down) to the one that turns `slow` times (rounded up)
+ *      MOSAIC_ROTARY_BANDS   f_i t + f_i/factor (1 - t), t a ramp over the number of turns in `length` positions, 0 at
+ *                            `slow` and 1 at `fast`
+ * Returns MOSAIC_E_INVALID_ARG where a number is out of its range (rot_dim odd or < 2, theta <= 1, factor < 1; for the
+ * last two kinds length <= 0 or not 0 < slow < fast). */
+enum { MOSAIC_ROTARY_PLAIN = 0, MOSAIC_ROTARY_LINEAR = 1, MOSAIC_ROTARY_BASE = 2, MOSAIC_ROTARY_PARTS = 3,
+       MOSAIC_ROTARY_BANDS = 4 };
+typedef struct mosaic_rotary_scaling {
+  int32_t kind, rot_dim;
+  double theta, factor, length, fast, slow;
+} mosaic_rotary_scaling;
+int mosaic_bsa_rotary_freqs(const mosaic_rotary_scaling *s, double *freqs_host);
+
+/* The rotation.
+ *   q [B,H,N,d], k [B,Hkv,N,d]  in
+ *   pos         in   int64 positions; token n of batch member b has pos[b * pos_stride + n] (pos_stride 0: shared by all)
+ *   freqs       in   [rot_dim/2] fp64 on the device
+ *   q_out, k_out  out  (may be q, k themselves)
+ * No workspace. */
+int mosaic_bsa_rotary(const mosaic_rotary_params *p, const mosaic_view *q, const mosaic_view *k, const int64_t *pos,
+                      int64_t pos_stride, const double *freqs, const mosaic_view *q_out, const mosaic_view *k_out,
+                      void *cuda_stream);
+
+/* Norm and rotation in one pass over Q and K.  wq, wk [d] fp32: weights, shared by all heads.  With rot_dim 0 pos and freqs
+ * are not read and may be NULL. */
+int mosaic_bsa_qk_norm(const mosaic_rotary_params *p, const mosaic_view *q, const mosaic_view *k, const float *wq,
+                       const float *wk, const int64_t *pos, int64_t pos_stride, const double *freqs,
+                       const mosaic_view *q_out, const mosaic_view *k_out, void *cuda_stream);
+
+/* Backward of mosaic_bsa_qk_norm: takes the forward's inputs and the gradients of its outputs (d_q_out, d_k_out).
+ *   dq, dk        out  gradients of q and k, in the storage type (may be d_q_out, d_k_out themselves)
+ *   dwq, dwk      out  [d] fp32, summed over batch, heads and tokens in a fixed order
+ *   ws            mosaic_bsa_qk_norm_workspace_bytes(p) bytes, 256-byte aligned (0 on invalid params) */
+size_t mosaic_bsa_qk_norm_workspace_bytes(const mosaic_rotary_params *p);
+int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params *p, const mosaic_view *q, const mosaic_view *k, const float *wq,
+                           const float *wk, const int64_t *pos, int64_t pos_stride, const double *freqs,
+                           const mosaic_view *d_q_out, const mosaic_view *d_k_out, const mosaic_view *dq,
+                           const mosaic_view *dk, float *dwq, float *dwk, void *ws, size_t ws_bytes, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.
  * Every op resets the word when it starts. */

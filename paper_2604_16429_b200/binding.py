@@ -20,10 +20,14 @@ _lib = None
 OP_SELECT, OP_FWD, OP_BWD, OP_FWD_BRANCHES, OP_BWD_BRANCHES = 0, 1, 2, 3, 4
 EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", "mosaic_bsa_bwd",
            "mosaic_bsa_last_status", "mosaic_bsa_strerror", "mosaic_bsa_select_static",
-           "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope")
+           "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
+           "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
+           "mosaic_bsa_qk_norm_bwd")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
+FLAG_FP32, FLAG_HALF_PAIRS, FLAG_INVERSE = 4, 8, 16
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS, ROTARY_BANDS = 0, 1, 2, 3, 4
 
 
 class MosaicError(RuntimeError):
@@ -37,6 +41,22 @@ class _Params(ctypes.Structure):
                 ("d", ctypes.c_int32), ("bh", ctypes.c_int32), ("bw", ctypes.c_int32),
                 ("rlat", ctypes.c_int32), ("rlon", ctypes.c_int32), ("topk", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32), ("Hkv", ctypes.c_int32)]
+
+
+class _View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("sb", ctypes.c_int64), ("sh", ctypes.c_int64), ("sn", ctypes.c_int64)]
+
+
+class _RotaryParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("amplitude", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _RotaryScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("theta", ctypes.c_double),
+                ("factor", ctypes.c_double), ("length", ctypes.c_double), ("fast", ctypes.c_double),
+                ("slow", ctypes.c_double)]
 
 
 @dataclass(frozen=True)
@@ -103,6 +123,18 @@ def lib():
         L.mosaic_bsa_rope.argtypes = [pp, vp, vp, fp, ctypes.c_float, vp, vp, vp]
         L.mosaic_bsa_bwd.restype = ctypes.c_int
         L.mosaic_bsa_bwd.argtypes = [pp, vp, vp, vp, vp, fp, vp, i32p, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        vw, rp = ctypes.POINTER(_View), ctypes.POINTER(_RotaryParams)
+        L.mosaic_bsa_rotary_freqs.restype = ctypes.c_int
+        L.mosaic_bsa_rotary_freqs.argtypes = [ctypes.POINTER(_RotaryScaling), vp]
+        L.mosaic_bsa_rotary.restype = ctypes.c_int
+        L.mosaic_bsa_rotary.argtypes = [rp, vw, vw, vp, ctypes.c_int64, vp, vw, vw, vp]
+        L.mosaic_bsa_qk_norm.restype = ctypes.c_int
+        L.mosaic_bsa_qk_norm.argtypes = [rp, vw, vw, fp, fp, vp, ctypes.c_int64, vp, vw, vw, vp]
+        L.mosaic_bsa_qk_norm_workspace_bytes.restype = ctypes.c_size_t
+        L.mosaic_bsa_qk_norm_workspace_bytes.argtypes = [rp]
+        L.mosaic_bsa_qk_norm_bwd.restype = ctypes.c_int
+        L.mosaic_bsa_qk_norm_bwd.argtypes = [rp, vw, vw, fp, fp, vp, ctypes.c_int64, vp, vw, vw, vw, vw, fp, fp, vp,
+                                             ctypes.c_size_t, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -289,3 +321,179 @@ def from_bits(bits, device="cuda", f16=False) -> torch.Tensor:
 
 def default_scale(d: int) -> float:
     return 1.0 / math.sqrt(d)
+
+
+# ---- operators on token sequences: strided tensors [B, heads, tokens, d] ---------------------------------------------
+_STORAGE = {torch.bfloat16: 0, torch.float16: FLAG_FP16, torch.float32: FLAG_FP32}
+
+
+@dataclass(frozen=True)
+class RotaryParams:
+    """What a model fixes of its rotary positions (the sizes come from the tensors)."""
+    d: int
+    rot_dim: int = -1          # channels that turn, -1: all of them
+    half: bool = False         # pairs (i, i + rot_dim/2) instead of (2i, 2i+1)
+    amplitude: float = 1.0     # factor of the turned channels
+    theta: float = 10000.0     # the rest is what `rotary_freqs` reads
+    scaling: int = ROTARY_PLAIN
+    factor: float = 1.0
+    length: float = 0.0        # positions the model was trained on (ROTARY_PARTS, ROTARY_BANDS)
+    fast: float = 32.0
+    slow: float = 1.0
+
+    @property
+    def rot(self): return self.d if self.rot_dim < 0 else self.rot_dim
+
+
+def rotary_freqs(rp: RotaryParams, device="cuda") -> torch.Tensor:
+    """Radians per position of the turned pairs, [rot_dim/2] fp64 on `device`: made once, passed to every call."""
+    out = torch.empty(max(rp.rot // 2, 1), dtype=torch.float64)
+    sc = _RotaryScaling(rp.scaling, rp.rot, rp.theta, rp.factor, rp.length, rp.fast, rp.slow)
+    rc = lib().mosaic_bsa_rotary_freqs(ctypes.byref(sc), out.data_ptr())
+    if rc:
+        raise MosaicError(rc, "mosaic_bsa_rotary_freqs")
+    return out.to(device)
+
+
+def _chk_view(name, t, shape, like):
+    """`t` as a strided tensor of `shape` with contiguous rows, of `like`'s type and device."""
+    if t.dtype != like.dtype or t.device != like.device or t.shape != shape or t.stride(3) != 1:
+        raise ValueError(f"{name}: expected {like.dtype} {tuple(shape)} on {like.device} with contiguous rows, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
+    sb, sh, sn, _ = t.stride()
+    return _View(t.data_ptr(), sb, sh, sn)
+
+
+def _chk_out(name, t, shape, like):
+    """The same for an output, which may not write a place twice."""
+    v = _chk_view(name, t, shape, like)
+    if any(st == 0 and n > 1 for st, n in zip(t.stride(), shape)):
+        raise ValueError(f"{name}: rows of an output may not overlap, got strides {t.stride()}")
+    return v
+
+
+def _chk_seq(q, k):
+    """Shapes of q [B,H,N,d] and k [B,Hkv,Nk,d]; (B, H, Hkv)."""
+    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda or q.dtype not in _STORAGE:
+        raise ValueError(f"expected cuda tensors [B, heads, tokens, d] in bf16, fp16 or fp32, got {q.dtype} {tuple(q.shape)} on "
+                         f"{q.device} and {tuple(k.shape)}")
+    return q.shape[0], q.shape[1], k.shape[1]
+
+
+class _Launch:
+    """The stream of a call on the tensors' own device, which is made current for the call; what the call allocates is kept
+    from being handed out again before that stream has passed it."""
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.new = device, stream, []
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors are on {device}")
+
+    def empty(self, shape, dtype):
+        return self.keep(torch.empty(shape, dtype=dtype, device=self.device))
+
+    def keep(self, t):
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t
+
+    def call(self, name, *args):
+        fn, index = getattr(lib(), name), self.device.index
+        if torch.cuda.current_device() == index:
+            rc = fn(*args, self.raw())
+        else:
+            with torch.cuda.device(index):
+                rc = fn(*args, self.raw())
+        if rc:
+            raise MosaicError(rc, name)
+
+    def raw(self):
+        return torch.cuda.current_stream(self.device).cuda_stream if self.stream is None else self.stream.cuda_stream
+
+
+def _rotary_params(rp, q, k, flags, eps):
+    B, H, Hkv = _chk_seq(q, k)
+    return _RotaryParams(B, H, Hkv, q.shape[2], rp.d, rp.rot, _STORAGE[q.dtype] | (FLAG_HALF_PAIRS if rp.half else 0) | flags,
+                         rp.amplitude, eps)
+
+
+def _chk_pos(rp, q, pos, freqs):
+    """(pointer, stride) of the positions, and the frequencies' pointer."""
+    if rp.rot == 0:
+        return 0, 0, 0
+    B, N = q.shape[0], q.shape[2]
+    if (pos.dtype != torch.int64 or pos.device != q.device or tuple(pos.shape) not in ((N,), (B, N))
+            or (N > 1 and pos.stride(-1) != 1)):
+        raise ValueError(f"expected int64 positions [{N}] or [{B},{N}] on {q.device}, got {pos.dtype} {tuple(pos.shape)}")
+    if freqs.dtype != torch.float64 or freqs.device != q.device or not freqs.is_contiguous() or tuple(freqs.shape) != (rp.rot // 2,):
+        raise ValueError(f"expected fp64 frequencies [{rp.rot // 2}] on {q.device}, got {freqs.dtype} {tuple(freqs.shape)}")
+    return pos.data_ptr(), pos.stride(0) if pos.dim() == 2 and B > 1 else 0, freqs.data_ptr()
+
+
+def _chk_weights(rp, q, *ws):
+    for w in ws:
+        if w.dtype != torch.float32 or w.device != q.device or not w.is_contiguous() or tuple(w.shape) != (rp.d,):
+            raise ValueError(f"expected contiguous fp32 weights [{rp.d}] on {q.device}, got {w.dtype} {tuple(w.shape)}")
+
+
+def _rotary_shapes(rp, q, k):
+    return (q.shape[0], q.shape[1], q.shape[2], rp.d), (q.shape[0], k.shape[1], q.shape[2], rp.d)
+
+
+def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=None, k_out=None, stream=None):
+    """Rotary positions of q [B,H,N,d] and k [B,Hkv,N,d] by token index; pos [N] or [B,N] int64, freqs from `rotary_freqs`.
+    `inverse` turns back (the transpose: what a backward applies to the gradients).  Returns (q_out, k_out)."""
+    p = _rotary_params(rp, q, k, FLAG_INVERSE if inverse else 0, 0.0)
+    sq, sk = _rotary_shapes(rp, q, k)
+    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
+    at, step, fr = _chk_pos(rp, q, pos, freqs)
+    run = _Launch(q.device, stream)
+    q_out = run.keep(torch.empty_like(q)) if q_out is None else q_out
+    k_out = run.keep(torch.empty_like(k)) if k_out is None else k_out
+    run.call("mosaic_bsa_rotary", p, vq, vk, at, step, fr, _chk_out("q_out", q_out, sq, q), _chk_out("k_out", k_out, sk, q))
+    return q_out, k_out
+
+
+def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps=1e-6, q_out=None, k_out=None, stream=None):
+    """Root-mean-square norm of every head of q and k (weights wq, wk [d] fp32), then the rotation, in one pass; with
+    rp.rot_dim 0 the norm alone.  Returns (q_out, k_out)."""
+    p = _rotary_params(rp, q, k, 0, eps)
+    sq, sk = _rotary_shapes(rp, q, k)
+    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
+    at, step, fr = _chk_pos(rp, q, pos, freqs)
+    _chk_weights(rp, q, wq, wk)
+    run = _Launch(q.device, stream)
+    q_out = run.keep(torch.empty_like(q)) if q_out is None else q_out
+    k_out = run.keep(torch.empty_like(k)) if k_out is None else k_out
+    run.call("mosaic_bsa_qk_norm", p, vq, vk, wq.data_ptr(), wk.data_ptr(), at, step, fr, _chk_out("q_out", q_out, sq, q),
+             _chk_out("k_out", k_out, sk, q))
+    return q_out, k_out
+
+
+def qk_norm_workspace_bytes(rp: RotaryParams, q, k) -> int:
+    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_rotary_params(rp, q, k, 0, 0.0)))
+
+
+def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, d_k_out, eps=1e-6, dq=None, dk=None, dwq=None,
+                           dwk=None, ws=None, stream=None):
+    """Backward of mosaic_bsa_qk_norm from its inputs and its outputs' gradients.  Returns (dq, dk, dwq, dwk); the weights'
+    gradients are [d] fp32."""
+    p = _rotary_params(rp, q, k, 0, eps)
+    sq, sk = _rotary_shapes(rp, q, k)
+    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
+    gq, gk = _chk_view("d_q_out", d_q_out, sq, q), _chk_view("d_k_out", d_k_out, sk, q)
+    at, step, fr = _chk_pos(rp, q, pos, freqs)
+    run = _Launch(q.device, stream)
+    dq = run.keep(torch.empty_like(q)) if dq is None else dq
+    dk = run.keep(torch.empty_like(k)) if dk is None else dk
+    dwq = run.empty((rp.d,), torch.float32) if dwq is None else dwq
+    dwk = run.empty((rp.d,), torch.float32) if dwk is None else dwk
+    _chk_weights(rp, q, wq, wk, dwq, dwk)
+    if ws is None:
+        n = int(lib().mosaic_bsa_qk_norm_workspace_bytes(p))
+        if n == 0:
+            raise MosaicError(-1, "mosaic_bsa_qk_norm_workspace_bytes")
+        ws = run.empty((n,), torch.uint8)
+    run.call("mosaic_bsa_qk_norm_bwd", p, vq, vk, wq.data_ptr(), wk.data_ptr(), at, step, fr, gq, gk, _chk_out("dq", dq, sq, q),
+             _chk_out("dk", dk, sk, q), dwq.data_ptr(), dwk.data_ptr(), ws.data_ptr(), ws.numel())
+    return dq, dk, dwq, dwk

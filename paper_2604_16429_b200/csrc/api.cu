@@ -47,6 +47,17 @@ int validate(const mosaic_bsa_params* p, Geo* g) {
   return MOSAIC_OK;
 }
 
+int device_ok() {
+  static int cached[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return MOSAIC_E_CUDA;
+  if (dev < 64 && cached[dev]) return cached[dev] > 0 ? MOSAIC_OK : MOSAIC_E_UNSUPPORTED;
+  int major = 0;
+  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return MOSAIC_E_CUDA;
+  if (dev < 64) cached[dev] = major == 10 ? 1 : -1;
+  return major == 10 ? MOSAIC_OK : MOSAIC_E_UNSUPPORTED;
+}
+
 SelectWs select_layout(const Geo& g) {
   SelectWs w;
   const size_t pooled = align256(sizeof(float) * (size_t)g.U * g.m * kD), norms = align256(sizeof(float) * (size_t)g.U * g.m);
@@ -118,17 +129,6 @@ PoolArgs branch_pool(const Geo& g, const void* q, const void* k, const void* v, 
 size_t select_total(const Geo& g) { return select_layout(g).total; }
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int device_ok() {
-  static int cached[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return MOSAIC_E_CUDA;
-  if (dev < 64 && cached[dev]) return cached[dev] > 0 ? MOSAIC_OK : MOSAIC_E_UNSUPPORTED;
-  int major = 0;
-  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return MOSAIC_E_CUDA;
-  if (dev < 64) cached[dev] = major == 10 ? 1 : -1;
-  return major == 10 ? MOSAIC_OK : MOSAIC_E_UNSUPPORTED;
-}
 
 // Clears the status block.  A memset there ended the overlap of launches: a pass over 2048 tokens 40.4 against 38.0 us.
 __global__ void reset_kernel(int* status) { status[threadIdx.x + await_stream()] = 0; }
