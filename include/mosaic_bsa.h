@@ -314,6 +314,37 @@ int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params *p, const mosaic_view *q, 
                            const mosaic_view *d_q_out, const mosaic_view *d_k_out, const mosaic_view *dq,
                            const mosaic_view *dk, float *dwq, float *dwk, void *ws, size_t ws_bytes, void *cuda_stream);
 
+/*
+ * Causal attention inside a sliding window whose first tokens stay visible (the sliding-window branch of the paper's
+ * "Native Sparse Attention" section, with sink tokens): the row at position p sees the keys j <= p with p - j < window or
+ * j < sinks, under one softmax.
+ *   Nq, Nk      rows of q (and o) and of k, v.  A batch member's first q_len[b] and k_len[b] of them exist (int32 on the
+ *               device; NULL: all).  Its queries are its last tokens: row i has position k_len[b] - q_len[b] + i, so q_len =
+ *               k_len is a whole sequence and q_len < k_len a chunk behind what a cache holds.  Lengths outside
+ *               [0, Nq], [0, Nk] are clamped to it.
+ *   A row that sees nothing (k_len 0, or more queries than keys) gives o = 0, lse = -inf and no gradient.
+ *   Rows of o, lse, dq from q_len[b] on and of dk, dv from k_len[b] on are left as they were, and what q, k, v, o, lse, d_o
+ *   hold there is never used.  Rows below are expected finite: a value that is not spreads to the rows that see it, and may
+ *   spread to rows near them that do not.
+ */
+typedef struct mosaic_window_params {
+  int32_t B, H, Hkv, Nq, Nk;
+  int32_t d;       /* 64 or 128                                                                   */
+  int32_t window;  /* >= 1; Nk or more is plain causal attention                                  */
+  int32_t sinks;   /* 0 .. 128                                                                    */
+  float scale;     /* softmax scale; <= 0 means 1/sqrt(d)                                         */
+  uint32_t flags;  /* 0, MOSAIC_FLAG_FP16; decode also MOSAIC_FLAG_ROLLING                        */
+} mosaic_window_params;
+
+/* Bytes of workspace of the forward (MOSAIC_OP_FWD) and the backward (MOSAIC_OP_BWD); 0 on invalid params.  The first 256
+ * bytes are the status block, as for the block-sparse calls. */
+size_t mosaic_bsa_window_workspace_bytes(const mosaic_window_params *p, int op);
+
+/* Forward: q [B,H,Nq,d], k, v [B,Hkv,Nk,d] in; o like q, lse [B,H,Nq] fp32 (natural log, contiguous) out. */
+int mosaic_bsa_window_fwd(const mosaic_window_params *p, const mosaic_view *q, const mosaic_view *k, const mosaic_view *v,
+                          const int32_t *q_len, const int32_t *k_len, const mosaic_view *o, float *lse, void *ws,
+                          size_t ws_bytes, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.
  * Every op resets the word when it starts. */

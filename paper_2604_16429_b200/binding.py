@@ -22,7 +22,7 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_last_status", "mosaic_bsa_strerror", "mosaic_bsa_select_static",
            "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
-           "mosaic_bsa_qk_norm_bwd")
+           "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
@@ -57,6 +57,12 @@ class _RotaryScaling(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("theta", ctypes.c_double),
                 ("factor", ctypes.c_double), ("length", ctypes.c_double), ("fast", ctypes.c_double),
                 ("slow", ctypes.c_double)]
+
+
+class _WindowParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Nq", ctypes.c_int32),
+                ("Nk", ctypes.c_int32), ("d", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 @dataclass(frozen=True)
@@ -135,6 +141,11 @@ def lib():
         L.mosaic_bsa_qk_norm_bwd.restype = ctypes.c_int
         L.mosaic_bsa_qk_norm_bwd.argtypes = [rp, vw, vw, fp, fp, vp, ctypes.c_int64, vp, vw, vw, vw, vw, fp, fp, vp,
                                              ctypes.c_size_t, vp]
+        wp = ctypes.POINTER(_WindowParams)
+        L.mosaic_bsa_window_workspace_bytes.restype = ctypes.c_size_t
+        L.mosaic_bsa_window_workspace_bytes.argtypes = [wp, ctypes.c_int]
+        L.mosaic_bsa_window_fwd.restype = ctypes.c_int
+        L.mosaic_bsa_window_fwd.argtypes = [wp, vw, vw, vw, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -497,3 +508,60 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     run.call("mosaic_bsa_qk_norm_bwd", p, vq, vk, wq.data_ptr(), wk.data_ptr(), at, step, fr, gq, gk, _chk_out("dq", dq, sq, q),
              _chk_out("dk", dk, sk, q), dwq.data_ptr(), dwk.data_ptr(), ws.data_ptr(), ws.numel())
     return dq, dk, dwq, dwk
+
+
+@dataclass(frozen=True)
+class WindowParams:
+    """Sliding-window attention: the row at position p sees the keys j <= p with p - j < window or j < sinks."""
+    window: int
+    sinks: int = 0
+    scale: float = 0.0       # <= 0: 1/sqrt(d)
+    rolling: bool = False    # decode: the cache keeps the sinks and, in turn, the last positions that fit behind them
+
+
+def _window_params(wp, q, k, flags=0):
+    B, H, Hkv = _chk_seq(q, k)
+    if q.dtype == torch.float32:
+        raise ValueError("window attention takes bf16 or fp16 tensors")
+    return _WindowParams(B, H, Hkv, q.shape[2], k.shape[2], q.shape[3], wp.window, wp.sinks, wp.scale, _STORAGE[q.dtype] | flags)
+
+
+def window_workspace_bytes(wp: WindowParams, q, k, op: int) -> int:
+    return int(lib().mosaic_bsa_window_workspace_bytes(_window_params(wp, q, k), op))
+
+
+def _window_ws(p, op, run, ws):
+    if ws is not None:
+        return ws
+    n = int(lib().mosaic_bsa_window_workspace_bytes(p, op))
+    if n == 0:
+        raise MosaicError(-1, "mosaic_bsa_window_workspace_bytes")
+    return run.empty((n,), torch.uint8)
+
+
+def _chk_len(name, t, q):
+    if t is None:
+        return 0
+    if t.dtype != torch.int32 or t.device != q.device or not t.is_contiguous() or tuple(t.shape) != (q.shape[0],):
+        raise ValueError(f"{name}: expected contiguous int32 [{q.shape[0]}] on {q.device}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _chk_lse(t, q):
+    if t.dtype != torch.float32 or t.device != q.device or not t.is_contiguous() or t.shape != q.shape[:3]:
+        raise ValueError(f"lse: expected contiguous fp32 {tuple(q.shape[:3])} on {q.device}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=None, lse=None, ws=None, stream=None):
+    """Forward of the sliding-window attention: q [B,H,Nq,d], k and v [B,Hkv,Nk,d]; the first q_len[b] and k_len[b] rows of a
+    batch member exist (None: all), its queries are its last tokens.  Returns (o, lse)."""
+    p = _window_params(wp, q, k)
+    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
+    run = _Launch(q.device, stream)
+    o = run.keep(torch.empty_like(q)) if o is None else o
+    lse = run.empty(q.shape[:3], torch.float32) if lse is None else lse
+    ws = _window_ws(p, OP_FWD, run, ws)
+    run.call("mosaic_bsa_window_fwd", p, vq, vk, vv, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
+             _chk_out("o", o, q.shape, q), _chk_lse(lse, q), ws.data_ptr(), ws.numel())
+    return o, lse

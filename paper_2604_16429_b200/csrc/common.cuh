@@ -149,8 +149,13 @@ struct HostCtx {
 int validate(const mosaic_bsa_params* p, Geo* g);
 // Whether the current device is one that the kernels are built for.
 int device_ok();
-// A tensor [B, heads, N, d] of `size`-byte elements: its strides in bytes (those of extents of one are zero).
-int check_view(const mosaic_view* v, int B, int heads, int N, int size, long long* sb, long long* sh, long long* sn);
+// A tensor [B, heads, N, d] with its strides in bytes (those of extents of one are zero); check_view takes it from the
+// caller's view of `size`-byte elements.
+struct View {
+  char* data;
+  long long sb, sh, sn;
+};
+int check_view(const mosaic_view* v, int B, int heads, int N, int size, View* out);
 // Current device, its SM count (cached), and the opt-in to `smem` bytes of dynamic shared memory for `func`
 // (set once per device; `done` is the caller's per-kernel bit set of devices already configured).
 int launch_setup(const void* func, size_t smem, unsigned long long* done, int* sms);

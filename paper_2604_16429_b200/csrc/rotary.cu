@@ -25,9 +25,8 @@ constexpr int kAhead = 4;      // rows a lane group has in flight (forward)
 constexpr int kAheadBwd = 2;   // the same in the backward, where a row comes with its gradient
 
 struct HeadTensor {
-  const char *x, *g;  // input; gradient of the output (backward)
-  char* y;            // output, or gradient of the input
-  long long xb, xh, xn, gb, gh, gn, yb, yh, yn;  // byte strides
+  View x, g;  // input; gradient of the output (backward)
+  View y;     // output, or gradient of the input
   const float* w;
   int heads;
 };
@@ -156,8 +155,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
     const HeadTensor& t = a.t[i];
     int r0, r1;
     rows_of(t.heads, part, a.parts, r0, r1);
-    const char* x = t.x + b * t.xb + n * t.xn;
-    char* y = t.y + b * t.yb + n * t.yn;
+    const char* x = t.x.data + b * t.x.sb + n * t.x.sn;
+    char* y = t.y.data + b * t.y.sb + n * t.y.sn;
     float wa[V], wb[V];
     if constexpr (NORM) load_weights<V>(t.w, pl, wa, wb);
     for (int r = r0 + pl.group; r - pl.group < r1; r += pl.groups * kAhead) {  // (the same trips for the whole warp)
@@ -167,8 +166,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
         const int h = r + k * pl.groups;
         va[k] = vb[k] = make_uint4(0u, 0u, 0u, 0u);
         if (h < r1 && pl.on) {
-          va[k] = *reinterpret_cast<const uint4*>(x + h * t.xh + pl.ca * SZ);
-          vb[k] = *reinterpret_cast<const uint4*>(x + h * t.xh + pl.cb * SZ);
+          va[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.ca * SZ);
+          vb[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.cb * SZ);
         }
       }
 #pragma unroll
@@ -191,8 +190,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
         }
         turn<V, HALF>(fa, fb, c, s);
         if (h < r1 && pl.on) {
-          *reinterpret_cast<uint4*>(y + h * t.yh + pl.ca * SZ) = narrow<T>(fa);
-          *reinterpret_cast<uint4*>(y + h * t.yh + pl.cb * SZ) = narrow<T>(fb);
+          *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.ca * SZ) = narrow<T>(fa);
+          *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.cb * SZ) = narrow<T>(fb);
         }
       }
     }
@@ -222,8 +221,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_bwd_kernel(const __grid_con
       rows_of(t.heads, (int)(task - token * a.parts), a.parts, r0, r1);
       float c[V], s[V];
       make_angles<V>(a, a.rot ? __ldg(a.pos + b * a.pos_stride + n) : 0, angles[warp], pl, lane, c, s);
-      const char *x = t.x + b * t.xb + n * t.xn, *g = t.g + b * t.gb + n * t.gn;
-      char* y = t.y + b * t.yb + n * t.yn;
+      const char *x = t.x.data + b * t.x.sb + n * t.x.sn, *g = t.g.data + b * t.g.sb + n * t.g.sn;
+      char* y = t.y.data + b * t.y.sb + n * t.y.sn;
       for (int r = r0 + pl.group; r - pl.group < r1; r += pl.groups * kAheadBwd) {
         uint4 va[kAheadBwd], vb[kAheadBwd], ga[kAheadBwd], gb[kAheadBwd];
 #pragma unroll
@@ -231,10 +230,10 @@ __global__ void __launch_bounds__(kHeadThreads) head_bwd_kernel(const __grid_con
           const int h = r + k * pl.groups;
           va[k] = vb[k] = ga[k] = gb[k] = make_uint4(0u, 0u, 0u, 0u);
           if (h < r1 && pl.on) {
-            va[k] = *reinterpret_cast<const uint4*>(x + h * t.xh + pl.ca * SZ);
-            vb[k] = *reinterpret_cast<const uint4*>(x + h * t.xh + pl.cb * SZ);
-            ga[k] = *reinterpret_cast<const uint4*>(g + h * t.gh + pl.ca * SZ);
-            gb[k] = *reinterpret_cast<const uint4*>(g + h * t.gh + pl.cb * SZ);
+            va[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.ca * SZ);
+            vb[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.cb * SZ);
+            ga[k] = *reinterpret_cast<const uint4*>(g + h * t.g.sh + pl.ca * SZ);
+            gb[k] = *reinterpret_cast<const uint4*>(g + h * t.g.sh + pl.cb * SZ);
           }
         }
 #pragma unroll
@@ -266,8 +265,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_bwd_kernel(const __grid_con
             fb[j] = rr * (hb[j] * wb[j] - fb[j] * back);
           }
           if (h < r1 && pl.on) {
-            *reinterpret_cast<uint4*>(y + h * t.yh + pl.ca * SZ) = narrow<T>(fa);
-            *reinterpret_cast<uint4*>(y + h * t.yh + pl.cb * SZ) = narrow<T>(fb);
+            *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.ca * SZ) = narrow<T>(fa);
+            *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.cb * SZ) = narrow<T>(fb);
           }
         }
       }
@@ -388,14 +387,16 @@ constexpr size_t kMaxBwdRows = 1024;  // partial rows that the workspace holds: 
 
 }  // namespace
 
-int check_view(const mosaic_view* v, int B, int heads, int N, int size, long long* sb, long long* sh, long long* sn) {
+int check_view(const mosaic_view* v, int B, int heads, int N, int size, View* out) {
   if (!v || !v->data || v->sb < 0 || v->sh < 0 || v->sn < 0) return MOSAIC_E_INVALID_ARG;
-  if (v->sb > (1ll << 44) || v->sh > (1ll << 44) || v->sn > (1ll << 44)) return MOSAIC_E_UNSUPPORTED;
+  constexpr long long kMost = 1ll << 37;  // a tensor copy's strides end at 2^40 bytes
+  if (v->sb >= kMost || v->sh >= kMost || v->sn >= kMost) return MOSAIC_E_UNSUPPORTED;
   if (!aligned16(v->data)) return MOSAIC_E_MISALIGNED;
-  *sb = B > 1 ? v->sb * size : 0;
-  *sh = heads > 1 ? v->sh * size : 0;
-  *sn = N > 1 ? v->sn * size : 0;
-  return (*sb | *sh | *sn) & 15 ? MOSAIC_E_MISALIGNED : MOSAIC_OK;
+  out->data = (char*)v->data;
+  out->sb = B > 1 ? v->sb * size : 0;
+  out->sh = heads > 1 ? v->sh * size : 0;
+  out->sn = N > 1 ? v->sn * size : 0;
+  return (out->sb | out->sh | out->sn) & 15 ? MOSAIC_E_MISALIGNED : MOSAIC_OK;
 }
 
 namespace {
@@ -411,10 +412,8 @@ int rotary_forward(const mosaic_rotary_params* p, const mosaic_view* q, const mo
   const mosaic_view *xs[2] = {q, k}, *ys[2] = {q_out, k_out};
   for (int i = 0; i < 2; ++i) {
     HeadTensor& t = a.t[i];
-    if ((rc = check_view(xs[i], p->B, t.heads, p->N, size, &t.xb, &t.xh, &t.xn))) return rc;
-    if ((rc = check_view(ys[i], p->B, t.heads, p->N, size, &t.yb, &t.yh, &t.yn))) return rc;
-    t.x = (const char*)xs[i]->data;
-    t.y = (char*)ys[i]->data;
+    if ((rc = check_view(xs[i], p->B, t.heads, p->N, size, &t.x))) return rc;
+    if ((rc = check_view(ys[i], p->B, t.heads, p->N, size, &t.y))) return rc;
     t.w = i ? wk : wq;
   }
   if (((uintptr_t)wq | (uintptr_t)wk) & 3 || ((uintptr_t)pos | (uintptr_t)freqs) & 7) return MOSAIC_E_MISALIGNED;
@@ -484,12 +483,9 @@ int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params* p, const mosaic_view* q, 
   const mosaic_view *xs[2] = {q, k}, *gs[2] = {d_q_out, d_k_out}, *ys[2] = {dq, dk};
   for (int i = 0; i < 2; ++i) {
     HeadTensor& t = a.t[i];
-    if ((rc = check_view(xs[i], p->B, t.heads, p->N, size, &t.xb, &t.xh, &t.xn))) return rc;
-    if ((rc = check_view(gs[i], p->B, t.heads, p->N, size, &t.gb, &t.gh, &t.gn))) return rc;
-    if ((rc = check_view(ys[i], p->B, t.heads, p->N, size, &t.yb, &t.yh, &t.yn))) return rc;
-    t.x = (const char*)xs[i]->data;
-    t.g = (const char*)gs[i]->data;
-    t.y = (char*)ys[i]->data;
+    if ((rc = check_view(xs[i], p->B, t.heads, p->N, size, &t.x))) return rc;
+    if ((rc = check_view(gs[i], p->B, t.heads, p->N, size, &t.g))) return rc;
+    if ((rc = check_view(ys[i], p->B, t.heads, p->N, size, &t.y))) return rc;
     t.w = i ? wk : wq;
   }
   if (((uintptr_t)wq | (uintptr_t)wk | (uintptr_t)dwq | (uintptr_t)dwk) & 3 || ((uintptr_t)pos | (uintptr_t)freqs) & 7 ||

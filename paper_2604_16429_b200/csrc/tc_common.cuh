@@ -755,6 +755,9 @@ inline Queue make_queue(long long items, int sms) {
 // again encodes nothing.
 // [units, nlat, nlon, d] bf16 view, box = one 64-token chunk {d, bw, 64/bw, 1}, 128-byte swizzle.
 bool make_map(CUtensorMap* map, const void* base, const Geo& g, int units);
+// Strided tensor [B, heads, N, d], box = 64 channels by `rows` tokens, 128-byte swizzle; coordinates {channel, token, head, member},
+// head and member 0 where the stride between them is 0.  Encoded anew by every call.
+bool make_map_view(CUtensorMap* map, const View& v, int d, int N, int heads, int B, int rows);
 // [units, nlat, nlon] fp32 view (one value per token), box = the 64 tokens of one chunk {bw, 64/bw, 1}, no swizzle.
 bool make_map_rows(CUtensorMap* map, const void* base, const Geo& g, int units);
 }  // namespace mosaic

@@ -84,12 +84,30 @@ bool cached_map(CUtensorMap* out, const void* base, const Geo& g, int kind, int 
   return true;
 }
 
+// Strided tensor [B, heads, N, d] of 16-bit elements in boxes of 64 channels (128 bytes, swizzled) by `rows` tokens.  Extents of one
+// get a stride that the encoder takes.
+bool encode_view(CUtensorMap* map, const void* base, int d, int N, int heads, int B, long long sn, long long sh, long long sb,
+                 int rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  g_encodes.fetch_add(1, std::memory_order_relaxed);
+  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)N, (cuuint64_t)heads, (cuuint64_t)B};
+  cuuint64_t strides[3] = {(cuuint64_t)(N > 1 ? sn : 2 * d), (cuuint64_t)(heads > 1 ? sh : 2 * d), (cuuint64_t)(B > 1 ? sb : 2 * d)};
+  cuuint32_t box[4] = {64u, (cuuint32_t)rows, 1u, 1u};
+  cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_sms[kMaxDevices];
 
 }  // namespace
 
 bool make_map(CUtensorMap* map, const void* base, const Geo& g, int units) { return cached_map(map, base, g, 0, units); }
+bool make_map_view(CUtensorMap* map, const View& v, int d, int N, int heads, int B, int rows) {
+  return encode_view(map, v.data, d, N, v.sh ? heads : 1, v.sb ? B : 1, v.sn, v.sh, v.sb, rows);
+}
 bool make_map_rows(CUtensorMap* map, const void* base, const Geo& g, int units) { return cached_map(map, base, g, 1, units); }
 
 int launch_setup(const void* func, size_t smem, unsigned long long* done, int* sms) {

@@ -1,0 +1,116 @@
+// Geometry of the sliding-window attention shared by its kernels.
+#pragma once
+#include "tc_common.cuh"
+
+namespace mosaic {
+
+constexpr int kMaxSinks = 128;
+constexpr int kRows = 128;  // rows of a query or key tile (the M of one tensor-core product)
+
+struct WinGeo {
+  int B, H, Hkv, G;       // G = H / Hkv query heads share a key/value head
+  int Nq, Nk, d;
+  int window, sinks;      // both at most Nk
+  float scale, scale_log2;
+  const int32_t *q_len, *k_len;
+};
+
+// Lengths of batch member b: its queries are the last ql of its kl tokens
+struct Span {
+  int ql, kl, off;  // row i has position off + i
+};
+__device__ __forceinline__ Span span_of(const WinGeo& g, int b) {
+  Span s;
+  s.ql = g.q_len ? min(max(__ldg(g.q_len + b), 0), g.Nq) : g.Nq;
+  s.kl = g.k_len ? min(max(__ldg(g.k_len + b), 0), g.Nk) : g.Nk;
+  s.off = s.kl - s.ql;
+  return s;
+}
+
+// Does the row at position p see key j (j < kl)?
+__device__ __forceinline__ bool sees(const WinGeo& g, int p, int j) { return j <= p && (p - j < g.window || j < g.sinks); }
+
+// The bounded waits without a call: the registers of a warpgroup that raised or lowered its count would all be saved around one
+// (2 KB of stack and as many spills a thread in the forward).
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+#pragma unroll 1
+  for (uint32_t i = 1;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 63u) == 0u) {
+      if (*abort) return false;
+      if (clock64() - t0 > kSpinCycles) {
+        set_status(status, MOSAIC_E_DEVICE_TIMEOUT);
+        *abort = 1;
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
+  return __all_sync(0xffffffffu, wait_here(bar, parity, abort, status));
+}
+
+// The lowest n bits (n any integer)
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// 2^x for two values on the FMA pipe: x = n + f with n = round(x), |f| <= 1/2, 2^f by a quartic (largest relative error 2.9e-6:
+// the sum of a row, which log-sum-exp returns in fp32, keeps five digits more than the 16-bit weights need), 2^n into the exponent.
+// Clamped at -125.  A NaN does not come out as one, but as a number beyond every 16-bit type, which makes the row not finite.
+__device__ __forceinline__ float clamp_nan(float x) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(-125.f));
+  return y;
+}
+__device__ __forceinline__ void ex2_quartic(uint64_t x2, float& p0, float& p1) {
+  float x0, x1;
+  unpack2(x2, x0, x1);
+  const uint64_t xc = pack2(clamp_nan(x0), clamp_nan(x1));
+  const uint64_t t = add2(xc, pack2(12582912.f, 12582912.f));
+  const uint64_t n = add2(t, pack2(-12582912.f, -12582912.f));
+  const uint64_t f = fma2(n, pack2(-1.f, -1.f), xc);
+  uint64_t p = fma2(f, pack2(0.009582853f, 0.009582853f), pack2(0.055906426f, 0.055906426f));
+  p = fma2(p, f, pack2(0.240240991f, 0.240240991f));
+  p = fma2(p, f, pack2(0.693124175f, 0.693124175f));
+  p = fma2(p, f, pack2(1.f, 1.f));
+  float t0, t1, q0, q1;
+  unpack2(t, t0, t1);
+  unpack2(p, q0, q1);
+  p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
+  p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+}
+
+// Operand descriptors.  A tile of R rows by d channels lies in d/64 parts of R x 64 channels (128-byte swizzled rows), `part`
+// bytes apart.  K-major operand (contraction over channels): the descriptor of 16 channels at 16 kk.  MN-major operand
+// (contraction over rows, all d channels side by side): the descriptor of rows 16 kk .. 16 kk + 15, its 64-channel groups `part` apart.
+__device__ __forceinline__ uint64_t k_major(uint64_t tile, int kk, uint32_t part) {
+  return tile + (uint64_t)(((kk >> 2) * part + (kk & 3) * 32) >> 4);
+}
+__device__ __forceinline__ uint64_t mn_major(uint32_t addr, uint32_t part) {
+  return (smem_desc(addr) & ~((uint64_t)0x3fff << 16)) | ((uint64_t)(part >> 4) << 16);
+}
+__device__ __forceinline__ uint32_t idesc_n(uint32_t base, int n) { return base | ((uint32_t)(n >> 3) << 17); }
+
+// Rows first .. R - 1 of a tile to zero (rows that do not exist may hold anything, and a weight of zero does not silence a NaN),
+// by a whole warp; visible to the tensor core afterwards.
+template <int D>
+__device__ __forceinline__ void zero_rows(unsigned char* tile, int first, int rows, int lane) {
+  for (int r = max(first, 0); r < rows; ++r)
+    if (lane < D / 8) *reinterpret_cast<uint4*>(tile + (lane >> 3) * rows * 128 + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+}
+
+int make_win_geo(const mosaic_window_params* p, const int32_t* q_len, const int32_t* k_len, WinGeo* g);
+
+// Views whose heads or members all lie at one place (stride 0) have a map with one of them.
+struct Fold {
+  int h, b;  // factor of the head's and the member's coordinate
+};
+inline Fold fold_of(const View& v) { return {v.sh ? 1 : 0, v.sb ? 1 : 0}; }
+
+int launch_window_fwd(const HostCtx& c, const WinGeo& g, bool f16, const View& q, const View& k, const View& v, const View& o,
+                      float* lse);
+
+}  // namespace mosaic

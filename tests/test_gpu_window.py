@@ -1,0 +1,115 @@
+"""Sliding-window attention with sinks against the definition in 64 bits.
+
+Tolerances.  u = eps/2 of the 16-bit type (2^-9 * 2 = 2^-8 for bf16, 2^-11 for fp16) bounds a rounding to nearest, relative.  The
+forward rounds every weight to 16 bits once (u of it) and the result once, and works in fp32 otherwise: scores are sums of d
+exact products (d * 2^-24 of the sum of magnitudes, as an absolute error of the exponent), exponentials are good to 3e-6.  So
+|o - o64| <= u |o| + (u + E) sum_j p_j |v_j|, E = 2 (d 2^-24 smax + 4e-6), smax the largest sum of magnitudes in a score;
+|lse - lse64| <= E + 2^-23 |lse|."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_16429_b200 import binding as mb
+from tests import gpu_util as G
+from tests import window_ref as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16}
+NAN = float("nan")
+
+
+def make(B, H, Hkv, Nq, Nk, d, dtype="bf16", layout="bhnd", seed=0, sharp=1.0):
+    g = torch.Generator().manual_seed(seed)
+
+    def one(heads, N, f=1.0):
+        x = (f * torch.randn((B, N, heads, d) if layout == "bnhd" else (B, heads, N, d), generator=g)).to(DT[dtype]).cuda()
+        return x.transpose(1, 2) if layout == "bnhd" else x
+
+    return one(H, Nq, sharp), one(Hkv, Nk), one(Hkv, Nk), one(H, Nq)
+
+
+def lens(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def score_error(q, k, scale):
+    d = q.shape[-1]
+    smax = float(q.double().abs().amax(-1).max() * k.double().abs().sum(-1).max()) * (scale or d ** -0.5)
+    return 2 * (d * 2.0 ** -24 * smax + 4e-6)
+
+
+def check_fwd(wp, q, k, v, q_len=None, k_len=None, **kw):
+    want = ref.attention(q, k, v, wp.window, wp.sinks, wp.scale, q_len, k_len)
+    B, H, Nq, d = q.shape
+    o, lse = G.Guarded((B, H, Nq, d), q.dtype, fill=NAN), G.Guarded((B, H, Nq), torch.float32, fill=NAN)
+    ws = G.Guarded((mb.window_workspace_bytes(wp, q, k, mb.OP_FWD),), torch.uint8)
+    mb.mosaic_bsa_window_fwd(wp, q, k, v, q_len=lens(q_len), k_len=lens(k_len), o=o.t, lse=lse.t, ws=ws.t, **kw)
+    mb.check_status(ws.t, "window_fwd")
+    for x, name in ((o, "o"), (lse, "lse"), (ws, "workspace")):
+        x.check(name)
+    there = ~torch.isnan(want["lse"])
+    assert torch.isnan(o.t[~there]).all() and torch.isnan(lse.t[~there]).all(), "rows that do not exist were written"
+    assert not torch.isnan(o.t[there]).any() and not torch.isnan(lse.t[there]).any()
+    E, u = score_error(q, k, wp.scale), torch.finfo(q.dtype).eps / 2
+    empty = there & (want["lse"] == -math.inf)
+    assert (lse.t[empty] == -math.inf).all() and (o.t[empty] == 0).all()
+    full = there & ~empty
+    if full.any():
+        tol = E + 2.0 ** -23 * want["lse"][full].abs()
+        assert ((lse.t[full] - want["lse"][full]).abs() <= tol).all(), float(((lse.t[full] - want["lse"][full]).abs() - tol).max())
+        tol = u * want["o"][full].abs() + (u + E) * want["p_abs"][full] + 1e-7
+        off = (o.t[full].double() - want["o"][full]).abs()
+        assert (off <= tol).all(), f"o: over by {float((off - tol).max()):.3g}"
+    return o.t, lse.t
+
+
+CASES = [  # B, H, Hkv, Nq, Nk, d, window, sinks
+    (1, 1, 1, 1, 1, 64, 1, 0),
+    (1, 1, 1, 1, 1, 128, 5, 3),
+    (1, 2, 1, 128, 128, 64, 128, 0),
+    (1, 2, 2, 129, 129, 64, 32, 4),
+    (2, 4, 2, 300, 300, 128, 100, 7),
+    (1, 3, 1, 400, 400, 64, 1000, 0),      # plain causal
+    (1, 3, 1, 500, 500, 128, 1, 1),        # itself and the first token
+    (1, 6, 2, 1000, 1000, 64, 127, 33),
+    (1, 1, 1, 777, 777, 128, 129, 128),
+    (1, 8, 1, 260, 2000, 64, 509, 64),     # a chunk behind a cache
+    (1, 2, 1, 7, 1500, 128, 300, 5),
+    (3, 5, 5, 257, 1025, 64, 256, 32),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("dtype,layout", [("bf16", "bhnd"), ("fp16", "bnhd")])
+def test_forward(case, dtype, layout):
+    B, H, Hkv, Nq, Nk, d, window, sinks = case
+    q, k, v, _ = make(B, H, Hkv, Nq, Nk, d, dtype, layout, seed=Nq + window)
+    check_fwd(mb.WindowParams(window=window, sinks=sinks), q, k, v)
+
+
+@pytest.mark.parametrize("q_len,k_len", [
+    ([0, 1, 300, 17], [0, 1, 300, 900]),        # nothing, one token, a whole sequence, a chunk
+    ([300, 200, 5, 128], [100, 0, 900, 128]),   # more queries than keys: the first rows see nothing
+    ([1, 1, 1, 1], [900, 899, 1, 128]),
+])
+@pytest.mark.parametrize("d,G_", [(64, 1), (128, 3)])
+def test_ragged_lengths_and_what_lies_behind_them(q_len, k_len, d, G_):
+    q, k, v, _ = make(4, 2 * G_, 2, 300, 900, d, seed=5)
+    for b in range(4):  # whatever lies behind a sequence's last row is never used
+        q[b, :, q_len[b]:] = NAN
+        k[b, :, k_len[b]:] = NAN
+        v[b, :, k_len[b]:] = math.inf
+    kc, vc, qc = k.clone(), v.clone(), q.clone()
+    for b in range(4):
+        qc[b, :, q_len[b]:] = kc[b, :, k_len[b]:] = vc[b, :, k_len[b]:] = 0
+    wp = mb.WindowParams(window=150, sinks=3)
+    want = mb.mosaic_bsa_window_fwd(wp, qc, kc, vc, q_len=lens(q_len), k_len=lens(k_len))
+    E = score_error(qc, kc, 0)
+    o = torch.full_like(q, 7.0)
+    lse = torch.full(q.shape[:3], 7.0, device="cuda")
+    mb.mosaic_bsa_window_fwd(wp, q, k, v, q_len=lens(q_len), k_len=lens(k_len), o=o, lse=lse)
+    for b in range(4):
+        assert torch.equal(o[b, :, :q_len[b]], want[0][b, :, :q_len[b]]) and torch.equal(lse[b, :, :q_len[b]], want[1][b, :, :q_len[b]])
+        assert (o[b, :, q_len[b]:] == 7).all() and (lse[b, :, q_len[b]:] == 7).all()
+    check_fwd(wp, qc, kc, vc, q_len, k_len)
