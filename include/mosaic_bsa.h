@@ -345,6 +345,14 @@ int mosaic_bsa_window_fwd(const mosaic_window_params *p, const mosaic_view *q, c
                           const int32_t *q_len, const int32_t *k_len, const mosaic_view *o, float *lse, void *ws,
                           size_t ws_bytes, void *cuda_stream);
 
+/* One new token per sequence over a cache (Nq = 1; position k_len[b] - 1).  q [B,H,1,d], k, v [B,Hkv,Nk,d] in, the new token's
+ * own key and value among them; o like q, lse [B,H,1] out.  k_len NULL: Nk for all.  No workspace.
+ * With MOSAIC_FLAG_ROLLING the cache forgets: position j < sinks lies in slot j, a later one in slot
+ * sinks + (j - sinks) % (Nk - sinks), and k_len may be any length (below 2^31); window + sinks <= Nk. */
+#define MOSAIC_FLAG_ROLLING 32u
+int mosaic_bsa_window_decode(const mosaic_window_params *p, const mosaic_view *q, const mosaic_view *k, const mosaic_view *v,
+                             const int32_t *k_len, const mosaic_view *o, float *lse, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.
  * Every op resets the word when it starts. */

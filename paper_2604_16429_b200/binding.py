@@ -22,11 +22,12 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_last_status", "mosaic_bsa_strerror", "mosaic_bsa_select_static",
            "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
-           "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd")
+           "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd",
+           "mosaic_bsa_window_decode")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
-FLAG_FP32, FLAG_HALF_PAIRS, FLAG_INVERSE = 4, 8, 16
+FLAG_FP32, FLAG_HALF_PAIRS, FLAG_INVERSE, FLAG_ROLLING = 4, 8, 16, 32
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS, ROTARY_BANDS = 0, 1, 2, 3, 4
 
 
@@ -146,6 +147,8 @@ def lib():
         L.mosaic_bsa_window_workspace_bytes.argtypes = [wp, ctypes.c_int]
         L.mosaic_bsa_window_fwd.restype = ctypes.c_int
         L.mosaic_bsa_window_fwd.argtypes = [wp, vw, vw, vw, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
+        L.mosaic_bsa_window_decode.restype = ctypes.c_int
+        L.mosaic_bsa_window_decode.argtypes = [wp, vw, vw, vw, i32p, vw, fp, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -556,7 +559,7 @@ def _chk_lse(t, q):
 def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=None, lse=None, ws=None, stream=None):
     """Forward of the sliding-window attention: q [B,H,Nq,d], k and v [B,Hkv,Nk,d]; the first q_len[b] and k_len[b] rows of a
     batch member exist (None: all), its queries are its last tokens.  Returns (o, lse)."""
-    p = _window_params(wp, q, k)
+    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
     vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
     run = _Launch(q.device, stream)
     o = run.keep(torch.empty_like(q)) if o is None else o
@@ -564,4 +567,17 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     ws = _window_ws(p, OP_FWD, run, ws)
     run.call("mosaic_bsa_window_fwd", p, vq, vk, vv, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
              _chk_out("o", o, q.shape, q), _chk_lse(lse, q), ws.data_ptr(), ws.numel())
+    return o, lse
+
+
+def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=None, stream=None):
+    """One new token per sequence: q [B,H,1,d] at position k_len[b] - 1 (None: the whole cache is filled), k and v [B,Hkv,Nk,d]
+    with the token's own row in place.  `wp.rolling`: position j >= sinks lies in slot sinks + (j - sinks) % (Nk - sinks).
+    Returns (o, lse)."""
+    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
+    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
+    run = _Launch(q.device, stream)
+    o = run.keep(torch.empty_like(q)) if o is None else o
+    lse = run.empty(q.shape[:3], torch.float32) if lse is None else lse
+    run.call("mosaic_bsa_window_decode", p, vq, vk, vv, _chk_len("k_len", k_len, q), _chk_out("o", o, q.shape, q), _chk_lse(lse, q))
     return o, lse

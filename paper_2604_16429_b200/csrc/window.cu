@@ -71,4 +71,24 @@ int mosaic_bsa_window_fwd(const mosaic_window_params* p, const mosaic_view* q, c
   return launch_window_fwd(c, g, (p->flags & MOSAIC_FLAG_FP16) != 0, vq, vk, vv, vo, lse);
 }
 
+int mosaic_bsa_window_decode(const mosaic_window_params* p, const mosaic_view* q, const mosaic_view* k, const mosaic_view* v,
+                             const int32_t* k_len, const mosaic_view* o, float* lse, void* cuda_stream) {
+  int rc = check(p, MOSAIC_FLAG_ROLLING);
+  if (rc) return rc;
+  const bool rolling = (p->flags & MOSAIC_FLAG_ROLLING) != 0;
+  if (p->Nq != 1 || (rolling && (long long)p->window + p->sinks > p->Nk)) return MOSAIC_E_INVALID_ARG;
+  View vq, vk, vv, vo;
+  if ((rc = check_view(q, p->B, p->H, 1, 2, &vq)) || (rc = check_view(k, p->B, p->Hkv, p->Nk, 2, &vk)) ||
+      (rc = check_view(v, p->B, p->Hkv, p->Nk, 2, &vv)) || (rc = check_view(o, p->B, p->H, 1, 2, &vo)))
+    return rc;
+  if (!lse) return MOSAIC_E_INVALID_ARG;
+  if (!aligned(lse, 4)) return MOSAIC_E_MISALIGNED;
+  WinGeo g;
+  if ((rc = make_win_geo(p, nullptr, k_len, &g))) return rc;
+  if ((rc = device_ok())) return rc;
+  HostCtx c = {};
+  c.stream = (cudaStream_t)cuda_stream;
+  return launch_window_decode(c, g, (p->flags & MOSAIC_FLAG_FP16) != 0, rolling ? p->Nk - p->sinks : 0, vq, vk, vv, vo, lse);
+}
+
 }  // extern "C"

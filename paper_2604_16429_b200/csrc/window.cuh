@@ -112,5 +112,7 @@ inline Fold fold_of(const View& v) { return {v.sh ? 1 : 0, v.sb ? 1 : 0}; }
 
 int launch_window_fwd(const HostCtx& c, const WinGeo& g, bool f16, const View& q, const View& k, const View& v, const View& o,
                       float* lse);
+int launch_window_decode(const HostCtx& c, const WinGeo& g, bool f16, int ring, const View& q, const View& k, const View& v,
+                         const View& o, float* lse);
 
 }  // namespace mosaic

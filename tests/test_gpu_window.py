@@ -113,3 +113,59 @@ def test_ragged_lengths_and_what_lies_behind_them(q_len, k_len, d, G_):
         assert torch.equal(o[b, :, :q_len[b]], want[0][b, :, :q_len[b]]) and torch.equal(lse[b, :, :q_len[b]], want[1][b, :, :q_len[b]])
         assert (o[b, :, q_len[b]:] == 7).all() and (lse[b, :, q_len[b]:] == 7).all()
     check_fwd(wp, qc, kc, vc, q_len, k_len)
+
+
+def ring_of(x, kl, sinks, cap):
+    """The rolling cache [.., cap, d] that keeps the sinks and the last positions of the first kl rows of x."""
+    out = torch.full((*x.shape[:-2], cap, x.shape[-1]), NAN, dtype=x.dtype, device=x.device)
+    for j in list(range(min(sinks, kl))) + list(range(max(sinks, kl - (cap - sinks)), kl)):
+        out[..., j if j < sinks else sinks + (j - sinks) % (cap - sinks), :] = x[..., j, :]
+    return out
+
+
+DEC = [  # B, H, Hkv, Nk, d, window, sinks, k_len
+    (1, 1, 1, 1, 64, 1, 0, None),
+    (2, 4, 2, 300, 64, 64, 4, [300, 299]),
+    (3, 16, 2, 1000, 128, 333, 7, [0, 1, 1000]),
+    (2, 24, 2, 777, 128, 5000, 0, [777, 130]),        # more than eight heads in a group
+    (1, 20, 1, 515, 64, 100, 128, [515]),
+    (2, 34, 1, 90, 128, 17, 3, [90, 4]),              # more heads than a CTA takes
+    (4, 6, 3, 4099, 64, 4000, 33, [4099, 40, 33, 2000]),
+    (1, 8, 8, 9000, 128, 8999, 1, None),
+]
+
+
+@pytest.mark.parametrize("case", DEC, ids=str)
+@pytest.mark.parametrize("dtype,layout", [("bf16", "bhnd"), ("fp16", "bnhd")])
+@pytest.mark.parametrize("rolling", [False, True])
+def test_decode(case, dtype, layout, rolling):
+    B, H, Hkv, Nk, d, window, sinks, k_len = case
+    q, k, v, _ = make(B, H, Hkv, 1, Nk, d, dtype, layout, seed=Nk)
+    full = k_len or [Nk] * B
+    want = ref.attention(q, k, v, window, sinks, 0.0, [1] * B, full)
+    for b in range(B):  # never read
+        k[b, :, full[b]:] = NAN
+        v[b, :, full[b]:] = NAN
+    E, u = score_error(q, torch.nan_to_num(k), 0), torch.finfo(q.dtype).eps / 2
+    if rolling:
+        cap = min(window, Nk) + min(sinks, Nk) + 5
+        window, sinks = min(window, Nk), min(sinks, Nk)
+        k, v = (torch.cat([ring_of(x[b:b + 1], full[b], sinks, cap) for b in range(B)]) for x in (k, v))
+    wp = mb.WindowParams(window=window, sinks=sinks, rolling=rolling)
+    o, lse = G.Guarded((B, H, 1, d), q.dtype, fill=NAN), G.Guarded((B, H, 1), torch.float32, fill=NAN)
+    mb.mosaic_bsa_window_decode(wp, q, k, v, k_len=lens(k_len) if not rolling else lens(full), o=o.t, lse=lse.t)
+    o.check("o"); lse.check("lse")
+    for b in range(B):
+        if full[b] == 0:
+            assert (o.t[b] == 0).all() and (lse.t[b] == -math.inf).all()
+            continue
+        tol = E + 2.0 ** -22 * want["lse"][b].abs()
+        assert ((lse.t[b] - want["lse"][b]).abs() <= tol).all()
+        tol = u * want["o"][b].abs() + (u + E) * want["p_abs"][b] + 1e-7
+        off = (o.t[b].double() - want["o"][b]).abs()
+        assert (off <= tol).all(), float((off - tol).max())
+    again = mb.mosaic_bsa_window_decode(wp, q, k, v, k_len=lens(full) if rolling or k_len else None)
+    assert torch.equal(again[0], o.t) and torch.equal(again[1], lse.t)
+    if B > 1:  # a member's bits do not depend on the others
+        one = mb.mosaic_bsa_window_decode(wp, q[1:2], k[1:2], v[1:2], k_len=lens(full[1:2]))
+        assert torch.equal(one[0], o.t[1:2]) and torch.equal(one[1], lse.t[1:2])
