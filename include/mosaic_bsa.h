@@ -345,6 +345,13 @@ int mosaic_bsa_window_fwd(const mosaic_window_params *p, const mosaic_view *q, c
                           const int32_t *q_len, const int32_t *k_len, const mosaic_view *o, float *lse, void *ws,
                           size_t ws_bytes, void *cuda_stream);
 
+/* Backward: the forward's inputs, its o and lse, and d_o (like o) in; dq like q, dk and dv like k out, summed in a fixed order
+ * over the query heads of a group. */
+int mosaic_bsa_window_bwd(const mosaic_window_params *p, const mosaic_view *q, const mosaic_view *k, const mosaic_view *v,
+                          const mosaic_view *o, const float *lse, const mosaic_view *d_o, const int32_t *q_len,
+                          const int32_t *k_len, const mosaic_view *dq, const mosaic_view *dk, const mosaic_view *dv, void *ws,
+                          size_t ws_bytes, void *cuda_stream);
+
 /* One new token per sequence over a cache (Nq = 1; position k_len[b] - 1).  q [B,H,1,d], k, v [B,Hkv,Nk,d] in, the new token's
  * own key and value among them; o like q, lse [B,H,1] out.  k_len NULL: Nk for all.  No workspace.
  * With MOSAIC_FLAG_ROLLING the cache forgets: position j < sinks lies in slot j, a later one in slot

@@ -23,7 +23,7 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
            "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd",
-           "mosaic_bsa_window_decode")
+           "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
@@ -147,6 +147,8 @@ def lib():
         L.mosaic_bsa_window_workspace_bytes.argtypes = [wp, ctypes.c_int]
         L.mosaic_bsa_window_fwd.restype = ctypes.c_int
         L.mosaic_bsa_window_fwd.argtypes = [wp, vw, vw, vw, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
+        L.mosaic_bsa_window_bwd.restype = ctypes.c_int
+        L.mosaic_bsa_window_bwd.argtypes = [wp, vw, vw, vw, vw, fp, vw, i32p, i32p, vw, vw, vw, vp, ctypes.c_size_t, vp]
         L.mosaic_bsa_window_decode.restype = ctypes.c_int
         L.mosaic_bsa_window_decode.argtypes = [wp, vw, vw, vw, i32p, vw, fp, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
@@ -568,6 +570,23 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     run.call("mosaic_bsa_window_fwd", p, vq, vk, vv, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
              _chk_out("o", o, q.shape, q), _chk_lse(lse, q), ws.data_ptr(), ws.numel())
     return o, lse
+
+
+def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_len=None, dq=None, dk=None, dv=None, ws=None,
+                          stream=None):
+    """Backward of the sliding-window attention from the forward's inputs, its o and lse, and the gradient of o.
+    Returns (dq, dk, dv)."""
+    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
+    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
+    vo, vd = _chk_view("o", o, q.shape, q), _chk_view("d_o", d_o, q.shape, q)
+    run = _Launch(q.device, stream)
+    dq = run.keep(torch.empty_like(q)) if dq is None else dq
+    dk = run.keep(torch.empty_like(k)) if dk is None else dk
+    dv = run.keep(torch.empty_like(v)) if dv is None else dv
+    ws = _window_ws(p, OP_BWD, run, ws)
+    run.call("mosaic_bsa_window_bwd", p, vq, vk, vv, vo, _chk_lse(lse, q), vd, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
+             _chk_out("dq", dq, q.shape, q), _chk_out("dk", dk, k.shape, q), _chk_out("dv", dv, k.shape, q), ws.data_ptr(), ws.numel())
+    return dq, dk, dv
 
 
 def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=None, stream=None):

@@ -46,8 +46,9 @@ using namespace mosaic;
 extern "C" {
 
 size_t mosaic_bsa_window_workspace_bytes(const mosaic_window_params* p, int op) {
-  if (check(p, 0)) return 0;
-  return op == MOSAIC_OP_FWD ? kStatusBytes : 0;
+  WinGeo g;
+  if (check(p, 0) || make_win_geo(p, nullptr, nullptr, &g)) return 0;
+  return op == MOSAIC_OP_FWD ? kStatusBytes : op == MOSAIC_OP_BWD ? window_bwd_layout(g).total : 0;
 }
 
 int mosaic_bsa_window_fwd(const mosaic_window_params* p, const mosaic_view* q, const mosaic_view* k, const mosaic_view* v,
@@ -69,6 +70,31 @@ int mosaic_bsa_window_fwd(const mosaic_window_params* p, const mosaic_view* q, c
   c.stream = (cudaStream_t)cuda_stream;
   c.status = (int*)ws;
   return launch_window_fwd(c, g, (p->flags & MOSAIC_FLAG_FP16) != 0, vq, vk, vv, vo, lse);
+}
+
+int mosaic_bsa_window_bwd(const mosaic_window_params* p, const mosaic_view* q, const mosaic_view* k, const mosaic_view* v,
+                          const mosaic_view* o, const float* lse, const mosaic_view* d_o, const int32_t* q_len,
+                          const int32_t* k_len, const mosaic_view* dq, const mosaic_view* dk, const mosaic_view* dv, void* ws,
+                          size_t ws_bytes, void* cuda_stream) {
+  int rc = check(p, 0);
+  if (rc) return rc;
+  WinBwd t;
+  if ((rc = check_input(q, p->B, p->H, p->Nq, &t.q)) || (rc = check_input(k, p->B, p->Hkv, p->Nk, &t.k)) ||
+      (rc = check_input(v, p->B, p->Hkv, p->Nk, &t.v)) || (rc = check_view(o, p->B, p->H, p->Nq, 2, &t.o)) ||
+      (rc = check_input(d_o, p->B, p->H, p->Nq, &t.d_o)) || (rc = check_view(dq, p->B, p->H, p->Nq, 2, &t.dq)) ||
+      (rc = check_view(dk, p->B, p->Hkv, p->Nk, 2, &t.dk)) || (rc = check_view(dv, p->B, p->Hkv, p->Nk, 2, &t.dv)))
+    return rc;
+  if (!lse || !ws) return MOSAIC_E_INVALID_ARG;
+  if (!aligned(lse, 4) || !aligned(ws, 256)) return MOSAIC_E_MISALIGNED;
+  WinGeo g;
+  if ((rc = make_win_geo(p, q_len, k_len, &g))) return rc;
+  if (ws_bytes < window_bwd_layout(g).total) return MOSAIC_E_WORKSPACE_TOO_SMALL;
+  if ((rc = device_ok())) return rc;
+  t.lse = lse;
+  HostCtx c = {};
+  c.stream = (cudaStream_t)cuda_stream;
+  c.status = (int*)ws;
+  return launch_window_bwd(c, g, (p->flags & MOSAIC_FLAG_FP16) != 0, t, ws);
 }
 
 int mosaic_bsa_window_decode(const mosaic_window_params* p, const mosaic_view* q, const mosaic_view* k, const mosaic_view* v,

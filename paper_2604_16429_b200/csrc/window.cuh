@@ -81,6 +81,13 @@ __device__ __forceinline__ void ex2_quartic(uint64_t x2, float& p0, float& p1) {
   p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
 }
 
+// `bytes` (a multiple of 16, both ends aligned) of global memory to shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(bar)
+               : "memory");
+}
+
 // Operand descriptors.  A tile of R rows by d channels lies in d/64 parts of R x 64 channels (128-byte swizzled rows), `part`
 // bytes apart.  K-major operand (contraction over channels): the descriptor of 16 channels at 16 kk.  MN-major operand
 // (contraction over rows, all d channels side by side): the descriptor of rows 16 kk .. 16 kk + 15, its 64-channel groups `part` apart.
@@ -112,6 +119,16 @@ inline Fold fold_of(const View& v) { return {v.sh ? 1 : 0, v.sb ? 1 : 0}; }
 
 int launch_window_fwd(const HostCtx& c, const WinGeo& g, bool f16, const View& q, const View& k, const View& v, const View& o,
                       float* lse);
+struct WinBwd {
+  View q, k, v, o, d_o, dq, dk, dv;
+  const float* lse;
+};
+struct WinBwdWs {
+  size_t neg_lse2, neg_d, partial, total;
+  int pad, pieces, piece_rows;
+};
+WinBwdWs window_bwd_layout(const WinGeo& g);
+int launch_window_bwd(const HostCtx& c, const WinGeo& g, bool f16, const WinBwd& t, void* ws);
 int launch_window_decode(const HostCtx& c, const WinGeo& g, bool f16, int ring, const View& q, const View& k, const View& v,
                          const View& o, float* lse);
 

@@ -1,0 +1,527 @@
+// Backward of the causal sliding-window attention with sinks on Blackwell tensor cores (tcgen05 + TMEM + TMA).
+//
+//   P_ij = exp(s_ij - lse_i), dP_ij = dO_i . v_j, D_i = dO_i . O_i, dS_ij = P_ij (dP_ij - D_i)
+//   dq_i = scale sum_j dS_ij k_j;  dk_j = scale sum_i dS_ij q_i;  dv_j = sum_i P_ij dO_i
+//
+// Two passes of one kernel, each with the tile that it writes resident and the other side streaming by in chunks of 64 rows, so
+// that every sum has one owner and a fixed order (no atomics):
+//   query-stationary  tile = 128 query rows (Q, dO); chunks of K and V: the sinks in front of the window, then the window
+//   key-stationary    tile = 128 keys (K, V); chunks of Q and dO of every head of the group, the rows whose window holds a key of
+//                     the tile.  The sinks' keys have all later rows besides; these are cut into pieces as long as a tile's own
+//                     list, items of their own whose sums (fp32) a last kernel adds in order.
+// Per chunk the first product pair is S and dP (key-stationary: their transposes), then the row threads (thread = row of the tile
+// = TMEM lane) form P and dS in 16 bits in the place of S and dP, operands from tensor memory of the sums' products.  Two chunk
+// buffers, two groups of row threads: while one group works on a chunk the tensor core adds the previous one's sums and forms the
+// next one's S and dP.  TMEM (512 columns): S, dP of buffer b at 128 b and 128 b + 64; dS x at 256, P^T y at 256 + d.
+// Rounded to 16 bits: P and dS as operands, the results.  Every wait is bounded.
+#include <type_traits>
+
+#include "window.cuh"
+
+namespace mosaic {
+
+namespace {
+
+constexpr int kThreads = 384, kChunkRows = 64;
+constexpr int kLaunchRegs = 168, kRowRegs = 208, kOtherRegs = 88;  // as in the forward: the shares add up to the launch's
+static_assert(2 * kRowRegs + kOtherRegs <= 3 * kLaunchRegs, "the shares exceed the launch's registers");
+constexpr uint32_t kTmemCols = 512, kColAcc = 256;
+
+template <int D>
+struct Smem {
+  static constexpr int kTileBytes = kRows * D * 2, kChunkBytes = kChunkRows * D * 2;
+  static constexpr int kSlots = D == 128 ? 4 : 8;
+  struct Slot {
+    unsigned char x[kChunkBytes], y[kChunkBytes];
+  };
+  unsigned char x0[kTileBytes], y0[kTileBytes];  // the resident tiles
+  Slot ring[kSlots];
+  float stat[kSlots][2][kChunkRows];             // key-stationary: -lse (base 2) and -D of the chunk's rows
+  unsigned long long st_full, st_empty, ring_full[kSlots], ring_empty[kSlots], sd_full[2], p_full[2], acc_full, acc_free, drain;
+  uint32_t tmem_base;
+  int abort;
+};
+
+struct BwdArgs {
+  View dx0, dy0;                  // dq; or dk, dv
+  const float *neg_lse2, *neg_d;  // [B, H, pad]
+  float* partial;                 // [B, Hkv, pieces + 1, 2, sinks, d]
+  int pad, tiles, pieces;         // tiles and sink pieces of a unit
+  int piece_rows;
+};
+
+// Rows of the sinks' keys beyond the window of tile 0: its own list ends at row `end`, in whole chunks
+__device__ __forceinline__ int first_tile_end(const WinGeo& g, const Span& s) {
+  const int first = max(0, -s.off) / kChunkRows * kChunkRows, e = min(s.ql, kRows - 1 + g.window - s.off);
+  return e > first ? first + (e - first + kChunkRows - 1) / kChunkRows * kChunkRows : first;
+}
+
+template <bool KEYS>
+struct Item {
+  int b, hk, head, piece, row0, rows;  // rows: of the tile that exist
+  int off, ql, kl;
+  int per, chunks;          // chunks of a head, of all
+  int front, base, end, ns; // query-stationary: chunks of sinks in front, then keys base .. end - 1; key-stationary: rows base .. end - 1
+  __device__ __forceinline__ void make(const WinGeo& g, const BwdArgs& a, int index) {
+    const int heads = KEYS ? g.Hkv : g.H;
+    const int unit = index % (g.B * heads), i = index / (g.B * heads);
+    b = unit / heads;
+    head = unit - b * heads;
+    hk = KEYS ? head : head / g.G;
+    const Span s = span_of(g, b);
+    off = s.off; ql = s.ql; kl = s.kl;
+    front = ns = 0;
+    if constexpr (KEYS) {
+      head = hk * g.G;
+      piece = max(0, i - a.tiles + 1);
+      row0 = piece ? 0 : i * kRows;
+      rows = min(kRows, kl - row0);
+      if (piece == 0) {
+        base = max(0, row0 - off) / kChunkRows * kChunkRows;
+        end = min(ql, row0 + kRows - 1 + g.window - off);
+      } else {
+        base = first_tile_end(g, s) + (piece - 1) * a.piece_rows;
+        end = min(ql, base + a.piece_rows);
+      }
+      per = rows > 0 && end > base ? (end - base + kChunkRows - 1) / kChunkRows : 0;
+      chunks = per * g.G;
+    } else {
+      piece = 0;
+      row0 = (a.tiles - 1 - i) * kRows;  // the last rows first: in plain causal attention they have the most keys
+      rows = min(kRows, ql - row0);
+      base = max(0, off + row0 - g.window + 1);
+      end = off + min(row0 + kRows, ql);
+      ns = min(g.sinks, base);
+      front = (ns + kChunkRows - 1) / kChunkRows;
+      per = chunks = rows > 0 && end > 0 ? front + (end - base + kChunkRows - 1) / kChunkRows : 0;
+    }
+  }
+  // head, first row and number of rows of chunk n
+  __device__ __forceinline__ void chunk(int n, int& h, int& start, int& cols) const {
+    if constexpr (KEYS) {
+      const int r = n / per;
+      h = head + r;
+      start = base + (n - r * per) * kChunkRows;
+      cols = min(kChunkRows, ql - start);
+    } else {
+      h = hk;
+      start = n < front ? n * kChunkRows : base + (n - front) * kChunkRows;
+      cols = min(kChunkRows, (n < front ? ns : end) - start);
+    }
+  }
+};
+
+}  // namespace
+
+template <int D, bool F16, bool KEYS>
+__global__ void __launch_bounds__(kThreads, 1)
+    window_bwd_kernel(const WinGeo g, const __grid_constant__ CUtensorMap map_x0, const __grid_constant__ CUtensorMap map_y0,
+                      const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const Fold fx0,
+                      const Fold fy0, const Fold fx, const Fold fy, const __grid_constant__ BwdArgs a, int* status, int total) {
+  extern __shared__ unsigned char smem_raw[];
+  using S = Smem<D>;
+  S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr uint32_t kPart = kRows * 128, kChunkPart = kChunkRows * 128;
+  constexpr int kParts = D / 64;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    mbar_init(s32(&sm.st_full), 1);
+    mbar_init(s32(&sm.st_empty), 1);
+    for (int s = 0; s < S::kSlots; ++s) { mbar_init(s32(&sm.ring_full[s]), 1); mbar_init(s32(&sm.ring_empty[s]), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s32(&sm.sd_full[i]), 1); mbar_init(s32(&sm.p_full[i]), 128); }
+    mbar_init(s32(&sm.acc_full), 1);
+    mbar_init(s32(&sm.acc_free), 256);
+    mbar_init(s32(&sm.drain), 1);
+    sm.abort = 0;
+    cta_publish_barriers();
+  }
+  const int first_item = (int)blockIdx.x + await_stream();
+  const uint32_t tmem = cta_tmem_alloc(warp == 9, &sm.tmem_base, kTmemCols);
+  volatile int* abort = &sm.abort;
+  Item<KEYS> it;
+
+  if (warp == 8) {
+    // ------------------------------------------------------------- TMA producer
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (lane == 0) {
+      uint32_t cc = 0, items = 0;
+      bool ok = true;
+#ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
+      total = 0;  // test build only: nothing is ever loaded
+#endif
+      for (int index = first_item; index < total && ok; index += gridDim.x) {
+        it.make(g, a, index);
+        if (it.chunks == 0) continue;
+        ok = wait_here(s32(&sm.st_empty), (items & 1) ^ 1, abort, status);
+        if (!ok) break;
+        mbar_expect_tx(s32(&sm.st_full), 2 * S::kTileBytes);
+#pragma unroll
+        for (int c = 0; c < kParts; ++c) {
+          tma_load_4d(s32(sm.x0) + c * kPart, &map_x0, s32(&sm.st_full), 64 * c, it.row0, (KEYS ? it.hk : it.head) * fx0.h, it.b * fx0.b);
+          tma_load_4d(s32(sm.y0) + c * kPart, &map_y0, s32(&sm.st_full), 64 * c, it.row0, (KEYS ? it.hk : it.head) * fy0.h, it.b * fy0.b);
+        }
+        ++items;
+        for (int n = 0; n < it.chunks; ++n, ++cc) {
+          const uint32_t s = cc % S::kSlots, bar = s32(&sm.ring_full[s]);
+          ok = wait_here(s32(&sm.ring_empty[s]), ((cc / S::kSlots) & 1) ^ 1, abort, status);
+          if (!ok) break;
+          int h, start, cols;
+          it.chunk(n, h, start, cols);
+          mbar_expect_tx(bar, 2 * S::kChunkBytes + (KEYS ? 2 * kChunkRows * 4 : 0));
+#pragma unroll
+          for (int c = 0; c < kParts; ++c) {
+            tma_load_4d(s32(sm.ring[s].x) + c * kChunkPart, &map_x, bar, 64 * c, start, h * fx.h, it.b * fx.b);
+            tma_load_4d(s32(sm.ring[s].y) + c * kChunkPart, &map_y, bar, 64 * c, start, h * fy.h, it.b * fy.b);
+          }
+          if constexpr (KEYS) {
+            const long long at = ((long long)it.b * g.H + h) * a.pad + start;  // start is a multiple of 64
+            bulk_load(s32(sm.stat[s][0]), a.neg_lse2 + at, kChunkRows * 4, bar);
+            bulk_load(s32(sm.stat[s][1]), a.neg_d + at, kChunkRows * 4, bar);
+          }
+        }
+      }
+      // copies must have landed, and their readers be done, before the CTA's memory is released
+      const uint32_t first = cc > S::kSlots ? cc - S::kSlots : 0;
+      for (uint32_t s = first; s < cc; ++s) {
+        if (*abort) mbar_drain(s32(&sm.ring_full[s % S::kSlots]), (s / S::kSlots) & 1);
+        else wait_here(s32(&sm.ring_empty[s % S::kSlots]), (s / S::kSlots) & 1, abort, status);
+      }
+      if (*abort && items) mbar_drain(s32(&sm.st_full), (items - 1) & 1);
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------- all products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    constexpr uint32_t idesc_sd = make_idesc(false, 64u, F16), idesc_acc = make_idesc(true, (uint32_t)D, F16);
+    uint32_t cc = 0, items = 0;
+    bool ok = true;
+    // the sums of chunk c (its P and dS are ready), the `fresh` ones starting anew
+    auto add = [&](uint32_t c, bool fresh, bool last) {
+      const uint32_t s = c % S::kSlots, buf = c & 1;
+      ok = warp_wait_here(s32(&sm.p_full[buf]), (c >> 1) & 1, abort, status);
+      if (!ok) return;
+      tc_fence_after();
+      const uint64_t xd = mn_major(s32(sm.ring[s].x), kChunkPart), yd = mn_major(s32(sm.ring[s].y), kChunkPart);
+      if (elect_one()) {
+        if constexpr (KEYS) {
+#pragma unroll
+          for (int kk = 0; kk < kChunkRows / 16; ++kk)
+            umma_ts(tmem + kColAcc + D, tmem + 128 * buf + 8 * kk, yd + (uint64_t)((2048 * kk) >> 4), idesc_acc, !fresh || kk > 0);
+        }
+#pragma unroll
+        for (int kk = 0; kk < kChunkRows / 16; ++kk)
+          umma_ts(tmem + kColAcc, tmem + 128 * buf + 64 + 8 * kk, xd + (uint64_t)((2048 * kk) >> 4), idesc_acc, !fresh || kk > 0);
+        tc_commit(s32(&sm.ring_empty[s]));
+        if (last) tc_commit(s32(&sm.acc_full));
+      }
+      __syncwarp();
+    };
+    for (int index = first_item; index < total && ok; index += gridDim.x) {
+      it.make(g, a, index);
+      if (it.chunks == 0) continue;
+      ok = warp_wait_here(s32(&sm.st_full), items & 1, abort, status);
+      if (!ok) break;
+      const uint64_t x0d = smem_desc(s32(sm.x0)), y0d = smem_desc(s32(sm.y0));
+      for (int n = 0; n <= it.chunks && ok; ++n) {
+        if (n < it.chunks) {
+          const uint32_t c = cc + n, s = c % S::kSlots, buf = c & 1;
+          ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);
+          if (!ok) break;
+          int h, start, cols;
+          it.chunk(n, h, start, cols);
+          const int there = (KEYS ? it.ql : it.kl) - start;  // rows of the chunk that exist
+          if (there < kChunkRows && start + there < (KEYS ? g.Nq : g.Nk)) {
+            zero_rows<D>(sm.ring[s].x, there, kChunkRows, lane);
+            if constexpr (KEYS) zero_rows<D>(sm.ring[s].y, there, kChunkRows, lane);
+          }
+          tc_fence_after();
+          const uint64_t xd = smem_desc(s32(sm.ring[s].x)), yd = smem_desc(s32(sm.ring[s].y));
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              umma_ss(tmem + 128 * buf, k_major(x0d, kk, kPart), k_major(xd, kk, kChunkPart), idesc_sd, kk > 0);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              umma_ss(tmem + 128 * buf + 64, k_major(y0d, kk, kPart), k_major(yd, kk, kChunkPart), idesc_sd, kk > 0);
+            tc_commit(s32(&sm.sd_full[buf]));
+            if (n == it.chunks - 1) tc_commit(s32(&sm.st_empty));
+          }
+          __syncwarp();
+        }
+        if (n > 0) {
+          if (n == 1 && items > 0) ok = warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
+          if (ok) add(cc + n - 1, n == 1, n == it.chunks);
+        }
+      }
+      cc += it.chunks;
+      ++items;
+    }
+    if (*abort) {
+      if (elect_one()) mma_drain(s32(&sm.drain));
+      __syncwarp();
+    }
+  } else if (warp >= 10) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  } else {
+    // ------------------------------------------------------------- row threads
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
+    const int grp = warp >> 2, row = tid & 127;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tb = tmem + lane_off + 128 * grp;  // a group's chunks are all in its own buffer
+    const uint64_t scale2 = pack2(g.scale_log2, g.scale_log2);
+    uint32_t cc = 0, items = 0;
+    bool ok = true;
+    for (int index = first_item; index < total && ok; index += gridDim.x) {
+      it.make(g, a, index);
+      const int r = it.row0 + row;
+      float nl = 0.f, nd = 0.f;
+      if (!KEYS && it.chunks > 0 && row < it.rows) {
+        const long long at = ((long long)it.b * g.H + it.head) * a.pad + r;
+        nl = __ldg(a.neg_lse2 + at);
+        nd = __ldg(a.neg_d + at);
+      }
+      const uint64_t nl2 = pack2(nl, nl), nd2 = pack2(nd, nd);
+      for (int n = (int)((cc ^ (uint32_t)grp) & 1); n < it.chunks; n += 2) {
+        const uint32_t c = cc + n, s = c % S::kSlots;
+        int h, start, cols;
+        it.chunk(n, h, start, cols);
+        // columns that the row sees: [from, upto), and the first `sink`; and whether all rows see all of them
+        int from, upto, sink = 0;
+        bool whole;
+        if constexpr (KEYS) {
+          from = r - it.off - start;
+          upto = r < g.sinks ? cols : min(cols, r + g.window - it.off - start);
+          whole = cols == kChunkRows && it.off + start >= it.row0 + kRows - 1 && it.off + start + kChunkRows <= it.row0 + g.window;
+        } else {
+          const int p = it.off + r;
+          from = p - g.window + 1 - start;
+          upto = min(cols, p - start + 1);
+          sink = g.sinks - start;
+          whole = cols == kChunkRows && start + kChunkRows <= it.off + it.row0 + 1 &&
+                  (start + kChunkRows <= g.sinks || start > it.off + it.row0 + kRows - 1 - g.window);
+        }
+        ok = warp_wait_here(s32(&sm.sd_full[grp]), (c >> 1) & 1, abort, status);
+        if (KEYS && ok) ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);  // (landed: for the copies' visibility)
+        if (!ok) break;
+        tc_fence_after();
+        // 32 columns at a time: P and dS, stored in the places of S and dP that have been read
+        auto part = [&](int half, auto masked) {
+          uint32_t sv[32], dv[32], pk[16], dk[16];
+          tmem_ld32(tb + 32 * half, sv);
+          tmem_ld32(tb + 64 + 32 * half, dv);
+          tmem_wait_ld();
+          const uint32_t see = low_bits(upto - 32 * half) & (~low_bits(from - 32 * half) | low_bits(sink - 32 * half));
+          const float* st = &sm.stat[s][0][32 * half];
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            uint64_t l01 = nl2, l23 = nl2, d01 = nd2, d23 = nd2;
+            if constexpr (KEYS) {
+              const float4 l4 = *reinterpret_cast<const float4*>(st + x), d4 = *reinterpret_cast<const float4*>(st + kChunkRows + x);
+              l01 = pack2(l4.x, l4.y); l23 = pack2(l4.z, l4.w);
+              d01 = pack2(d4.x, d4.y); d23 = pack2(d4.z, d4.w);
+            }
+            float y0, y1, y2, y3, p2, p3;
+            const uint64_t y01 = fma2(pack2(__uint_as_float(sv[x]), __uint_as_float(sv[x + 1])), scale2, l01);
+            const uint64_t y23 = fma2(pack2(__uint_as_float(sv[x + 2]), __uint_as_float(sv[x + 3])), scale2, l23);
+            unpack2(y01, y0, y1);
+            unpack2(y23, y2, y3);
+            float p0 = ex2(y0), p1 = ex2(y1);
+            if (!decltype(masked)::value && ((x >> 2) & 1)) { ex2_quartic(y23, p2, p3); } else { p2 = ex2(y2); p3 = ex2(y3); }
+            float e0, e1, e2, e3;
+            unpack2(mul2(pack2(p0, p1), add2(pack2(__uint_as_float(dv[x]), __uint_as_float(dv[x + 1])), d01)), e0, e1);
+            unpack2(mul2(pack2(p2, p3), add2(pack2(__uint_as_float(dv[x + 2]), __uint_as_float(dv[x + 3])), d23)), e2, e3);
+            if (decltype(masked)::value) {
+              const bool v0 = (see >> x) & 1u, v1 = (see >> (x + 1)) & 1u, v2 = (see >> (x + 2)) & 1u, v3 = (see >> (x + 3)) & 1u;
+              p0 = v0 ? p0 : 0.f; p1 = v1 ? p1 : 0.f; p2 = v2 ? p2 : 0.f; p3 = v3 ? p3 : 0.f;
+              e0 = v0 ? e0 : 0.f; e1 = v1 ? e1 : 0.f; e2 = v2 ? e2 : 0.f; e3 = v3 ? e3 : 0.f;
+            }
+            pk[x >> 1] = pack2<F16>(p0, p1);
+            pk[(x >> 1) + 1] = pack2<F16>(p2, p3);
+            dk[x >> 1] = pack2<F16>(e0, e1);
+            dk[(x >> 1) + 1] = pack2<F16>(e2, e3);
+          }
+          if constexpr (KEYS) tmem_st16(tb + 16 * half, pk);
+          tmem_st16(tb + 64 + 16 * half, dk);
+        };
+        if (whole) {
+          part(0, std::false_type{});
+          part(1, std::false_type{});
+        } else {
+          part(0, std::true_type{});
+          part(1, std::true_type{});
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(s32(&sm.p_full[grp]));
+      }
+      if (!ok) break;
+      cc += it.chunks;
+      // results: the groups share dq's columns; or group 0 writes dv, group 1 dk
+      if (it.chunks > 0) {
+        ok = warp_wait_here(s32(&sm.acc_full), items & 1, abort, status);
+        if (!ok) break;
+        ++items;
+        tc_fence_after();
+      }
+      constexpr int kCols = KEYS ? D : D / 2;
+      const uint32_t ta = tmem + lane_off + kColAcc + (KEYS ? (grp ? 0 : D) : grp * (D / 2));
+      const View& out = KEYS && grp == 0 ? a.dy0 : a.dx0;
+      const float f = KEYS && grp == 0 ? 1.f : g.scale;
+      const bool sink_row = KEYS && r < g.sinks && a.pieces > 0 && it.row0 == 0;
+      char* dst = out.data + it.b * out.sb + (KEYS ? it.hk : it.head) * out.sh + (long long)r * out.sn + (KEYS ? 0 : grp * D);
+      float* sums = a.partial + ((((long long)it.b * g.Hkv + it.hk) * (a.pieces + 1) + it.piece) * 2 + (grp == 0)) * g.sinks * D + (long long)r * D;
+#pragma unroll 1
+      for (int part = 0; part < kCols / 32; ++part) {
+        uint32_t v[32];
+        if (it.chunks > 0) {
+          tmem_ld32(ta + 32 * part, v);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] = 0u;
+        }
+        if (row < it.rows && sink_row) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 4)
+            *reinterpret_cast<float4*>(sums + 32 * part + x) = make_float4(__uint_as_float(v[x]) * f, __uint_as_float(v[x + 1]) * f,
+                                                                           __uint_as_float(v[x + 2]) * f, __uint_as_float(v[x + 3]) * f);
+        } else if (row < it.rows && it.piece == 0) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) w[y] = pack2<F16>(__uint_as_float(v[x + 2 * y]) * f, __uint_as_float(v[x + 2 * y + 1]) * f);
+            *reinterpret_cast<uint4*>(dst + 64 * part + 2 * x) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (it.chunks > 0) {
+        tc_fence_before();
+        mbar_arrive(s32(&sm.acc_free));
+      }
+    }
+  }
+  cta_tmem_free(warp == 9, tmem, kTmemCols);
+}
+
+// -lse in base 2 and -D = -<dO, O> of every row, eight lanes a row.  Rows that do not exist, and rows that see nothing (whose
+// weights are masked whatever stands here), get zeros.  Clears the status block.
+namespace {
+template <int D, bool F16>
+__global__ void __launch_bounds__(256) window_rows_kernel(const WinGeo g, const View o, const View d_o, const float* __restrict__ lse,
+                                                          float* __restrict__ neg_lse2, float* __restrict__ neg_d, int pad, int* status) {
+  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x + await_stream()) >> 3;
+  if (blockIdx.x == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
+  const int part = threadIdx.x & 7;
+  if (at >= (long long)g.B * g.H * pad) return;  // (whole rows: 32 rows a block)
+  const long long unit = at / pad;
+  const int i = (int)(at - unit * pad), b = (int)(unit / g.H), h = (int)(unit - (long long)b * g.H);
+  const bool there = i < span_of(g, b).ql;
+  float dot = 0.f;
+  if (there) {
+    const char *x = o.data + b * o.sb + h * o.sh + (long long)i * o.sn, *y = d_o.data + b * d_o.sb + h * d_o.sh + (long long)i * d_o.sn;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(x) + part + 8 * c), w = __ldg(reinterpret_cast<const uint4*>(y) + part + 8 * c);
+      const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float u0, u1, w0, w1;
+        unpack16x2(uw[k], F16, u0, u1);
+        unpack16x2(ww[k], F16, w0, w1);
+        dot = fmaf(u0, w0, fmaf(u1, w1, dot));
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 4; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
+  if (part == 0) {
+    const float l = there ? lse[unit * g.Nq + i] : 0.f;
+    neg_lse2[at] = l == -INFINITY ? 0.f : -l * 1.4426950408889634f;
+    neg_d[at] = -dot;
+  }
+}
+
+// The sinks' gradients: the window's part and the pieces', in order.
+template <int D, bool F16>
+__global__ void __launch_bounds__(256) window_sinks_kernel(const WinGeo g, const __grid_constant__ BwdArgs a) {
+  const int unit = (int)blockIdx.x + await_stream(), b = unit / g.Hkv, hk = unit - b * g.Hkv;
+  const Span s = span_of(g, b);
+  const int left = s.ql - first_tile_end(g, s), pieces = left > 0 ? (left + a.piece_rows - 1) / a.piece_rows : 0;
+  const int n = min(g.sinks, s.kl) * D, step = g.sinks * D;
+  const float* p = a.partial + (long long)unit * (a.pieces + 1) * 2 * step;
+  for (int e = 2 * (blockIdx.y * 256 + threadIdx.x); e < 2 * n; e += 512 * gridDim.y) {
+    const int which = e >= n, x = e - which * n;  // 0: dk, 1: dv; two channels
+    float2 v = make_float2(0.f, 0.f);
+    for (int k = 0; k <= pieces; ++k) {
+      const float2 w = *reinterpret_cast<const float2*>(p + (long long)(2 * k + which) * step + x);
+      v.x += w.x;
+      v.y += w.y;
+    }
+    const View& out = which ? a.dy0 : a.dx0;
+    *reinterpret_cast<uint32_t*>(out.data + b * out.sb + hk * out.sh + (long long)(x / D) * out.sn + 2 * (x % D)) = pack2<F16>(v.x, v.y);
+  }
+}
+
+template <int D, bool F16, bool KEYS>
+int launch_pass(const HostCtx& c, const WinGeo& g, const View& x0, const View& y0, const View& x, const View& y, const BwdArgs& a) {
+  CUtensorMap mx0, my0, mx, my;
+  const int h0 = KEYS ? g.Hkv : g.H, h1 = KEYS ? g.H : g.Hkv, n0 = KEYS ? g.Nk : g.Nq, n1 = KEYS ? g.Nq : g.Nk;
+  if (!make_map_view(&mx0, x0, D, n0, h0, g.B, kRows) || !make_map_view(&my0, y0, D, n0, h0, g.B, kRows) ||
+      !make_map_view(&mx, x, D, n1, h1, g.B, kChunkRows) || !make_map_view(&my, y, D, n1, h1, g.B, kChunkRows))
+    return MOSAIC_E_CUDA;
+  const size_t smem = sizeof(Smem<D>) + 1024;
+  static unsigned long long configured = 0;
+  int sms = 0;
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(window_bwd_kernel<D, F16, KEYS>), smem, &configured, &sms)) return rc;
+  const long long total = (long long)g.B * h0 * (a.tiles + a.pieces);
+  if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
+  return launch_kernel(window_bwd_kernel<D, F16, KEYS>, dim3((unsigned)(total < sms ? total : sms)), kThreads, smem, c.stream, true, 0, g,
+                       mx0, my0, mx, my, fold_of(x0), fold_of(y0), fold_of(x), fold_of(y), a, c.status, (int)total);
+}
+
+template <int D, bool F16>
+int launch(const HostCtx& c, const WinGeo& g, const WinBwd& t, const WinBwdWs& w, char* ws) {
+  const long long rows = (long long)g.B * g.H * w.pad, blocks = (rows * 8 + 255) / 256;
+  if (blocks > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
+  float *nl = (float*)(ws + w.neg_lse2), *nd = (float*)(ws + w.neg_d);
+  int rc = launch_kernel(window_rows_kernel<D, F16>, dim3((unsigned)blocks), 256, 0, c.stream, true, 0, g, t.o, t.d_o, t.lse, nl, nd, w.pad,
+                         c.status);
+  if (rc) return rc;
+  BwdArgs a = {t.dk, t.dv, nl, nd, (float*)(ws + w.partial), w.pad, (g.Nk + kRows - 1) / kRows, w.pieces, w.piece_rows};
+  if ((rc = launch_pass<D, F16, true>(c, g, t.k, t.v, t.q, t.d_o, a))) return rc;
+  if (w.pieces > 0) {
+    const int split = (2 * g.sinks * D + 511) / 512;
+    rc = launch_kernel(window_sinks_kernel<D, F16>, dim3((unsigned)(g.B * g.Hkv), (unsigned)split), 256, 0, c.stream, true, 0, g, a);
+    if (rc) return rc;
+  }
+  a.dx0 = t.dq;
+  a.tiles = (g.Nq + kRows - 1) / kRows;
+  a.pieces = 0;
+  return launch_pass<D, F16, false>(c, g, t.q, t.d_o, t.k, t.v, a);
+}
+}  // namespace
+
+WinBwdWs window_bwd_layout(const WinGeo& g) {
+  WinBwdWs w;
+  w.pad = (g.Nq + kRows - 1) / kRows * kRows;
+  // A piece of the sinks' further rows is as long as a tile's own list of a head.  Rows beyond tile 0's list have positions from
+  // kRows - 1 + window on; how many there are is only known on the device, this is the most.
+  w.piece_rows = (int)(((long long)g.window + kRows + kChunkRows - 1) / kChunkRows * kChunkRows);
+  const int behind = g.Nk - (kRows - 1) - g.window, beyond = behind < g.Nq ? behind : g.Nq;
+  w.pieces = g.sinks > 0 && beyond > 0 ? (beyond + w.piece_rows - 1) / w.piece_rows : 0;
+  size_t at = kStatusBytes;
+  w.neg_lse2 = at; at = align256(at + sizeof(float) * (size_t)g.B * g.H * w.pad);
+  w.neg_d = at; at = align256(at + sizeof(float) * (size_t)g.B * g.H * w.pad);
+  w.partial = at; at = align256(at + (w.pieces > 0 ? sizeof(float) * (size_t)g.B * g.Hkv * (w.pieces + 1) * 2 * g.sinks * g.d : 0));
+  w.total = at;
+  return w;
+}
+
+int launch_window_bwd(const HostCtx& c, const WinGeo& g, bool f16, const WinBwd& t, void* ws) {
+  const WinBwdWs w = window_bwd_layout(g);
+  if (g.d == 64) return f16 ? launch<64, true>(c, g, t, w, (char*)ws) : launch<64, false>(c, g, t, w, (char*)ws);
+  return f16 ? launch<128, true>(c, g, t, w, (char*)ws) : launch<128, false>(c, g, t, w, (char*)ws);
+}
+
+}  // namespace mosaic

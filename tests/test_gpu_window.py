@@ -169,3 +169,75 @@ def test_decode(case, dtype, layout, rolling):
     if B > 1:  # a member's bits do not depend on the others
         one = mb.mosaic_bsa_window_decode(wp, q[1:2], k[1:2], v[1:2], k_len=lens(full[1:2]))
         assert torch.equal(one[0], o.t[1:2]) and torch.equal(one[1], lse.t[1:2])
+
+
+def check_bwd(wp, q, k, v, d_o, q_len=None, k_len=None):
+    """dv: every weight rounds to 16 bits (u) and is off by E; dS: the same, and D comes from an o that rounded twice (2 u, its
+    weights and itself); each result rounds once.  fp16 has steps of 2^-25 for weights below its normal range, per key or row."""
+    want = ref.attention(q, k, v, wp.window, wp.sinks, wp.scale, q_len, k_len, d_o)
+    o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v, q_len=lens(q_len), k_len=lens(k_len))
+    outs = [G.Guarded(tuple(x.shape), x.dtype, fill=NAN) for x in (q, k, v)]
+    ws = G.Guarded((mb.window_workspace_bytes(wp, q, k, mb.OP_BWD),), torch.uint8)
+    mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, q_len=lens(q_len), k_len=lens(k_len), dq=outs[0].t, dk=outs[1].t, dv=outs[2].t,
+                             ws=ws.t)
+    mb.check_status(ws.t, "window_bwd")
+    ws.check("workspace")
+    E, u = score_error(q, k, wp.scale), torch.finfo(q.dtype).eps / 2
+    sc = wp.scale or q.shape[-1] ** -0.5
+    n = q.shape[2] * (q.shape[1] // k.shape[1])
+    sub = 2.0 ** -25 if q.dtype == torch.float16 else 0.0
+    lo = {"dq": sub * sc * k.shape[2] * float(torch.nan_to_num(k).abs().max()), "dk": sub * sc * n * float(torch.nan_to_num(q).abs().max()),
+          "dv": sub * n * float(torch.nan_to_num(d_o).abs().max())}
+    for name, x in zip(("dq", "dk", "dv"), outs):
+        x.check(name)
+        there = ~torch.isnan(want[name])
+        assert torch.isnan(x.t[~there]).all(), f"{name}: rows that do not exist were written"
+        assert not torch.isnan(x.t[there]).any(), name
+        f = (u + E) if name == "dv" else 2 * (u + E)
+        tol = u * want[name][there].abs() + f * want[name + "_abs"][there] + lo[name] + 1e-7
+        off = (x.t[there].double() - want[name][there]).abs()
+        assert (off <= tol).all(), f"{name}: over by {float((off - tol).max()):.3g}, worst {float(off.max()):.3g}"
+    again = mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, q_len=lens(q_len), k_len=lens(k_len))
+    for a, x, name in zip(again, outs, ("dq", "dk", "dv")):
+        there = ~torch.isnan(want[name])
+        assert torch.equal(a[there], x.t[there]), f"{name}: other bits the second time"
+    return want, [x.t for x in outs]
+
+
+BWD = CASES + [(1, 2, 1, 900, 900, 64, 64, 5), (1, 3, 1, 700, 1100, 128, 70, 100), (2, 2, 2, 1500, 1500, 64, 1, 3)]
+
+
+@pytest.mark.parametrize("case", BWD, ids=str)
+@pytest.mark.parametrize("dtype,layout", [("bf16", "bhnd"), ("fp16", "bnhd")])
+def test_backward(case, dtype, layout):
+    B, H, Hkv, Nq, Nk, d, window, sinks = case
+    q, k, v, d_o = make(B, H, Hkv, Nq, Nk, d, dtype, layout, seed=Nq + window + 1)
+    check_bwd(mb.WindowParams(window=window, sinks=sinks), q, k, v, d_o)
+
+
+@pytest.mark.parametrize("q_len,k_len", [
+    ([0, 1, 300, 17], [0, 1, 300, 900]),
+    ([300, 200, 5, 128], [100, 0, 900, 128]),
+    ([1, 1, 1, 299], [900, 899, 1, 900]),
+])
+@pytest.mark.parametrize("d,G_", [(64, 1), (128, 3)])
+def test_backward_of_ragged_lengths(q_len, k_len, d, G_):
+    q, k, v, d_o = make(4, 2 * G_, 2, 300, 900, d, seed=6)
+    for b in range(4):
+        q[b, :, q_len[b]:] = d_o[b, :, q_len[b]:] = NAN
+        k[b, :, k_len[b]:] = NAN
+        v[b, :, k_len[b]:] = math.inf
+    for W, S in ((150, 3), (20, 70)):
+        wp = mb.WindowParams(window=W, sinks=S)
+        want = ref.attention(q, k, v, W, S, 0.0, q_len, k_len, d_o)
+        o = torch.full_like(q, NAN)  # what lies behind the sequences is never used
+        lse = torch.full(q.shape[:3], NAN, device="cuda")
+        mb.mosaic_bsa_window_fwd(wp, q, k, v, q_len=lens(q_len), k_len=lens(k_len), o=o, lse=lse)
+        got = [torch.full_like(x, 7.0) for x in (q, k, v)]
+        mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, q_len=lens(q_len), k_len=lens(k_len), dq=got[0], dk=got[1], dv=got[2])
+        E, u = score_error(torch.nan_to_num(q), torch.nan_to_num(k), 0), torch.finfo(q.dtype).eps / 2
+        for name, x in zip(("dq", "dk", "dv"), got):
+            there = ~torch.isnan(want[name])
+            assert (x[~there] == 7).all(), name
+            tol = u * want[name][there].abs() + 2 * (u + E) * want[name + "_abs"][there] + 1e-7
+            assert ((x[there].double() - want[name][there]).abs() <= tol).all(), name
