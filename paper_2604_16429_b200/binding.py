@@ -371,147 +371,156 @@ def rotary_freqs(rp: RotaryParams, device="cuda") -> torch.Tensor:
     return out.to(device)
 
 
-def _chk_view(name, t, shape, like):
-    """`t` as a strided tensor of `shape` with contiguous rows, of `like`'s type and device."""
-    if t.dtype != like.dtype or t.device != like.device or t.shape != shape or t.stride(3) != 1:
-        raise ValueError(f"{name}: expected {like.dtype} {tuple(shape)} on {like.device} with contiguous rows, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
-    sb, sh, sn, _ = t.stride()
-    return _View(t.data_ptr(), sb, sh, sn)
+# Small calls are as long as what happens here before the launch (a rotation of 64 tokens: 24 us with a stream object, device
+# objects and a launch object made per call, 13 us so), hence the plain comparisons.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _chk_out(name, t, shape, like):
+def _bad(name, t, what):
+    return ValueError(f"{name}: expected {what}, got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+
+
+def _view(name, t, shape, dtype, index):
+    """`t` as a strided tensor of `shape` and `dtype` on cuda device `index`, its rows contiguous."""
+    st = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or st[3] != 1:
+        raise _bad(name, t, f"{dtype} {tuple(shape)} on cuda:{index} with contiguous rows")
+    return _View(t.data_ptr(), st[0], st[1], st[2])
+
+
+def _out(name, t, shape, dtype, index):
     """The same for an output, which may not write a place twice."""
-    v = _chk_view(name, t, shape, like)
-    if any(st == 0 and n > 1 for st, n in zip(t.stride(), shape)):
-        raise ValueError(f"{name}: rows of an output may not overlap, got strides {t.stride()}")
+    v = _view(name, t, shape, dtype, index)
+    if (v.sb == 0 and shape[0] > 1) or (v.sh == 0 and shape[1] > 1) or (v.sn == 0 and shape[2] > 1):
+        raise _bad(name, t, "rows that do not overlap")
     return v
 
 
+def _flat(name, t, shape, dtype, index):
+    """Pointer of a contiguous tensor."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        raise _bad(name, t, f"contiguous {dtype} {tuple(shape)} on cuda:{index}")
+    return t.data_ptr()
+
+
 def _chk_seq(q, k):
-    """Shapes of q [B,H,N,d] and k [B,Hkv,Nk,d]; (B, H, Hkv)."""
-    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda or q.dtype not in _STORAGE:
+    """The device of q [B,H,N,d] and k [B,Hkv,Nk,d]."""
+    index = q.get_device()
+    if q.dim() != 4 or k.dim() != 4 or index < 0 or q.dtype not in _STORAGE:
         raise ValueError(f"expected cuda tensors [B, heads, tokens, d] in bf16, fp16 or fp32, got {q.dtype} {tuple(q.shape)} on "
                          f"{q.device} and {tuple(k.shape)}")
-    return q.shape[0], q.shape[1], k.shape[1]
+    return index
 
 
-class _Launch:
-    """The stream of a call on the tensors' own device, which is made current for the call; what the call allocates is kept
-    from being handed out again before that stream has passed it."""
+def _new(t, stream):
+    """A tensor that the call itself made: not handed out again before `stream` has passed the call."""
+    if stream is not None:
+        t.record_stream(stream)
+    return t
 
-    def __init__(self, device, stream):
-        self.device, self.stream, self.new = device, stream, []
-        if stream is not None and stream.device != device:
-            raise ValueError(f"the stream belongs to {stream.device}, the tensors are on {device}")
 
-    def empty(self, shape, dtype):
-        return self.keep(torch.empty(shape, dtype=dtype, device=self.device))
+def _scratch(n, name, index, ws, stream):
+    """The caller's workspace, or one of n bytes."""
+    if ws is not None:
+        if ws.get_device() != index or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+            raise _bad("ws", ws, f"contiguous uint8 on cuda:{index}")
+        return ws
+    if n == 0:
+        raise MosaicError(-1, name)
+    return _new(torch.empty(n, dtype=torch.uint8, device=index), stream)
 
-    def keep(self, t):
-        if self.stream is not None:
-            t.record_stream(self.stream)
-        return t
 
-    def call(self, name, *args):
-        fn, index = getattr(lib(), name), self.device.index
-        if torch.cuda.current_device() == index:
-            rc = fn(*args, self.raw())
-        else:
-            with torch.cuda.device(index):
-                rc = fn(*args, self.raw())
-        if rc:
-            raise MosaicError(rc, name)
-
-    def raw(self):
-        return torch.cuda.current_stream(self.device).cuda_stream if self.stream is None else self.stream.cuda_stream
+def _call(name, index, stream, *args):
+    """The entry point on the tensors' own device, on `stream` or that device's current one."""
+    if stream is None:
+        raw = _raw_stream(index)
+    else:
+        if stream.device_index != index:
+            raise ValueError(f"the stream belongs to cuda:{stream.device_index}, the tensors are on cuda:{index}")
+        raw = stream.cuda_stream
+    fn = getattr(_lib or lib(), name)
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
+    if rc:
+        raise MosaicError(rc, name)
 
 
 def _rotary_params(rp, q, k, flags, eps):
-    B, H, Hkv = _chk_seq(q, k)
-    return _RotaryParams(B, H, Hkv, q.shape[2], rp.d, rp.rot, _STORAGE[q.dtype] | (FLAG_HALF_PAIRS if rp.half else 0) | flags,
-                         rp.amplitude, eps)
+    """(device, parameters, shape of q, shape of k)"""
+    index = _chk_seq(q, k)
+    B, H, N, _ = q.shape
+    Hkv = k.shape[1]
+    d = rp.d
+    return index, _RotaryParams(B, H, Hkv, N, d, rp.rot, _STORAGE[q.dtype] | (FLAG_HALF_PAIRS if rp.half else 0) | flags,
+                                rp.amplitude, eps), (B, H, N, d), (B, Hkv, N, d)
 
 
-def _chk_pos(rp, q, pos, freqs):
+def _positions(rp, pos, freqs, shape, index):
     """(pointer, stride) of the positions, and the frequencies' pointer."""
-    if rp.rot == 0:
+    rot = rp.rot
+    if rot == 0:
         return 0, 0, 0
-    B, N = q.shape[0], q.shape[2]
-    if (pos.dtype != torch.int64 or pos.device != q.device or tuple(pos.shape) not in ((N,), (B, N))
-            or (N > 1 and pos.stride(-1) != 1)):
-        raise ValueError(f"expected int64 positions [{N}] or [{B},{N}] on {q.device}, got {pos.dtype} {tuple(pos.shape)}")
-    if freqs.dtype != torch.float64 or freqs.device != q.device or not freqs.is_contiguous() or tuple(freqs.shape) != (rp.rot // 2,):
-        raise ValueError(f"expected fp64 frequencies [{rp.rot // 2}] on {q.device}, got {freqs.dtype} {tuple(freqs.shape)}")
-    return pos.data_ptr(), pos.stride(0) if pos.dim() == 2 and B > 1 else 0, freqs.data_ptr()
-
-
-def _chk_weights(rp, q, *ws):
-    for w in ws:
-        if w.dtype != torch.float32 or w.device != q.device or not w.is_contiguous() or tuple(w.shape) != (rp.d,):
-            raise ValueError(f"expected contiguous fp32 weights [{rp.d}] on {q.device}, got {w.dtype} {tuple(w.shape)}")
-
-
-def _rotary_shapes(rp, q, k):
-    return (q.shape[0], q.shape[1], q.shape[2], rp.d), (q.shape[0], k.shape[1], q.shape[2], rp.d)
+    B, _, N, _ = shape
+    if pos.dtype is not torch.int64 or pos.get_device() != index or (pos.shape != (B, N) and pos.shape != (N,)) or (
+            N > 1 and pos.stride(-1) != 1):
+        raise _bad("pos", pos, f"int64 [{N}] or [{B},{N}] on cuda:{index}")
+    return (pos.data_ptr(), pos.stride(0) if B > 1 and pos.dim() == 2 else 0,
+            _flat("freqs", freqs, (rot // 2,), torch.float64, index))
 
 
 def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=None, k_out=None, stream=None):
     """Rotary positions of q [B,H,N,d] and k [B,Hkv,N,d] by token index; pos [N] or [B,N] int64, freqs from `rotary_freqs`.
     `inverse` turns back (the transpose: what a backward applies to the gradients).  Returns (q_out, k_out)."""
-    p = _rotary_params(rp, q, k, FLAG_INVERSE if inverse else 0, 0.0)
-    sq, sk = _rotary_shapes(rp, q, k)
-    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
-    at, step, fr = _chk_pos(rp, q, pos, freqs)
-    run = _Launch(q.device, stream)
-    q_out = run.keep(torch.empty_like(q)) if q_out is None else q_out
-    k_out = run.keep(torch.empty_like(k)) if k_out is None else k_out
-    run.call("mosaic_bsa_rotary", p, vq, vk, at, step, fr, _chk_out("q_out", q_out, sq, q), _chk_out("k_out", k_out, sk, q))
+    index, p, sq, sk = _rotary_params(rp, q, k, FLAG_INVERSE if inverse else 0, 0.0)
+    t = q.dtype
+    vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
+    at, step, fr = _positions(rp, pos, freqs, sq, index)
+    q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
+    k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
+    _call("mosaic_bsa_rotary", index, stream, p, vq, vk, at, step, fr, _out("q_out", q_out, sq, t, index),
+          _out("k_out", k_out, sk, t, index))
     return q_out, k_out
 
 
 def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps=1e-6, q_out=None, k_out=None, stream=None):
     """Root-mean-square norm of every head of q and k (weights wq, wk [d] fp32), then the rotation, in one pass; with
     rp.rot_dim 0 the norm alone.  Returns (q_out, k_out)."""
-    p = _rotary_params(rp, q, k, 0, eps)
-    sq, sk = _rotary_shapes(rp, q, k)
-    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
-    at, step, fr = _chk_pos(rp, q, pos, freqs)
-    _chk_weights(rp, q, wq, wk)
-    run = _Launch(q.device, stream)
-    q_out = run.keep(torch.empty_like(q)) if q_out is None else q_out
-    k_out = run.keep(torch.empty_like(k)) if k_out is None else k_out
-    run.call("mosaic_bsa_qk_norm", p, vq, vk, wq.data_ptr(), wk.data_ptr(), at, step, fr, _chk_out("q_out", q_out, sq, q),
-             _chk_out("k_out", k_out, sk, q))
+    index, p, sq, sk = _rotary_params(rp, q, k, 0, eps)
+    t, f32, w = q.dtype, torch.float32, (rp.d,)
+    vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
+    at, step, fr = _positions(rp, pos, freqs, sq, index)
+    q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
+    k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
+    _call("mosaic_bsa_qk_norm", index, stream, p, vq, vk, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at, step,
+          fr, _out("q_out", q_out, sq, t, index), _out("k_out", k_out, sk, t, index))
     return q_out, k_out
 
 
 def qk_norm_workspace_bytes(rp: RotaryParams, q, k) -> int:
-    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_rotary_params(rp, q, k, 0, 0.0)))
+    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_rotary_params(rp, q, k, 0, 0.0)[1]))
 
 
 def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, d_k_out, eps=1e-6, dq=None, dk=None, dwq=None,
                            dwk=None, ws=None, stream=None):
     """Backward of mosaic_bsa_qk_norm from its inputs and its outputs' gradients.  Returns (dq, dk, dwq, dwk); the weights'
     gradients are [d] fp32."""
-    p = _rotary_params(rp, q, k, 0, eps)
-    sq, sk = _rotary_shapes(rp, q, k)
-    vq, vk = _chk_view("q", q, sq, q), _chk_view("k", k, sk, q)
-    gq, gk = _chk_view("d_q_out", d_q_out, sq, q), _chk_view("d_k_out", d_k_out, sk, q)
-    at, step, fr = _chk_pos(rp, q, pos, freqs)
-    run = _Launch(q.device, stream)
-    dq = run.keep(torch.empty_like(q)) if dq is None else dq
-    dk = run.keep(torch.empty_like(k)) if dk is None else dk
-    dwq = run.empty((rp.d,), torch.float32) if dwq is None else dwq
-    dwk = run.empty((rp.d,), torch.float32) if dwk is None else dwk
-    _chk_weights(rp, q, wq, wk, dwq, dwk)
-    if ws is None:
-        n = int(lib().mosaic_bsa_qk_norm_workspace_bytes(p))
-        if n == 0:
-            raise MosaicError(-1, "mosaic_bsa_qk_norm_workspace_bytes")
-        ws = run.empty((n,), torch.uint8)
-    run.call("mosaic_bsa_qk_norm_bwd", p, vq, vk, wq.data_ptr(), wk.data_ptr(), at, step, fr, gq, gk, _chk_out("dq", dq, sq, q),
-             _chk_out("dk", dk, sk, q), dwq.data_ptr(), dwk.data_ptr(), ws.data_ptr(), ws.numel())
+    index, p, sq, sk = _rotary_params(rp, q, k, 0, eps)
+    t, f32, w = q.dtype, torch.float32, (rp.d,)
+    vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
+    gq, gk = _view("d_q_out", d_q_out, sq, t, index), _view("d_k_out", d_k_out, sk, t, index)
+    at, step, fr = _positions(rp, pos, freqs, sq, index)
+    dq = _new(torch.empty_like(q), stream) if dq is None else dq
+    dk = _new(torch.empty_like(k), stream) if dk is None else dk
+    dwq = _new(torch.empty(w, dtype=f32, device=index), stream) if dwq is None else dwq
+    dwk = _new(torch.empty(w, dtype=f32, device=index), stream) if dwk is None else dwk
+    name = "mosaic_bsa_qk_norm_workspace_bytes"
+    ws = _scratch(0 if ws is not None else int(getattr(lib(), name)(p)), name, index, ws, stream)
+    _call("mosaic_bsa_qk_norm_bwd", index, stream, p, vq, vk, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at,
+          step, fr, gq, gk, _out("dq", dq, sq, t, index), _out("dk", dk, sk, t, index), _flat("dwq", dwq, w, f32, index),
+          _flat("dwk", dwk, w, f32, index), ws.data_ptr(), ws.numel())
     return dq, dk, dwq, dwk
 
 
@@ -524,51 +533,41 @@ class WindowParams:
     rolling: bool = False    # decode: the cache keeps the sinks and, in turn, the last positions that fit behind them
 
 
-def _window_params(wp, q, k, flags=0):
-    B, H, Hkv = _chk_seq(q, k)
-    if q.dtype == torch.float32:
+def _window_params(wp, q, k):
+    """(device, parameters, shape of k and v)"""
+    index = _chk_seq(q, k)
+    if q.dtype is torch.float32:
         raise ValueError("window attention takes bf16 or fp16 tensors")
-    return _WindowParams(B, H, Hkv, q.shape[2], k.shape[2], q.shape[3], wp.window, wp.sinks, wp.scale, _STORAGE[q.dtype] | flags)
+    B, H, Nq, d = q.shape
+    Hkv, Nk = k.shape[1], k.shape[2]
+    flags = _STORAGE[q.dtype] | (FLAG_ROLLING if wp.rolling else 0)
+    return index, _WindowParams(B, H, Hkv, Nq, Nk, d, wp.window, wp.sinks, wp.scale, flags), (B, Hkv, Nk, d)
 
 
 def window_workspace_bytes(wp: WindowParams, q, k, op: int) -> int:
-    return int(lib().mosaic_bsa_window_workspace_bytes(_window_params(wp, q, k), op))
+    return int(lib().mosaic_bsa_window_workspace_bytes(_window_params(wp, q, k)[1], op))
 
 
-def _window_ws(p, op, run, ws):
-    if ws is not None:
-        return ws
-    n = int(lib().mosaic_bsa_window_workspace_bytes(p, op))
-    if n == 0:
-        raise MosaicError(-1, "mosaic_bsa_window_workspace_bytes")
-    return run.empty((n,), torch.uint8)
+def _window_ws(p, op, index, ws, stream):
+    name = "mosaic_bsa_window_workspace_bytes"
+    return _scratch(0 if ws is not None else int(getattr(lib(), name)(p, op)), name, index, ws, stream)
 
 
-def _chk_len(name, t, q):
-    if t is None:
-        return 0
-    if t.dtype != torch.int32 or t.device != q.device or not t.is_contiguous() or tuple(t.shape) != (q.shape[0],):
-        raise ValueError(f"{name}: expected contiguous int32 [{q.shape[0]}] on {q.device}, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr()
-
-
-def _chk_lse(t, q):
-    if t.dtype != torch.float32 or t.device != q.device or not t.is_contiguous() or t.shape != q.shape[:3]:
-        raise ValueError(f"lse: expected contiguous fp32 {tuple(q.shape[:3])} on {q.device}, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr()
+def _len(name, t, p, index):
+    return 0 if t is None else _flat(name, t, (p.B,), torch.int32, index)
 
 
 def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=None, lse=None, ws=None, stream=None):
     """Forward of the sliding-window attention: q [B,H,Nq,d], k and v [B,Hkv,Nk,d]; the first q_len[b] and k_len[b] rows of a
     batch member exist (None: all), its queries are its last tokens.  Returns (o, lse)."""
-    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
-    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
-    run = _Launch(q.device, stream)
-    o = run.keep(torch.empty_like(q)) if o is None else o
-    lse = run.empty(q.shape[:3], torch.float32) if lse is None else lse
-    ws = _window_ws(p, OP_FWD, run, ws)
-    run.call("mosaic_bsa_window_fwd", p, vq, vk, vv, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
-             _chk_out("o", o, q.shape, q), _chk_lse(lse, q), ws.data_ptr(), ws.numel())
+    index, p, sk = _window_params(wp, q, k)
+    t, sq = q.dtype, q.shape
+    vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
+    o = _new(torch.empty_like(q), stream) if o is None else o
+    lse = _new(torch.empty(sq[:3], dtype=torch.float32, device=index), stream) if lse is None else lse
+    ws = _window_ws(p, OP_FWD, index, ws, stream)
+    _call("mosaic_bsa_window_fwd", index, stream, p, vq, vk, vv, _len("q_len", q_len, p, index), _len("k_len", k_len, p, index),
+          _out("o", o, sq, t, index), _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
     return o, lse
 
 
@@ -576,16 +575,17 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
                           stream=None):
     """Backward of the sliding-window attention from the forward's inputs, its o and lse, and the gradient of o.
     Returns (dq, dk, dv)."""
-    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
-    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
-    vo, vd = _chk_view("o", o, q.shape, q), _chk_view("d_o", d_o, q.shape, q)
-    run = _Launch(q.device, stream)
-    dq = run.keep(torch.empty_like(q)) if dq is None else dq
-    dk = run.keep(torch.empty_like(k)) if dk is None else dk
-    dv = run.keep(torch.empty_like(v)) if dv is None else dv
-    ws = _window_ws(p, OP_BWD, run, ws)
-    run.call("mosaic_bsa_window_bwd", p, vq, vk, vv, vo, _chk_lse(lse, q), vd, _chk_len("q_len", q_len, q), _chk_len("k_len", k_len, q),
-             _chk_out("dq", dq, q.shape, q), _chk_out("dk", dk, k.shape, q), _chk_out("dv", dv, k.shape, q), ws.data_ptr(), ws.numel())
+    index, p, sk = _window_params(wp, q, k)
+    t, sq = q.dtype, q.shape
+    vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
+    vo, vd = _view("o", o, sq, t, index), _view("d_o", d_o, sq, t, index)
+    dq = _new(torch.empty_like(q), stream) if dq is None else dq
+    dk = _new(torch.empty_like(k), stream) if dk is None else dk
+    dv = _new(torch.empty_like(v), stream) if dv is None else dv
+    ws = _window_ws(p, OP_BWD, index, ws, stream)
+    _call("mosaic_bsa_window_bwd", index, stream, p, vq, vk, vv, vo, _flat("lse", lse, sq[:3], torch.float32, index), vd,
+          _len("q_len", q_len, p, index), _len("k_len", k_len, p, index), _out("dq", dq, sq, t, index),
+          _out("dk", dk, sk, t, index), _out("dv", dv, sk, t, index), ws.data_ptr(), ws.numel())
     return dq, dk, dv
 
 
@@ -593,10 +593,11 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     """One new token per sequence: q [B,H,1,d] at position k_len[b] - 1 (None: the whole cache is filled), k and v [B,Hkv,Nk,d]
     with the token's own row in place.  `wp.rolling`: position j >= sinks lies in slot sinks + (j - sinks) % (Nk - sinks).
     Returns (o, lse)."""
-    p = _window_params(wp, q, k, FLAG_ROLLING if wp.rolling else 0)
-    vq, vk, vv = _chk_view("q", q, q.shape, q), _chk_view("k", k, (p.B, p.Hkv, p.Nk, p.d), q), _chk_view("v", v, k.shape, q)
-    run = _Launch(q.device, stream)
-    o = run.keep(torch.empty_like(q)) if o is None else o
-    lse = run.empty(q.shape[:3], torch.float32) if lse is None else lse
-    run.call("mosaic_bsa_window_decode", p, vq, vk, vv, _chk_len("k_len", k_len, q), _chk_out("o", o, q.shape, q), _chk_lse(lse, q))
+    index, p, sk = _window_params(wp, q, k)
+    t, sq = q.dtype, q.shape
+    vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
+    o = _new(torch.empty_like(q), stream) if o is None else o
+    lse = _new(torch.empty(sq[:3], dtype=torch.float32, device=index), stream) if lse is None else lse
+    _call("mosaic_bsa_window_decode", index, stream, p, vq, vk, vv, _len("k_len", k_len, p, index), _out("o", o, sq, t, index),
+          _flat("lse", lse, sq[:3], torch.float32, index))
     return o, lse
