@@ -10,11 +10,16 @@
 // Only steps at the window's edges are masked element by element.
 //
 // Warps (384 threads, persistent, one CTA per SM): 0-3 and 4-7 softmax of tile 0 and 1 (thread = row = TMEM lane), 8 TMA, 9 and 10
-// the products of tile 0 and 1.  While the softmax warps of one tile work, the tensor core adds P V of the other one and forms its
-// next Q K^T.  TMEM (512 columns): S of tile t at 128 t (fp32), P over its first half (16 bit), O at 256 + d t.
-// Softmax in base 2 with the scale folded in; the maximum moves (and O is scaled) only when it grows by more than 2^8; a
-// quarter of the exponentials run on the FMA pipe, because MUFU gives 16 a clock and SM against 4 d tensor FLOP each.
+// the products of tile 0 and 1.  TMEM (512 columns): two score buffers of a tile at 128 t + 64 b (fp32), P over a buffer's first
+// half (16 bit), O at 256 + d t.  Q K^T of a step is issued ahead of P V of the step before, so that the tensor core fills one
+// buffer while the softmax warps work on the other.  Softmax in base 2 with the scale folded in; the maximum moves (and O is
+// scaled) only when it grows by more than 2^8.
 // Every wait is bounded (status MOSAIC_E_DEVICE_TIMEOUT, copies and products in flight awaited, TMEM freed).
+//
+// Bound by the softmax warps: a step of 64 keys takes 1630 cycles at d = 64 and 1950 at d = 128, of which MUFU is busy 1024 (two
+// warps a scheduler), the tensor core 680 and 1310.  Measured beside it (us of 8192 tokens, 16 heads of 128 on 4, window 1024; this
+// form 91): one warp for both tiles' products 111, 128 keys a step 102, a quarter or an eighth of the exponentials on the FMA pipe
+// 101 and 92; a step's two buffers in the hands of two warpgroups each, which pass the running maximum on, 118.
 #include <type_traits>
 
 #include "window.cuh"
@@ -28,36 +33,26 @@ constexpr int kThreads = 384;
 // launched with (384 threads of 168, which is what the compiler reports), or the increase would wait for good.
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * kLaunchRegs, "the shares exceed the launch's registers");
-constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kTmemCols = 512, kColO = 256;  // S, and P over it, below; O of tile t at kColO + d t
 constexpr float kRescaleThreshold = 8.0f;  // log2 units: P stays below 2^8
 
-// How a tile's scores and weights lie in tensor memory
-template <int D>
-struct Plan {
-  static constexpr bool kApart = D == 64;        // P has columns of its own
-  static constexpr int U = kApart ? 128 : 64;    // keys of a step
-  static constexpr int kBufs = kApart ? 1 : 2;   // score buffers
-  __host__ __device__ static constexpr uint32_t scores(int t, int b) { return 128 * t + 64 * b; }
-  __host__ __device__ static constexpr uint32_t weights(int t, int b) { return kApart ? 256 + 64 * t : 128 * t + 64 * b; }
-  __host__ __device__ static constexpr uint32_t sums(int t) { return kApart ? 384 + 64 * t : 256 + 128 * t; }
-  static constexpr int kTileBytes = kRows * D * 2, kSlotBytes = U * D * 2;
-  static constexpr int kSlots = 8;               // ring of key and value tiles
-};
+constexpr int U = 64;          // keys of a step
+constexpr int kSlots = 8;      // ring of key and value tiles
+__host__ __device__ constexpr uint32_t score_col(int t, uint32_t b) { return 128 * t + 64 * b; }
 
 template <int D>
 struct Smem {
-  using P = Plan<D>;
-  unsigned char q[2][P::kTileBytes];
-  unsigned char kv[P::kSlots][P::kSlotBytes];
+  static constexpr int kTileBytes = kRows * D * 2, kSlotBytes = U * D * 2;
+  unsigned char q[2][kTileBytes];
+  unsigned char kv[kSlots][kSlotBytes];
   uint4 rows[8][32 * 4];  // a softmax warp's 32 rows of 32 results on their way out
-  unsigned long long q_full[2], q_empty[2], kv_full[P::kSlots], kv_empty[P::kSlots];
-  unsigned long long s_full[2][2], s_free[2], p_full[2][2], pv_done[2], drain[2];
+  unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots];
+  unsigned long long s_full[2][2], p_full[2][2], pv_done[2], drain[2];
   uint32_t tmem_base;
   int abort;
 };
 
 // What a CTA does at a time: two tiles of a key/value head and the keys that they see.
-template <int U>
 struct Item {
   int b, hk;
   int kl, off, ql;
@@ -117,14 +112,13 @@ struct Item {
 };
 
 // All steps of a CTA's items, one after the other
-template <int U>
 struct Walk {
-  Item<U> it;
+  Item it;
   int index, n;
   template <bool UNIFORM = false>
   __device__ __forceinline__ bool seek(const WinGeo& g, int per, int total) {  // to the next item that has steps, from `index` on
     for (; index < total; index += gridDim.x) {
-      it.template make<UNIFORM>(g, per, index);
+      it.make<UNIFORM>(g, per, index);
       if (it.steps > 0) { n = 0; return true; }
     }
     return false;
@@ -147,9 +141,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                       const __grid_constant__ CUtensorMap map_v, const Fold fq, const Fold fk, const Fold fv, const View o,
                       float* __restrict__ lse, int* status, int per, int total) {
   extern __shared__ unsigned char smem_raw[];
-  using P = Plan<D>;
-  constexpr int U = P::U, kSlots = P::kSlots;
-  Smem<D>& sm = *reinterpret_cast<Smem<D>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  using S = Smem<D>;
+  S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr uint32_t kPart = kRows * 128, kSlotPart = U * 128;  // bytes of a tile's 64 channels
   constexpr int kParts = D / 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -163,7 +156,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(s32(&sm.s_full[t][b]), 1);
         mbar_init(s32(&sm.p_full[t][b]), 128);
       }
-      mbar_init(s32(&sm.s_free[t]), 128);
       mbar_init(s32(&sm.pv_done[t]), 1);
       mbar_init(s32(&sm.drain[t]), 1);
     }
@@ -182,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     uint32_t slot_no = 0, q_no[2] = {0, 0};
     bool ok = true;
-    Walk<U> w;
+    Walk w;
     w.index = (int)blockIdx.x + zero;
 #ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
     w.index = total;  // test build only: nothing is ever loaded, so that every wait for it runs out
@@ -192,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t s = slot_no % kSlots, bar = s32(&sm.kv_full[s]);
         ok = wait_here(s32(&sm.kv_empty[s]), ((slot_no / kSlots) & 1) ^ 1, abort, status);
         if (!ok) return;
-        mbar_expect_tx(bar, P::kSlotBytes);
+        mbar_expect_tx(bar, S::kSlotBytes);
 #pragma unroll
         for (int c = 0; c < kParts; ++c) tma_load_4d(s32(sm.kv[s]) + c * kSlotPart, map, bar, 64 * c, row, head * f.h, b * f.b);
         ++slot_no;
@@ -206,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok || w.it.hi[t] <= 0) continue;
             ok = wait_here(s32(&sm.q_empty[t]), (q_no[t] & 1) ^ 1, abort, status);
             if (!ok) continue;
-            mbar_expect_tx(s32(&sm.q_full[t]), P::kTileBytes);
+            mbar_expect_tx(s32(&sm.q_full[t]), S::kTileBytes);
 #pragma unroll
             for (int c = 0; c < kParts; ++c)
               tma_load_4d(s32(sm.q[t]) + c * kPart, &map_q, s32(&sm.q_full[t]), 64 * c, w.it.row0[t], w.it.head[t] * fq.h, w.it.b * fq.b);
@@ -233,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     constexpr uint32_t idesc_qk = make_idesc(false, 0u, F16), idesc_pv = make_idesc(true, (uint32_t)D, F16);
     const int t = warp - 9;
-    const uint32_t tco = tmem + P::sums(t);
+    const uint32_t tco = tmem + kColO + D * t;
     const uint64_t qd = smem_desc(s32(sm.q[t]));
     uint32_t slot_no = 0, u = 0, n_q = 0;
     bool ok = true;
@@ -242,14 +234,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t v_no = 0;
     int kks = 0, v_there = 0;  // keys of the step in sixteens; rows of the value tile that exist (beyond them it may hold anything)
     auto issue_pv = [&]() {  // of step u - 1
-      const uint32_t b = (u - 1) % P::kBufs;
+      const uint32_t b = (u - 1) % 2;
       ok = warp_wait_here(s32(&sm.kv_full[v_no % kSlots]), (v_no / kSlots) & 1, abort, status);
       if (!ok) return;
       unsigned char* vt = sm.kv[v_no % kSlots];
       if (v_there < 16 * kks) zero_rows<D>(vt, v_there, U, lane);
       const uint64_t vd = mn_major(s32(vt), kSlotPart);
-      const uint32_t tcp = tmem + P::weights(t, b);
-      ok = warp_wait_here(s32(&sm.p_full[t][b]), ((u - 1) / P::kBufs) & 1, abort, status);
+      const uint32_t tcp = tmem + score_col(t, b);
+      ok = warp_wait_here(s32(&sm.p_full[t][b]), ((u - 1) / 2) & 1, abort, status);
       if (!ok) return;
       tc_fence_after();
       if (elect_one()) {
@@ -266,9 +258,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       pending = false;
     };
-    Walk<U> w;
+    Walk w;
     w.index = __shfl_sync(0xffffffffu, (int)blockIdx.x + zero, 0);
-    for (bool more = w.template seek<true>(g, per, total); more && ok; more = w.template next<true>(g, per, total), slot_no += 2) {
+    for (bool more = w.seek<true>(g, per, total); more && ok; more = w.next<true>(g, per, total), slot_no += 2) {
       int start, cols;
       w.it.step(w.n, start, cols);
       const uint32_t k_slot = slot_no % kSlots, v_slot = (slot_no + 1) % kSlots;
@@ -291,13 +283,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = ok && warp_wait_here(s32(&sm.q_full[t]), n_q & 1, abort, status);
         ++n_q;
       }
-      const uint32_t id = idesc_n(idesc_qk, round32(cols)), b = u % P::kBufs;
-      const uint32_t tcs = tmem + P::scores(t, b);
+      const uint32_t id = idesc_n(idesc_qk, round32(cols)), b = u % 2;
+      const uint32_t tcs = tmem + score_col(t, b);
       const uint64_t kd = smem_desc(s32(sm.kv[k_slot]));
       ok = ok && warp_wait_here(s32(&sm.kv_full[k_slot]), (slot_no / kSlots) & 1, abort, status);
-      // The buffer is free: with P apart, once the softmax threads hold the scores before; otherwise P V of the step that last had
-      // the buffer was issued before, and one thread's products run in order
-      if (P::kApart && u > 0) ok = ok && warp_wait_here(s32(&sm.s_free[t]), (u - 1) & 1, abort, status);
+      // (the buffer is free: P V of the step that had it was issued before, and one thread's products run in order)
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -328,11 +318,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------- softmax of tile t, then epilogue
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int t = warp >> 2, row = tid & 127;
-    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), to = mine + P::sums(t);
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), to = mine + kColO + D * t;
     const uint64_t scale2 = pack2(g.scale_log2, g.scale_log2);
     uint32_t u = 0;
     bool ok = true;
-    Item<U> it;
+    Item it;
     for (int index = (int)blockIdx.x + zero; index < total && ok; index += gridDim.x) {
       it.make(g, per, index);
       const int i = it.row0_of(t) + row, p0 = it.off + it.row0_of(t), p = p0 + row;
@@ -340,11 +330,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int whole0 = p0 + kRows - g.window, whole1 = p0 + 1 - U;
       float m_ref = -INFINITY, l = 0.f;
       const int last = it.last_of(t), first = it.first_of(t);
-      for (int n = last < 0 || it.front ? 0 : first; n <= last; n = n + 1 == it.front ? first : n + 1) {
-        int start, cols;
-        it.step(n, start, cols);
-        const uint32_t b = u % P::kBufs, ts = mine + P::scores(t, b), tp = mine + P::weights(t, b);
-        ok = warp_wait_here(s32(&sm.s_full[t][b]), (u / P::kBufs) & 1, abort, status);
+      const int front = it.front, steps = last < 0 ? 0 : front + last + 1 - first, window0 = it.base + (first - 2 * front) * U;
+      for (int n = 0; n < steps; ++n) {
+        const int start = n < front ? n * U : window0 + n * U, cols = min(U, (n < front ? it.ns : it.end) - start);
+        const uint32_t b = u % 2, ts = mine + score_col(t, b);
+        ok = warp_wait_here(s32(&sm.s_full[t][b]), (u / 2) & 1, abort, status);
         if (!ok) break;
         tc_fence_after();
         bool need = false;
@@ -359,22 +349,30 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
-        // P of 32 keys
+        // P of 32 keys: the exponentials of eight are under way while the eight before are added up and rounded
         auto weights = [&](const uint32_t (&sc)[32], uint64_t negm2, uint32_t column) {
           uint32_t pk[16];
+          float e[4][8];
 #pragma unroll
-          for (int x = 0; x < 32; x += 4) {
-            float x0, x1, x2, x3, p2, p3;
-            const uint64_t y01 = fma2(pack2(__uint_as_float(sc[x]), __uint_as_float(sc[x + 1])), scale2, negm2);
-            const uint64_t y23 = fma2(pack2(__uint_as_float(sc[x + 2]), __uint_as_float(sc[x + 3])), scale2, negm2);
-            unpack2(y01, x0, x1);
-            unpack2(y23, x2, x3);
-            const float e0 = ex2(x0), e1 = ex2(x1);
-            if ((x >> 2) & 1) { ex2_quartic(y23, p2, p3); } else { p2 = ex2(x2); p3 = ex2(x3); }
-            sum_a = add2(sum_a, pack2(e0, e1));
-            sum_b = add2(sum_b, pack2(p2, p3));
-            pk[x >> 1] = pack2<F16>(e0, e1);
-            pk[(x >> 1) + 1] = pack2<F16>(p2, p3);
+          for (int x = 0; x < 5; ++x) {
+            if (x < 4) {
+#pragma unroll
+              for (int y = 0; y < 8; y += 2) {
+                float a, c;
+                unpack2(fma2(pack2(__uint_as_float(sc[8 * x + y]), __uint_as_float(sc[8 * x + y + 1])), scale2, negm2), a, c);
+                e[x][y] = ex2(a);
+                e[x][y + 1] = ex2(c);
+              }
+            }
+            if (x > 0) {
+#pragma unroll
+              for (int y = 0; y < 8; y += 4) {
+                sum_a = add2(sum_a, pack2(e[x - 1][y], e[x - 1][y + 1]));
+                sum_b = add2(sum_b, pack2(e[x - 1][y + 2], e[x - 1][y + 3]));
+                pk[(8 * (x - 1) + y) >> 1] = pack2<F16>(e[x - 1][y], e[x - 1][y + 1]);
+                pk[((8 * (x - 1) + y) >> 1) + 1] = pack2<F16>(e[x - 1][y + 2], e[x - 1][y + 3]);
+              }
+            }
           }
           tmem_st16(column, pk);
         };
@@ -387,57 +385,44 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           return fmaxf(a, c);
         };
-        const int below = min(p - start + 1, cols), from = p - g.window + 1 - start, sink = g.sinks - start;
-        // What the row does not see becomes -inf.  (The quartic makes 2^-125 of it, which no 16-bit product or fp32 sum of such
-        // weights notices beside a real one; a row without any is empty by its maximum.)  On an edge most groups of 32 keys are
-        // seen by all rows of the warp.
+        // What the row does not see becomes -inf.  On an edge most groups of 32 keys are seen by all rows of the warp.
         auto mask = [&](int c, uint32_t (&sc)[32]) {
-          const uint32_t see = low_bits(below - 32 * c) & (~low_bits(from - 32 * c) | low_bits(sink - 32 * c));
+          const int at = start + 32 * c;
+          const uint32_t see = low_bits(min(p + 1 - at, cols - 32 * c)) & (~low_bits(p + 1 - g.window - at) | low_bits(g.sinks - at));
           if (__all_sync(0xffffffffu, see == 0xffffffffu)) return;
 #pragma unroll
           for (int x = 0; x < 32; ++x) sc[x] = (see >> x) & 1u ? sc[x] : 0xff800000u;
-        };
-        // P V of the step before must be done before O is scaled and, with P apart, before P is overwritten
-        auto await_pv = [&]() {
-          ok = u == 0 || warp_wait_here(s32(&sm.pv_done[t]), (u - 1) & 1, abort, status);
-          tc_fence_after();
         };
         if (cols <= 32) {  // the sinks, or the end of a chunk
           uint32_t sc[32];
           tmem_ld32(ts, sc);
           tmem_wait_ld();
-          if (P::kApart) { tc_fence_before(); mbar_arrive(s32(&sm.s_free[t])); }
           mask(0, sc);
           move_max(largest(sc) * g.scale_log2);
           const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-          if (P::kApart) await_pv();
-          weights(sc, pack2(-m_use, -m_use), tp);
+          weights(sc, pack2(-m_use, -m_use), ts);
         } else {
-          uint32_t sc[U / 32][32];
-#pragma unroll
-          for (int c = 0; c < U / 32; ++c) tmem_ld32(ts + 32 * c, sc[c]);
+          uint32_t s0[32], s1[32];
+          tmem_ld32(ts, s0);
+          tmem_ld32(ts + 32, s1);
           tmem_wait_ld();
-          if (P::kApart) { tc_fence_before(); mbar_arrive(s32(&sm.s_free[t])); }
           if (start < whole0 || start > whole1) {
-#pragma unroll
-            for (int c = 0; c < U / 32; ++c) mask(c, sc[c]);
+            mask(0, s0);
+            mask(1, s1);
           }
-          float mx = fmaxf(largest(sc[0]), largest(sc[1]));
-          if constexpr (U == 128) mx = fmaxf(mx, fmaxf(largest(sc[2]), largest(sc[3])));
-          move_max(mx * g.scale_log2);  // scale > 0 commutes with max
+          move_max(fmaxf(largest(s0), largest(s1)) * g.scale_log2);  // scale > 0 commutes with max
           const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
           const uint64_t negm2 = pack2(-m_use, -m_use);
-          if (P::kApart) await_pv();
-#pragma unroll
-          for (int c = 0; c < U / 32; ++c) weights(sc[c], negm2, tp + 16 * c);
+          weights(s0, negm2, ts);
+          weights(s1, negm2, ts + 16);
         }
-        if (!ok) break;
-        float s0, s1;
-        unpack2(add2(sum_a, sum_b), s0, s1);
-        l += s0 + s1;
+        float la, lb;
+        unpack2(add2(sum_a, sum_b), la, lb);
+        l += la + lb;
         if (__any_sync(0xffffffffu, need)) {
-          if (!P::kApart) await_pv();
+          if (u > 0) ok = warp_wait_here(s32(&sm.pv_done[t]), (u - 1) & 1, abort, status);  // O is scaled between two products
           if (!ok) break;
+          tc_fence_after();
           const uint64_t alpha2 = pack2(alpha, alpha);
 #pragma unroll 1
           for (int part = 0; part < D / 32; ++part) {
@@ -508,8 +493,8 @@ namespace {
 template <int D, bool F16>
 int launch(const HostCtx& c, const WinGeo& g, const View& q, const View& k, const View& v, const View& o, float* lse) {
   CUtensorMap mq, mk, mv;
-  if (!make_map_view(&mq, q, D, g.Nq, g.H, g.B, kRows) || !make_map_view(&mk, k, D, g.Nk, g.Hkv, g.B, Plan<D>::U) ||
-      !make_map_view(&mv, v, D, g.Nk, g.Hkv, g.B, Plan<D>::U))
+  if (!make_map_view(&mq, q, D, g.Nq, g.H, g.B, kRows) || !make_map_view(&mk, k, D, g.Nk, g.Hkv, g.B, U) ||
+      !make_map_view(&mv, v, D, g.Nk, g.Hkv, g.B, U))
     return MOSAIC_E_CUDA;
   const size_t smem = sizeof(Smem<D>) + 1024;
   static unsigned long long configured = 0;
