@@ -21,8 +21,8 @@ namespace {
 enum { kBf16 = 0, kF16 = 1, kF32 = 2 };
 constexpr int kHeadThreads = 256, kHeadWarps = kHeadThreads / 32;
 constexpr int kMaxHeadDim = 256;
-constexpr int kAhead = 4;      // rows a lane group has in flight (forward)
-constexpr int kAheadBwd = 2;   // the same in the backward, where a row comes with its gradient
+constexpr int kCtas = 2;       // per SM
+constexpr int kAhead = 2;      // rows that a group of lanes has in flight
 
 struct HeadTensor {
   View x, g;  // input; gradient of the output (backward)
@@ -34,14 +34,36 @@ struct HeadArgs {
   HeadTensor t[2];
   const int64_t* pos;
   const double* freqs;
-  float* partial;  // backward: [CTAs, 2, d] sums of the weights' gradients
-  long long pos_stride, tokens;  // tokens: of all batch members
+  float* partial;  // backward: [CTAs, d] sums of the weights' gradients
+  long long pos_stride;
+  unsigned tokens, tasks, step;  // tokens of all batch members; tasks: tokens x parts; step: warps of the grid
+  int step_b, step_n;            // the step in members and tokens
+  unsigned k_step;               // backward: the same for the CTAs of K's rows, which come after q_ctas of Q's
+  int k_step_b, k_step_n, q_ctas;
   int N, d, rot, lanes, parts;
-  float amplitude, eps;
+  float amplitude, eps, inv_d;
 };
 
 template <int T>
 struct Vec { static constexpr int n = T == kF32 ? 4 : 8, bytes = T == kF32 ? 4 : 2; };
+
+// two fp32 numbers in one register pair (packed arithmetic)
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void one(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2f(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 template <int T>
 __device__ __forceinline__ void widen(const uint4& v, float (&f)[Vec<T>::n]) {
@@ -64,57 +86,85 @@ __device__ __forceinline__ uint4 narrow(const float (&f)[Vec<T>::n]) {
   }
 }
 
-// What a lane does in every row: its two pieces' channels, and the warp's share of rows.
+// What a lane does in every row: its two pieces' channels, and the warp's share of rows.  Neighbouring lanes have neighbouring
+// pieces, so that a load of either covers whole sectors.
 struct Place {
-  int ca, cb, first_pair;  // first channel of either piece; the pairs first_pair .. first_pair + V - 1 are this lane's
-  int group, groups;       // this lane's row of the `groups` rows that a warp takes at a time
-  bool on;                 // the lane has channels (d / 2V may be less than P)
+  int ca, cb;         // first channel of either piece
+  int group, groups;  // this lane's row of the `groups` rows that a warp takes at a time
+  bool on;            // the lane has channels (d / 2V may be less than P)
 };
 template <int T, bool HALF>
 __device__ __forceinline__ Place place(const HeadArgs& a, int lane) {
   constexpr int V = Vec<T>::n;
   Place p;
-  const int slot = lane & (a.lanes - 1), turning = a.rot / (2 * V);
+  const int slot = lane & (a.lanes - 1), turning = HALF ? a.rot / (2 * V) : 0, from = HALF ? a.rot : 0;
   p.on = slot * 2 * V < a.d;
-  p.ca = HALF && slot < turning ? slot * V : slot * 2 * V;
-  p.cb = HALF && slot < turning ? a.rot / 2 + slot * V : slot * 2 * V + V;
-  p.first_pair = slot * V;
+  p.ca = slot < turning ? slot * V : from + (slot - turning) * V;
+  p.cb = slot < turning ? a.rot / 2 + slot * V : from + (a.d - from) / 2 + (slot - turning) * V;
   p.group = lane / a.lanes;
   p.groups = 32 / a.lanes;
   return p;
 }
 
-// (cos, sin) of the token's angles, shared out over the warp; pairs that do not turn get (1, 0)
-template <int V>
-__device__ __forceinline__ void make_angles(const HeadArgs& a, long long pos, float2* cs, const Place& pl, int lane, float (&c)[V],
-                                            float (&s)[V]) {
+// Cosines and sines of a token's angles, of all its pairs and V more; pairs that do not turn have (1, 0), which stand there from the start
+constexpr int kAngles = kMaxHeadDim / 2 + 8;
+struct Angles {
+  float cosine[kAngles], sine[kAngles];
+};
+__device__ __forceinline__ void still_angles(const HeadArgs& a, Angles& t, int lane) {
+  for (int i = a.rot / 2 + lane; i < kAngles; i += 32) {
+    t.cosine[i] = 1.f;
+    t.sine[i] = 0.f;
+  }
+}
+// The token's angles, shared out over the warp
+__device__ __forceinline__ void make_angles(const HeadArgs& a, long long pos, Angles& t, int lane) {
+  __syncwarp();  // the token before has been read
   for (int i = lane; i < a.rot / 2; i += 32) {
     const double turns = (double)pos * (__ldg(a.freqs + i) * 0.31830988618379067154);  // half turns
     const float r = (float)(turns - 2.0 * rint(0.5 * turns));
     float sn, cn;
     sincospif(r, &sn, &cn);
-    cs[i] = make_float2(cn * fabsf(a.amplitude), sn * a.amplitude);  // the launcher negates the factor to turn back
-  }
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int i = pl.first_pair + j;
-    const float2 v = i < a.rot / 2 ? cs[i] : make_float2(1.f, 0.f);
-    c[j] = v.x;
-    s[j] = v.y;
+    t.cosine[i] = cn * fabsf(a.amplitude);
+    t.sine[i] = sn * a.amplitude;  // the launcher negates the factor to turn back
   }
   __syncwarp();
 }
+// N floats from an address that N floats align
+template <int N>
+__device__ __forceinline__ void read_floats(const float* p, float* out) {
+  if constexpr (N == 2) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    out[0] = v.x; out[1] = v.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p + j);
+      out[j] = v.x; out[j + 1] = v.y; out[j + 2] = v.z; out[j + 3] = v.w;
+    }
+  }
+}
 
+// Turns the pairs of a row's two pieces.  (The angles are read anew for every row: kept over a token's rows they cost sixteen registers,
+// which are worth a second CTA on the SM.)
 template <int V, bool HALF>
-__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (&c)[V], const float (&s)[V]) {
+__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const HeadArgs& args, const Place& pl) {
+  constexpr int N = HALF ? V : V / 2;  // pairs of one piece that lie side by side
+  float c[V], s[V];
+  const int i0 = HALF ? min(pl.ca, args.rot / 2) : pl.ca / 2;
+  read_floats<N>(t.cosine + i0, c);
+  read_floats<N>(t.sine + i0, s);
+  if constexpr (!HALF) {
+    read_floats<N>(t.cosine + pl.cb / 2, c + N);
+    read_floats<N>(t.sine + pl.cb / 2, s + N);
+  }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     float& x = HALF ? a[j] : j < V / 2 ? a[2 * j] : b[2 * j - V];
     float& y = HALF ? b[j] : j < V / 2 ? a[2 * j + 1] : b[2 * j - V + 1];
-    const float t = x * c[j] - y * s[j];
+    const float u = x * c[j] - y * s[j];
     y = x * s[j] + y * c[j];
-    x = t;
+    x = u;
   }
 }
 
@@ -124,192 +174,289 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
 }
 
 template <int V>
-__device__ __forceinline__ void load_weights(const float* w, const Place& pl, float (&wa)[V], float (&wb)[V]) {
+__device__ __forceinline__ void read_weights(const float* w, const Place& pl, float (&wa)[V], float (&wb)[V]) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    wa[j] = pl.on ? __ldg(w + pl.ca + j) : 0.f;
-    wb[j] = pl.on ? __ldg(w + pl.cb + j) : 0.f;
+  for (int j = 0; j < V; j += 4) {  // (a lane without channels reads what it multiplies with zeros)
+    const float4 x = *reinterpret_cast<const float4*>(w + (pl.on ? pl.ca : 0) + j), y = *reinterpret_cast<const float4*>(w + (pl.on ? pl.cb : 0) + j);
+    wa[j] = x.x; wa[j + 1] = x.y; wa[j + 2] = x.z; wa[j + 3] = x.w;
+    wb[j] = y.x; wb[j + 1] = y.y; wb[j + 2] = y.z; wb[j + 3] = y.w;
   }
 }
 
-// A token's rows of one tensor: `part` of `parts`
-__device__ __forceinline__ void rows_of(int heads, int part, int parts, int& r0, int& r1) {
-  r0 = (int)((long long)heads * part / parts);
-  r1 = (int)((long long)heads * (part + 1) / parts);
-}
+// Where a warp is: a batch of rows of one token.  The warps of the grid take tasks (a token, or a part of its rows) in turn; with
+// more than one part a token every warp has one task.
+struct Spot {
+  unsigned task, step;
+  int step_b, step_n;
+  int b, n, r0, r1;  // rows r0 .. r1 - 1 of the task are left
+  bool more;
+  __device__ __forceinline__ void start(const HeadArgs& a, unsigned first, int rows) {
+    task = first;
+    const unsigned token = task / (unsigned)a.parts, part = task - token * a.parts;
+    b = (int)(token / (unsigned)a.N);
+    n = (int)(token - b * (unsigned)a.N);
+    more = task < a.tasks;
+    r0 = (int)(rows * part / a.parts);
+    r1 = (int)(rows * (part + 1) / a.parts);
+  }
+  __device__ __forceinline__ void stride(unsigned by, int by_b, int by_n) {
+    step = by;
+    step_b = by_b;
+    step_n = by_n;
+  }
+  __device__ __forceinline__ void next(const HeadArgs& a, int rows) {
+    task += step;
+    more = a.parts == 1 && task < a.tasks && task >= step;
+    b += step_b;
+    n += step_n;
+    if (n >= a.N) { n -= a.N; ++b; }
+    r0 = 0;
+    r1 = rows;
+  }
+};
 
+// The warps walk their tasks with the next batch's rows already asked for.  A token's rows are Q's heads, then K's.
 template <int T, bool HALF, bool NORM>
 __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes;
-  __shared__ float2 angles[kHeadWarps][kMaxHeadDim / 2];
+  __shared__ alignas(16) Angles angles[kHeadWarps];
+  __shared__ alignas(16) float weights[2][kMaxHeadDim];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long task = (long long)blockIdx.x * kHeadWarps + warp + await_stream(), token = task / a.parts;
-  if (token >= a.tokens) return;
-  const int part = (int)(task - token * a.parts);
-  const long long b = token / a.N, n = token - b * a.N;
   const Place pl = place<T, HALF>(a, lane);
-  float c[V], s[V];
-  make_angles<V>(a, a.rot ? __ldg(a.pos + b * a.pos_stride + n) : 0, angles[warp], pl, lane, c, s);
-#pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
-    const HeadTensor& t = a.t[i];
-    int r0, r1;
-    rows_of(t.heads, part, a.parts, r0, r1);
-    const char* x = t.x.data + b * t.x.sb + n * t.x.sn;
-    char* y = t.y.data + b * t.y.sb + n * t.y.sn;
-    float wa[V], wb[V];
-    if constexpr (NORM) load_weights<V>(t.w, pl, wa, wb);
-    for (int r = r0 + pl.group; r - pl.group < r1; r += pl.groups * kAhead) {  // (the same trips for the whole warp)
-      uint4 va[kAhead], vb[kAhead];
+  const int heads = a.t[0].heads, rows = heads + a.t[1].heads, ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ;
+  Spot sp;
+  sp.start(a, blockIdx.x * kHeadWarps + warp + await_stream(), rows);
+  sp.stride(a.step, a.step_b, a.step_n);
+  uint4 va[kAhead], vb[kAhead];
+  const char *xq = nullptr, *xk = nullptr;  // the rows' first
+  auto find = [&]() {
+    xq = a.t[0].x.data + sp.b * a.t[0].x.sb + sp.n * a.t[0].x.sn + ca;
+    xk = a.t[1].x.data + sp.b * a.t[1].x.sb + sp.n * a.t[1].x.sn + ca - heads * a.t[1].x.sh;
+  };
+  auto fetch = [&]() {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int h = r + k * pl.groups;
-        va[k] = vb[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (h < r1 && pl.on) {
-          va[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.ca * SZ);
-          vb[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.cb * SZ);
+    for (int k = 0; k < kAhead; ++k) {
+      const int h = sp.r0 + pl.group + k * pl.groups;
+      va[k] = vb[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (h < sp.r1 && pl.on) {
+        const char* x = h < heads ? xq + h * a.t[0].x.sh : xk + h * a.t[1].x.sh;
+        va[k] = *reinterpret_cast<const uint4*>(x);
+        vb[k] = *reinterpret_cast<const uint4*>(x + ba);
+      }
+    }
+  };
+  long long pos = 0;
+  if (sp.more) {
+    find();
+    fetch();
+    if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
+  }
+  still_angles(a, angles[warp], lane);
+  if constexpr (NORM) {
+    for (int c = threadIdx.x; c < 2 * a.d; c += kHeadThreads) weights[c >= a.d][c >= a.d ? c - a.d : c] = __ldg(c < a.d ? a.t[0].w + c : a.t[1].w + (c - a.d));
+    __syncthreads();
+  }
+  bool turned = false;  // the angles are this token's
+  while (sp.more) {
+    uint4 wa[kAhead], wb[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) { wa[k] = va[k]; wb[k] = vb[k]; }
+    const int r0 = sp.r0, r1 = sp.r1;
+    char* yq = a.t[0].y.data + sp.b * a.t[0].y.sb + sp.n * a.t[0].y.sn + ca;
+    char* yk = a.t[1].y.data + sp.b * a.t[1].y.sb + sp.n * a.t[1].y.sn + ca - heads * a.t[1].y.sh;
+    const long long p = pos;
+    const bool fresh = !turned;
+    turned = true;
+    sp.r0 += kAhead * pl.groups;
+    if (sp.r0 >= sp.r1) {
+      sp.next(a, rows);
+      turned = false;
+      if (sp.more) {
+        find();
+        if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
+      }
+    }
+    if (sp.more) fetch();
+    if (fresh) make_angles(a, p, angles[warp], lane);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int h = r0 + pl.group + k * pl.groups;
+      if (h - pl.group >= r1) break;
+      float fa[V], fb[V];
+      widen<T>(wa[k], fa);
+      widen<T>(wb[k], fb);
+      if constexpr (NORM) {
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) ss = fmaf(fa[j], fa[j], fmaf(fb[j], fb[j], ss));
+        const float rr = rsqrtf(row_sum(ss, a.lanes) * a.inv_d + a.eps);
+        float ga[V], gb[V];
+        read_weights<V>(weights[h >= heads], pl, ga, gb);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          fa[j] *= rr * ga[j];
+          fb[j] *= rr * gb[j];
         }
       }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int h = r + k * pl.groups;
-        if (h - pl.group >= r1) break;
-        float fa[V], fb[V];
-        widen<T>(va[k], fa);
-        widen<T>(vb[k], fb);
-        if constexpr (NORM) {
-          float ss = 0.f;
-#pragma unroll
-          for (int j = 0; j < V; ++j) ss = fmaf(fa[j], fa[j], fmaf(fb[j], fb[j], ss));
-          const float rr = rsqrtf(row_sum(ss, a.lanes) / (float)a.d + a.eps);
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            fa[j] *= rr * wa[j];
-            fb[j] *= rr * wb[j];
-          }
-        }
-        turn<V, HALF>(fa, fb, c, s);
-        if (h < r1 && pl.on) {
-          *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.ca * SZ) = narrow<T>(fa);
-          *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.cb * SZ) = narrow<T>(fb);
-        }
+      turn<V, HALF>(fa, fb, angles[warp], a, pl);
+      if (h < r1 && pl.on) {
+        char* y = h < heads ? yq + h * a.t[0].y.sh : yk + h * a.t[1].y.sh;
+        *reinterpret_cast<uint4*>(y) = narrow<T>(fa);
+        *reinterpret_cast<uint4*>(y + ba) = narrow<T>(fb);
       }
     }
   }
 }
 
-// Persistent: the sums of the weights' gradients stay in registers over a CTA's tokens (a lane has the same channels in every
-// row), and every CTA leaves one row of partial sums.
+// The sums of the weights' gradients stay in registers over a CTA's tokens (a lane has the same channels in every row); the first
+// CTAs have Q's rows, the others K's, and each leaves one row of partial sums.  Packed fp32 arithmetic: the pass is as much bound
+// by instructions as by memory.
 template <int T, bool HALF>
-__global__ void __launch_bounds__(kHeadThreads) head_bwd_kernel(const __grid_constant__ HeadArgs a) {
-  constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes;
-  __shared__ float2 angles[kHeadWarps][kMaxHeadDim / 2];
+__global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_constant__ HeadArgs a) {
+  constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes, P = V / 2;
+  __shared__ alignas(16) Angles angles[kHeadWarps];
+  __shared__ alignas(16) float weights[kMaxHeadDim];
   __shared__ float sums[kHeadWarps][kMaxHeadDim];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place pl = place<T, HALF>(a, lane);
-  const long long first = (long long)blockIdx.x * kHeadWarps + warp + await_stream();
-#pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
-    const HeadTensor& t = a.t[i];
-    float wa[V], wb[V], da[V], db[V];
-    load_weights<V>(t.w, pl, wa, wb);
-#pragma unroll
-    for (int j = 0; j < V; ++j) da[j] = db[j] = 0.f;
-    for (long long task = first; task < a.tokens * a.parts; task += (long long)gridDim.x * kHeadWarps) {
-      const long long token = task / a.parts, b = token / a.N, n = token - b * a.N;
-      int r0, r1;
-      rows_of(t.heads, (int)(task - token * a.parts), a.parts, r0, r1);
-      float c[V], s[V];
-      make_angles<V>(a, a.rot ? __ldg(a.pos + b * a.pos_stride + n) : 0, angles[warp], pl, lane, c, s);
-      const char *x = t.x.data + b * t.x.sb + n * t.x.sn, *g = t.g.data + b * t.g.sb + n * t.g.sn;
-      char* y = t.y.data + b * t.y.sb + n * t.y.sn;
-      for (int r = r0 + pl.group; r - pl.group < r1; r += pl.groups * kAheadBwd) {
-        uint4 va[kAheadBwd], vb[kAheadBwd], ga[kAheadBwd], gb[kAheadBwd];
-#pragma unroll
-        for (int k = 0; k < kAheadBwd; ++k) {
-          const int h = r + k * pl.groups;
-          va[k] = vb[k] = ga[k] = gb[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (h < r1 && pl.on) {
-            va[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.ca * SZ);
-            vb[k] = *reinterpret_cast<const uint4*>(x + h * t.x.sh + pl.cb * SZ);
-            ga[k] = *reinterpret_cast<const uint4*>(g + h * t.g.sh + pl.ca * SZ);
-            gb[k] = *reinterpret_cast<const uint4*>(g + h * t.g.sh + pl.cb * SZ);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < kAheadBwd; ++k) {
-          const int h = r + k * pl.groups;
-          if (h - pl.group >= r1) break;
-          float fa[V], fb[V], ha[V], hb[V];
-          widen<T>(va[k], fa);
-          widen<T>(vb[k], fb);
-          widen<T>(ga[k], ha);
-          widen<T>(gb[k], hb);
-          turn<V, HALF>(ha, hb, c, s);
-          float ss = 0.f, dot = 0.f;
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            ss = fmaf(fa[j], fa[j], fmaf(fb[j], fb[j], ss));
-            dot = fmaf(ha[j] * wa[j], fa[j], fmaf(hb[j] * wb[j], fb[j], dot));
-          }
-          const float rr = rsqrtf(row_sum(ss, a.lanes) / (float)a.d + a.eps);
-          const float back = row_sum(dot, a.lanes) * rr * rr / (float)a.d;
-#pragma unroll
-          for (int j = 0; j < V; ++j) {  // (rows that do not exist are zeros: rr is finite or multiplies zeros)
-            const float xa = fa[j] * rr, xb = fb[j] * rr;
-            if (h < r1) {
-              da[j] = fmaf(ha[j], xa, da[j]);
-              db[j] = fmaf(hb[j], xb, db[j]);
-            }
-            fa[j] = rr * (ha[j] * wa[j] - fa[j] * back);
-            fb[j] = rr * (hb[j] * wb[j] - fb[j] * back);
-          }
-          if (h < r1 && pl.on) {
-            *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.ca * SZ) = narrow<T>(fa);
-            *reinterpret_cast<uint4*>(y + h * t.y.sh + pl.cb * SZ) = narrow<T>(fb);
-          }
-        }
-      }
+  const bool keys = (int)blockIdx.x >= a.q_ctas;
+  const HeadTensor& t = a.t[keys];
+  const int ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ, cta = (int)blockIdx.x - (keys ? a.q_ctas : 0);
+  Spot sp;
+  sp.start(a, cta * kHeadWarps + warp + await_stream(), t.heads);
+  if (keys) sp.stride(a.k_step, a.k_step_b, a.k_step_n);
+  else sp.stride(a.step, a.step_b, a.step_n);
+  uint4 va = make_uint4(0u, 0u, 0u, 0u), vb = va, ga = va, gb = va;
+  const char *x = nullptr, *g = nullptr;  // this lane's next row
+  char* y = nullptr;
+  const long long ox = pl.group * t.x.sh + ca, og = pl.group * t.g.sh + ca, oy = pl.group * t.y.sh + ca;
+  const long long jx = pl.groups * t.x.sh, jg = pl.groups * t.g.sh, jy = pl.groups * t.y.sh;
+  auto find = [&]() {
+    x = t.x.data + sp.b * t.x.sb + sp.n * t.x.sn + sp.r0 * t.x.sh + ox;
+    g = t.g.data + sp.b * t.g.sb + sp.n * t.g.sn + sp.r0 * t.g.sh + og;
+  };
+  auto fetch = [&]() {
+    va = vb = ga = gb = make_uint4(0u, 0u, 0u, 0u);
+    if (sp.r0 + pl.group < sp.r1 && pl.on) {
+      va = *reinterpret_cast<const uint4*>(x);
+      vb = *reinterpret_cast<const uint4*>(x + ba);
+      ga = *reinterpret_cast<const uint4*>(g);
+      gb = *reinterpret_cast<const uint4*>(g + ba);
     }
-    // lane groups, then warps, each in a fixed order
+  };
+  long long pos = 0;
+  if (sp.more) {
+    find();
+    fetch();
+    if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
+  }
+  still_angles(a, angles[warp], lane);
+  for (int c = threadIdx.x; c < a.d; c += kHeadThreads) weights[c] = __ldg(t.w + c);
+  __syncthreads();
+  uint64_t da[P], db[P];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      for (int o = a.lanes; o < 32; o <<= 1) {
-        da[j] += __shfl_xor_sync(0xffffffffu, da[j], o);
-        db[j] += __shfl_xor_sync(0xffffffffu, db[j], o);
-      }
-      if (pl.group == 0 && pl.on) {
-        sums[warp][pl.ca + j] = da[j];
-        sums[warp][pl.cb + j] = db[j];
-      }
+  for (int j = 0; j < P; ++j) da[j] = db[j] = 0ull;
+  bool turned = false;
+  while (sp.more) {
+    float ha[V], hb[V], fa[V], fb[V];
+    widen<T>(ga, ha);
+    widen<T>(gb, hb);
+    widen<T>(va, fa);
+    widen<T>(vb, fb);
+    const bool there = sp.r0 + pl.group < sp.r1;
+    if (!turned) {
+      make_angles(a, pos, angles[warp], lane);
+      y = t.y.data + sp.b * t.y.sb + sp.n * t.y.sn + sp.r0 * t.y.sh + oy;
+      turned = true;
     }
-    __syncthreads();
-    if ((int)threadIdx.x < a.d) {
-      float v = 0.f;
+    char* out = y;
+    y += jy;
+    sp.r0 += pl.groups;
+    if (sp.r0 >= sp.r1) {
+      sp.next(a, t.heads);
+      turned = false;
+      if (sp.more) {
+        find();
+        if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
+      }
+    } else {
+      x += jx;
+      g += jg;
+    }
+    if (sp.more) fetch();
+    turn<V, HALF>(ha, hb, angles[warp], a, pl);
+    float wa[V], wb[V];
+    read_weights<V>(weights, pl, wa, wb);
+    uint64_t ss2 = 0ull, dot2 = 0ull, wh[V];  // wh: the weighted gradient
 #pragma unroll
-      for (int w = 0; w < kHeadWarps; ++w) v += sums[w][threadIdx.x];
-      a.partial[((long long)blockIdx.x * 2 + i) * a.d + threadIdx.x] = v;
+    for (int j = 0; j < P; ++j) {
+      const uint64_t f0 = two(fa[2 * j], fa[2 * j + 1]), f1 = two(fb[2 * j], fb[2 * j + 1]);
+      wh[j] = mul2f(two(ha[2 * j], ha[2 * j + 1]), two(wa[2 * j], wa[2 * j + 1]));
+      wh[P + j] = mul2f(two(hb[2 * j], hb[2 * j + 1]), two(wb[2 * j], wb[2 * j + 1]));
+      ss2 = fma2f(f0, f0, fma2f(f1, f1, ss2));
+      dot2 = fma2f(wh[j], f0, fma2f(wh[P + j], f1, dot2));
     }
-    __syncthreads();
+    float s0, s1, d0, d1;
+    one(ss2, s0, s1);
+    one(dot2, d0, d1);
+    const float ss = row_sum(s0 + s1, a.lanes), dot = row_sum(d0 + d1, a.lanes);
+    const float rr = there ? rsqrtf(ss * a.inv_d + a.eps) : 0.f;  // (of zeros that are no row it may be infinite)
+    const uint64_t rr2 = two(rr, rr), back2 = two(-dot * rr * rr * a.inv_d, -dot * rr * rr * a.inv_d);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const uint64_t t0 = mul2f(two(fa[2 * j], fa[2 * j + 1]), rr2), t1 = mul2f(two(fb[2 * j], fb[2 * j + 1]), rr2);
+      da[j] = fma2f(two(ha[2 * j], ha[2 * j + 1]), t0, da[j]);
+      db[j] = fma2f(two(hb[2 * j], hb[2 * j + 1]), t1, db[j]);
+      one(fma2f(t0, back2, mul2f(wh[j], rr2)), fa[2 * j], fa[2 * j + 1]);
+      one(fma2f(t1, back2, mul2f(wh[P + j], rr2)), fb[2 * j], fb[2 * j + 1]);
+    }
+    if (there && pl.on) {
+      *reinterpret_cast<uint4*>(out) = narrow<T>(fa);
+      *reinterpret_cast<uint4*>(out + ba) = narrow<T>(fb);
+    }
+  }
+  // lane groups, then warps, each in a fixed order
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    float u, v, lo, hi;
+    one(da[j / 2], lo, hi);
+    u = j & 1 ? hi : lo;
+    one(db[j / 2], lo, hi);
+    v = j & 1 ? hi : lo;
+    for (int o = a.lanes; o < 32; o <<= 1) {
+      u += __shfl_xor_sync(0xffffffffu, u, o);
+      v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    if (pl.group == 0 && pl.on) {
+      sums[warp][pl.ca + j] = u;
+      sums[warp][pl.cb + j] = v;
+    }
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < a.d) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kHeadWarps; ++w) v += sums[w][threadIdx.x];
+    a.partial[(long long)blockIdx.x * a.d + threadIdx.x] = v;
   }
 }
 
-// Sums of the CTAs' partial rows: 32 columns a CTA, 32 threads a column, joined in a fixed order.
-__global__ void __launch_bounds__(1024) weight_sum_kernel(const float* __restrict__ partial, int rows, int d, float* __restrict__ dwq,
-                                                          float* __restrict__ dwk) {
+// Sums of the CTAs' partial rows, Q's and K's: 32 columns a CTA, 32 threads a column, joined in a fixed order.
+__global__ void __launch_bounds__(1024) weight_sum_kernel(const float* __restrict__ partial, int q_rows, int k_rows, int d,
+                                                          float* __restrict__ dwq, float* __restrict__ dwk) {
   __shared__ float part[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
-  partial += await_stream();
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c0 = blockIdx.x * 32, col = c0 + x;
+  const bool keys = blockIdx.y != 0;
+  partial += await_stream() + (keys ? (long long)q_rows * d : 0);
   float v = 0.f;
-  if (col < 2 * d)
-    for (int r = y; r < rows; r += 32) v += partial[(long long)r * 2 * d + col];
+  if (col < d)
+    for (int r = y; r < (keys ? k_rows : q_rows); r += 32) v += partial[(long long)r * d + col];
   part[y][x] = v;
   __syncthreads();
   v = part[x][y];  // a warp per column now
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  const int c = blockIdx.x * 32 + y;
-  if (x == 0 && c < 2 * d) (c < d ? dwq[c] : dwk[c - d]) = v;
+  if (x == 0 && c0 + y < d) (keys ? dwk : dwq)[c0 + y] = v;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -322,7 +469,7 @@ int check(const mosaic_rotary_params* p, bool norm) {
   if (!(p->amplitude >= 0.f) || isinf(p->amplitude) || (norm && (!(p->eps >= 0.f) || isinf(p->eps)))) return MOSAIC_E_INVALID_ARG;
   if (p->d <= 0 || p->d % 16 || p->d > kMaxHeadDim) return MOSAIC_E_UNSUPPORTED;
   if ((p->flags & MOSAIC_FLAG_HALF_PAIRS) && p->rot_dim % 16) return MOSAIC_E_UNSUPPORTED;
-  if ((long long)p->B * p->N > (1ll << 32)) return MOSAIC_E_UNSUPPORTED;
+  if ((long long)p->B * p->N > (1 << 30) || (long long)p->H + p->Hkv > (1 << 16)) return MOSAIC_E_UNSUPPORTED;
   return MOSAIC_OK;
 }
 
@@ -331,7 +478,7 @@ HeadArgs base_args(const mosaic_rotary_params* p, const int64_t* pos, int64_t po
   a.pos = pos;
   a.freqs = freqs;
   a.pos_stride = pos_stride;
-  a.tokens = (long long)p->B * p->N;
+  a.tokens = (unsigned)((long long)p->B * p->N);
   a.N = p->N;
   a.d = p->d;
   a.rot = p->rot_dim;
@@ -339,27 +486,37 @@ HeadArgs base_args(const mosaic_rotary_params* p, const int64_t* pos, int64_t po
   for (a.lanes = 1; a.lanes * 2 * v < p->d;) a.lanes *= 2;
   a.amplitude = p->amplitude > 0.f ? p->amplitude : 1.f;
   a.eps = p->eps;
+  a.inv_d = 1.f / (float)p->d;
   a.t[0].heads = p->H;
   a.t[1].heads = p->Hkv;
   return a;
 }
 
-// Few tokens: a token's heads go to several warps, until there are sixteen warps an SM or a warp has one round of rows.
-int split(const HeadArgs& a, int sms) {
-  int parts = 1;
-  while (a.tokens * parts < 16ll * sms && parts * (32 / a.lanes) < a.t[0].heads) parts *= 2;
-  return parts;
+// Few tokens: a token's rows go to several warps, until there are sixteen warps an SM or a warp has one round of rows.  (`most`: warps
+// that a token's rows keep busy.)  Then the grid: as many CTAs as there are tasks, or, one task a token, `ctas` at the most.
+int spread(HeadArgs* a, long long ctas) {
+  a->tasks = a->tokens * a->parts;
+  long long blocks = ((long long)a->tasks + kHeadWarps - 1) / kHeadWarps;
+  if (a->parts == 1 && blocks > ctas) blocks = ctas;
+  a->step = (unsigned)blocks * kHeadWarps;
+  a->step_b = (int)(a->step / (unsigned)a->N);
+  a->step_n = (int)(a->step % (unsigned)a->N);
+  return (int)blocks;
+}
+
+int plan(HeadArgs* a, int rows, int sms, long long ctas) {
+  a->parts = 1;
+  while ((long long)a->tokens * a->parts < 16ll * sms && a->parts * (32 / a->lanes) < rows) a->parts *= 2;
+  return spread(a, ctas);
 }
 
 template <int T, bool HALF>
 int launch_head(HeadArgs a, bool norm, cudaStream_t stream) {
   int sms = 0;
   if (const int rc = launch_setup(nullptr, 0, nullptr, &sms)) return rc;
-  a.parts = split(a, sms);
-  const long long blocks = (a.tokens * a.parts + kHeadWarps - 1) / kHeadWarps;
-  if (blocks > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
-  return launch_kernel(norm ? head_kernel<T, HALF, true> : head_kernel<T, HALF, false>, dim3((unsigned)blocks), kHeadThreads, 0,
-                       stream, true, 0, a);
+  const int blocks = plan(&a, a.t[0].heads + a.t[1].heads, sms, (long long)kCtas * sms);
+  return launch_kernel(norm ? head_kernel<T, HALF, true> : head_kernel<T, HALF, false>, dim3((unsigned)blocks), kHeadThreads, 0, stream,
+                       true, 0, a);
 }
 int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;
@@ -368,22 +525,20 @@ int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t strea
   return half ? launch_head<kBf16, true>(a, norm, stream) : launch_head<kBf16, false>(a, norm, stream);
 }
 
-constexpr int kBwdCtas = 4;  // per SM
 template <int T, bool HALF>
-int launch_head_bwd(HeadArgs a, int ctas, int sms, cudaStream_t stream) {
-  a.parts = split(a, sms);
+int launch_head_bwd(const HeadArgs& a, int ctas, cudaStream_t stream) {
   return launch_kernel(head_bwd_kernel<T, HALF>, dim3((unsigned)ctas), kHeadThreads, 0, stream, true, 0, a);
 }
-int launch_head_bwd(const HeadArgs& a, uint32_t flags, int ctas, int sms, cudaStream_t stream) {
+int launch_head_bwd(const HeadArgs& a, uint32_t flags, int ctas, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;
   if (flags & MOSAIC_FLAG_FP32)
-    return half ? launch_head_bwd<kF32, true>(a, ctas, sms, stream) : launch_head_bwd<kF32, false>(a, ctas, sms, stream);
+    return half ? launch_head_bwd<kF32, true>(a, ctas, stream) : launch_head_bwd<kF32, false>(a, ctas, stream);
   if (flags & MOSAIC_FLAG_FP16)
-    return half ? launch_head_bwd<kF16, true>(a, ctas, sms, stream) : launch_head_bwd<kF16, false>(a, ctas, sms, stream);
-  return half ? launch_head_bwd<kBf16, true>(a, ctas, sms, stream) : launch_head_bwd<kBf16, false>(a, ctas, sms, stream);
+    return half ? launch_head_bwd<kF16, true>(a, ctas, stream) : launch_head_bwd<kF16, false>(a, ctas, stream);
+  return half ? launch_head_bwd<kBf16, true>(a, ctas, stream) : launch_head_bwd<kBf16, false>(a, ctas, stream);
 }
 
-constexpr size_t kMaxBwdRows = 1024;  // partial rows that the workspace holds: the most CTAs of the backward
+constexpr size_t kMaxBwdRows = 2048;  // partial rows that the workspace holds: the most CTAs of the backward
 
 }  // namespace
 
@@ -467,7 +622,7 @@ int mosaic_bsa_qk_norm(const mosaic_rotary_params* p, const mosaic_view* q, cons
 }
 
 size_t mosaic_bsa_qk_norm_workspace_bytes(const mosaic_rotary_params* p) {
-  return check(p, true) ? 0 : kMaxBwdRows * 2 * (size_t)p->d * sizeof(float);
+  return check(p, true) ? 0 : kMaxBwdRows * (size_t)p->d * sizeof(float);
 }
 
 int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params* p, const mosaic_view* q, const mosaic_view* k, const float* wq,
@@ -495,14 +650,22 @@ int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params* p, const mosaic_view* q, 
   if ((rc = device_ok())) return rc;
   int sms = 0;
   if ((rc = launch_setup(nullptr, 0, nullptr, &sms))) return rc;
-  const long long want = (a.tokens * split(a, sms) + kHeadWarps - 1) / kHeadWarps;
-  const int most = kBwdCtas * sms < (int)kMaxBwdRows ? kBwdCtas * sms : (int)kMaxBwdRows;
-  const int ctas = want < most ? (int)want : most;
+  // CTAs in the ratio of the work: a token's rows by rounds of the warp, and its angles as much as two rounds
+  const int groups = 32 / a.lanes, work_q = 2 + (p->H + groups - 1) / groups, work_k = 2 + (p->Hkv + groups - 1) / groups, most = kCtas * sms;
+  const int most_q = most * work_q / (work_q + work_k) > 0 ? most * work_q / (work_q + work_k) : 1;
+  HeadArgs k_plan = a;
+  a.q_ctas = plan(&a, p->H, sms, most_q);
+  k_plan.parts = a.parts;
+  const int k_ctas = spread(&k_plan, most - most_q > 0 ? most - most_q : 1), ctas = a.q_ctas + k_ctas;
+  a.k_step = k_plan.step;
+  a.k_step_b = k_plan.step_b;
+  a.k_step_n = k_plan.step_n;
+  if (ctas > (int)kMaxBwdRows) return MOSAIC_E_UNSUPPORTED;
   a.partial = (float*)ws;
   const cudaStream_t stream = (cudaStream_t)cuda_stream;
-  if ((rc = launch_head_bwd(a, p->flags, ctas, sms, stream))) return rc;
-  return launch_kernel(weight_sum_kernel, dim3((unsigned)((2 * p->d + 31) / 32)), 1024, 0, stream, true, 0, a.partial, ctas, p->d,
-                       dwq, dwk);
+  if ((rc = launch_head_bwd(a, p->flags, ctas, stream))) return rc;
+  return launch_kernel(weight_sum_kernel, dim3((unsigned)((p->d + 31) / 32), 2u), 1024, 0, stream, true, 0, a.partial, a.q_ctas, k_ctas,
+                       p->d, dwq, dwk);
 }
 
 }  // extern "C"
