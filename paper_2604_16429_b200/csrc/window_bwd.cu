@@ -10,9 +10,10 @@
 //                     the tile.  The sinks' keys have all later rows besides; these are cut into pieces as long as a tile's own
 //                     list, items of their own whose sums (fp32) a last kernel adds in order.
 // Per chunk the first product pair is S and dP (key-stationary: their transposes), then the row threads (thread = row of the tile
-// = TMEM lane) form P and dS in 16 bits in the place of S and dP, operands from tensor memory of the sums' products.  Two chunk
-// buffers, two groups of row threads: while one group works on a chunk the tensor core adds the previous one's sums and forms the
-// next one's S and dP.  TMEM (512 columns): S, dP of buffer b at 128 b and 128 b + 64; dS x at 256, P^T y at 256 + d.
+// = TMEM lane) form P and dS in 16 bits in the place of S and dP, operands from tensor memory of the sums' products.  As many chunk
+// buffers as groups of row threads (three; two where the sums of d = 128 leave no more tensor memory): while the groups work on
+// their chunks the tensor core adds an earlier one's sums and forms a later one's S and dP.  TMEM (512 columns): S, dP of buffer b
+// at 128 b and 128 b + 64, behind them dS x, then P^T y.
 // Rounded to 16 bits: P and dS as operands, the results.  Every wait is bounded.
 #include <type_traits>
 
@@ -22,10 +23,21 @@ namespace mosaic {
 
 namespace {
 
-constexpr int kThreads = 384, kChunkRows = 64;
-constexpr int kLaunchRegs = 168, kRowRegs = 208, kOtherRegs = 88;  // as in the forward: the shares add up to the launch's
-static_assert(2 * kRowRegs + kOtherRegs <= 3 * kLaunchRegs, "the shares exceed the launch's registers");
-constexpr uint32_t kTmemCols = 512, kColAcc = 256;
+constexpr int kChunkRows = 64;
+constexpr uint32_t kTmemCols = 512;
+
+// Groups of row threads, each with a chunk buffer: three, where tensor memory holds three beside the sums.
+template <int D, bool KEYS>
+struct Plan {
+  static constexpr int kGroups = KEYS && D == 128 ? 2 : 3;
+  static constexpr uint32_t kColAcc = 128 * kGroups;
+  static constexpr int kWTma = 4 * kGroups, kWMma = kWTma + 1, kThreads = 128 * (kGroups + 1);
+  // Registers a thread: the warpgroups' shares add up to what the block is launched with (which is what the compiler reports), or
+  // the increase would wait for good.
+  static constexpr int kLaunchRegs = kGroups == 2 ? 168 : 128, kRowRegs = kGroups == 2 ? 208 : 144, kOtherRegs = kGroups == 2 ? 88 : 80;
+  static_assert(kGroups * kRowRegs + kOtherRegs <= (kGroups + 1) * kLaunchRegs, "the shares exceed the launch's registers");
+  static_assert(kColAcc + (KEYS ? 2 * D : D) <= kTmemCols, "tensor memory");
+};
 
 template <int D>
 struct Smem {
@@ -37,7 +49,7 @@ struct Smem {
   unsigned char x0[kTileBytes], y0[kTileBytes];  // the resident tiles
   Slot ring[kSlots];
   float stat[kSlots][2][kChunkRows];             // key-stationary: -lse (base 2) and -D of the chunk's rows
-  unsigned long long st_full, st_empty, ring_full[kSlots], ring_empty[kSlots], sd_full[2], p_full[2], acc_full, acc_free, drain;
+  unsigned long long st_full, st_empty, ring_full[kSlots], ring_empty[kSlots], sd_full[3], p_full[3], added[3], acc_full, acc_free, drain[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -62,13 +74,19 @@ struct Item {
   int off, ql, kl;
   int per, chunks;          // chunks of a head, of all
   int front, base, end, ns; // query-stationary: chunks of sinks in front, then keys base .. end - 1; key-stationary: rows base .. end - 1
+  template <bool UNIFORM = false>  // by a whole warp, all of it uniform
   __device__ __forceinline__ void make(const WinGeo& g, const BwdArgs& a, int index) {
     const int heads = KEYS ? g.Hkv : g.H;
     const int unit = index % (g.B * heads), i = index / (g.B * heads);
     b = unit / heads;
     head = unit - b * heads;
     hk = KEYS ? head : head / g.G;
-    const Span s = span_of(g, b);
+    Span s = span_of(g, b);
+    if (UNIFORM) {
+      s.ql = __shfl_sync(0xffffffffu, s.ql, 0);
+      s.kl = __shfl_sync(0xffffffffu, s.kl, 0);
+      s.off = s.kl - s.ql;
+    }
     off = s.off; ql = s.ql; kl = s.kl;
     front = ns = 0;
     if constexpr (KEYS) {
@@ -96,30 +114,25 @@ struct Item {
       per = chunks = rows > 0 && end > 0 ? front + (end - base + kChunkRows - 1) / kChunkRows : 0;
     }
   }
-  // head, first row and number of rows of chunk n
-  __device__ __forceinline__ void chunk(int n, int& h, int& start, int& cols) const {
-    if constexpr (KEYS) {
-      const int r = n / per;
-      h = head + r;
-      start = base + (n - r * per) * kChunkRows;
-      cols = min(kChunkRows, ql - start);
-    } else {
-      h = hk;
-      start = n < front ? n * kChunkRows : base + (n - front) * kChunkRows;
-      cols = min(kChunkRows, (n < front ? ns : end) - start);
-    }
+  // first row and number of rows of chunk n of a head
+  __device__ __forceinline__ void chunk(int n, int& start, int& cols) const {
+    start = !KEYS && n < front ? n * kChunkRows : base + (n - (KEYS ? 0 : front)) * kChunkRows;
+    cols = min(kChunkRows, (KEYS ? ql : n < front ? ns : end) - start);
   }
 };
 
 }  // namespace
 
 template <int D, bool F16, bool KEYS>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
     window_bwd_kernel(const WinGeo g, const __grid_constant__ CUtensorMap map_x0, const __grid_constant__ CUtensorMap map_y0,
                       const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const Fold fx0,
                       const Fold fy0, const Fold fx, const Fold fy, const __grid_constant__ BwdArgs a, int* status, int total) {
   extern __shared__ unsigned char smem_raw[];
   using S = Smem<D>;
+  using P = Plan<D, KEYS>;
+  constexpr int kGroups = P::kGroups;
+  constexpr uint32_t kColAcc = P::kColAcc;
   S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr uint32_t kPart = kRows * 128, kChunkPart = kChunkRows * 128;
   constexpr int kParts = D / 64;
@@ -129,21 +142,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(s32(&sm.st_full), 1);
     mbar_init(s32(&sm.st_empty), 1);
     for (int s = 0; s < S::kSlots; ++s) { mbar_init(s32(&sm.ring_full[s]), 1); mbar_init(s32(&sm.ring_empty[s]), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(s32(&sm.sd_full[i]), 1); mbar_init(s32(&sm.p_full[i]), 128); }
+    for (int i = 0; i < kGroups; ++i) { mbar_init(s32(&sm.sd_full[i]), 1); mbar_init(s32(&sm.p_full[i]), 128); mbar_init(s32(&sm.added[i]), 1); }
     mbar_init(s32(&sm.acc_full), 1);
     mbar_init(s32(&sm.acc_free), 256);
-    mbar_init(s32(&sm.drain), 1);
+    mbar_init(s32(&sm.drain[0]), 1);
+    mbar_init(s32(&sm.drain[1]), 1);
     sm.abort = 0;
     cta_publish_barriers();
   }
   const int first_item = (int)blockIdx.x + await_stream();
-  const uint32_t tmem = cta_tmem_alloc(warp == 9, &sm.tmem_base, kTmemCols);
+  const uint32_t tmem = cta_tmem_alloc(warp == P::kWMma, &sm.tmem_base, kTmemCols);
   volatile int* abort = &sm.abort;
   Item<KEYS> it;
 
-  if (warp == 8) {
+  if (warp == P::kWTma) {
     // ------------------------------------------------------------- TMA producer
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
     if (lane == 0) {
       uint32_t cc = 0, items = 0;
       bool ok = true;
@@ -162,12 +176,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           tma_load_4d(s32(sm.y0) + c * kPart, &map_y0, s32(&sm.st_full), 64 * c, it.row0, (KEYS ? it.hk : it.head) * fy0.h, it.b * fy0.b);
         }
         ++items;
-        for (int n = 0; n < it.chunks; ++n, ++cc) {
+        int h = KEYS ? it.head : it.hk;
+        for (int n = 0, j = 0; n < it.chunks; ++n, ++cc) {
           const uint32_t s = cc % S::kSlots, bar = s32(&sm.ring_full[s]);
           ok = wait_here(s32(&sm.ring_empty[s]), ((cc / S::kSlots) & 1) ^ 1, abort, status);
           if (!ok) break;
-          int h, start, cols;
-          it.chunk(n, h, start, cols);
+          int start, cols;
+          it.chunk(j, start, cols);
           mbar_expect_tx(bar, 2 * S::kChunkBytes + (KEYS ? 2 * kChunkRows * 4 : 0));
 #pragma unroll
           for (int c = 0; c < kParts; ++c) {
@@ -179,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bulk_load(s32(sm.stat[s][0]), a.neg_lse2 + at, kChunkRows * 4, bar);
             bulk_load(s32(sm.stat[s][1]), a.neg_d + at, kChunkRows * 4, bar);
           }
+          if (++j == it.per) { j = 0; ++h; }
         }
       }
       // copies must have landed, and their readers be done, before the CTA's memory is released
@@ -189,82 +205,95 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (*abort && items) mbar_drain(s32(&sm.st_full), (items - 1) & 1);
     }
-  } else if (warp == 9) {
-    // ------------------------------------------------------------- all products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    constexpr uint32_t idesc_sd = make_idesc(false, 64u, F16), idesc_acc = make_idesc(true, (uint32_t)D, F16);
-    uint32_t cc = 0, items = 0;
+  } else if (warp == P::kWMma) {
+    // ------------------------------------------------------------- S and dP
+    // (The whole warp walks the loop, one elected lane issues; what it walks by is uniform, so that operands stay in uniform registers.)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
+    constexpr uint32_t idesc = make_idesc(false, 64u, F16);
+    const uint64_t x0d = smem_desc(s32(sm.x0)), y0d = smem_desc(s32(sm.y0));
+    uint32_t c = 0, items = 0;
     bool ok = true;
-    // the sums of chunk c (its P and dS are ready), the `fresh` ones starting anew
-    auto add = [&](uint32_t c, bool fresh, bool last) {
-      const uint32_t s = c % S::kSlots, buf = c & 1;
-      ok = warp_wait_here(s32(&sm.p_full[buf]), (c >> 1) & 1, abort, status);
-      if (!ok) return;
-      tc_fence_after();
-      const uint64_t xd = mn_major(s32(sm.ring[s].x), kChunkPart), yd = mn_major(s32(sm.ring[s].y), kChunkPart);
-      if (elect_one()) {
-        if constexpr (KEYS) {
-#pragma unroll
-          for (int kk = 0; kk < kChunkRows / 16; ++kk)
-            umma_ts(tmem + kColAcc + D, tmem + 128 * buf + 8 * kk, yd + (uint64_t)((2048 * kk) >> 4), idesc_acc, !fresh || kk > 0);
-        }
-#pragma unroll
-        for (int kk = 0; kk < kChunkRows / 16; ++kk)
-          umma_ts(tmem + kColAcc, tmem + 128 * buf + 64 + 8 * kk, xd + (uint64_t)((2048 * kk) >> 4), idesc_acc, !fresh || kk > 0);
-        tc_commit(s32(&sm.ring_empty[s]));
-        if (last) tc_commit(s32(&sm.acc_full));
-      }
-      __syncwarp();
-    };
-    for (int index = first_item; index < total && ok; index += gridDim.x) {
-      it.make(g, a, index);
+    for (int index = __shfl_sync(0xffffffffu, first_item, 0); index < total && ok; index += gridDim.x) {
+      it.template make<true>(g, a, index);
       if (it.chunks == 0) continue;
       ok = warp_wait_here(s32(&sm.st_full), items & 1, abort, status);
-      if (!ok) break;
-      const uint64_t x0d = smem_desc(s32(sm.x0)), y0d = smem_desc(s32(sm.y0));
-      for (int n = 0; n <= it.chunks && ok; ++n) {
-        if (n < it.chunks) {
-          const uint32_t c = cc + n, s = c % S::kSlots, buf = c & 1;
-          ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);
-          if (!ok) break;
-          int h, start, cols;
-          it.chunk(n, h, start, cols);
-          const int there = (KEYS ? it.ql : it.kl) - start;  // rows of the chunk that exist
-          if (there < kChunkRows && start + there < (KEYS ? g.Nq : g.Nk)) {
-            zero_rows<D>(sm.ring[s].x, there, kChunkRows, lane);
-            if constexpr (KEYS) zero_rows<D>(sm.ring[s].y, there, kChunkRows, lane);
-          }
-          tc_fence_after();
-          const uint64_t xd = smem_desc(s32(sm.ring[s].x)), yd = smem_desc(s32(sm.ring[s].y));
-          if (elect_one()) {
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              umma_ss(tmem + 128 * buf, k_major(x0d, kk, kPart), k_major(xd, kk, kChunkPart), idesc_sd, kk > 0);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              umma_ss(tmem + 128 * buf + 64, k_major(y0d, kk, kPart), k_major(yd, kk, kChunkPart), idesc_sd, kk > 0);
-            tc_commit(s32(&sm.sd_full[buf]));
-            if (n == it.chunks - 1) tc_commit(s32(&sm.st_empty));
-          }
-          __syncwarp();
+      ++items;
+      for (int n = 0, j = 0; n < it.chunks && ok; ++n, ++c) {
+        const uint32_t s = c % S::kSlots, buf = c % kGroups;
+        ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);
+        // the sums of the chunk that had the buffer read its P and dS there (products of different shapes are not ordered by being
+        // issued in order)
+        if (c >= (uint32_t)kGroups) ok = ok && warp_wait_here(s32(&sm.added[buf]), (c / kGroups - 1) & 1, abort, status);
+        if (!ok) break;
+        int start, cols;
+        it.chunk(j, start, cols);
+        if (++j == it.per) j = 0;
+        const int there = (KEYS ? it.ql : it.kl) - start;  // rows of the chunk that exist
+        if (there < kChunkRows && start + there < (KEYS ? g.Nq : g.Nk)) {
+          zero_rows<D>(sm.ring[s].x, there, kChunkRows, lane);
+          if constexpr (KEYS) zero_rows<D>(sm.ring[s].y, there, kChunkRows, lane);
         }
-        if (n > 0) {
-          if (n == 1 && items > 0) ok = warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
-          if (ok) add(cc + n - 1, n == 1, n == it.chunks);
+        tc_fence_after();
+        const uint64_t xd = smem_desc(s32(sm.ring[s].x)), yd = smem_desc(s32(sm.ring[s].y));
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            umma_ss(tmem + 128 * buf, k_major(x0d, kk, kPart), k_major(xd, kk, kChunkPart), idesc, kk > 0);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            umma_ss(tmem + 128 * buf + 64, k_major(y0d, kk, kPart), k_major(yd, kk, kChunkPart), idesc, kk > 0);
+          tc_commit(s32(&sm.sd_full[buf]));
+          if (n == it.chunks - 1) tc_commit(s32(&sm.st_empty));
         }
+        __syncwarp();
       }
-      cc += it.chunks;
+    }
+    if (*abort) {
+      if (elect_one()) mma_drain(s32(&sm.drain[0]));
+      __syncwarp();
+    }
+  } else if (warp == P::kWMma + 1) {
+    // ------------------------------------------------------------- sums: dS x, and P^T y
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
+    constexpr uint32_t idesc = make_idesc(true, (uint32_t)D, F16);
+    uint32_t c = 0, items = 0;
+    bool ok = true;
+    for (int index = __shfl_sync(0xffffffffu, first_item, 0); index < total && ok; index += gridDim.x) {
+      it.template make<true>(g, a, index);
+      if (it.chunks == 0) continue;
+      for (int n = 0; n < it.chunks && ok; ++n, ++c) {
+        const uint32_t s = c % S::kSlots, buf = c % kGroups;
+        ok = warp_wait_here(s32(&sm.p_full[buf]), (c / kGroups) & 1, abort, status);
+        if (n == 0 && items > 0) ok = ok && warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t xd = mn_major(s32(sm.ring[s].x), kChunkPart), yd = mn_major(s32(sm.ring[s].y), kChunkPart);
+        if (elect_one()) {
+          if constexpr (KEYS) {
+#pragma unroll
+            for (int kk = 0; kk < kChunkRows / 16; ++kk)
+              umma_ts(tmem + kColAcc + D, tmem + 128 * buf + 8 * kk, yd + (uint64_t)((2048 * kk) >> 4), idesc, n > 0 || kk > 0);
+          }
+#pragma unroll
+          for (int kk = 0; kk < kChunkRows / 16; ++kk)
+            umma_ts(tmem + kColAcc, tmem + 128 * buf + 64 + 8 * kk, xd + (uint64_t)((2048 * kk) >> 4), idesc, n > 0 || kk > 0);
+          tc_commit(s32(&sm.added[buf]));
+          tc_commit(s32(&sm.ring_empty[s]));
+          if (n == it.chunks - 1) tc_commit(s32(&sm.acc_full));
+        }
+        __syncwarp();
+      }
       ++items;
     }
     if (*abort) {
-      if (elect_one()) mma_drain(s32(&sm.drain));
+      if (elect_one()) mma_drain(s32(&sm.drain[1]));
       __syncwarp();
     }
-  } else if (warp >= 10) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  } else if (warp > P::kWMma + 1) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
   } else {
     // ------------------------------------------------------------- row threads
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P::kRowRegs));
     const int grp = warp >> 2, row = tid & 127;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tb = tmem + lane_off + 128 * grp;  // a group's chunks are all in its own buffer
@@ -281,10 +310,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         nd = __ldg(a.neg_d + at);
       }
       const uint64_t nl2 = pack2(nl, nl), nd2 = pack2(nd, nd);
-      for (int n = (int)((cc ^ (uint32_t)grp) & 1); n < it.chunks; n += 2) {
+      const int first = (grp + kGroups - (int)(cc % kGroups)) % kGroups;
+      for (int n = first, j = KEYS ? first % max(it.per, 1) : first; n < it.chunks; n += kGroups) {
         const uint32_t c = cc + n, s = c % S::kSlots;
-        int h, start, cols;
-        it.chunk(n, h, start, cols);
+        int start, cols;
+        it.chunk(j, start, cols);
+        j += kGroups;
+        if (KEYS)
+          while (j >= it.per) j -= it.per;
         // columns that the row sees: [from, upto), and the first `sink`; and whether all rows see all of them
         int from, upto, sink = 0;
         bool whole;
@@ -300,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           whole = cols == kChunkRows && start + kChunkRows <= it.off + it.row0 + 1 &&
                   (start + kChunkRows <= g.sinks || start > it.off + it.row0 + kRows - 1 - g.window);
         }
-        ok = warp_wait_here(s32(&sm.sd_full[grp]), (c >> 1) & 1, abort, status);
+        ok = warp_wait_here(s32(&sm.sd_full[grp]), (c / kGroups) & 1, abort, status);
         if (KEYS && ok) ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);  // (landed: for the copies' visibility)
         if (!ok) break;
         tc_fence_after();
@@ -311,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld32(tb + 64 + 32 * half, dv);
           tmem_wait_ld();
           const uint32_t see = low_bits(upto - 32 * half) & (~low_bits(from - 32 * half) | low_bits(sink - 32 * half));
-          const float* st = &sm.stat[s][0][32 * half];
+          [[maybe_unused]] const float* st = &sm.stat[s][0][32 * half];
 #pragma unroll
           for (int x = 0; x < 32; x += 4) {
             uint64_t l01 = nl2, l23 = nl2, d01 = nd2, d23 = nd2;
@@ -320,13 +353,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               l01 = pack2(l4.x, l4.y); l23 = pack2(l4.z, l4.w);
               d01 = pack2(d4.x, d4.y); d23 = pack2(d4.z, d4.w);
             }
-            float y0, y1, y2, y3, p2, p3;
-            const uint64_t y01 = fma2(pack2(__uint_as_float(sv[x]), __uint_as_float(sv[x + 1])), scale2, l01);
-            const uint64_t y23 = fma2(pack2(__uint_as_float(sv[x + 2]), __uint_as_float(sv[x + 3])), scale2, l23);
-            unpack2(y01, y0, y1);
-            unpack2(y23, y2, y3);
-            float p0 = ex2(y0), p1 = ex2(y1);
-            if (!decltype(masked)::value && ((x >> 2) & 1)) { ex2_quartic(y23, p2, p3); } else { p2 = ex2(y2); p3 = ex2(y3); }
+            float y0, y1, y2, y3;
+            unpack2(fma2(pack2(__uint_as_float(sv[x]), __uint_as_float(sv[x + 1])), scale2, l01), y0, y1);
+            unpack2(fma2(pack2(__uint_as_float(sv[x + 2]), __uint_as_float(sv[x + 3])), scale2, l23), y2, y3);
+            float p0 = ex2(y0), p1 = ex2(y1), p2 = ex2(y2), p3 = ex2(y3);
             float e0, e1, e2, e3;
             unpack2(mul2(pack2(p0, p1), add2(pack2(__uint_as_float(dv[x]), __uint_as_float(dv[x + 1])), d01)), e0, e1);
             unpack2(mul2(pack2(p2, p3), add2(pack2(__uint_as_float(dv[x + 2]), __uint_as_float(dv[x + 3])), d23)), e2, e3);
@@ -356,7 +386,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       cc += it.chunks;
-      // results: the groups share dq's columns; or group 0 writes dv, group 1 dk
+      // results: two groups share dq's columns; or group 0 writes dv, group 1 dk
+      if (grp >= 2) continue;
       if (it.chunks > 0) {
         ok = warp_wait_here(s32(&sm.acc_full), items & 1, abort, status);
         if (!ok) break;
@@ -401,29 +432,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   }
-  cta_tmem_free(warp == 9, tmem, kTmemCols);
+  cta_tmem_free(warp == P::kWMma, tmem, kTmemCols);
 }
 
-// -lse in base 2 and -D = -<dO, O> of every row, eight lanes a row.  Rows that do not exist, and rows that see nothing (whose
-// weights are masked whatever stands here), get zeros.  Clears the status block.
+// -lse in base 2 and -D = -<dO, O> of every row, eight lanes a row and kRowsAhead rows a lane.  Rows that do not exist, and rows that
+// see nothing (whose weights are masked whatever stands here), get zeros.  Clears the status block.
 namespace {
+constexpr int kRowsAhead = 4;
 template <int D, bool F16>
 __global__ void __launch_bounds__(256) window_rows_kernel(const WinGeo g, const View o, const View d_o, const float* __restrict__ lse,
                                                           float* __restrict__ neg_lse2, float* __restrict__ neg_d, int pad, int* status) {
-  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x + await_stream()) >> 3;
-  if (blockIdx.x == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
-  const int part = threadIdx.x & 7;
-  if (at >= (long long)g.B * g.H * pad) return;  // (whole rows: 32 rows a block)
-  const long long unit = at / pad;
-  const int i = (int)(at - unit * pad), b = (int)(unit / g.H), h = (int)(unit - (long long)b * g.H);
-  const bool there = i < span_of(g, b).ql;
-  float dot = 0.f;
-  if (there) {
-    const char *x = o.data + b * o.sb + h * o.sh + (long long)i * o.sn, *y = d_o.data + b * d_o.sb + h * d_o.sh + (long long)i * d_o.sn;
+  const int first = (int)blockIdx.x * (32 * kRowsAhead) + (threadIdx.x >> 3) + await_stream(), part = threadIdx.x & 7;
+  const int unit = blockIdx.y, b = unit / g.H, h = unit - b * g.H;
+  if (blockIdx.x == 0 && unit == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
+  const int ql = span_of(g, b).ql;
+  const char *x = o.data + b * o.sb + h * o.sh + 16 * part, *y = d_o.data + b * d_o.sb + h * d_o.sh + 16 * part;
+  uint4 u[kRowsAhead][D / 64], w[kRowsAhead][D / 64];
+  float l[kRowsAhead];
+#pragma unroll
+  for (int r = 0; r < kRowsAhead; ++r) {
+    const int i = first + 32 * r;
+    l[r] = i < ql ? __ldg(lse + (long long)unit * g.Nq + i) : 0.f;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(x) + part + 8 * c), w = __ldg(reinterpret_cast<const uint4*>(y) + part + 8 * c);
-      const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
+      u[r][c] = w[r][c] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < ql) {
+        u[r][c] = __ldg(reinterpret_cast<const uint4*>(x + (long long)i * o.sn + 128 * c));
+        w[r][c] = __ldg(reinterpret_cast<const uint4*>(y + (long long)i * d_o.sn + 128 * c));
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kRowsAhead; ++r) {
+    float dot = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const uint32_t uw[4] = {u[r][c].x, u[r][c].y, u[r][c].z, u[r][c].w}, ww[4] = {w[r][c].x, w[r][c].y, w[r][c].z, w[r][c].w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         float u0, u1, w0, w1;
@@ -432,13 +476,13 @@ __global__ void __launch_bounds__(256) window_rows_kernel(const WinGeo g, const 
         dot = fmaf(u0, w0, fmaf(u1, w1, dot));
       }
     }
-  }
 #pragma unroll
-  for (int x = 4; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-  if (part == 0) {
-    const float l = there ? lse[unit * g.Nq + i] : 0.f;
-    neg_lse2[at] = l == -INFINITY ? 0.f : -l * 1.4426950408889634f;
-    neg_d[at] = -dot;
+    for (int k = 4; k; k >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, k);
+    const int i = first + 32 * r;
+    if (part == 0 && i < pad) {
+      neg_lse2[(long long)unit * pad + i] = l[r] == -INFINITY ? 0.f : -l[r] * 1.4426950408889634f;
+      neg_d[(long long)unit * pad + i] = -dot;
+    }
   }
 }
 
@@ -476,16 +520,15 @@ int launch_pass(const HostCtx& c, const WinGeo& g, const View& x0, const View& y
   if (const int rc = launch_setup(reinterpret_cast<const void*>(window_bwd_kernel<D, F16, KEYS>), smem, &configured, &sms)) return rc;
   const long long total = (long long)g.B * h0 * (a.tiles + a.pieces);
   if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
-  return launch_kernel(window_bwd_kernel<D, F16, KEYS>, dim3((unsigned)(total < sms ? total : sms)), kThreads, smem, c.stream, true, 0, g,
+  return launch_kernel(window_bwd_kernel<D, F16, KEYS>, dim3((unsigned)(total < sms ? total : sms)), Plan<D, KEYS>::kThreads, smem, c.stream, true, 0, g,
                        mx0, my0, mx, my, fold_of(x0), fold_of(y0), fold_of(x), fold_of(y), a, c.status, (int)total);
 }
 
 template <int D, bool F16>
 int launch(const HostCtx& c, const WinGeo& g, const WinBwd& t, const WinBwdWs& w, char* ws) {
-  const long long rows = (long long)g.B * g.H * w.pad, blocks = (rows * 8 + 255) / 256;
-  if (blocks > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
+  if ((long long)g.B * g.H > 65535) return MOSAIC_E_UNSUPPORTED;
   float *nl = (float*)(ws + w.neg_lse2), *nd = (float*)(ws + w.neg_d);
-  int rc = launch_kernel(window_rows_kernel<D, F16>, dim3((unsigned)blocks), 256, 0, c.stream, true, 0, g, t.o, t.d_o, t.lse, nl, nd, w.pad,
+  int rc = launch_kernel(window_rows_kernel<D, F16>, dim3((unsigned)((w.pad + 32 * kRowsAhead - 1) / (32 * kRowsAhead)), (unsigned)(g.B * g.H)), 256, 0, c.stream, true, 0, g, t.o, t.d_o, t.lse, nl, nd, w.pad,
                          c.status);
   if (rc) return rc;
   BwdArgs a = {t.dk, t.dv, nl, nd, (float*)(ws + w.partial), w.pad, (g.Nk + kRows - 1) / kRows, w.pieces, w.piece_rows};

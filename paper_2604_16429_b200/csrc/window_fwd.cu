@@ -47,7 +47,8 @@ struct Smem {
   unsigned char kv[kSlots][kSlotBytes];
   uint4 rows[8][32 * 4];  // a softmax warp's 32 rows of 32 results on their way out
   unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots];
-  unsigned long long s_full[2][2], p_full[2][2], pv_done[2], drain[2];
+  unsigned long long s_full[2][2], p_full[2][2], drain[2];
+  unsigned long long pv_done[2][2];  // one a buffer: a thread that has seen a step's scores is at most one phase behind it
   uint32_t tmem_base;
   int abort;
 };
@@ -155,8 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int b = 0; b < 2; ++b) {
         mbar_init(s32(&sm.s_full[t][b]), 1);
         mbar_init(s32(&sm.p_full[t][b]), 128);
+        mbar_init(s32(&sm.pv_done[t][b]), 1);
       }
-      mbar_init(s32(&sm.pv_done[t]), 1);
       mbar_init(s32(&sm.drain[t]), 1);
     }
     sm.abort = 0;
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
           for (int kk = 0; kk < kks; ++kk) umma_ts(tco, tcp + 8 * kk, vd + (uint64_t)((2048 * kk) >> 4), idesc_pv, !fresh || kk > 0);
         }
-        tc_commit(s32(&sm.pv_done[t]));
+        tc_commit(s32(&sm.pv_done[t][b]));
         tc_commit(s32(&sm.kv_empty[v_no % kSlots]));
       }
       __syncwarp();
@@ -287,7 +288,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t tcs = tmem + score_col(t, b);
       const uint64_t kd = smem_desc(s32(sm.kv[k_slot]));
       ok = ok && warp_wait_here(s32(&sm.kv_full[k_slot]), (slot_no / kSlots) & 1, abort, status);
-      // (the buffer is free: P V of the step that had it was issued before, and one thread's products run in order)
+      // P V of the step that had the buffer (two before) reads its weights there.  It was issued before, and products of one shape run
+      // in issue order; of different shapes they need not.  (Waiting always costs 8 % at d = 128, where the shapes differ.)
+      if (u >= 2 && (D != U || round32(cols) != U)) ok = ok && warp_wait_here(s32(&sm.pv_done[t][b]), (u / 2 - 1) & 1, abort, status);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -420,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         unpack2(add2(sum_a, sum_b), la, lb);
         l += la + lb;
         if (__any_sync(0xffffffffu, need)) {
-          if (u > 0) ok = warp_wait_here(s32(&sm.pv_done[t]), (u - 1) & 1, abort, status);  // O is scaled between two products
+          if (u > 0) ok = warp_wait_here(s32(&sm.pv_done[t][b ^ 1]), ((u - 1) / 2) & 1, abort, status);  // O is scaled between two products
           if (!ok) break;
           tc_fence_after();
           const uint64_t alpha2 = pack2(alpha, alpha);
@@ -448,7 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = i < it.ql && t < it.tiles;
       const float inv = m_ref == -INFINITY ? 0.f : 1.f / l;
       if (last >= 0) {
-        ok = warp_wait_here(s32(&sm.pv_done[t]), (u - 1) & 1, abort, status);
+        ok = warp_wait_here(s32(&sm.pv_done[t][(u - 1) % 2]), ((u - 1) / 2) & 1, abort, status);
         if (!ok) break;
         tc_fence_after();
       }
