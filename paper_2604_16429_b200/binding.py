@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
+import threading
 from dataclasses import dataclass
 
 import torch
@@ -130,7 +132,7 @@ def lib():
         L.mosaic_bsa_rope.argtypes = [pp, vp, vp, fp, ctypes.c_float, vp, vp, vp]
         L.mosaic_bsa_bwd.restype = ctypes.c_int
         L.mosaic_bsa_bwd.argtypes = [pp, vp, vp, vp, vp, fp, vp, i32p, vp, vp, vp, vp, ctypes.c_size_t, vp]
-        vw, rp = ctypes.POINTER(_View), ctypes.POINTER(_RotaryParams)
+        vw = rp = vp  # pointers to a view, to a parameter block
         L.mosaic_bsa_rotary_freqs.restype = ctypes.c_int
         L.mosaic_bsa_rotary_freqs.argtypes = [ctypes.POINTER(_RotaryScaling), vp]
         L.mosaic_bsa_rotary.restype = ctypes.c_int
@@ -142,7 +144,7 @@ def lib():
         L.mosaic_bsa_qk_norm_bwd.restype = ctypes.c_int
         L.mosaic_bsa_qk_norm_bwd.argtypes = [rp, vw, vw, fp, fp, vp, ctypes.c_int64, vp, vw, vw, vw, vw, fp, fp, vp,
                                              ctypes.c_size_t, vp]
-        wp = ctypes.POINTER(_WindowParams)
+        wp = vp
         L.mosaic_bsa_window_workspace_bytes.restype = ctypes.c_size_t
         L.mosaic_bsa_window_workspace_bytes.argtypes = [wp, ctypes.c_int]
         L.mosaic_bsa_window_fwd.restype = ctypes.c_int
@@ -372,7 +374,18 @@ def rotary_freqs(rp: RotaryParams, device="cuda") -> torch.Tensor:
 
 
 # Small calls are as long as what happens here before the launch (a rotation of 64 tokens: 24 us with a stream object, device
-# objects and a launch object made per call, 13 us so), hence the plain comparisons.
+# objects and a ctypes structure made per argument), hence the plain comparisons, and the parameter block and all views of a call
+# written at once into a buffer that the thread keeps.
+class _Block(threading.local):
+    def __init__(self):
+        self.buf = (ctypes.c_int64 * 48)()
+        self.at = ctypes.addressof(self.buf)
+
+
+_block = _Block()
+# (both parameter blocks are 40 bytes long with their padding, a view is 32)
+_rotary_pack = {n: struct.Struct("=6iI2f4x%dq" % (4 * n)).pack_into for n in (4, 6)}
+_window_pack = {n: struct.Struct("=8ifI%dq" % (4 * n)).pack_into for n in (4, 8)}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
@@ -385,13 +398,13 @@ def _view(name, t, shape, dtype, index):
     st = t.stride()
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape or st[3] != 1:
         raise _bad(name, t, f"{dtype} {tuple(shape)} on cuda:{index} with contiguous rows")
-    return _View(t.data_ptr(), st[0], st[1], st[2])
+    return t.data_ptr(), st[0], st[1], st[2]
 
 
 def _out(name, t, shape, dtype, index):
     """The same for an output, which may not write a place twice."""
     v = _view(name, t, shape, dtype, index)
-    if (v.sb == 0 and shape[0] > 1) or (v.sh == 0 and shape[1] > 1) or (v.sn == 0 and shape[2] > 1):
+    if (v[1] == 0 and shape[0] > 1) or (v[2] == 0 and shape[1] > 1) or (v[3] == 0 and shape[2] > 1):
         raise _bad(name, t, "rows that do not overlap")
     return v
 
@@ -454,8 +467,8 @@ def _rotary_params(rp, q, k, flags, eps):
     B, H, N, _ = q.shape
     Hkv = k.shape[1]
     d = rp.d
-    return index, _RotaryParams(B, H, Hkv, N, d, rp.rot, _STORAGE[q.dtype] | (FLAG_HALF_PAIRS if rp.half else 0) | flags,
-                                rp.amplitude, eps), (B, H, N, d), (B, Hkv, N, d)
+    return index, (B, H, Hkv, N, d, rp.rot, _STORAGE[q.dtype] | (FLAG_HALF_PAIRS if rp.half else 0) | flags, rp.amplitude,
+                   eps), (B, H, N, d), (B, Hkv, N, d)
 
 
 def _positions(rp, pos, freqs, shape, index):
@@ -480,8 +493,10 @@ def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=N
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
     k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
-    _call("mosaic_bsa_rotary", index, stream, p, vq, vk, at, step, fr, _out("q_out", q_out, sq, t, index),
-          _out("k_out", k_out, sk, t, index))
+    block = _block
+    a = block.at
+    _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    _call("mosaic_bsa_rotary", index, stream, a, a + 40, a + 72, at, step, fr, a + 104, a + 136)
     return q_out, k_out
 
 
@@ -494,13 +509,16 @@ def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
     k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
-    _call("mosaic_bsa_qk_norm", index, stream, p, vq, vk, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at, step,
-          fr, _out("q_out", q_out, sq, t, index), _out("k_out", k_out, sk, t, index))
+    block = _block
+    a = block.at
+    _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    _call("mosaic_bsa_qk_norm", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at,
+          step, fr, a + 104, a + 136)
     return q_out, k_out
 
 
 def qk_norm_workspace_bytes(rp: RotaryParams, q, k) -> int:
-    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_rotary_params(rp, q, k, 0, 0.0)[1]))
+    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(ctypes.byref(_RotaryParams(*_rotary_params(rp, q, k, 0, 0.0)[1]))))
 
 
 def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, d_k_out, eps=1e-6, dq=None, dk=None, dwq=None,
@@ -516,11 +534,14 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     dk = _new(torch.empty_like(k), stream) if dk is None else dk
     dwq = _new(torch.empty(w, dtype=f32, device=index), stream) if dwq is None else dwq
     dwk = _new(torch.empty(w, dtype=f32, device=index), stream) if dwk is None else dwk
+    block = _block
+    a = block.at
+    _rotary_pack[6](block.buf, 0, *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
     name = "mosaic_bsa_qk_norm_workspace_bytes"
-    ws = _scratch(0 if ws is not None else int(getattr(lib(), name)(p)), name, index, ws, stream)
-    _call("mosaic_bsa_qk_norm_bwd", index, stream, p, vq, vk, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at,
-          step, fr, gq, gk, _out("dq", dq, sq, t, index), _out("dk", dk, sk, t, index), _flat("dwq", dwq, w, f32, index),
-          _flat("dwk", dwk, w, f32, index), ws.data_ptr(), ws.numel())
+    ws = _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(a)), name, index, ws, stream)
+    _call("mosaic_bsa_qk_norm_bwd", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index),
+          at, step, fr, a + 104, a + 136, a + 168, a + 200, _flat("dwq", dwq, w, f32, index), _flat("dwk", dwk, w, f32, index),
+          ws.data_ptr(), ws.numel())
     return dq, dk, dwq, dwk
 
 
@@ -541,20 +562,20 @@ def _window_params(wp, q, k):
     B, H, Nq, d = q.shape
     Hkv, Nk = k.shape[1], k.shape[2]
     flags = _STORAGE[q.dtype] | (FLAG_ROLLING if wp.rolling else 0)
-    return index, _WindowParams(B, H, Hkv, Nq, Nk, d, wp.window, wp.sinks, wp.scale, flags), (B, Hkv, Nk, d)
+    return index, (B, H, Hkv, Nq, Nk, d, wp.window, wp.sinks, wp.scale, flags), (B, Hkv, Nk, d)
 
 
 def window_workspace_bytes(wp: WindowParams, q, k, op: int) -> int:
-    return int(lib().mosaic_bsa_window_workspace_bytes(_window_params(wp, q, k)[1], op))
+    return int(lib().mosaic_bsa_window_workspace_bytes(ctypes.byref(_WindowParams(*_window_params(wp, q, k)[1])), op))
 
 
-def _window_ws(p, op, index, ws, stream):
+def _window_ws(at, op, index, ws, stream):
     name = "mosaic_bsa_window_workspace_bytes"
-    return _scratch(0 if ws is not None else int(getattr(lib(), name)(p, op)), name, index, ws, stream)
+    return _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(at, op)), name, index, ws, stream)
 
 
-def _len(name, t, p, index):
-    return 0 if t is None else _flat(name, t, (p.B,), torch.int32, index)
+def _len(name, t, B, index):
+    return 0 if t is None else _flat(name, t, (B,), torch.int32, index)
 
 
 def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=None, lse=None, ws=None, stream=None):
@@ -565,9 +586,12 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _new(torch.empty_like(q), stream) if o is None else o
     lse = _new(torch.empty(sq[:3], dtype=torch.float32, device=index), stream) if lse is None else lse
-    ws = _window_ws(p, OP_FWD, index, ws, stream)
-    _call("mosaic_bsa_window_fwd", index, stream, p, vq, vk, vv, _len("q_len", q_len, p, index), _len("k_len", k_len, p, index),
-          _out("o", o, sq, t, index), _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
+    block = _block
+    a = block.at
+    _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    ws = _window_ws(a, OP_FWD, index, ws, stream)
+    _call("mosaic_bsa_window_fwd", index, stream, a, a + 40, a + 72, a + 104, _len("q_len", q_len, sq[0], index),
+          _len("k_len", k_len, sq[0], index), a + 136, _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
     return o, lse
 
 
@@ -582,10 +606,14 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
     dq = _new(torch.empty_like(q), stream) if dq is None else dq
     dk = _new(torch.empty_like(k), stream) if dk is None else dk
     dv = _new(torch.empty_like(v), stream) if dv is None else dv
-    ws = _window_ws(p, OP_BWD, index, ws, stream)
-    _call("mosaic_bsa_window_bwd", index, stream, p, vq, vk, vv, vo, _flat("lse", lse, sq[:3], torch.float32, index), vd,
-          _len("q_len", q_len, p, index), _len("k_len", k_len, p, index), _out("dq", dq, sq, t, index),
-          _out("dk", dk, sk, t, index), _out("dv", dv, sk, t, index), ws.data_ptr(), ws.numel())
+    block = _block
+    a = block.at
+    _window_pack[8](block.buf, 0, *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
+                    *_out("dv", dv, sk, t, index))
+    ws = _window_ws(a, OP_BWD, index, ws, stream)
+    _call("mosaic_bsa_window_bwd", index, stream, a, a + 40, a + 72, a + 104, a + 136, _flat("lse", lse, sq[:3], torch.float32, index),
+          a + 168, _len("q_len", q_len, sq[0], index), _len("k_len", k_len, sq[0], index), a + 200, a + 232, a + 264, ws.data_ptr(),
+          ws.numel())
     return dq, dk, dv
 
 
@@ -598,6 +626,9 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _new(torch.empty_like(q), stream) if o is None else o
     lse = _new(torch.empty(sq[:3], dtype=torch.float32, device=index), stream) if lse is None else lse
-    _call("mosaic_bsa_window_decode", index, stream, p, vq, vk, vv, _len("k_len", k_len, p, index), _out("o", o, sq, t, index),
+    block = _block
+    a = block.at
+    _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    _call("mosaic_bsa_window_decode", index, stream, a, a + 40, a + 72, a + 104, _len("k_len", k_len, sq[0], index), a + 136,
           _flat("lse", lse, sq[:3], torch.float32, index))
     return o, lse

@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
   const Place pl = place<T, HALF>(a, lane);
   const int heads = a.t[0].heads, rows = heads + a.t[1].heads, ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ;
   Spot sp;
-  sp.start(a, blockIdx.x * kHeadWarps + warp + await_stream(), rows);
+  const int zero = await_stream();
+  sp.start(a, blockIdx.x * kHeadWarps + warp + zero, rows);
   sp.stride(a.step, a.step_b, a.step_n);
   uint4 va[kAhead], vb[kAhead];
   const char *xq = nullptr, *xk = nullptr;  // the rows' first
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
   }
   still_angles(a, angles[warp], lane);
   if constexpr (NORM) {
-    for (int c = threadIdx.x; c < 2 * a.d; c += kHeadThreads) weights[c >= a.d][c >= a.d ? c - a.d : c] = __ldg(c < a.d ? a.t[0].w + c : a.t[1].w + (c - a.d));
+    for (int c = threadIdx.x; c < 2 * a.d; c += kHeadThreads) weights[c >= a.d][c >= a.d ? c - a.d : c] = __ldg((c < a.d ? a.t[0].w + c : a.t[1].w + (c - a.d)) + zero);
     __syncthreads();
   }
   bool turned = false;  // the angles are this token's
@@ -323,7 +324,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_
   const HeadTensor& t = a.t[keys];
   const int ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ, cta = (int)blockIdx.x - (keys ? a.q_ctas : 0);
   Spot sp;
-  sp.start(a, cta * kHeadWarps + warp + await_stream(), t.heads);
+  const int zero = await_stream();
+  sp.start(a, cta * kHeadWarps + warp + zero, t.heads);
   if (keys) sp.stride(a.k_step, a.k_step_b, a.k_step_n);
   else sp.stride(a.step, a.step_b, a.step_n);
   uint4 va = make_uint4(0u, 0u, 0u, 0u), vb = va, ga = va, gb = va;
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_
     if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
   }
   still_angles(a, angles[warp], lane);
-  for (int c = threadIdx.x; c < a.d; c += kHeadThreads) weights[c] = __ldg(t.w + c);
+  for (int c = threadIdx.x; c < a.d; c += kHeadThreads) weights[c] = __ldg(t.w + c + zero);
   __syncthreads();
   uint64_t da[P], db[P];
 #pragma unroll

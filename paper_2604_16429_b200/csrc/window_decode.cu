@@ -19,7 +19,7 @@ namespace mosaic {
 
 namespace {
 
-constexpr int kDecThreads = 256, kDecWarps = kDecThreads / 32;
+constexpr int kDecThreads = 128, kDecWarps = kDecThreads / 32;
 constexpr int kStepKeys = 16;
 constexpr long long kKeysPerCta = 512;
 

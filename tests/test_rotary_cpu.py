@@ -75,10 +75,10 @@ def test_bad_scalings_are_refused(kw):
 def _call(name="rotary", ptr=256, strides=(64 * 8, 64, 64 * 4), pos_stride=0, ws=1 << 24, **kw):
     base = dict(B=1, H=4, Hkv=2, N=2, d=64, rot_dim=64, flags=0, amplitude=1.0, eps=1e-6)
     base.update(kw)
-    p = mb._RotaryParams(*(base[k] for k, _ in mb._RotaryParams._fields_))
+    p = ctypes.byref(mb._RotaryParams(*(base[k] for k, _ in mb._RotaryParams._fields_)))
     L = mb.lib()
-    v = mb._View(ptr, *strides)
-    good = mb._View(256, 64 * 8, 64, 64 * 4)
+    v = ctypes.byref(mb._View(ptr, *strides))
+    good = ctypes.byref(mb._View(256, 64 * 8, 64, 64 * 4))
     if name == "rotary":
         return L.mosaic_bsa_rotary(p, v, good, 256, pos_stride, 256, good, good, None)
     if name == "norm":
@@ -107,12 +107,12 @@ def test_what_only_one_entry_point_refuses():
     assert _call("norm", eps=float("nan")) == -1
     assert _call("bwd", ws=16) == -3
     assert mb.lib().mosaic_bsa_rotary(None, None, None, None, 0, None, None, None, None) == -1
-    p = mb._RotaryParams(1, 4, 2, 2, 64, 64, 0, 1.0, 1e-6)
-    v = mb._View(256, 512, 64, 256)
+    p = ctypes.byref(mb._RotaryParams(1, 4, 2, 2, 64, 64, 0, 1.0, 1e-6))
+    v = ctypes.byref(mb._View(256, 512, 64, 256))
     assert mb.lib().mosaic_bsa_rotary(p, v, v, None, 0, 256, v, v, None) == -1
     assert mb.lib().mosaic_bsa_rotary(p, v, v, 256, 0, 256 + 4, v, v, None) == -4
     assert mb.lib().mosaic_bsa_rotary(p, v, None, 256, 0, 256, v, v, None) == -1
-    assert mb.lib().mosaic_bsa_qk_norm_workspace_bytes(mb._RotaryParams(1, 4, 3, 2, 64, 64, 0, 1.0, 1e-6)) == 0
+    assert mb.lib().mosaic_bsa_qk_norm_workspace_bytes(ctypes.byref(mb._RotaryParams(1, 4, 3, 2, 64, 64, 0, 1.0, 1e-6))) == 0
     assert mb.lib().mosaic_bsa_qk_norm_workspace_bytes(p) % 256 == 0
 
 
