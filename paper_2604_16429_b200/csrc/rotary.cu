@@ -22,6 +22,8 @@ enum { kBf16 = 0, kF16 = 1, kF32 = 2 };
 constexpr int kHeadThreads = 256, kHeadWarps = kHeadThreads / 32;
 constexpr int kMaxHeadDim = 256;
 constexpr int kCtas = 2;       // per SM
+constexpr int kDeep = 3;       // batches of rows of the backward on their way (shared memory)
+constexpr size_t kBwdRing = (size_t)kHeadWarps * kDeep * 4 * 32 * 16;
 constexpr int kAhead = 2;      // rows that a group of lanes has in flight
 
 struct HeadTensor {
@@ -63,6 +65,11 @@ __device__ __forceinline__ uint64_t mul2f(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+
+// 16 bytes of global memory to shared memory, or (bytes 0) zeros
+__device__ __forceinline__ void copy_async(uint32_t dst, const char* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 template <int T>
@@ -318,40 +325,52 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_
   __shared__ alignas(16) Angles angles[kHeadWarps];
   __shared__ alignas(16) float weights[kMaxHeadDim];
   __shared__ float sums[kHeadWarps][kMaxHeadDim];
+  extern __shared__ uint4 ring[];  // [warp][kDeep][x, x, g, g][lane]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place pl = place<T, HALF>(a, lane);
   const bool keys = (int)blockIdx.x >= a.q_ctas;
   const HeadTensor& t = a.t[keys];
   const int ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ, cta = (int)blockIdx.x - (keys ? a.q_ctas : 0);
-  Spot sp;
+  Spot sp, ft;  // the batch that is worked on, and the one that is asked for, kDeep - 1 further
   const int zero = await_stream();
   sp.start(a, cta * kHeadWarps + warp + zero, t.heads);
   if (keys) sp.stride(a.k_step, a.k_step_b, a.k_step_n);
   else sp.stride(a.step, a.step_b, a.step_n);
-  uint4 va = make_uint4(0u, 0u, 0u, 0u), vb = va, ga = va, gb = va;
+  ft = sp;
   const char *x = nullptr, *g = nullptr;  // this lane's next row
   char* y = nullptr;
   const long long ox = pl.group * t.x.sh + ca, og = pl.group * t.g.sh + ca, oy = pl.group * t.y.sh + ca;
   const long long jx = pl.groups * t.x.sh, jg = pl.groups * t.g.sh, jy = pl.groups * t.y.sh;
   auto find = [&]() {
-    x = t.x.data + sp.b * t.x.sb + sp.n * t.x.sn + sp.r0 * t.x.sh + ox;
-    g = t.g.data + sp.b * t.g.sb + sp.n * t.g.sn + sp.r0 * t.g.sh + og;
+    x = t.x.data + ft.b * t.x.sb + ft.n * t.x.sn + ft.r0 * t.x.sh + ox;
+    g = t.g.data + ft.b * t.g.sb + ft.n * t.g.sn + ft.r0 * t.g.sh + og;
   };
-  auto fetch = [&]() {
-    va = vb = ga = gb = make_uint4(0u, 0u, 0u, 0u);
-    if (sp.r0 + pl.group < sp.r1 && pl.on) {
-      va = *reinterpret_cast<const uint4*>(x);
-      vb = *reinterpret_cast<const uint4*>(x + ba);
-      ga = *reinterpret_cast<const uint4*>(g);
-      gb = *reinterpret_cast<const uint4*>(g + ba);
+  if (ft.more) find();
+  const uint4* mine = ring + (warp * kDeep * 4) * 32 + lane;  // (a lane reads what it copied itself)
+  const uint32_t at = (uint32_t)__cvta_generic_to_shared(mine);
+  auto fetch = [&](int slot) {
+    if (ft.more) {
+      const uint32_t dst = at + slot * 4 * 32 * 16, bytes = ft.r0 + pl.group < ft.r1 && pl.on ? 16u : 0u;  // 0: zeros
+      const char *p = bytes ? x : t.x.data, *q = bytes ? g : t.g.data;
+      copy_async(dst, p, bytes);
+      copy_async(dst + 512, p + (bytes ? ba : 0), bytes);
+      copy_async(dst + 1024, q, bytes);
+      copy_async(dst + 1536, q + (bytes ? ba : 0), bytes);
+      ft.r0 += pl.groups;
+      if (ft.r0 >= ft.r1) {
+        ft.next(a, t.heads);
+        if (ft.more) find();
+      } else {
+        x += jx;
+        g += jg;
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  long long pos = 0;
-  if (sp.more) {
-    find();
-    fetch();
-    if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
-  }
+#pragma unroll
+  for (int i = 0; i < kDeep - 1; ++i) fetch(i);
+  auto position = [&](const Spot& s) { return s.more && a.rot ? __ldg(a.pos + s.b * a.pos_stride + s.n) : 0ll; };
+  long long pos = position(sp);
   still_angles(a, angles[warp], lane);
   for (int c = threadIdx.x; c < a.d; c += kHeadThreads) weights[c] = __ldg(t.w + c + zero);
   __syncthreads();
@@ -359,17 +378,24 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_
 #pragma unroll
   for (int j = 0; j < P; ++j) da[j] = db[j] = 0ull;
   bool turned = false;
+  int slot = 0;
   while (sp.more) {
+    fetch(slot ? slot - 1 : kDeep - 1);  // where the batch before was
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
     float ha[V], hb[V], fa[V], fb[V];
-    widen<T>(ga, ha);
-    widen<T>(gb, hb);
-    widen<T>(va, fa);
-    widen<T>(vb, fb);
+    widen<T>(mine[(slot * 4 + 0) * 32], fa);
+    widen<T>(mine[(slot * 4 + 1) * 32], fb);
+    widen<T>(mine[(slot * 4 + 2) * 32], ha);
+    widen<T>(mine[(slot * 4 + 3) * 32], hb);
+    slot = slot + 1 == kDeep ? 0 : slot + 1;
     const bool there = sp.r0 + pl.group < sp.r1;
     if (!turned) {
       make_angles(a, pos, angles[warp], lane);
       y = t.y.data + sp.b * t.y.sb + sp.n * t.y.sn + sp.r0 * t.y.sh + oy;
       turned = true;
+      Spot after = sp;
+      after.next(a, t.heads);
+      pos = position(after);  // (asked for a token ahead)
     }
     char* out = y;
     y += jy;
@@ -377,15 +403,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_
     if (sp.r0 >= sp.r1) {
       sp.next(a, t.heads);
       turned = false;
-      if (sp.more) {
-        find();
-        if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
-      }
-    } else {
-      x += jx;
-      g += jg;
     }
-    if (sp.more) fetch();
     turn<V, HALF>(ha, hb, angles[warp], a, pl);
     float wa[V], wb[V];
     read_weights<V>(weights, pl, wa, wb);
@@ -529,7 +547,10 @@ int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t strea
 
 template <int T, bool HALF>
 int launch_head_bwd(const HeadArgs& a, int ctas, cudaStream_t stream) {
-  return launch_kernel(head_bwd_kernel<T, HALF>, dim3((unsigned)ctas), kHeadThreads, 0, stream, true, 0, a);
+  static unsigned long long configured = 0;
+  int sms = 0;
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_bwd_kernel<T, HALF>), kBwdRing, &configured, &sms)) return rc;
+  return launch_kernel(head_bwd_kernel<T, HALF>, dim3((unsigned)ctas), kHeadThreads, kBwdRing, stream, true, 0, a);
 }
 int launch_head_bwd(const HeadArgs& a, uint32_t flags, int ctas, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;

@@ -288,9 +288,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t tcs = tmem + score_col(t, b);
       const uint64_t kd = smem_desc(s32(sm.kv[k_slot]));
       ok = ok && warp_wait_here(s32(&sm.kv_full[k_slot]), (slot_no / kSlots) & 1, abort, status);
-      // P V of the step that had the buffer (two before) reads its weights there.  It was issued before, and products of one shape run
-      // in issue order; of different shapes they need not.  (Waiting always costs 8 % at d = 128, where the shapes differ.)
-      if (u >= 2 && (D != U || round32(cols) != U)) ok = ok && warp_wait_here(s32(&sm.pv_done[t][b]), (u / 2 - 1) & 1, abort, status);
+      // P V of the step that had the buffer (two before) reads its weights there: it was issued before, but only products of one
+      // shape into one accumulator are sure to run in issue order.  (The wait costs 8 % at d = 128, nothing at 64.)
+      if (u >= 2) ok = ok && warp_wait_here(s32(&sm.pv_done[t][b]), (u / 2 - 1) & 1, abort, status);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
