@@ -21,10 +21,11 @@ namespace {
 enum { kBf16 = 0, kF16 = 1, kF32 = 2 };
 constexpr int kHeadThreads = 256, kHeadWarps = kHeadThreads / 32;
 constexpr int kMaxHeadDim = 256;
-constexpr int kCtas = 2;       // per SM
+constexpr int kCtas = 4, kBwdCtas = 2;  // per SM
 constexpr int kDeep = 3;       // batches of rows of the backward on their way (shared memory)
 constexpr size_t kBwdRing = (size_t)kHeadWarps * kDeep * 4 * 32 * 16;
-constexpr int kAhead = 2;      // rows that a group of lanes has in flight
+constexpr int kDeepFwd = 3;    // the same of the forward, where a row comes without a gradient
+constexpr size_t kFwdRing = (size_t)kHeadWarps * kDeepFwd * 2 * 32 * 16;
 
 struct HeadTensor {
   View x, g;  // input; gradient of the output (backward)
@@ -222,96 +223,98 @@ struct Spot {
   }
 };
 
-// The warps walk their tasks with the next batch's rows already asked for.  A token's rows are Q's heads, then K's.
+// The warps walk their tasks with the next batches' rows already asked for: they land in shared memory, where every lane reads what
+// it copied itself (held in registers instead, 62 us became 84 in the backward).  A token's rows are Q's heads, then K's.
 template <int T, bool HALF, bool NORM>
-__global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constant__ HeadArgs a) {
+__global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes;
   __shared__ alignas(16) Angles angles[kHeadWarps];
   __shared__ alignas(16) float weights[2][kMaxHeadDim];
+  extern __shared__ uint4 ring[];  // [warp][kDeepFwd][piece][lane]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place pl = place<T, HALF>(a, lane);
   const int heads = a.t[0].heads, rows = heads + a.t[1].heads, ca = pl.ca * SZ, ba = (pl.cb - pl.ca) * SZ;
-  Spot sp;
+  Spot sp, ft;  // the batch that is worked on, and the one that is asked for, kDeepFwd - 1 further
   const int zero = await_stream();
   sp.start(a, blockIdx.x * kHeadWarps + warp + zero, rows);
   sp.stride(a.step, a.step_b, a.step_n);
-  uint4 va[kAhead], vb[kAhead];
+  ft = sp;
   const char *xq = nullptr, *xk = nullptr;  // the rows' first
   auto find = [&]() {
-    xq = a.t[0].x.data + sp.b * a.t[0].x.sb + sp.n * a.t[0].x.sn + ca;
-    xk = a.t[1].x.data + sp.b * a.t[1].x.sb + sp.n * a.t[1].x.sn + ca - heads * a.t[1].x.sh;
+    xq = a.t[0].x.data + ft.b * a.t[0].x.sb + ft.n * a.t[0].x.sn + ca;
+    xk = a.t[1].x.data + ft.b * a.t[1].x.sb + ft.n * a.t[1].x.sn + ca - heads * a.t[1].x.sh;
   };
-  auto fetch = [&]() {
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int h = sp.r0 + pl.group + k * pl.groups;
-      va[k] = vb[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < sp.r1 && pl.on) {
-        const char* x = h < heads ? xq + h * a.t[0].x.sh : xk + h * a.t[1].x.sh;
-        va[k] = *reinterpret_cast<const uint4*>(x);
-        vb[k] = *reinterpret_cast<const uint4*>(x + ba);
+  if (ft.more) find();
+  const uint4* mine = ring + (warp * kDeepFwd * 2) * 32 + lane;
+  const uint32_t at = (uint32_t)__cvta_generic_to_shared(mine);
+  auto fetch = [&](int slot) {
+    if (ft.more) {
+      const int h = ft.r0 + pl.group;
+      const uint32_t dst = at + slot * 2 * 32 * 16, bytes = h < ft.r1 && pl.on ? 16u : 0u;  // 0: zeros
+      const char* p = !bytes ? a.t[0].x.data : h < heads ? xq + h * a.t[0].x.sh : xk + h * a.t[1].x.sh;
+      copy_async(dst, p, bytes);
+      copy_async(dst + 512, p + (bytes ? ba : 0), bytes);
+      ft.r0 += pl.groups;
+      if (ft.r0 >= ft.r1) {
+        ft.next(a, rows);
+        if (ft.more) find();
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  long long pos = 0;
-  if (sp.more) {
-    find();
-    fetch();
-    if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
-  }
+#pragma unroll
+  for (int i = 0; i < kDeepFwd - 1; ++i) fetch(i);
+  auto position = [&](const Spot& s) { return s.more && a.rot ? __ldg(a.pos + s.b * a.pos_stride + s.n) : 0ll; };
+  long long pos = position(sp);
   still_angles(a, angles[warp], lane);
   if constexpr (NORM) {
     for (int c = threadIdx.x; c < 2 * a.d; c += kHeadThreads) weights[c >= a.d][c >= a.d ? c - a.d : c] = __ldg((c < a.d ? a.t[0].w + c : a.t[1].w + (c - a.d)) + zero);
     __syncthreads();
   }
+  char *yq = nullptr, *yk = nullptr;
   bool turned = false;  // the angles are this token's
+  int slot = 0;
   while (sp.more) {
-    uint4 wa[kAhead], wb[kAhead];
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) { wa[k] = va[k]; wb[k] = vb[k]; }
-    const int r0 = sp.r0, r1 = sp.r1;
-    char* yq = a.t[0].y.data + sp.b * a.t[0].y.sb + sp.n * a.t[0].y.sn + ca;
-    char* yk = a.t[1].y.data + sp.b * a.t[1].y.sb + sp.n * a.t[1].y.sn + ca - heads * a.t[1].y.sh;
-    const long long p = pos;
-    const bool fresh = !turned;
-    turned = true;
-    sp.r0 += kAhead * pl.groups;
+    fetch(slot ? slot - 1 : kDeepFwd - 1);  // where the batch before was
+    if (!turned) {
+      make_angles(a, pos, angles[warp], lane);
+      yq = a.t[0].y.data + sp.b * a.t[0].y.sb + sp.n * a.t[0].y.sn + ca;
+      yk = a.t[1].y.data + sp.b * a.t[1].y.sb + sp.n * a.t[1].y.sn + ca - heads * a.t[1].y.sh;
+      turned = true;
+      Spot after = sp;
+      after.next(a, rows);
+      pos = position(after);  // (asked for a token ahead)
+    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDeepFwd - 1) : "memory");
+    float fa[V], fb[V];
+    widen<T>(mine[(slot * 2 + 0) * 32], fa);
+    widen<T>(mine[(slot * 2 + 1) * 32], fb);
+    slot = slot + 1 == kDeepFwd ? 0 : slot + 1;
+    const int h = sp.r0 + pl.group;
+    const bool there = h < sp.r1;
+    sp.r0 += pl.groups;
     if (sp.r0 >= sp.r1) {
       sp.next(a, rows);
       turned = false;
-      if (sp.more) {
-        find();
-        if (a.rot) pos = __ldg(a.pos + sp.b * a.pos_stride + sp.n);
+    }
+    if constexpr (NORM) {
+      float ss = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) ss = fmaf(fa[j], fa[j], fmaf(fb[j], fb[j], ss));
+      const float rr = rsqrtf(row_sum(ss, a.lanes) * a.inv_d + a.eps);
+      float ga[V], gb[V];
+      read_weights<V>(weights[h >= heads], pl, ga, gb);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        fa[j] *= rr * ga[j];
+        fb[j] *= rr * gb[j];
       }
     }
-    if (sp.more) fetch();
-    if (fresh) make_angles(a, p, angles[warp], lane);
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int h = r0 + pl.group + k * pl.groups;
-      if (h - pl.group >= r1) break;
-      float fa[V], fb[V];
-      widen<T>(wa[k], fa);
-      widen<T>(wb[k], fb);
-      if constexpr (NORM) {
-        float ss = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) ss = fmaf(fa[j], fa[j], fmaf(fb[j], fb[j], ss));
-        const float rr = rsqrtf(row_sum(ss, a.lanes) * a.inv_d + a.eps);
-        float ga[V], gb[V];
-        read_weights<V>(weights[h >= heads], pl, ga, gb);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          fa[j] *= rr * ga[j];
-          fb[j] *= rr * gb[j];
-        }
-      }
-      turn<V, HALF>(fa, fb, angles[warp], a, pl);
-      if (h < r1 && pl.on) {
-        char* y = h < heads ? yq + h * a.t[0].y.sh : yk + h * a.t[1].y.sh;
-        *reinterpret_cast<uint4*>(y) = narrow<T>(fa);
-        *reinterpret_cast<uint4*>(y + ba) = narrow<T>(fb);
-      }
+    turn<V, HALF>(fa, fb, angles[warp], a, pl);
+    if (there && pl.on) {
+      char* y = h < heads ? yq + h * a.t[0].y.sh : yk + h * a.t[1].y.sh;
+      *reinterpret_cast<uint4*>(y) = narrow<T>(fa);
+      *reinterpret_cast<uint4*>(y + ba) = narrow<T>(fb);
     }
   }
 }
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constan
 // CTAs have Q's rows, the others K's, and each leaves one row of partial sums.  Packed fp32 arithmetic: the pass is as much bound
 // by instructions as by memory.
 template <int T, bool HALF>
-__global__ void __launch_bounds__(kHeadThreads, 2) head_bwd_kernel(const __grid_constant__ HeadArgs a) {
+__global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes, P = V / 2;
   __shared__ alignas(16) Angles angles[kHeadWarps];
   __shared__ alignas(16) float weights[kMaxHeadDim];
@@ -530,13 +533,17 @@ int plan(HeadArgs* a, int rows, int sms, long long ctas) {
   return spread(a, ctas);
 }
 
-template <int T, bool HALF>
-int launch_head(HeadArgs a, bool norm, cudaStream_t stream) {
+template <int T, bool HALF, bool NORM>
+int launch_head(HeadArgs a, cudaStream_t stream) {
+  static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(nullptr, 0, nullptr, &sms)) return rc;
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_kernel<T, HALF, NORM>), kFwdRing, &configured, &sms)) return rc;
   const int blocks = plan(&a, a.t[0].heads + a.t[1].heads, sms, (long long)kCtas * sms);
-  return launch_kernel(norm ? head_kernel<T, HALF, true> : head_kernel<T, HALF, false>, dim3((unsigned)blocks), kHeadThreads, 0, stream,
-                       true, 0, a);
+  return launch_kernel(head_kernel<T, HALF, NORM>, dim3((unsigned)blocks), kHeadThreads, kFwdRing, stream, true, 0, a);
+}
+template <int T, bool HALF>
+int launch_head(const HeadArgs& a, bool norm, cudaStream_t stream) {
+  return norm ? launch_head<T, HALF, true>(a, stream) : launch_head<T, HALF, false>(a, stream);
 }
 int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;
@@ -674,7 +681,7 @@ int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params* p, const mosaic_view* q, 
   int sms = 0;
   if ((rc = launch_setup(nullptr, 0, nullptr, &sms))) return rc;
   // CTAs in the ratio of the work: a token's rows by rounds of the warp, and its angles as much as two rounds
-  const int groups = 32 / a.lanes, work_q = 2 + (p->H + groups - 1) / groups, work_k = 2 + (p->Hkv + groups - 1) / groups, most = kCtas * sms;
+  const int groups = 32 / a.lanes, work_q = 2 + (p->H + groups - 1) / groups, work_k = 2 + (p->Hkv + groups - 1) / groups, most = kBwdCtas * sms;
   const int most_q = most * work_q / (work_q + work_k) > 0 ? most * work_q / (work_q + work_k) : 1;
   HeadArgs k_plan = a;
   a.q_ctas = plan(&a, p->H, sms, most_q);
