@@ -27,9 +27,6 @@ __device__ __forceinline__ Span span_of(const WinGeo& g, int b) {
   return s;
 }
 
-// Does the row at position p see key j (j < kl)?
-__device__ __forceinline__ bool sees(const WinGeo& g, int p, int j) { return j <= p && (p - j < g.window || j < g.sinks); }
-
 // The bounded waits without a call: the registers of a warpgroup that raised or lowered its count would all be saved around one
 // (2 KB of stack and as many spills a thread in the forward).
 __device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int* abort, int* status) {
@@ -54,32 +51,6 @@ __device__ __forceinline__ bool warp_wait_here(uint32_t bar, uint32_t parity, vo
 
 // The lowest n bits (n any integer)
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
-
-// 2^x for two values on the FMA pipe: x = n + f with n = round(x), |f| <= 1/2, 2^f by a quartic (largest relative error 2.9e-6:
-// the sum of a row, which log-sum-exp returns in fp32, keeps five digits more than the 16-bit weights need), 2^n into the exponent.
-// Clamped at -125.  A NaN does not come out as one, but as a number beyond every 16-bit type, which makes the row not finite.
-__device__ __forceinline__ float clamp_nan(float x) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(-125.f));
-  return y;
-}
-__device__ __forceinline__ void ex2_quartic(uint64_t x2, float& p0, float& p1) {
-  float x0, x1;
-  unpack2(x2, x0, x1);
-  const uint64_t xc = pack2(clamp_nan(x0), clamp_nan(x1));
-  const uint64_t t = add2(xc, pack2(12582912.f, 12582912.f));
-  const uint64_t n = add2(t, pack2(-12582912.f, -12582912.f));
-  const uint64_t f = fma2(n, pack2(-1.f, -1.f), xc);
-  uint64_t p = fma2(f, pack2(0.009582853f, 0.009582853f), pack2(0.055906426f, 0.055906426f));
-  p = fma2(p, f, pack2(0.240240991f, 0.240240991f));
-  p = fma2(p, f, pack2(0.693124175f, 0.693124175f));
-  p = fma2(p, f, pack2(1.f, 1.f));
-  float t0, t1, q0, q1;
-  unpack2(t, t0, t1);
-  unpack2(p, q0, q1);
-  p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
-  p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
-}
 
 // `bytes` (a multiple of 16, both ends aligned) of global memory to shared memory
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -110,6 +81,18 @@ __device__ __forceinline__ void zero_rows(unsigned char* tile, int first, int ro
 }
 
 int make_win_geo(const mosaic_window_params* p, const int32_t* q_len, const int32_t* k_len, WinGeo* g);
+
+// launch_setup for a kernel whose warpgroups share out `regs` registers a thread anew: refused if the compiler gave it another
+// number, because the increase would then wait for registers that nobody has.  (`done` as there.)
+inline int launch_setup_regs(const void* func, int regs, size_t smem, unsigned long long* done, int* sms) {
+  const unsigned long long before = *done;
+  const int rc = launch_setup(func, smem, done, sms);
+  if (rc || *done == before) return rc;
+  cudaFuncAttributes at;
+  if (cudaFuncGetAttributes(&at, func) != cudaSuccess) { *done = before; return MOSAIC_E_CUDA; }
+  if (at.numRegs != regs) { *done = before; return MOSAIC_E_UNSUPPORTED; }
+  return MOSAIC_OK;
+}
 
 // Views whose heads or members all lie at one place (stride 0) have a map with one of them.
 struct Fold {

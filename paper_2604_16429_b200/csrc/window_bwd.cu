@@ -517,7 +517,8 @@ int launch_pass(const HostCtx& c, const WinGeo& g, const View& x0, const View& y
   const size_t smem = sizeof(Smem<D>) + 1024;
   static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(reinterpret_cast<const void*>(window_bwd_kernel<D, F16, KEYS>), smem, &configured, &sms)) return rc;
+  const void* func = reinterpret_cast<const void*>(window_bwd_kernel<D, F16, KEYS>);
+  if (const int rc = launch_setup_regs(func, Plan<D, KEYS>::kLaunchRegs, smem, &configured, &sms)) return rc;
   const long long total = (long long)g.B * h0 * (a.tiles + a.pieces);
   if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
   return launch_kernel(window_bwd_kernel<D, F16, KEYS>, dim3((unsigned)(total < sms ? total : sms)), Plan<D, KEYS>::kThreads, smem, c.stream, true, 0, g,

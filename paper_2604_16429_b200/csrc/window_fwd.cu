@@ -502,7 +502,7 @@ int launch(const HostCtx& c, const WinGeo& g, const View& q, const View& k, cons
   const size_t smem = sizeof(Smem<D>) + 1024;
   static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(reinterpret_cast<const void*>(window_fwd_kernel<D, F16>), smem, &configured, &sms)) return rc;
+  if (const int rc = launch_setup_regs(reinterpret_cast<const void*>(window_fwd_kernel<D, F16>), kLaunchRegs, smem, &configured, &sms)) return rc;
   const long long tiles = (long long)g.G * ((g.Nq + kRows - 1) / kRows), per = (tiles + 1) / 2, total = per * g.B * g.Hkv;
   if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
   return launch_kernel(window_fwd_kernel<D, F16>, dim3((unsigned)(total < sms ? total : sms)), kThreads, smem, c.stream, true, 0, g, mq,

@@ -263,3 +263,174 @@ def test_the_same_bits_every_time(case):
     for _ in range(25):
         for name, a, b in zip(("o", "lse", "dq", "dk", "dv"), first, both()):
             assert torch.equal(a, b), name
+
+
+def test_a_scale_of_the_callers():
+    q, k, v, d_o = make(1, 2, 1, 200, 200, 64, seed=7)
+    check_bwd(mb.WindowParams(window=50, sinks=2, scale=0.3), q, k, v, d_o)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_scores(d):
+    """Scores of some hundreds, falling and rising along the rows, so that the running maximum moves in most steps."""
+    q, k, v, _ = make(1, 2, 1, 600, 600, d, seed=8, sharp=6.0)
+    k *= (1 + torch.arange(600, device="cuda")[:, None] % 150 / 30).to(k.dtype)
+    check_fwd(mb.WindowParams(window=333, sinks=9), q, k, v)
+
+
+def test_slices_of_a_fused_projection_and_broadcast_heads():
+    B, H, Hkv, N, d = 2, 4, 2, 270, 64
+    g = torch.Generator().manual_seed(9)
+    fused = torch.randn((B, N, H + 2 * Hkv, d), generator=g).bfloat16().cuda()
+    q, k, v = (fused[:, :, a:b].transpose(1, 2) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+    d_o = torch.randn((B, N, H, d), generator=g).bfloat16().cuda().transpose(1, 2)
+    wp = mb.WindowParams(window=77, sinks=3)
+    check_bwd(wp, q, k, v, d_o)
+    # one key head for all, broadcast by a stride of zero; the gradients then come a head each
+    k1, v1 = k[:, :1].expand(B, H, N, d), v[:1, :1].expand(B, H, N, d)
+    check_bwd(wp, q, k1, v1, d_o)
+    o, lse = mb.mosaic_bsa_window_decode(wp, q[:, :, -1:], k1, v1)
+    want = mb.mosaic_bsa_window_decode(wp, q[:, :, -1:].contiguous(), k1.contiguous(), v1.contiguous())
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 2.4e9 elements: its last head starts at 4.3e9 bytes, its last rows lie at 4.8e9."""
+    Hkv, Nk, d = 9, 1 << 21, 128
+    k = torch.zeros((1, Hkv, Nk, d), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    n = 400
+    qs, ks, vs, _ = make(1, Hkv, Hkv, 130, n, d, seed=10)
+    k[:, :, -n:], v[:, :, -n:] = ks, vs
+    wp = mb.WindowParams(window=250, sinks=0)
+    want = mb.mosaic_bsa_window_fwd(wp, qs, ks, vs)
+    got = mb.mosaic_bsa_window_fwd(wp, qs, k, v)
+    # steps start at other keys here: the same sums in another order
+    E, u = score_error(qs, ks, 0), torch.finfo(qs.dtype).eps / 2
+    ref64 = ref.attention(qs[:, -1:], ks[:, -1:], vs[:, -1:], 250, 0)
+    for o, lse in (want, got):
+        tol = u * ref64["o"].abs() + (u + E) * ref64["p_abs"] + 1e-7
+        assert ((o[:, -1:].double() - ref64["o"]).abs() <= tol).all()
+        assert ((lse[:, -1:] - ref64["lse"]).abs() <= E + 2.0 ** -23 * ref64["lse"].abs()).all()
+    one = mb.mosaic_bsa_window_decode(wp, qs[:, :, -1:].contiguous(), k, v)
+    tol = u * ref64["o"][:, :, -1:].abs() + (u + E) * ref64["p_abs"][:, :, -1:] + 1e-7
+    assert ((one[0][:, -1:].double() - ref64["o"][:, :, -1:]).abs() <= tol).all()
+
+
+def test_on_another_stream_and_in_two_graphs():
+    q, k, v, d_o = make(2, 4, 2, 300, 300, 64, seed=11)
+    wp = mb.WindowParams(window=100, sinks=4)
+
+    def all_of_it(**kw):
+        o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v, **kw)
+        return (o, lse) + mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, **kw) + mb.mosaic_bsa_window_decode(wp, q[:, :, -1:], k, v, **kw)
+
+    want = all_of_it()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = all_of_it(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    ws = torch.empty(mb.window_workspace_bytes(wp, q, k, mb.OP_BWD), dtype=torch.uint8, device="cuda")
+    graphs, outs = [], []
+    for _ in range(2):  # two graphs on one workspace, replayed in turn on one stream
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v, ws=ws)
+            outs.append((o, lse) + mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, ws=ws))
+    for x in outs[0] + outs[1]:
+        x.fill_(NAN)
+    for i in (0, 1, 0):
+        graphs[i].replay()
+    torch.cuda.synchronize()
+    for got in outs:
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_refusals_of_the_binding():
+    q, k, v, d_o = make(2, 4, 2, 30, 40, 64, seed=12)
+    wp = mb.WindowParams(window=10)
+    ln = lens([30, 30])
+    for kw in (dict(q=q.float()), dict(k=k.half()), dict(v=v[:, :, :39]), dict(q=q[..., ::2]), dict(k=k[:1]), dict(q_len=ln.long()),
+               dict(k_len=ln[:1]), dict(k_len=ln.cpu()), dict(o=q.float()), dict(lse=torch.empty(2, 4, 29, device="cuda")), dict(q=q.cpu()),
+               dict(o=q[:1].expand_as(q)), dict(q=q.double()), dict(ws=torch.empty(256, device="cuda"))):
+        with pytest.raises(ValueError):
+            mb.mosaic_bsa_window_fwd(wp, **{**dict(q=q, k=k, v=v), **kw})
+    o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v)
+    for kw in (dict(d_o=d_o.half()), dict(lse=lse.double()), dict(dk=k[:, :1].expand_as(k)), dict(dv=q), dict(dq=q.transpose(0, 1))):
+        with pytest.raises(ValueError):
+            mb.mosaic_bsa_window_bwd(wp, **{**dict(q=q, k=k, v=v, o=o, lse=lse, d_o=d_o), **kw})
+    with pytest.raises(mb.MosaicError) as e:
+        mb.mosaic_bsa_window_decode(wp, q, k, v)  # thirty tokens at once
+    assert e.value.code == -1
+    with pytest.raises(mb.MosaicError) as e:
+        mb.mosaic_bsa_window_fwd(wp, q, k, v, ws=torch.empty(128, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == -3
+
+
+@pytest.mark.parametrize("d,half", [(64, False), (128, True)])
+def test_a_layer_in_training(d, half):
+    """Norm and rotation, attention, and both backward passes, as a layer chains them, each stage against 64 bits on what the stage
+    before it really gave."""
+    from tests import test_gpu_rotary as R
+    B, H, Hkv, N = 2, 6, 2, 333
+    q, k, v, d_o = make(B, H, Hkv, N, N, d, "bf16", "bnhd", seed=13)
+    rp = mb.RotaryParams(d=d, half=half, scaling=mb.ROTARY_PARTS, factor=4.0, length=4096.0)
+    pos, fr = torch.arange(N, device="cuda") + 5000, mb.rotary_freqs(rp)
+    wq, wk = 1 + 0.1 * torch.randn(d, device="cuda"), 1 + 0.1 * torch.randn(d, device="cuda")
+    wp = mb.WindowParams(window=90, sinks=4)
+    qn, kn = mb.mosaic_bsa_qk_norm(rp, q, k, wq, wk, pos, fr)
+    for x, w, y in ((q, wq, qn), (k, wk, kn)):
+        n = R.norm64(x.double(), w, 1e-6)
+        R.near(y, R.turn64(n, pos, rp), 2e-6, R.length(n), "norm")
+    want, (dqn, dkn, dv) = check_bwd(wp, qn, kn, v, d_o)
+    dq, dk, dwq, dwk = mb.mosaic_bsa_qk_norm_bwd(rp, q, k, wq, wk, pos, fr, dqn, dkn)
+    for x, w, dy, dx, dw in ((q, wq, dqn, dq, dwq), (k, wk, dkn, dk, dwk)):
+        ref_dx, ref_dw, size, terms = R.grads64(x, w, dy, pos, rp, 1e-6)
+        R.near(dx, ref_dx, 4e-6, size, "dx")
+        assert ((dw.double() - ref_dw).abs() <= 1.2e-5 * terms).all()
+
+
+def test_tokens_one_by_one_over_a_rolling_cache_are_the_prompt():
+    """A stream of 300 tokens, rotated at its true positions, whose cache keeps 3 sinks and 40 places."""
+    H, Hkv, d, N, W, S = 4, 2, 64, 300, 40, 3
+    q, k, v, _ = make(1, H, Hkv, N, N, d, seed=14)
+    rp = mb.RotaryParams(d=d, half=True)
+    fr = mb.rotary_freqs(rp)
+    qr, kr = mb.mosaic_bsa_rotary(rp, q, k, torch.arange(N, device="cuda"), fr)
+    wp = mb.WindowParams(window=W, sinks=S, rolling=True)
+    o, lse = mb.mosaic_bsa_window_fwd(mb.WindowParams(window=W, sinks=S), qr, kr, v)
+    want = ref.attention(qr, kr, v, W, S)
+    kc, vc = torch.full((1, Hkv, W + S, d), NAN, dtype=k.dtype, device="cuda"), torch.full((1, Hkv, W + S, d), NAN, dtype=k.dtype, device="cuda")
+    E, u = score_error(qr, kr, 0), torch.finfo(q.dtype).eps / 2
+    for j in range(N):
+        q1, k1 = mb.mosaic_bsa_rotary(rp, q[:, :, j:j + 1], k[:, :, j:j + 1], torch.tensor([j], device="cuda"), fr)
+        assert torch.equal(q1, qr[:, :, j:j + 1]) and torch.equal(k1, kr[:, :, j:j + 1])
+        slot = j if j < S else S + (j - S) % W
+        kc[:, :, slot], vc[:, :, slot] = k1[:, :, 0], v[:, :, j]
+        if j in (0, 1, 2, 3, 42, 43, 44, 150, 299):
+            o1, l1 = mb.mosaic_bsa_window_decode(wp, q1, kc, vc, k_len=lens([j + 1]))
+            for a, b in ((o1, o[:, :, j:j + 1]),):
+                tol = u * want["o"][:, :, j:j + 1].abs() + (u + E) * want["p_abs"][:, :, j:j + 1] + 1e-7
+                assert ((a.double() - want["o"][:, :, j:j + 1]).abs() <= tol).all() and ((b.double() - want["o"][:, :, j:j + 1]).abs() <= tol).all()
+            assert ((l1[..., 0] - want["lse"][:, :, j]).abs() <= E + 2.0 ** -22 * want["lse"][:, :, j].abs()).all()
+
+
+def test_gradients_against_differences():
+    """Central differences of the 64-bit forward along random directions: a step of 1e-4 leaves some 1e-8 of third derivatives, and a
+    gradient of n elements that are off by tol each is off by tol times the direction's sum of magnitudes."""
+    q, k, v, d_o = make(1, 2, 1, 40, 40, 64, "fp16", seed=15)
+    wp = mb.WindowParams(window=9, sinks=2)
+    o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v)
+    grads = mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o)
+    want = ref.attention(q, k, v, 9, 2, 0.0, None, None, d_o)
+    E, u = score_error(q, k, 0), torch.finfo(q.dtype).eps / 2
+    g = torch.Generator().manual_seed(16)
+    x = [q.double(), k.double(), v.double()]
+    loss = lambda y: (ref.attention(*y, 9, 2)["o"] * d_o.double()).sum()  # noqa: E731
+    for i, name in enumerate(("dq", "dk", "dv")):
+        t = torch.randn(x[i].shape, generator=g).double().cuda()
+        up, down = ([y + s * 1e-4 * t if j == i else y for j, y in enumerate(x)] for s in (1, -1))
+        diff = float(loss(up) - loss(down)) / 2e-4
+        tol = u * want[name].abs() + 2 * (u + E) * want[name + "_abs"] + 40 * 2.0 ** -25 * 4
+        assert abs(float((grads[i].double() * t).sum()) - diff) <= float((tol * t.abs()).sum()) + 1e-5, name
