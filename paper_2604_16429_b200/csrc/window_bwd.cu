@@ -32,6 +32,7 @@ struct Plan {
   static constexpr int kGroups = KEYS && D == 128 ? 2 : 3;
   static constexpr uint32_t kColAcc = 128 * kGroups;
   static constexpr int kWTma = 4 * kGroups, kWMma = kWTma + 1, kThreads = 128 * (kGroups + 1);
+  static constexpr int kIssuers = KEYS ? 1 : 2;  // warps that issue S and dP, of every other chunk each
   // Registers a thread: the warpgroups' shares add up to what the block is launched with (which is what the compiler reports), or
   // the increase would wait for good.
   static constexpr int kLaunchRegs = kGroups == 2 ? 168 : 128, kRowRegs = kGroups == 2 ? 208 : 144, kOtherRegs = kGroups == 2 ? 88 : 80;
@@ -49,7 +50,7 @@ struct Smem {
   unsigned char x0[kTileBytes], y0[kTileBytes];  // the resident tiles
   Slot ring[kSlots];
   float stat[kSlots][2][kChunkRows];             // key-stationary: -lse (base 2) and -D of the chunk's rows
-  unsigned long long st_full, st_empty, ring_full[kSlots], ring_empty[kSlots], sd_full[3], p_full[3], added[3], acc_full, acc_free, drain[2];
+  unsigned long long st_full, st_empty, ring_full[kSlots], ring_empty[kSlots], sd_full[3], p_full[3], added[3], acc_full, acc_free, drain[3];
   uint32_t tmem_base;
   int abort;
 };
@@ -140,13 +141,14 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
 
   if (tid == 0) {
     mbar_init(s32(&sm.st_full), 1);
-    mbar_init(s32(&sm.st_empty), 1);
+    mbar_init(s32(&sm.st_empty), P::kIssuers);
     for (int s = 0; s < S::kSlots; ++s) { mbar_init(s32(&sm.ring_full[s]), 1); mbar_init(s32(&sm.ring_empty[s]), 1); }
     for (int i = 0; i < kGroups; ++i) { mbar_init(s32(&sm.sd_full[i]), 1); mbar_init(s32(&sm.p_full[i]), 128); mbar_init(s32(&sm.added[i]), 1); }
     mbar_init(s32(&sm.acc_full), 1);
     mbar_init(s32(&sm.acc_free), 256);
     mbar_init(s32(&sm.drain[0]), 1);
     mbar_init(s32(&sm.drain[1]), 1);
+    mbar_init(s32(&sm.drain[2]), 1);
     sm.abort = 0;
     cta_publish_barriers();
   }
@@ -205,36 +207,45 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
       }
       if (*abort && items) mbar_drain(s32(&sm.st_full), (items - 1) & 1);
     }
-  } else if (warp == P::kWMma) {
+  } else if (warp == P::kWMma || (P::kIssuers == 2 && warp == P::kWMma + 2)) {
     // ------------------------------------------------------------- S and dP
     // (The whole warp walks the loop, one elected lane issues; what it walks by is uniform, so that operands stay in uniform registers.)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
-    constexpr uint32_t idesc = make_idesc(false, 64u, F16);
-    const uint64_t x0d = smem_desc(s32(sm.x0)), y0d = smem_desc(s32(sm.y0));
-    uint32_t c = 0, items = 0;
+    constexpr uint32_t idesc = make_idesc(false, 64u, F16), kStep = P::kIssuers;
+    const uint32_t mine = P::kIssuers == 1 || warp == P::kWMma ? 0u : 1u;
+    const uint64_t x0d = smem_desc(s32(sm.x0)), y0d = smem_desc(s32(sm.y0)), ring = smem_desc(s32(sm.ring));
+    uint32_t s = mine, buf = mine, ring_phase = 0, buf_phase = 0, items = 0;
+    int n = (int)mine;
     bool ok = true;
     for (int index = __shfl_sync(0xffffffffu, first_item, 0); index < total && ok; index += gridDim.x) {
       it.template make<true>(g, a, index);
       if (it.chunks == 0) continue;
       ok = warp_wait_here(s32(&sm.st_full), items & 1, abort, status);
       ++items;
-      for (int n = 0, j = 0; n < it.chunks && ok; ++n, ++c) {
-        const uint32_t s = c % S::kSlots, buf = c % kGroups;
-        ok = warp_wait_here(s32(&sm.ring_full[s]), (c / S::kSlots) & 1, abort, status);
+      if (n >= it.chunks && elect_one()) mbar_arrive(s32(&sm.st_empty));
+      __syncwarp();
+      int j = KEYS ? n % it.per : n;
+#pragma unroll 1
+      for (; n < it.chunks && ok; n += kStep) {
+        ok = warp_wait_here(s32(&sm.ring_full[s]), ring_phase, abort, status);
         // the sums of the chunk that had the buffer read its P and dS there (products of different shapes are not ordered by being
         // issued in order)
-        if (c >= (uint32_t)kGroups) ok = ok && warp_wait_here(s32(&sm.added[buf]), (c / kGroups - 1) & 1, abort, status);
+        ok = ok && warp_wait_here(s32(&sm.added[buf]), buf_phase ^ 1, abort, status);
         if (!ok) break;
-        int start, cols;
-        it.chunk(j, start, cols);
-        if (++j == it.per) j = 0;
-        const int there = (KEYS ? it.ql : it.kl) - start;  // rows of the chunk that exist
-        if (there < kChunkRows && start + there < (KEYS ? g.Nq : g.Nk)) {
-          zero_rows<D>(sm.ring[s].x, there, kChunkRows, lane);
-          if constexpr (KEYS) zero_rows<D>(sm.ring[s].y, there, kChunkRows, lane);
+        // (of the rows of a chunk only a list's last ones may not exist)
+        if (j == it.per - 1 || (!KEYS && j < it.front)) {
+          int start, cols;
+          it.chunk(j, start, cols);
+          const int there = (KEYS ? it.ql : it.kl) - start;  // rows of the chunk that exist
+          if (there < kChunkRows && start + there < (KEYS ? g.Nq : g.Nk)) {
+            zero_rows<D>(sm.ring[s].x, there, kChunkRows, lane);
+            if constexpr (KEYS) zero_rows<D>(sm.ring[s].y, there, kChunkRows, lane);
+          }
         }
+        j += kStep;
+        if (KEYS && j >= it.per) j = kStep == 1 ? 0 : j % it.per;
         tc_fence_after();
-        const uint64_t xd = smem_desc(s32(sm.ring[s].x)), yd = smem_desc(s32(sm.ring[s].y));
+        const uint64_t xd = ring + (uint64_t)(s * (uint32_t)(sizeof(typename S::Slot) >> 4)), yd = xd + (S::kChunkBytes >> 4);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
@@ -243,31 +254,36 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
           for (int kk = 0; kk < D / 16; ++kk)
             umma_ss(tmem + 128 * buf + 64, k_major(y0d, kk, kPart), k_major(yd, kk, kChunkPart), idesc, kk > 0);
           tc_commit(s32(&sm.sd_full[buf]));
-          if (n == it.chunks - 1) tc_commit(s32(&sm.st_empty));
+          if (n >= it.chunks - (int)kStep) tc_commit(s32(&sm.st_empty));
         }
         __syncwarp();
+        if ((s += kStep) >= (uint32_t)S::kSlots) { s -= S::kSlots; ring_phase ^= 1; }
+        if ((buf += kStep) >= (uint32_t)kGroups) { buf -= kGroups; buf_phase ^= 1; }
       }
+      n -= it.chunks;
     }
     if (*abort) {
-      if (elect_one()) mma_drain(s32(&sm.drain[0]));
+      if (elect_one()) mma_drain(s32(&sm.drain[2 * mine]));
       __syncwarp();
     }
   } else if (warp == P::kWMma + 1) {
     // ------------------------------------------------------------- sums: dS x, and P^T y
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
     constexpr uint32_t idesc = make_idesc(true, (uint32_t)D, F16);
-    uint32_t c = 0, items = 0;
+    const uint64_t ring = mn_major(s32(sm.ring), kChunkPart);
+    uint32_t s = 0, buf = 0, buf_phase = 0, items = 0;
     bool ok = true;
     for (int index = __shfl_sync(0xffffffffu, first_item, 0); index < total && ok; index += gridDim.x) {
       it.template make<true>(g, a, index);
       if (it.chunks == 0) continue;
-      for (int n = 0; n < it.chunks && ok; ++n, ++c) {
-        const uint32_t s = c % S::kSlots, buf = c % kGroups;
-        ok = warp_wait_here(s32(&sm.p_full[buf]), (c / kGroups) & 1, abort, status);
-        if (n == 0 && items > 0) ok = ok && warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
+      if (items > 0) ok = warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
+      ++items;
+#pragma unroll 1
+      for (int n = 0; n < it.chunks && ok; ++n) {
+        ok = warp_wait_here(s32(&sm.p_full[buf]), buf_phase, abort, status);
         if (!ok) break;
         tc_fence_after();
-        const uint64_t xd = mn_major(s32(sm.ring[s].x), kChunkPart), yd = mn_major(s32(sm.ring[s].y), kChunkPart);
+        const uint64_t xd = ring + (uint64_t)(s * (uint32_t)(sizeof(typename S::Slot) >> 4)), yd = xd + (S::kChunkBytes >> 4);
         if (elect_one()) {
           if constexpr (KEYS) {
 #pragma unroll
@@ -282,8 +298,9 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
           if (n == it.chunks - 1) tc_commit(s32(&sm.acc_full));
         }
         __syncwarp();
+        if (++s == (uint32_t)S::kSlots) s = 0;
+        if (++buf == (uint32_t)kGroups) { buf = 0; buf_phase ^= 1; }
       }
-      ++items;
     }
     if (*abort) {
       if (elect_one()) mma_drain(s32(&sm.drain[1]));
