@@ -5,7 +5,7 @@
 //
 // A tile is 128 query rows of one head.  The tiles of a key/value head are numbered with the heads of its group fastest, and a
 // CTA takes two neighbours: heads of a group read the same keys, so a staged key tile serves 256 rows.  The two tiles walk a
-// common sequence of steps of at most 128 keys: the sinks (as many columns as there are, rounded up to 32) unless the window
+// common sequence of steps of at most 64 keys: the sinks (as many columns as there are, rounded up to 32) unless the window
 // still holds them, then the union of the two windows from its first key on; a step that a tile sees nothing of it leaves out.
 // Only steps at the window's edges are masked element by element.
 //
@@ -16,10 +16,13 @@
 // scaled) only when it grows by more than 2^8.
 // Every wait is bounded (status MOSAIC_E_DEVICE_TIMEOUT, copies and products in flight awaited, TMEM freed).
 //
-// Bound by the softmax warps: a step of 64 keys takes 1630 cycles at d = 64 and 1950 at d = 128, of which MUFU is busy 1024 (two
-// warps a scheduler), the tensor core 680 and 1310.  Measured beside it (us of 8192 tokens, 16 heads of 128 on 4, window 1024; this
-// form 91): one warp for both tiles' products 111, 128 keys a step 102, a quarter or an eighth of the exponentials on the FMA pipe
-// 101 and 92; a step's two buffers in the hands of two warpgroups each, which pass the running maximum on, 118.
+// Bound by the softmax warps and the way round (scores, softmax, P V, the buffer's next scores): a step of 64 keys for both tiles
+// takes 1760 cycles at d = 64 and 1970 at d = 128, of which MUFU is busy 1024 (two warps a scheduler), the tensor core 680 and 1310.
+// Measured for 8192 tokens, 16 heads of 128 on 4, window 1024 (us): this form 95; the issuing warps finding a step's slots and limits
+// anew each time 99; P in columns of its own beside one score buffer, so that no product has to end before the next scores, 101;
+// the two tiles taking turns at the exponentials 96 (at d = 64: 6 % slower).  Beside a form of 91 that left out the wait for the
+// buffer's earlier product: one warp for both tiles' products 111, 128 keys a step 102, a quarter or an eighth of the exponentials
+// on the FMA pipe 101 and 92, a step's two buffers in the hands of two warpgroups each, which pass the running maximum on, 118.
 #include <type_traits>
 
 #include "window.cuh"
@@ -29,7 +32,7 @@ namespace mosaic {
 namespace {
 
 constexpr int kThreads = 384;
-// Registers a thread: the softmax threads hold a row of up to 128 scores.  The three warpgroups' shares add up to what the block is
+// Registers a thread: the softmax threads hold a row's 64 scores of a step.  The three warpgroups' shares add up to what the block is
 // launched with (384 threads of 168, which is what the compiler reports), or the increase would wait for good.
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * kLaunchRegs, "the shares exceed the launch's registers");
@@ -222,25 +225,25 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 9 || warp == 10) {
     // ------------------------------------------------------------- products of tile t
     // The whole warp walks the loop, one elected lane issues; what it walks by is made uniform, so that operands stay in uniform
-    // registers.  `u` counts the tile's own steps: score buffer u % kBufs.
+    // registers.  `u` counts the tile's own steps: score buffer u % 2.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     constexpr uint32_t idesc_qk = make_idesc(false, 0u, F16), idesc_pv = make_idesc(true, (uint32_t)D, F16);
     const int t = warp - 9;
+    constexpr uint32_t kPair = 2 * S::kSlotBytes;  // the ring's slots are taken in pairs, a step's keys and its values
     const uint32_t tco = tmem + kColO + D * t;
-    const uint64_t qd = smem_desc(s32(sm.q[t]));
-    uint32_t slot_no = 0, u = 0, n_q = 0;
+    const uint64_t qd = smem_desc(s32(sm.q[t])), k_ring = smem_desc(s32(sm.kv[0])), v_ring = mn_major(s32(sm.kv[1]), kSlotPart);
+    uint32_t pair = 0, phase = 0, u = 0, n_q = 0;
     bool ok = true;
     // P V of the tile's latest step
     bool pending = false, fresh = false;
-    uint32_t v_no = 0;
+    uint32_t v_pair = 0, v_phase = 0;
     int kks = 0, v_there = 0;  // keys of the step in sixteens; rows of the value tile that exist (beyond them it may hold anything)
     auto issue_pv = [&]() {  // of step u - 1
       const uint32_t b = (u - 1) % 2;
-      ok = warp_wait_here(s32(&sm.kv_full[v_no % kSlots]), (v_no / kSlots) & 1, abort, status);
+      ok = warp_wait_here(s32(&sm.kv_full[2 * v_pair + 1]), v_phase, abort, status);
       if (!ok) return;
-      unsigned char* vt = sm.kv[v_no % kSlots];
-      if (v_there < 16 * kks) zero_rows<D>(vt, v_there, U, lane);
-      const uint64_t vd = mn_major(s32(vt), kSlotPart);
+      if (v_there < 16 * kks) zero_rows<D>(sm.kv[2 * v_pair + 1], v_there, U, lane);
+      const uint64_t vd = v_ring + (uint64_t)(v_pair * (kPair >> 4));
       const uint32_t tcp = tmem + score_col(t, b);
       ok = warp_wait_here(s32(&sm.p_full[t][b]), ((u - 1) / 2) & 1, abort, status);
       if (!ok) return;
@@ -254,61 +257,65 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < kks; ++kk) umma_ts(tco, tcp + 8 * kk, vd + (uint64_t)((2048 * kk) >> 4), idesc_pv, !fresh || kk > 0);
         }
         tc_commit(s32(&sm.pv_done[t][b]));
-        tc_commit(s32(&sm.kv_empty[v_no % kSlots]));
+        tc_commit(s32(&sm.kv_empty[2 * v_pair + 1]));
       }
       __syncwarp();
       pending = false;
     };
-    Walk w;
-    w.index = __shfl_sync(0xffffffffu, (int)blockIdx.x + zero, 0);
-    for (bool more = w.seek<true>(g, per, total); more && ok; more = w.next<true>(g, per, total), slot_no += 2) {
-      int start, cols;
-      w.it.step(w.n, start, cols);
-      const uint32_t k_slot = slot_no % kSlots, v_slot = (slot_no + 1) % kSlots;
-      const int first = w.it.first_of(t), last = w.it.last_of(t);
-      if (w.n > last || (w.n < first && w.n >= w.it.front)) {
-        // a tile that leaves a step out hands its slots on, once they have landed (so never twice in a round)
-        if (pending) issue_pv();
-        ok = ok && warp_wait_here(s32(&sm.kv_full[k_slot]), (slot_no / kSlots) & 1, abort, status) &&
-             warp_wait_here(s32(&sm.kv_full[v_slot]), ((slot_no + 1) / kSlots) & 1, abort, status);
-        if (ok && elect_one()) {
-          mbar_arrive(s32(&sm.kv_empty[k_slot]));
-          mbar_arrive(s32(&sm.kv_empty[v_slot]));
-        }
-        __syncwarp();
-        continue;
-      }
-      const bool opens = w.n == (w.it.front ? 0 : first);
-      if (opens) {  // (a new query tile may be a while: the item before is finished first)
-        if (pending) issue_pv();
-        ok = ok && warp_wait_here(s32(&sm.q_full[t]), n_q & 1, abort, status);
-        ++n_q;
-      }
-      const uint32_t id = idesc_n(idesc_qk, round32(cols)), b = u % 2;
-      const uint32_t tcs = tmem + score_col(t, b);
-      const uint64_t kd = smem_desc(s32(sm.kv[k_slot]));
-      ok = ok && warp_wait_here(s32(&sm.kv_full[k_slot]), (slot_no / kSlots) & 1, abort, status);
-      // P V of the step that had the buffer (two before) reads its weights there: it was issued before, but only products of one
-      // shape into one accumulator are sure to run in issue order.  (The wait costs 8 % at d = 128, nothing at 64.)
-      if (u >= 2) ok = ok && warp_wait_here(s32(&sm.pv_done[t][b]), (u / 2 - 1) & 1, abort, status);
-      if (!ok) break;
-      tc_fence_after();
-      if (elect_one()) {
+    Item it;
+    for (int index = __shfl_sync(0xffffffffu, (int)blockIdx.x + zero, 0); index < total && ok; index += gridDim.x) {
+      it.make<true>(g, per, index);
+      const int first = it.first_of(t), last = it.last_of(t), opens = it.front ? 0 : first;
+      const bool some_rows = it.kl < g.Nk;  // only then a tile has rows that do not exist
+#pragma unroll 1
+      for (int n = 0; n < it.steps; ++n) {
+        const uint32_t k_full = s32(&sm.kv_full[2 * pair]), k_empty = s32(&sm.kv_empty[2 * pair]);
+        if (n > last || (n < first && n >= it.front)) {
+          // a tile that leaves a step out hands its slots on, once they have landed (so never twice in a round)
+          if (pending) issue_pv();
+          ok = ok && warp_wait_here(k_full, phase, abort, status) && warp_wait_here(k_full + 8, phase, abort, status);
+          if (!ok) break;
+          if (elect_one()) {
+            mbar_arrive(k_empty);
+            mbar_arrive(k_empty + 8);
+          }
+          __syncwarp();
+        } else {
+          if (n == opens) {  // (a new query tile may be a while: the item before is finished first)
+            if (pending) issue_pv();
+            ok = ok && warp_wait_here(s32(&sm.q_full[t]), n_q & 1, abort, status);
+            ++n_q;
+          }
+          int start, cols;
+          it.step(n, start, cols);
+          const uint32_t id = idesc_n(idesc_qk, round32(cols)), tcs = tmem + score_col(t, u % 2);
+          const uint64_t kd = k_ring + (uint64_t)(pair * (kPair >> 4));
+          ok = ok && warp_wait_here(k_full, phase, abort, status);
+          // P V of the step that had the buffer (two before) reads its weights there: it was issued before, but only products of
+          // one shape into one accumulator are sure to run in issue order.  (The wait costs 8 % at d = 128, nothing at 64.)
+          if (u >= 2) ok = ok && warp_wait_here(s32(&sm.pv_done[t][u % 2]), (u / 2 - 1) & 1, abort, status);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) umma_ss(tcs, k_major(qd, kk, kPart), k_major(kd, kk, kSlotPart), id, kk > 0);
-        tc_commit(s32(&sm.s_full[t][b]));
-        tc_commit(s32(&sm.kv_empty[k_slot]));
-        if (w.n == last) tc_commit(s32(&sm.q_empty[t]));
+            for (int kk = 0; kk < D / 16; ++kk) umma_ss(tcs, k_major(qd, kk, kPart), k_major(kd, kk, kSlotPart), id, kk > 0);
+            tc_commit(s32(&sm.s_full[t][u % 2]));
+            tc_commit(k_empty);
+            if (n == last) tc_commit(s32(&sm.q_empty[t]));
+          }
+          __syncwarp();
+          if (pending) issue_pv();
+          if (!ok) break;
+          ++u;
+          pending = true;
+          fresh = n == opens;
+          v_pair = pair;
+          v_phase = phase;
+          kks = round32(cols) / 16;
+          v_there = some_rows ? it.kl - start : U;
+        }
+        if (++pair == kSlots / 2) { pair = 0; phase ^= 1; }
       }
-      __syncwarp();
-      if (pending) issue_pv();
-      if (!ok) break;
-      ++u;
-      pending = true;
-      fresh = opens;
-      v_no = slot_no + 1;
-      kks = round32(cols) / 16;
-      v_there = w.it.kl < g.Nk ? w.it.kl - start : U;
     }
     if (ok && pending) issue_pv();
     if (*abort) {  // products already issued must finish before TMEM and shared memory are released
