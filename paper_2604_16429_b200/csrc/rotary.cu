@@ -9,7 +9,14 @@
 // leaves its lane, a row's sums are shuffles among P lanes, and 32 / P rows go through a warp at a time, a few fetched ahead.
 // The token's rot_dim/2 angles are the same for all its heads: the warp's lanes share them out, take the product with the
 // position in half turns and its remainder in fp64 (an angle of 1e6 radians has 2^-33 of error there, 2^-4 in fp32), and leave
-// (cos, sin) in shared memory, from where every lane keeps the V that it needs.
+// (cos, sin) in shared memory, from where every lane reads the V that it needs for each row.
+//
+// Measured (us on the device, beside the bytes at 6543 GB/s): rotation of [2, 16 + 4 heads, 8192, 128] fp16 with 32 channels turning
+// 31.1 (25.7); norm and rotation of [1, 16 + 16, 12288, 64] bf16 23.1 (15.4); its backward for [2, 16 + 4, 8192, 128] bf16 62.0 (38.5).
+// The forward is bound by HBM and a start and end of 5 us (7 MB of rows are on their way at a time), the norms besides by
+// instructions, the backward by instructions (four streams of rows, two row sums, three products an element) as much as by HBM.
+// Rows ahead through shared memory and CTAs an SM: forward 3 and 4 (2 CTAs 10 % slower), backward 3 and 2 (a deeper ring 89, rows
+// ahead in registers 84).
 #include <math.h>
 
 #include "common.cuh"

@@ -14,7 +14,16 @@
 // buffers as groups of row threads (three; two where the sums of d = 128 leave no more tensor memory): while the groups work on
 // their chunks the tensor core adds an earlier one's sums and forms a later one's S and dP.  TMEM (512 columns): S, dP of buffer b
 // at 128 b and 128 b + 64, behind them dS x, then P^T y.
-// Rounded to 16 bits: P and dS as operands, the results.  Every wait is bounded.
+// Rounded to 16 bits: P and dS as operands (the tensor core takes no wider ones; it makes the gradients' error 1.4 times that of
+// results rounded once), the results.  Every wait is bounded.
+//
+// Bound by the way round a chunk's buffer (products, row threads, sums, and their hand-offs) and by the issuing warps: a chunk takes
+// about 900 cycles at d = 64 where MUFU needs 512 and the tensor core 540 (query-stationary) or 680, and of that an issuing warp's
+// own instructions 600 to 800.  Measured for both passes (us, 37 heads of 4608 tokens, window 3968: query-, key-stationary): this
+// form 225, 264 at d = 64 and 326, 449 at d = 128; one warp issuing S and dP of the query-stationary pass 241 and 367, two in the
+// key-stationary 275 and 479; slots and limits found anew for each chunk 234, 275 and 335, 473 (with one warp 262, 264 and 380, 468);
+// P and dS in columns of their own, two groups 229, 284 and 364, 491; the two sums from a warp each 232, 270 and 330, 455; a part of
+// the exponentials on the FMA pipe changed nothing.  A change of items costs 2 to 5 us a CTA more than its chunks.
 #include <type_traits>
 
 #include "window.cuh"
@@ -458,10 +467,11 @@ namespace {
 constexpr int kRowsAhead = 4;
 template <int D, bool F16>
 __global__ void __launch_bounds__(256) window_rows_kernel(const WinGeo g, const View o, const View d_o, const float* __restrict__ lse,
-                                                          float* __restrict__ neg_lse2, float* __restrict__ neg_d, int pad, int* status) {
-  const int first = (int)blockIdx.x * (32 * kRowsAhead) + (threadIdx.x >> 3) + await_stream(), part = threadIdx.x & 7;
-  const int unit = blockIdx.y, b = unit / g.H, h = unit - b * g.H;
-  if (blockIdx.x == 0 && unit == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
+                                                          float* __restrict__ neg_lse2, float* __restrict__ neg_d, int pad, unsigned blocks,
+                                                          int* status) {
+  const int unit = (int)(blockIdx.x / blocks), b = unit / g.H, h = unit - b * g.H;
+  const int first = (int)(blockIdx.x - unit * blocks) * (32 * kRowsAhead) + (threadIdx.x >> 3) + await_stream(), part = threadIdx.x & 7;
+  if (blockIdx.x == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
   const int ql = span_of(g, b).ql;
   const char *x = o.data + b * o.sb + h * o.sh + 16 * part, *y = d_o.data + b * d_o.sb + h * d_o.sh + 16 * part;
   uint4 u[kRowsAhead][D / 64], w[kRowsAhead][D / 64];
@@ -544,10 +554,11 @@ int launch_pass(const HostCtx& c, const WinGeo& g, const View& x0, const View& y
 
 template <int D, bool F16>
 int launch(const HostCtx& c, const WinGeo& g, const WinBwd& t, const WinBwdWs& w, char* ws) {
-  if ((long long)g.B * g.H > 65535) return MOSAIC_E_UNSUPPORTED;
+  const unsigned blocks = (unsigned)((w.pad + 32 * kRowsAhead - 1) / (32 * kRowsAhead));  // of a unit's rows
+  if ((long long)blocks * g.B * g.H > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
   float *nl = (float*)(ws + w.neg_lse2), *nd = (float*)(ws + w.neg_d);
-  int rc = launch_kernel(window_rows_kernel<D, F16>, dim3((unsigned)((w.pad + 32 * kRowsAhead - 1) / (32 * kRowsAhead)), (unsigned)(g.B * g.H)), 256, 0, c.stream, true, 0, g, t.o, t.d_o, t.lse, nl, nd, w.pad,
-                         c.status);
+  int rc = launch_kernel(window_rows_kernel<D, F16>, dim3(blocks * (unsigned)(g.B * g.H)), 256, 0, c.stream, true, 0, g, t.o, t.d_o, t.lse, nl, nd,
+                         w.pad, blocks, c.status);
   if (rc) return rc;
   BwdArgs a = {t.dk, t.dv, nl, nd, (float*)(ws + w.partial), w.pad, (g.Nk + kRows - 1) / kRows, w.pieces, w.piece_rows};
   if ((rc = launch_pass<D, F16, true>(c, g, t.k, t.v, t.q, t.d_o, a))) return rc;

@@ -347,6 +347,42 @@ def test_on_another_stream_and_in_two_graphs():
         assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_more_units_than_a_grid_is_high():
+    q, k, v, d_o = make(11, 6000, 3000, 3, 3, 64, seed=14)
+    check_bwd(mb.WindowParams(window=2, sinks=1), q, k, v, d_o)
+
+
+def test_calls_of_two_threads_at_once():
+    """Each has its own stream, shapes and tensors; the results are those of calls one after the other."""
+    import threading
+
+    cases = [(make(2, 4, 2, 300, 300, 64, seed=15), mb.WindowParams(window=100, sinks=4)),
+             (make(1, 6, 3, 777, 901, 128, "fp16", "bnhd", seed=16), mb.WindowParams(window=333, sinks=9))]
+
+    def chain(x, wp, **kw):
+        q, k, v, d_o = x
+        o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v, **kw)
+        return (o, lse) + mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, **kw) + mb.mosaic_bsa_window_decode(wp, q[:, :, -1:], k, v, **kw)
+
+    want = [chain(*c) for c in cases]
+    torch.cuda.synchronize()
+    got, streams = [None, None], [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def work(i):
+        for _ in range(20):
+            with torch.cuda.stream(streams[i]):
+                got[i] = chain(*cases[i])
+        streams[i].synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for w, g in zip(want, got):
+        assert all(torch.equal(a, b) for a, b in zip(w, g))
+
+
 def test_refusals_of_the_binding():
     q, k, v, d_o = make(2, 4, 2, 30, 40, 64, seed=12)
     wp = mb.WindowParams(window=10)
