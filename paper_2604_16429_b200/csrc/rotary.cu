@@ -12,11 +12,12 @@
 // (cos, sin) in shared memory, from where every lane reads the V that it needs for each row.
 //
 // Measured (us on the device, beside the bytes at 6543 GB/s): rotation of [2, 16 + 4 heads, 8192, 128] fp16 with 32 channels turning
-// 31.1 (25.7); norm and rotation of [1, 16 + 16, 12288, 64] bf16 23.1 (15.4); its backward for [2, 16 + 4, 8192, 128] bf16 62.0 (38.5).
-// The forward is bound by HBM and a start and end of 5 us (7 MB of rows are on their way at a time), the norms besides by
+// 30.5 (25.7); norm and rotation of [1, 16 + 16, 12288, 64] bf16 22.3 (15.4); its backward for [2, 16 + 4, 8192, 128] bf16 60.7 (38.5).
+// The forward is bound by HBM and a start and end of 5 us (batches of 1 KB a warp, two ahead), the norms besides by
 // instructions, the backward by instructions (four streams of rows, two row sums, three products an element) as much as by HBM.
-// Rows ahead through shared memory and CTAs an SM: forward 3 and 4 (2 CTAs 10 % slower), backward 3 and 2 (a deeper ring 89, rows
-// ahead in registers 84).
+// Chosen by measurement, those three in order: CTAs an SM of the forward 3 (2: 31.2, 23.7; 4: 31.2, 23.1; 6: 38.6, 35.8), batches ahead
+// 2 (1: 31.2, 24.2; 3: 31.8, 24.2); CTAs an SM of the backward 2 (1: 80.2; 3: 103), batches ahead 1 (2: 61.8; 3: 64.3; held in
+// registers instead of shared memory: 84).
 #include <math.h>
 
 #include "common.cuh"
@@ -28,8 +29,8 @@ namespace {
 enum { kBf16 = 0, kF16 = 1, kF32 = 2 };
 constexpr int kHeadThreads = 256, kHeadWarps = kHeadThreads / 32;
 constexpr int kMaxHeadDim = 256;
-constexpr int kCtas = 4, kBwdCtas = 2;  // per SM
-constexpr int kDeep = 3;       // batches of rows of the backward on their way (shared memory)
+constexpr int kCtas = 3, kBwdCtas = 2;  // per SM
+constexpr int kDeep = 2;       // batches of rows of the backward on their way (shared memory)
 constexpr size_t kBwdRing = (size_t)kHeadWarps * kDeep * 4 * 32 * 16;
 constexpr int kDeepFwd = 3;    // the same of the forward, where a row comes without a gradient
 constexpr size_t kFwdRing = (size_t)kHeadWarps * kDeepFwd * 2 * 32 * 16;

@@ -11,6 +11,11 @@
 //                 stands at which place of the contraction does not matter as long as Q's operand has the same order
 //   O^T += V^T P^T (16 channels x 8 heads): a lane has 8 neighbouring channels of four keys; byte permutes pair up the keys
 // P^T turns from an accumulator into an operand by an 8 x 8 transpose within the warp.
+//
+// Measured (device, window 4096, 16 heads of 128 on 4): 64 members over rolling caches 94 us, 5.0 TB/s; one member 12.0 us, which are
+// the latencies of the launch, eight steps a warp and the two joins.  With one CTA for all of a head's keys 81 and 43 us, with four of
+// eight warps 93 and 14.5; how many CTAs share a head's keys left to the number of members (with joins whose bits do not depend on it) 105 to
+// 178 us for the former.
 #include <type_traits>
 
 #include "window.cuh"
@@ -68,7 +73,8 @@ struct Joint {
 };
 
 // NT: tiles of 8 query heads that a CTA takes
-template <int D, bool F16, int NT>
+// AHEAD: the next step's rows are asked for before this step's are worked on (the same arithmetic, so the same bits).
+template <int D, bool F16, int NT, bool AHEAD>
 __global__ void __launch_bounds__(kDecThreads) window_decode_kernel(const WinGeo g, const __grid_constant__ DecArgs a) {
   constexpr int kHeads = 8 * NT;
   extern __shared__ unsigned char smem_raw[];
@@ -112,20 +118,35 @@ __global__ void __launch_bounds__(kDecThreads) window_decode_kernel(const WinGeo
   }
 
   const int stride = ranks * kDecWarps * kStepKeys;
-  for (int t0 = (rank * kDecWarps + warp) * kStepKeys; t0 < n; t0 += stride) {
-    uint4 kf[2][D / 32], vf[4][D / 64];
+  int t0 = (rank * kDecWarps + warp) * kStepKeys;
+  uint4 kn[2][D / 32], vn[4][D / 64];  // a step's rows on their way
+  auto fetch = [&](int t) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const char* row = kp + slot(t0 + gq + 8 * r) * a.k.sn + 16 * tq;
+      const char* row = kp + slot(t + gq + 8 * r) * a.k.sn + 16 * tq;
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) kf[r][c] = stream_load(row + 64 * c);
+      for (int c = 0; c < D / 32; ++c) kn[r][c] = stream_load(row + 64 * c);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {  // keys 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9
-      const char* row = vp + slot(t0 + 2 * tq + (r & 1) + 4 * (r & 2)) * a.v.sn + 16 * gq;
+      const char* row = vp + slot(t + 2 * tq + (r & 1) + 4 * (r & 2)) * a.v.sn + 16 * gq;
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) vf[r][c] = stream_load(row + 128 * c);
+      for (int c = 0; c < D / 64; ++c) vn[r][c] = stream_load(row + 128 * c);
     }
+  };
+  if (AHEAD && t0 < n) fetch(t0);
+  for (; t0 < n; t0 += stride) {
+    if (!AHEAD) fetch(t0);
+    uint4 kf[2][D / 32], vf[4][D / 64];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) kf[r][c] = kn[r][c];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) vf[r][c] = vn[r][c];
+    if (AHEAD && t0 + stride < n) fetch(t0 + stride);
     uint32_t pt[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -231,12 +252,24 @@ __global__ void __launch_bounds__(kDecThreads) window_decode_kernel(const WinGeo
   cluster_sync();  // nobody leaves while its part may still be read
 }
 
-template <int D, bool F16, int NT>
-int launch(const HostCtx& c, const WinGeo& g, DecArgs a) {
+template <int D, bool F16, int NT, bool AHEAD>
+int launch(const HostCtx& c, const WinGeo& g, const DecArgs& a, long long ctas) {
   const size_t smem = sizeof(Joint<D, NT>);
   static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(reinterpret_cast<const void*>(window_decode_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(window_decode_kernel<D, F16, NT, AHEAD>), smem, &configured, &sms)) return rc;
+  return launch_kernel(window_decode_kernel<D, F16, NT, AHEAD>, dim3((unsigned)ctas), kDecThreads, smem, c.stream, true, a.ranks, g, a);
+}
+
+// Rows ahead cost registers.  Where they cost no CTA that the SM would need (d = 64 with 8 heads, 4 CTAs an SM; d = 128 with 16, 2 either
+// way) they are always taken, elsewhere as long as all CTAs fit two an SM: there the latency of a warp's few steps is all there is.
+// Measured with and without (us; caches of 4100 tokens, 4 key/value heads, window 4096, members in front): d = 64, 4 heads a group 1: 10.2
+// and 13.0, 32: 30.8 and 38.5; d = 128, 12 a group 1: 15.8 and 18.0, 32: 75 and 83; d = 128, 4 a group 1: 13.3 and 16.0, 8: 17.1 and 19.7,
+// but 16: 33.0 and 26.9; d = 64, 12 a group 8: 15.5 and 16.4, but 16: 28.8 and 20.5.
+template <int D, bool F16, int NT>
+int launch(const HostCtx& c, const WinGeo& g, DecArgs a) {
+  int sms = 0;
+  if (const int rc = launch_setup(nullptr, 0, nullptr, &sms)) return rc;
   a.head_blocks = (g.G + 8 * NT - 1) / (8 * NT);
   // How many CTAs share a head's keys follows from the most keys that it may have, alone: a unit's bits must not depend on the others.
   const long long keys = (long long)g.window + g.sinks < g.Nk ? (long long)g.window + g.sinks : g.Nk;
@@ -244,7 +277,9 @@ int launch(const HostCtx& c, const WinGeo& g, DecArgs a) {
   while (a.ranks < 8 && keys > a.ranks * kKeysPerCta) a.ranks *= 2;
   const long long ctas = (long long)g.B * g.Hkv * a.head_blocks * a.ranks;
   if (ctas > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
-  return launch_kernel(window_decode_kernel<D, F16, NT>, dim3((unsigned)ctas), kDecThreads, smem, c.stream, true, a.ranks, g, a);
+  if constexpr ((D == 64) != (NT == 1))
+    if (ctas > 2ll * sms) return launch<D, F16, NT, false>(c, g, a, ctas);
+  return launch<D, F16, NT, true>(c, g, a, ctas);
 }
 
 }  // namespace

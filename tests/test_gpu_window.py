@@ -348,8 +348,27 @@ def test_on_another_stream_and_in_two_graphs():
 
 
 def test_more_units_than_a_grid_is_high():
-    q, k, v, d_o = make(11, 6000, 3000, 3, 3, 64, seed=14)
-    check_bwd(mb.WindowParams(window=2, sinks=1), q, k, v, d_o)
+    """66000 units are 600, checked against the definition, 110 times over."""
+    x = make(1, 600, 300, 3, 3, 64, seed=14)
+    wp = mb.WindowParams(window=2, sinks=1)
+    _, want = check_bwd(wp, *x)
+    o, lse = mb.mosaic_bsa_window_fwd(wp, *x[:3])
+    q, k, v, d_o = (t.repeat(110, 1, 1, 1) for t in x)
+    got = mb.mosaic_bsa_window_fwd(wp, q, k, v)
+    for a, b in zip(got + mb.mosaic_bsa_window_bwd(wp, q, k, v, *got, d_o), [o, lse] + want):
+        assert torch.equal(a, b.expand(a.shape))
+
+
+@pytest.mark.parametrize("d,group", [(64, 4), (64, 12), (128, 4), (128, 12)])
+def test_decode_of_many_has_the_bits_of_decode_of_one(d, group):
+    """Few CTAs ask for rows ahead, many may not: a member's results are the same bits."""
+    q, k, v, _ = make(64, 4 * group, 4, 1, 1001, d, seed=17)
+    wp = mb.WindowParams(window=900, sinks=5)
+    k_len = lens([1001 - 15 * b for b in range(64)])
+    o, lse = mb.mosaic_bsa_window_decode(wp, q, k, v, k_len=k_len)
+    for b in (0, 1, 31, 63):
+        one = mb.mosaic_bsa_window_decode(wp, q[b:b + 1], k[b:b + 1], v[b:b + 1], k_len=k_len[b:b + 1])
+        assert torch.equal(one[0], o[b:b + 1]) and torch.equal(one[1], lse[b:b + 1])
 
 
 def test_calls_of_two_threads_at_once():
