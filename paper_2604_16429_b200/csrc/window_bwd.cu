@@ -23,7 +23,7 @@
 // form 225, 264 at d = 64 and 326, 449 at d = 128; one warp issuing S and dP of the query-stationary pass 241 and 367, two in the
 // key-stationary 275 and 479; slots and limits found anew for each chunk 234, 275 and 335, 473 (with one warp 262, 264 and 380, 468);
 // P and dS in columns of their own, two groups 229, 284 and 364, 491; the two sums from a warp each 232, 270 and 330, 455; a part of
-// the exponentials on the FMA pipe changed nothing.  A change of items costs 2 to 5 us a CTA more than its chunks.
+// the exponentials on the FMA pipe changed nothing, nor did a second pair of resident tiles for the next item (d = 64: 223, 264).
 #include <type_traits>
 
 #include "window.cuh"
