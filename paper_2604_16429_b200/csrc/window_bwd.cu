@@ -13,14 +13,17 @@
 // = TMEM lane) form P and dS in 16 bits in the place of S and dP, operands from tensor memory of the sums' products.  As many chunk
 // buffers as groups of row threads (three; two where the sums of d = 128 leave no more tensor memory): while the groups work on
 // their chunks the tensor core adds an earlier one's sums and forms a later one's S and dP.  TMEM (512 columns): S, dP of buffer b
-// at 128 b and 128 b + 64, behind them dS x, then P^T y.
+// at 128 b and 128 b + 64 (P and dS of rows 0 to 31 of the chunk in the first half of either, of the others in the second), behind
+// them dS x, then P^T y.
 // Rounded to 16 bits: P and dS as operands (the tensor core takes no wider ones; it makes the gradients' error 1.4 times that of
-// results rounded once), the results.  Every wait is bounded.
+// results rounded once), the results.  Items with the sinks' keys add what those roundings left off in a second product, so that the
+// few largest gradients, sums over all rows, are as exact as results rounded once (error over the sinks' keys 0.0023 -> 0.0017 of their
+// size in bf16; 4 % of a training pass of 49152 tokens with window 2048, 7 % of 4096 with window 1024).  Every wait is bounded.
 //
 // Bound by the way round a chunk's buffer (products, row threads, sums, and their hand-offs) and by the issuing warps: a chunk takes
 // about 900 cycles at d = 64 where MUFU needs 512 and the tensor core 540 (query-stationary) or 680, and of that an issuing warp's
 // own instructions 600 to 800.  Measured for both passes (us, 37 heads of 4608 tokens, window 3968: query-, key-stationary): this
-// form 225, 264 at d = 64 and 326, 449 at d = 128; one warp issuing S and dP of the query-stationary pass 241 and 367, two in the
+// form, without sinks, 225, 264 at d = 64 and 326, 449 at d = 128; one warp issuing S and dP of the query-stationary pass 241 and 367, two in the
 // key-stationary 275 and 479; slots and limits found anew for each chunk 234, 275 and 335, 473 (with one warp 262, 264 and 380, 468);
 // P and dS in columns of their own, two groups 229, 284 and 364, 491; the two sums from a warp each 232, 270 and 330, 455; a part of
 // the exponentials on the FMA pipe changed nothing, nor did a second pair of resident tiles for the next item (d = 64: 223, 264).
@@ -78,6 +81,14 @@ __device__ __forceinline__ int first_tile_end(const WinGeo& g, const Span& s) {
   return e > first ? first + (e - first + kChunkRows - 1) / kChunkRows * kChunkRows : first;
 }
 
+// What two numbers have beyond their 16-bit roundings, in 16 bits
+template <bool F16>
+__device__ __forceinline__ uint32_t rest(float a, float b, uint32_t rounded) {
+  float ra, rb;
+  unpack16x2(rounded, F16, ra, rb);
+  return pack2<F16>(a - ra, b - rb);
+}
+
 template <bool KEYS>
 struct Item {
   int b, hk, head, piece, row0, rows;  // rows: of the tile that exist
@@ -124,6 +135,8 @@ struct Item {
       per = chunks = rows > 0 && end > 0 ? front + (end - base + kChunkRows - 1) / kChunkRows : 0;
     }
   }
+  // Key-stationary: the sinks' keys are in the tile, whose gradients are sums over all rows and the largest there are.
+  __device__ __forceinline__ bool holds_sinks(const WinGeo& g) const { return row0 == 0 && g.sinks > 0; }
   // first row and number of rows of chunk n of a head
   __device__ __forceinline__ void chunk(int n, int& start, int& cols) const {
     start = !KEYS && n < front ? n * kChunkRows : base + (n - (KEYS ? 0 : front)) * kChunkRows;
@@ -280,11 +293,17 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kOtherRegs));
     constexpr uint32_t idesc = make_idesc(true, (uint32_t)D, F16);
     const uint64_t ring = mn_major(s32(sm.ring), kChunkPart);
+    auto add = [&](uint32_t acc, uint32_t weights, uint64_t rows, bool more) {
+#pragma unroll
+      for (int kk = 0; kk < kChunkRows / 16; ++kk)
+        umma_ts(acc, weights + 32 * (kk >> 1) + 8 * (kk & 1), rows + (uint64_t)((2048 * kk) >> 4), idesc, more || kk > 0);
+    };
     uint32_t s = 0, buf = 0, buf_phase = 0, items = 0;
     bool ok = true;
     for (int index = __shfl_sync(0xffffffffu, first_item, 0); index < total && ok; index += gridDim.x) {
       it.template make<true>(g, a, index);
       if (it.chunks == 0) continue;
+      const bool fine = KEYS && it.holds_sinks(g);
       if (items > 0) ok = warp_wait_here(s32(&sm.acc_free), (items - 1) & 1, abort, status);  // the item before has been read
       ++items;
 #pragma unroll 1
@@ -294,14 +313,12 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
         tc_fence_after();
         const uint64_t xd = ring + (uint64_t)(s * (uint32_t)(sizeof(typename S::Slot) >> 4)), yd = xd + (S::kChunkBytes >> 4);
         if (elect_one()) {
-          if constexpr (KEYS) {
-#pragma unroll
-            for (int kk = 0; kk < kChunkRows / 16; ++kk)
-              umma_ts(tmem + kColAcc + D, tmem + 128 * buf + 8 * kk, yd + (uint64_t)((2048 * kk) >> 4), idesc, n > 0 || kk > 0);
+          if constexpr (KEYS) add(tmem + kColAcc + D, tmem + 128 * buf, yd, n > 0);
+          add(tmem + kColAcc, tmem + 128 * buf + 64, xd, n > 0);
+          if (KEYS && fine) {
+            add(tmem + kColAcc + D, tmem + 128 * buf + 16, yd, true);
+            add(tmem + kColAcc, tmem + 128 * buf + 64 + 16, xd, true);
           }
-#pragma unroll
-          for (int kk = 0; kk < kChunkRows / 16; ++kk)
-            umma_ts(tmem + kColAcc, tmem + 128 * buf + 64 + 8 * kk, xd + (uint64_t)((2048 * kk) >> 4), idesc, n > 0 || kk > 0);
           tc_commit(s32(&sm.added[buf]));
           tc_commit(s32(&sm.ring_empty[s]));
           if (n == it.chunks - 1) tc_commit(s32(&sm.acc_full));
@@ -364,8 +381,9 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
         if (!ok) break;
         tc_fence_after();
         // 32 columns at a time: P and dS, stored in the places of S and dP that have been read
-        auto part = [&](int half, auto masked) {
+        auto part = [&](int half, auto masked, auto fine) {
           uint32_t sv[32], dv[32], pk[16], dk[16];
+          [[maybe_unused]] uint32_t pl[16], dl[16];
           tmem_ld32(tb + 32 * half, sv);
           tmem_ld32(tb + 64 + 32 * half, dv);
           tmem_wait_ld();
@@ -395,16 +413,29 @@ __global__ void __launch_bounds__(Plan<D, KEYS>::kThreads, 1)
             pk[(x >> 1) + 1] = pack2<F16>(p2, p3);
             dk[x >> 1] = pack2<F16>(e0, e1);
             dk[(x >> 1) + 1] = pack2<F16>(e2, e3);
+            if constexpr (decltype(fine)::value) {
+              pl[x >> 1] = rest<F16>(p0, p1, pk[x >> 1]);
+              pl[(x >> 1) + 1] = rest<F16>(p2, p3, pk[(x >> 1) + 1]);
+              dl[x >> 1] = rest<F16>(e0, e1, dk[x >> 1]);
+              dl[(x >> 1) + 1] = rest<F16>(e2, e3, dk[(x >> 1) + 1]);
+            }
           }
-          if constexpr (KEYS) tmem_st16(tb + 16 * half, pk);
-          tmem_st16(tb + 64 + 16 * half, dk);
+          if constexpr (KEYS) tmem_st16(tb + 32 * half, pk);
+          tmem_st16(tb + 64 + 32 * half, dk);
+          if constexpr (decltype(fine)::value) {
+            tmem_st16(tb + 32 * half + 16, pl);
+            tmem_st16(tb + 64 + 32 * half + 16, dl);
+          }
         };
-        if (whole) {
-          part(0, std::false_type{});
-          part(1, std::false_type{});
+        if (KEYS && it.holds_sinks(g)) {
+          part(0, std::true_type{}, std::integral_constant<bool, KEYS>{});
+          part(1, std::true_type{}, std::integral_constant<bool, KEYS>{});
+        } else if (whole) {
+          part(0, std::false_type{}, std::false_type{});
+          part(1, std::false_type{}, std::false_type{});
         } else {
-          part(0, std::true_type{});
-          part(1, std::true_type{});
+          part(0, std::true_type{}, std::false_type{});
+          part(1, std::true_type{}, std::false_type{});
         }
         tmem_wait_st();
         tc_fence_before();
