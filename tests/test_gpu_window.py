@@ -347,6 +347,19 @@ def test_on_another_stream_and_in_two_graphs():
         assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_the_sinks_round_once(d):
+    """dv of the sinks' keys: weights as two 16-bit numbers (u^2 of them is left off), sums in fp32, one rounding of the result."""
+    q, k, v, d_o = make(1, 4, 2, 1500, 1500, d, seed=18)
+    wp = mb.WindowParams(window=100, sinks=7)
+    want = ref.attention(q, k, v, 100, 7, 0.0, None, None, d_o)
+    o, lse = mb.mosaic_bsa_window_fwd(wp, q, k, v)
+    dv = mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o)[2][:, :, :7].double()
+    E, u = score_error(q, k, 0.0), torch.finfo(q.dtype).eps / 2
+    tol = u * want["dv"][:, :, :7].abs() + (u * u + E + 2.0 ** -20) * want["dv_abs"][:, :, :7]
+    assert ((dv - want["dv"][:, :, :7]).abs() <= tol).all()
+
+
 def test_more_units_than_a_grid_is_high():
     """66000 units are 600, checked against the definition, 110 times over."""
     x = make(1, 600, 300, 3, 3, 64, seed=14)
