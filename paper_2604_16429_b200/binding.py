@@ -425,10 +425,20 @@ def _chk_seq(q, k):
     return index
 
 
-def _new(t, stream):
-    """A tensor that the call itself made: not handed out again before `stream` has passed the call."""
+def _on(stream, make, *args, **kw):
+    """make(*args, **kw), a tensor that only the call itself uses, from the memory of the stream that the call runs on.  (The current
+    stream's may still be read or written by what is queued there, and nothing orders `stream` behind that.)"""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
+def _new(stream, make, *args, **kw):
+    """The same for a tensor that the call returns: once freed, not handed out again before the caller's stream has passed that."""
+    t = _on(stream, make, *args, **kw)
     if stream is not None:
-        t.record_stream(stream)
+        t.record_stream(torch.cuda.current_stream(t.device))
     return t
 
 
@@ -440,7 +450,7 @@ def _scratch(n, name, index, ws, stream):
         return ws
     if n == 0:
         raise MosaicError(-1, name)
-    return _new(torch.empty(n, dtype=torch.uint8, device=index), stream)
+    return _on(stream, torch.empty, n, dtype=torch.uint8, device=index)
 
 
 def _call(name, index, stream, *args):
@@ -491,8 +501,8 @@ def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=N
     t = q.dtype
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
-    k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
+    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
+    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
     block = _block
     a = block.at
     _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
@@ -507,8 +517,8 @@ def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps
     t, f32, w = q.dtype, torch.float32, (rp.d,)
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    q_out = _new(torch.empty_like(q), stream) if q_out is None else q_out
-    k_out = _new(torch.empty_like(k), stream) if k_out is None else k_out
+    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
+    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
     block = _block
     a = block.at
     _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
@@ -530,10 +540,10 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     gq, gk = _view("d_q_out", d_q_out, sq, t, index), _view("d_k_out", d_k_out, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    dq = _new(torch.empty_like(q), stream) if dq is None else dq
-    dk = _new(torch.empty_like(k), stream) if dk is None else dk
-    dwq = _new(torch.empty(w, dtype=f32, device=index), stream) if dwq is None else dwq
-    dwk = _new(torch.empty(w, dtype=f32, device=index), stream) if dwk is None else dwk
+    dq = _new(stream, torch.empty_like, q) if dq is None else dq
+    dk = _new(stream, torch.empty_like, k) if dk is None else dk
+    dwq = _new(stream, torch.empty, w, dtype=f32, device=index) if dwq is None else dwq
+    dwk = _new(stream, torch.empty, w, dtype=f32, device=index) if dwk is None else dwk
     block = _block
     a = block.at
     _rotary_pack[6](block.buf, 0, *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
@@ -590,8 +600,8 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     index, p, sk = _window_params(wp, q, k)
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
-    o = _new(torch.empty_like(q), stream) if o is None else o
-    lse = _new(_rows_like(q), stream) if lse is None else lse
+    o = _new(stream, torch.empty_like, q) if o is None else o
+    lse = _new(stream, _rows_like, q) if lse is None else lse
     block = _block
     a = block.at
     _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
@@ -609,9 +619,9 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     vo, vd = _view("o", o, sq, t, index), _view("d_o", d_o, sq, t, index)
-    dq = _new(torch.empty_like(q), stream) if dq is None else dq
-    dk = _new(torch.empty_like(k), stream) if dk is None else dk
-    dv = _new(torch.empty_like(v), stream) if dv is None else dv
+    dq = _new(stream, torch.empty_like, q) if dq is None else dq
+    dk = _new(stream, torch.empty_like, k) if dk is None else dk
+    dv = _new(stream, torch.empty_like, v) if dv is None else dv
     block = _block
     a = block.at
     _window_pack[8](block.buf, 0, *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
@@ -630,8 +640,8 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     index, p, sk = _window_params(wp, q, k)
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
-    o = _new(torch.empty_like(q), stream) if o is None else o
-    lse = _new(_rows_like(q), stream) if lse is None else lse
+    o = _new(stream, torch.empty_like, q) if o is None else o
+    lse = _new(stream, _rows_like, q) if lse is None else lse
     block = _block
     a = block.at
     _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
