@@ -196,13 +196,30 @@ def alloc_workspace(p: Params, op: int, device="cuda") -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+def _on(stream, make, *args, **kw):
+    """make(*args, **kw), a tensor that only the call itself uses, from the memory of the stream that the call runs on.  (The current
+    stream's may still be read or written by what is queued there, and nothing orders `stream` behind that.)"""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
+def _new(stream, make, *args, **kw):
+    """The same for a tensor that the call returns: once freed, not handed out again before the caller's stream has passed that."""
+    t = _on(stream, make, *args, **kw)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def mosaic_bsa_select(p: Params, q, k, block_idx=None, ws=None, stream=None):
     _chk_qkv(p, q)
     _chk_qkv(p, k, heads=p.kv_heads)
     if block_idx is None:
-        block_idx = torch.empty((p.B, p.H, p.m, p.topk), dtype=torch.int32, device=q.device)
+        block_idx = _new(stream, torch.empty, (p.B, p.H, p.m, p.topk), dtype=torch.int32, device=q.device)
     if ws is None:
-        ws = alloc_workspace(p, OP_SELECT, q.device)
+        ws = _on(stream, alloc_workspace, p, OP_SELECT, q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_select(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(block_idx), _ptr(ws), ws.numel(),
                                  _stream(stream))
@@ -217,7 +234,7 @@ def mosaic_bsa_select_static(p: Params, q, k, block_idx=None, stream=None):
     _chk_qkv(p, q)
     _chk_qkv(p, k, heads=p.kv_heads)
     if block_idx is None:
-        block_idx = torch.empty((p.B, p.H, p.m, p.topk), dtype=torch.int32, device=q.device)
+        block_idx = _new(stream, torch.empty, (p.B, p.H, p.m, p.topk), dtype=torch.int32, device=q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_select_static(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(block_idx), _stream(stream))
     if rc:
@@ -229,11 +246,11 @@ def mosaic_bsa_fwd(p: Params, q, k, v, block_idx, o=None, lse=None, ws=None, str
     _chk_qkv(p, q)
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if o is None:
-        o = torch.empty_like(q)
+        o = _new(stream, torch.empty_like, q)
     if lse is None:
-        lse = torch.empty((p.B, p.H, p.N), dtype=torch.float32, device=q.device)
+        lse = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device)
     if ws is None:
-        ws = alloc_workspace(p, OP_FWD, q.device)
+        ws = _on(stream, alloc_workspace, p, OP_FWD, q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_fwd(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(v), _ptr(block_idx), _ptr(o), _ptr(lse),
                               _ptr(ws), ws.numel(), _stream(stream))
@@ -249,11 +266,11 @@ def mosaic_bsa_fwd_branches(p: Params, q, k, v, block_idx, gates, o=None, lse_fg
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if gates.dtype != torch.float32 or not gates.is_contiguous() or tuple(gates.shape) != (p.B, p.H, p.N, 3):
         raise ValueError(f"expected contiguous cuda fp32 gates [{p.B},{p.H},{p.N},3]")
-    o = torch.empty_like(q) if o is None else o
-    lse_fg = torch.empty((p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_fg is None else lse_fg
-    lse_l = torch.empty((p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_l is None else lse_l
+    o = _new(stream, torch.empty_like, q) if o is None else o
+    lse_fg = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_fg is None else lse_fg
+    lse_l = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_l is None else lse_l
     if ws is None:
-        ws = alloc_workspace(p, OP_FWD_BRANCHES, q.device)
+        ws = _on(stream, alloc_workspace, p, OP_FWD_BRANCHES, q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_fwd_branches(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(v), _ptr(block_idx), _ptr(gates), _ptr(o),
                                        _ptr(lse_fg), _ptr(lse_l), _ptr(ws), ws.numel(), _stream(stream))
@@ -265,11 +282,11 @@ def mosaic_bsa_fwd_branches(p: Params, q, k, v, block_idx, gates, o=None, lse_fg
 def mosaic_bsa_bwd(p: Params, q, k, v, o, lse, d_o, block_idx, dq=None, dk=None, dv=None, ws=None, stream=None):
     _chk_qkv(p, q, o, d_o)
     _chk_qkv(p, k, v, heads=p.kv_heads)
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(k) if dv is None else dv
+    dq = _new(stream, torch.empty_like, q) if dq is None else dq
+    dk = _new(stream, torch.empty_like, k) if dk is None else dk
+    dv = _new(stream, torch.empty_like, k) if dv is None else dv
     if ws is None:
-        ws = alloc_workspace(p, OP_BWD, q.device)
+        ws = _on(stream, alloc_workspace, p, OP_BWD, q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_bwd(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o),
                               _ptr(block_idx), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream(stream))
@@ -285,12 +302,12 @@ def mosaic_bsa_bwd_branches(p: Params, q, k, v, block_idx, gates, d_o, dq=None, 
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if gates.dtype != torch.float32 or not gates.is_contiguous() or tuple(gates.shape) != (p.B, p.H, p.N, 3):
         raise ValueError(f"expected contiguous cuda fp32 gates [{p.B},{p.H},{p.N},3]")
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(k) if dv is None else dv
-    dgates = torch.empty_like(gates) if dgates is None else dgates
+    dq = _new(stream, torch.empty_like, q) if dq is None else dq
+    dk = _new(stream, torch.empty_like, k) if dk is None else dk
+    dv = _new(stream, torch.empty_like, k) if dv is None else dv
+    dgates = _new(stream, torch.empty_like, gates) if dgates is None else dgates
     if ws is None:
-        ws = alloc_workspace(p, OP_BWD_BRANCHES, q.device)
+        ws = _on(stream, alloc_workspace, p, OP_BWD_BRANCHES, q.device)
     pc = p.c()
     rc = lib().mosaic_bsa_bwd_branches(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(v), _ptr(block_idx), _ptr(gates), _ptr(d_o),
                                        _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dgates), _ptr(ws), ws.numel(), _stream(stream))
@@ -306,8 +323,8 @@ def mosaic_bsa_rope(p: Params, q, k, pos, theta=10000.0, q_out=None, k_out=None,
     _chk_qkv(p, k, heads=p.kv_heads)
     if pos.dtype != torch.float32 or not pos.is_cuda or not pos.is_contiguous() or tuple(pos.shape) != (p.N, 2):
         raise ValueError(f"expected contiguous cuda fp32 positions [{p.N},2]")
-    q_out = torch.empty_like(q) if q_out is None else q_out
-    k_out = torch.empty_like(k) if k_out is None else k_out
+    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
+    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
     pc = p.c()
     rc = lib().mosaic_bsa_rope(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(pos), float(theta), _ptr(q_out), _ptr(k_out),
                                _stream(stream))
@@ -423,23 +440,6 @@ def _chk_seq(q, k):
         raise ValueError(f"expected cuda tensors [B, heads, tokens, d] in bf16, fp16 or fp32, got {q.dtype} {tuple(q.shape)} on "
                          f"{q.device} and {tuple(k.shape)}")
     return index
-
-
-def _on(stream, make, *args, **kw):
-    """make(*args, **kw), a tensor that only the call itself uses, from the memory of the stream that the call runs on.  (The current
-    stream's may still be read or written by what is queued there, and nothing orders `stream` behind that.)"""
-    if stream is None:
-        return make(*args, **kw)
-    with torch.cuda.stream(stream):
-        return make(*args, **kw)
-
-
-def _new(stream, make, *args, **kw):
-    """The same for a tensor that the call returns: once freed, not handed out again before the caller's stream has passed that."""
-    t = _on(stream, make, *args, **kw)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream(t.device))
-    return t
 
 
 def _scratch(n, name, index, ws, stream):

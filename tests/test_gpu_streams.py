@@ -37,6 +37,27 @@ def sequence_calls(B=1, H=4, Hkv=2, N=1024, d=64):
     }
 
 
+def block_calls(B=1, H=2, d=64):
+    p = mb.Params(B=B, H=H, nlat=32, nlon=64, bh=8, bw=8, topk=4)
+    g = torch.Generator().manual_seed(2)
+    q, k, v, d_o = (torch.randn((B, H, p.N, d), generator=g).bfloat16().cuda() for _ in range(4))
+    gates = torch.rand((B, H, p.N, 3), generator=g).cuda()
+    pos = torch.rand((p.N, 2), generator=g).cuda()
+    idx = mb.mosaic_bsa_select(p, q, k)
+    mb.mosaic_bsa_select_static(p, q, k)
+    o, lse = mb.mosaic_bsa_fwd(p, q, k, v, idx)
+    return {
+        "select": lambda **kw: mb.mosaic_bsa_select(p, q, k, **kw),
+        "select_static": lambda **kw: mb.mosaic_bsa_select_static(p, q, k, **kw),
+        "fwd": lambda **kw: mb.mosaic_bsa_fwd(p, q, k, v, idx, **kw),
+        "bwd": lambda **kw: mb.mosaic_bsa_bwd(p, q, k, v, o, lse, d_o, idx, **kw),
+        "fwd_branches": lambda **kw: mb.mosaic_bsa_fwd_branches(p, q, k, v, idx, gates, **kw),
+        "bwd_branches": lambda **kw: mb.mosaic_bsa_bwd_branches(p, q, k, v, idx, gates, d_o, **kw),
+        "rope": lambda **kw: mb.mosaic_bsa_rope(p, q, k, pos, **kw),
+    }
+
+
+BLOCK = ("select", "select_static", "fwd", "bwd", "fwd_branches", "bwd_branches", "rope")
 SEQUENCE = ("rotary", "qk_norm", "qk_norm_bwd", "window_fwd", "window_bwd", "window_decode")
 
 
@@ -117,3 +138,18 @@ def test_sequence_operators_leave_queued_work_alone(name):
 @pytest.mark.parametrize("name", SEQUENCE)
 def test_results_of_sequence_operators_last(name):
     check_results_last_as_long_as_the_caller_needs_them(sequence_calls()[name])
+
+
+@pytest.mark.parametrize("name", BLOCK)
+def test_block_sparse_calls_take_the_memory_of_their_stream(name):
+    check_memory_of_the_stream(block_calls()[name])
+
+
+@pytest.mark.parametrize("name", BLOCK)
+def test_block_sparse_calls_leave_queued_work_alone(name):
+    check_queued_work_is_left_alone(block_calls()[name])
+
+
+@pytest.mark.parametrize("name", BLOCK)
+def test_results_of_block_sparse_calls_last(name):
+    check_results_last_as_long_as_the_caller_needs_them(block_calls()[name])

@@ -10,6 +10,8 @@ from paper_2604_16429_b200 import binding as mb
 
 SEQUENCE = ("mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_fwd", "mosaic_bsa_window_bwd",
             "mosaic_bsa_window_decode", "_scratch", "_window_ws")
+BLOCK = ("mosaic_bsa_select", "mosaic_bsa_select_static", "mosaic_bsa_fwd", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd",
+         "mosaic_bsa_bwd_branches", "mosaic_bsa_rope")
 
 
 class FakeTensor:
@@ -50,7 +52,7 @@ def test_a_call_takes_its_memory_on_its_stream(streams):
     assert streams == ["current"]
 
 
-@pytest.mark.parametrize("name", SEQUENCE)
+@pytest.mark.parametrize("name", SEQUENCE + BLOCK)
 def test_no_call_allocates_past_its_stream(name):
     """torch's allocation functions appear as arguments of `_on` and `_new` only."""
     tree = ast.parse(inspect.getsource(getattr(mb, name)))
