@@ -500,8 +500,9 @@ template <int D, bool F16>
 __global__ void __launch_bounds__(256) window_rows_kernel(const WinGeo g, const View o, const View d_o, const float* __restrict__ lse,
                                                           float* __restrict__ neg_lse2, float* __restrict__ neg_d, int pad, unsigned blocks,
                                                           int* status) {
-  const int unit = (int)(blockIdx.x / blocks), b = unit / g.H, h = unit - b * g.H;
-  const int first = (int)(blockIdx.x - unit * blocks) * (32 * kRowsAhead) + (threadIdx.x >> 3) + await_stream(), part = threadIdx.x & 7;
+  const unsigned cta = blockIdx.x + (unsigned)await_stream();
+  const int unit = (int)(cta / blocks), b = unit / g.H, h = unit - b * g.H;
+  const int first = (int)(cta - unit * blocks) * (32 * kRowsAhead) + (threadIdx.x >> 3), part = threadIdx.x & 7;
   if (blockIdx.x == 0 && threadIdx.x < kStatusBytes / 4) status[threadIdx.x] = 0;
   const int ql = span_of(g, b).ql;
   const char *x = o.data + b * o.sb + h * o.sh + 16 * part, *y = d_o.data + b * d_o.sb + h * d_o.sh + 16 * part;
