@@ -133,11 +133,11 @@ __device__ __forceinline__ void still_angles(const HeadArgs& a, Angles& t, int l
     t.sine[i] = 0.f;
   }
 }
-// The token's angles, shared out over the warp
-__device__ __forceinline__ void make_angles(const HeadArgs& a, long long pos, Angles& t, int lane) {
+// The token's angles, shared out over the warp.  (`freqs`: behind the wait for the stream)
+__device__ __forceinline__ void make_angles(const HeadArgs& a, const double* freqs, long long pos, Angles& t, int lane) {
   __syncwarp();  // the token before has been read
   for (int i = lane; i < a.rot / 2; i += 32) {
-    const double turns = (double)pos * (__ldg(a.freqs + i) * 0.31830988618379067154);  // half turns
+    const double turns = (double)pos * (__ldg(freqs + i) * 0.31830988618379067154);  // half turns
     const float r = (float)(turns - 2.0 * rint(0.5 * turns));
     float sn, cn;
     sincospif(r, &sn, &cn);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_
   while (sp.more) {
     fetch(slot ? slot - 1 : kDeepFwd - 1);  // where the batch before was
     if (!turned) {
-      make_angles(a, pos, angles[warp], lane);
+      make_angles(a, a.freqs + zero, pos, angles[warp], lane);
       yq = a.t[0].y.data + sp.b * a.t[0].y.sb + sp.n * a.t[0].y.sn + ca;
       yk = a.t[1].y.data + sp.b * a.t[1].y.sb + sp.n * a.t[1].y.sn + ca - heads * a.t[1].y.sh;
       turned = true;
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const 
     slot = slot + 1 == kDeep ? 0 : slot + 1;
     const bool there = sp.r0 + pl.group < sp.r1;
     if (!turned) {
-      make_angles(a, pos, angles[warp], lane);
+      make_angles(a, a.freqs + zero, pos, angles[warp], lane);
       y = t.y.data + sp.b * t.y.sb + sp.n * t.y.sn + sp.r0 * t.y.sh + oy;
       turned = true;
       Spot after = sp;

@@ -62,3 +62,24 @@ def test_lengths(op, what):
         return mb.mosaic_bsa_window_bwd(wp, q, k, v, o, lse, d_o, dq=out[0], dk=out[1], dv=out[2], **kw)
 
     check(full, short, lambda x: x, call)
+
+
+@pytest.mark.parametrize("op", ["rotary", "qk_norm", "qk_norm_bwd"])
+@pytest.mark.parametrize("what", ["freqs", "pos"])
+def test_frequencies_and_positions(op, what):
+    q, k, _, _ = make(1, 4, 2, 20, 20, 32, seed=2)
+    rp = mb.RotaryParams(d=32)
+    weights = torch.ones(32, device="cuda")
+    values = {"freqs": 2.0 ** -torch.arange(16, dtype=torch.float64), "pos": torch.arange(20) * 3}
+    values = {n: x.cuda() for n, x in values.items()}
+    words = values[what].view(torch.int32)
+
+    def call(x):
+        kw = {**values, what: x}
+        if op == "rotary":
+            return mb.mosaic_bsa_rotary(rp, q, k, kw["pos"], kw["freqs"])
+        if op == "qk_norm":
+            return mb.mosaic_bsa_qk_norm(rp, q, k, weights, weights, kw["pos"], kw["freqs"])
+        return mb.mosaic_bsa_qk_norm_bwd(rp, q, k, weights, weights, kw["pos"], kw["freqs"], q, k)
+
+    check(words, torch.zeros_like(words), lambda x: x.view(values[what].dtype), call)
