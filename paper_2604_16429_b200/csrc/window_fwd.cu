@@ -6,8 +6,9 @@
 // A tile is 128 query rows of one head.  The tiles of a key/value head are numbered with the heads of its group fastest, and a
 // CTA takes two neighbours: heads of a group read the same keys, so a staged key tile serves 256 rows.  The two tiles walk a
 // common sequence of steps of at most 64 keys: the sinks (as many columns as there are, rounded up to 32) unless the window
-// still holds them, then the union of the two windows from its first key on; a step that a tile sees nothing of it leaves out.
-// Only steps at the window's edges are masked element by element.
+// still holds them, then the union of the two windows; a step that a tile sees nothing of it leaves out.  Steps begin at multiples
+// of 64 keys, so that what a step holds of a row's keys, and with it the bits of the row's results, does not depend on the tile beside
+// it.  Only steps at the window's edges are masked element by element.
 //
 // Warps (384 threads, persistent, one CTA per SM): 0-3 and 4-7 softmax of tile 0 and 1 (thread = row = TMEM lane), 8 TMA, 9 and 10
 // the products of tile 0 and 1.  TMEM (512 columns): two score buffers of a tile at 128 t + 64 b (fp32), P over a buffer's first
@@ -62,7 +63,7 @@ struct Item {
   int kl, off, ql;
   int row0[2], head[2], tiles;  // tiles: how many of the two there are
   int lo[2], hi[2];  // keys of the tile's window (sinks aside); hi <= 0: nothing to compute
-  int base, end;     // union of the windows
+  int base, end;     // union of the windows, its first key rounded down to a multiple of U
   int sinks, ns;     // all sinks; those in front of base, which have steps of their own (the others lie in the first of the union)
   int front, steps;  // steps of the sinks, of all
   // UNIFORM: by a whole warp, all of it uniform
@@ -95,6 +96,7 @@ struct Item {
         end = max(end, hi[t]);
       }
     }
+    base = base / U * U;
     sinks = g.sinks;
     ns = end > 0 ? min(sinks, base) : 0;
     front = (ns + U - 1) / U;
