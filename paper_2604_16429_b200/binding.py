@@ -442,6 +442,14 @@ def _chk_seq(q, k):
     return index
 
 
+def _like(t, stream):
+    return torch.empty_like(t) if stream is None else _new(stream, torch.empty_like, t)
+
+
+def _floats(n, index, stream):
+    return torch.empty(n, dtype=torch.float32, device=index) if stream is None else _new(stream, _floats, n, index, None)
+
+
 def _scratch(n, name, index, ws, stream):
     """The caller's workspace, or one of n bytes."""
     if ws is not None:
@@ -450,7 +458,7 @@ def _scratch(n, name, index, ws, stream):
         return ws
     if n == 0:
         raise MosaicError(-1, name)
-    return _on(stream, torch.empty, n, dtype=torch.uint8, device=index)
+    return torch.empty(n, dtype=torch.uint8, device=index) if stream is None else _on(stream, _scratch, n, name, index, None, None)
 
 
 def _call(name, index, stream, *args):
@@ -501,8 +509,8 @@ def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=N
     t = q.dtype
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
-    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
+    q_out = _like(q, stream) if q_out is None else q_out
+    k_out = _like(k, stream) if k_out is None else k_out
     block = _block
     a = block.at
     _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
@@ -517,8 +525,8 @@ def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps
     t, f32, w = q.dtype, torch.float32, (rp.d,)
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
-    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
+    q_out = _like(q, stream) if q_out is None else q_out
+    k_out = _like(k, stream) if k_out is None else k_out
     block = _block
     a = block.at
     _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
@@ -540,10 +548,10 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     vq, vk = _view("q", q, sq, t, index), _view("k", k, sk, t, index)
     gq, gk = _view("d_q_out", d_q_out, sq, t, index), _view("d_k_out", d_k_out, sk, t, index)
     at, step, fr = _positions(rp, pos, freqs, sq, index)
-    dq = _new(stream, torch.empty_like, q) if dq is None else dq
-    dk = _new(stream, torch.empty_like, k) if dk is None else dk
-    dwq = _new(stream, torch.empty, w, dtype=f32, device=index) if dwq is None else dwq
-    dwk = _new(stream, torch.empty, w, dtype=f32, device=index) if dwk is None else dwk
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(k, stream) if dk is None else dk
+    dwq = _floats(rp.d, index, stream) if dwq is None else dwq
+    dwk = _floats(rp.d, index, stream) if dwk is None else dwk
     block = _block
     a = block.at
     _rotary_pack[6](block.buf, 0, *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
@@ -584,8 +592,10 @@ def _window_ws(at, op, index, ws, stream):
     return _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(at, op)), name, index, ws, stream)
 
 
-def _rows_like(q):
+def _rows_like(q, stream):
     """Contiguous fp32 [B, H, Nq] beside q (torch.empty takes a microsecond longer)."""
+    if stream is not None:
+        return _new(stream, _rows_like, q, None)
     B, H, N, _ = q.shape
     return torch.empty_strided((B, H, N), (H * N, N, 1), dtype=torch.float32, device=q.device)
 
@@ -600,8 +610,8 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     index, p, sk = _window_params(wp, q, k)
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
-    o = _new(stream, torch.empty_like, q) if o is None else o
-    lse = _new(stream, _rows_like, q) if lse is None else lse
+    o = _like(q, stream) if o is None else o
+    lse = _rows_like(q, stream) if lse is None else lse
     block = _block
     a = block.at
     _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
@@ -619,9 +629,9 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     vo, vd = _view("o", o, sq, t, index), _view("d_o", d_o, sq, t, index)
-    dq = _new(stream, torch.empty_like, q) if dq is None else dq
-    dk = _new(stream, torch.empty_like, k) if dk is None else dk
-    dv = _new(stream, torch.empty_like, v) if dv is None else dv
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(k, stream) if dk is None else dk
+    dv = _like(v, stream) if dv is None else dv
     block = _block
     a = block.at
     _window_pack[8](block.buf, 0, *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
@@ -640,8 +650,8 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     index, p, sk = _window_params(wp, q, k)
     t, sq = q.dtype, q.shape
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
-    o = _new(stream, torch.empty_like, q) if o is None else o
-    lse = _new(stream, _rows_like, q) if lse is None else lse
+    o = _like(q, stream) if o is None else o
+    lse = _rows_like(q, stream) if lse is None else lse
     block = _block
     a = block.at
     _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
