@@ -161,9 +161,15 @@ __device__ __forceinline__ void read_floats(const float* p, float* out) {
   }
 }
 
-// Turns the pairs of a row's two pieces.  (The angles are read anew for every row: kept over a token's rows they cost sixteen registers,
-// which are worth a second CTA on the SM.)
+// Whether pair j of the lane's two pieces turns
 template <int V, bool HALF>
+__device__ __forceinline__ bool turns(const HeadArgs& args, const Place& pl, int j) {
+  return HALF ? pl.ca < args.rot / 2 : (j < V / 2 ? pl.ca : pl.cb - V) + 2 * j < args.rot;
+}
+// Turns the pairs of a row's two pieces.  PART: some channels do not turn; they stay as they are, whatever they hold (a product with
+// (1, 0) makes no number of an infinite one's partner).  (The angles are read anew for every row: kept over a token's rows they cost
+// sixteen registers, which are worth a second CTA on the SM.)
+template <int V, bool HALF, bool PART>
 __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const HeadArgs& args, const Place& pl) {
   constexpr int N = HALF ? V : V / 2;  // pairs of one piece that lie side by side
   float c[V], s[V];
@@ -178,9 +184,48 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles&
   for (int j = 0; j < V; ++j) {
     float& x = HALF ? a[j] : j < V / 2 ? a[2 * j] : b[2 * j - V];
     float& y = HALF ? b[j] : j < V / 2 ? a[2 * j + 1] : b[2 * j - V + 1];
-    const float u = x * c[j] - y * s[j];
-    y = x * s[j] + y * c[j];
-    x = u;
+    const float u = x * c[j] - y * s[j], v = x * s[j] + y * c[j];
+    if (!PART || turns<V, HALF>(args, pl, j)) {
+      x = u;
+      y = v;
+    }
+  }
+}
+// Turns what turns of a row's two pieces as they lie in memory; the rest keeps its bits (narrowing would change those of what is no
+// number), and a piece without a turning pair is not looked at.
+template <int T, bool HALF>
+__device__ __forceinline__ void turn_part(uint4& va, uint4& vb, const Angles& t, const HeadArgs& args, const Place& pl) {
+  constexpr int V = Vec<T>::n, N = V / 2;
+  if constexpr (HALF) {
+    if (pl.ca >= args.rot / 2) return;
+    float a[V], b[V];
+    widen<T>(va, a);
+    widen<T>(vb, b);
+    turn<V, true, false>(a, b, t, args, pl);
+    va = narrow<T>(a);
+    vb = narrow<T>(b);
+  } else {
+    auto piece = [&](uint4& v, int first) {
+      if (first >= args.rot) return;
+      float f[V], c[N], s[N];
+      widen<T>(v, f);
+      read_floats<N>(t.cosine + first / 2, c);
+      read_floats<N>(t.sine + first / 2, s);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float x = f[2 * j], y = f[2 * j + 1];
+        f[2 * j] = x * c[j] - y * s[j];
+        f[2 * j + 1] = x * s[j] + y * c[j];
+      }
+      const uint4 u = narrow<T>(f);
+      const int words = (args.rot - first) * Vec<T>::bytes / 4;  // that turn
+      v.x = u.x;  // (a pair is one word or two)
+      if (T == kF32 || words > 1) v.y = u.y;
+      if (words > 2) v.z = u.z;
+      if (words > (T == kF32 ? 2 : 3)) v.w = u.w;
+    };
+    piece(va, pl.ca);
+    piece(vb, pl.cb);
   }
 }
 
@@ -233,7 +278,7 @@ struct Spot {
 
 // The warps walk their tasks with the next batches' rows already asked for: they land in shared memory, where every lane reads what
 // it copied itself (held in registers instead, 62 us became 84 in the backward).  A token's rows are Q's heads, then K's.
-template <int T, bool HALF, bool NORM>
+template <int T, bool HALF, bool NORM, bool PART>
 __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes;
   __shared__ alignas(16) Angles angles[kHeadWarps];
@@ -294,9 +339,10 @@ __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_
       pos = position(after);  // (asked for a token ahead)
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(kDeepFwd - 1) : "memory");
+    uint4 va = mine[(slot * 2 + 0) * 32], vb = mine[(slot * 2 + 1) * 32];
     float fa[V], fb[V];
-    widen<T>(mine[(slot * 2 + 0) * 32], fa);
-    widen<T>(mine[(slot * 2 + 1) * 32], fb);
+    widen<T>(va, fa);
+    widen<T>(vb, fb);
     slot = slot + 1 == kDeepFwd ? 0 : slot + 1;
     const int h = sp.r0 + pl.group;
     const bool there = h < sp.r1;
@@ -318,11 +364,17 @@ __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_
         fb[j] *= rr * gb[j];
       }
     }
-    turn<V, HALF>(fa, fb, angles[warp], a, pl);
+    if constexpr (PART && !NORM) {
+      turn_part<T, HALF>(va, vb, angles[warp], a, pl);
+    } else {
+      turn<V, HALF, PART>(fa, fb, angles[warp], a, pl);
+      va = narrow<T>(fa);
+      vb = narrow<T>(fb);
+    }
     if (there && pl.on) {
       char* y = h < heads ? yq + h * a.t[0].y.sh : yk + h * a.t[1].y.sh;
-      *reinterpret_cast<uint4*>(y) = narrow<T>(fa);
-      *reinterpret_cast<uint4*>(y + ba) = narrow<T>(fb);
+      *reinterpret_cast<uint4*>(y) = va;
+      *reinterpret_cast<uint4*>(y + ba) = vb;
     }
   }
 }
@@ -330,7 +382,7 @@ __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_
 // The sums of the weights' gradients stay in registers over a CTA's tokens (a lane has the same channels in every row); the first
 // CTAs have Q's rows, the others K's, and each leaves one row of partial sums.  Packed fp32 arithmetic: the pass is as much bound
 // by instructions as by memory.
-template <int T, bool HALF>
+template <int T, bool HALF, bool PART>
 __global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int V = Vec<T>::n, SZ = Vec<T>::bytes, P = V / 2;
   __shared__ alignas(16) Angles angles[kHeadWarps];
@@ -415,7 +467,7 @@ __global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const 
       sp.next(a, t.heads);
       turned = false;
     }
-    turn<V, HALF>(ha, hb, angles[warp], a, pl);
+    turn<V, HALF, PART>(ha, hb, angles[warp], a, pl);
     float wa[V], wb[V];
     read_weights<V>(weights, pl, wa, wb);
     uint64_t ss2 = 0ull, dot2 = 0ull, wh[V];  // wh: the weighted gradient
@@ -541,17 +593,19 @@ int plan(HeadArgs* a, int rows, int sms, long long ctas) {
   return spread(a, ctas);
 }
 
-template <int T, bool HALF, bool NORM>
+template <int T, bool HALF, bool NORM, bool PART>
 int launch_head(HeadArgs a, cudaStream_t stream) {
   static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_kernel<T, HALF, NORM>), kFwdRing, &configured, &sms)) return rc;
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_kernel<T, HALF, NORM, PART>), kFwdRing, &configured, &sms)) return rc;
   const int blocks = plan(&a, a.t[0].heads + a.t[1].heads, sms, (long long)kCtas * sms);
-  return launch_kernel(head_kernel<T, HALF, NORM>, dim3((unsigned)blocks), kHeadThreads, kFwdRing, stream, true, 0, a);
+  return launch_kernel(head_kernel<T, HALF, NORM, PART>, dim3((unsigned)blocks), kHeadThreads, kFwdRing, stream, true, 0, a);
 }
 template <int T, bool HALF>
 int launch_head(const HeadArgs& a, bool norm, cudaStream_t stream) {
-  return norm ? launch_head<T, HALF, true>(a, stream) : launch_head<T, HALF, false>(a, stream);
+  const bool part = a.rot < a.d;
+  if (norm) return part ? launch_head<T, HALF, true, true>(a, stream) : launch_head<T, HALF, true, false>(a, stream);
+  return part ? launch_head<T, HALF, false, true>(a, stream) : launch_head<T, HALF, false, false>(a, stream);
 }
 int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;
@@ -560,20 +614,23 @@ int launch_head(const HeadArgs& a, uint32_t flags, bool norm, cudaStream_t strea
   return half ? launch_head<kBf16, true>(a, norm, stream) : launch_head<kBf16, false>(a, norm, stream);
 }
 
-template <int T, bool HALF>
+template <int T, bool HALF, bool PART>
 int launch_head_bwd(const HeadArgs& a, int ctas, cudaStream_t stream) {
   static unsigned long long configured = 0;
   int sms = 0;
-  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_bwd_kernel<T, HALF>), kBwdRing, &configured, &sms)) return rc;
-  return launch_kernel(head_bwd_kernel<T, HALF>, dim3((unsigned)ctas), kHeadThreads, kBwdRing, stream, true, 0, a);
+  if (const int rc = launch_setup(reinterpret_cast<const void*>(head_bwd_kernel<T, HALF, PART>), kBwdRing, &configured, &sms)) return rc;
+  return launch_kernel(head_bwd_kernel<T, HALF, PART>, dim3((unsigned)ctas), kHeadThreads, kBwdRing, stream, true, 0, a);
+}
+template <int T>
+int launch_head_bwd(const HeadArgs& a, bool half, int ctas, cudaStream_t stream) {
+  const bool part = a.rot < a.d;
+  if (half) return part ? launch_head_bwd<T, true, true>(a, ctas, stream) : launch_head_bwd<T, true, false>(a, ctas, stream);
+  return part ? launch_head_bwd<T, false, true>(a, ctas, stream) : launch_head_bwd<T, false, false>(a, ctas, stream);
 }
 int launch_head_bwd(const HeadArgs& a, uint32_t flags, int ctas, cudaStream_t stream) {
   const bool half = (flags & MOSAIC_FLAG_HALF_PAIRS) != 0;
-  if (flags & MOSAIC_FLAG_FP32)
-    return half ? launch_head_bwd<kF32, true>(a, ctas, stream) : launch_head_bwd<kF32, false>(a, ctas, stream);
-  if (flags & MOSAIC_FLAG_FP16)
-    return half ? launch_head_bwd<kF16, true>(a, ctas, stream) : launch_head_bwd<kF16, false>(a, ctas, stream);
-  return half ? launch_head_bwd<kBf16, true>(a, ctas, stream) : launch_head_bwd<kBf16, false>(a, ctas, stream);
+  if (flags & MOSAIC_FLAG_FP32) return launch_head_bwd<kF32>(a, half, ctas, stream);
+  return flags & MOSAIC_FLAG_FP16 ? launch_head_bwd<kF16>(a, half, ctas, stream) : launch_head_bwd<kBf16>(a, half, ctas, stream);
 }
 
 constexpr size_t kMaxBwdRows = 2048;  // partial rows that the workspace holds: the most CTAs of the backward
