@@ -401,9 +401,19 @@ class _Block(threading.local):
 
 _block = _Block()
 # (both parameter blocks are 40 bytes long with their padding, a view is 32)
-_rotary_pack = {n: struct.Struct("=6iI2f4x%dq" % (4 * n)).pack_into for n in (4, 6)}
-_window_pack = {n: struct.Struct("=8ifI%dq" % (4 * n)).pack_into for n in (4, 8)}
+_rotary_pack = {n: struct.Struct("=6iI2f4x%dq" % (4 * n)).pack_into for n in (0, 4, 6)}
+_window_pack = {n: struct.Struct("=8ifI%dq" % (4 * n)).pack_into for n in (0, 4, 8)}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _pack(layout, *values):
+    """Writes a call's parameters and views into the thread's buffer; its address."""
+    block = _block
+    try:
+        layout(block.buf, 0, *values)
+    except (struct.error, OverflowError) as e:
+        raise ValueError(f"a parameter is out of range: {e}") from None
+    return block.at
 
 
 def _bad(name, t, what):
@@ -511,9 +521,7 @@ def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=N
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _like(q, stream) if q_out is None else q_out
     k_out = _like(k, stream) if k_out is None else k_out
-    block = _block
-    a = block.at
-    _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    a = _pack(_rotary_pack[4], *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
     _call("mosaic_bsa_rotary", index, stream, a, a + 40, a + 72, at, step, fr, a + 104, a + 136)
     return q_out, k_out
 
@@ -527,16 +535,14 @@ def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _like(q, stream) if q_out is None else q_out
     k_out = _like(k, stream) if k_out is None else k_out
-    block = _block
-    a = block.at
-    _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    a = _pack(_rotary_pack[4], *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
     _call("mosaic_bsa_qk_norm", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at,
           step, fr, a + 104, a + 136)
     return q_out, k_out
 
 
 def qk_norm_workspace_bytes(rp: RotaryParams, q, k) -> int:
-    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(ctypes.byref(_RotaryParams(*_rotary_params(rp, q, k, 0, 0.0)[1]))))
+    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_pack(_rotary_pack[0], *_rotary_params(rp, q, k, 0, 0.0)[1])))
 
 
 def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, d_k_out, eps=1e-6, dq=None, dk=None, dwq=None,
@@ -552,9 +558,7 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     dk = _like(k, stream) if dk is None else dk
     dwq = _floats(rp.d, index, stream) if dwq is None else dwq
     dwk = _floats(rp.d, index, stream) if dwk is None else dwk
-    block = _block
-    a = block.at
-    _rotary_pack[6](block.buf, 0, *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
+    a = _pack(_rotary_pack[6], *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
     name = "mosaic_bsa_qk_norm_workspace_bytes"
     ws = _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(a)), name, index, ws, stream)
     _call("mosaic_bsa_qk_norm_bwd", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index),
@@ -580,11 +584,12 @@ def _window_params(wp, q, k):
     B, H, Nq, d = q.shape
     Hkv, Nk = k.shape[1], k.shape[2]
     flags = _STORAGE[q.dtype] | (FLAG_ROLLING if wp.rolling else 0)
-    return index, (B, H, Hkv, Nq, Nk, d, wp.window, wp.sinks, wp.scale, flags), (B, Hkv, Nk, d)
+    window = wp.window if wp.window < Nk or wp.rolling else Nk  # (Nk or more, whatever the number, is plain causal attention)
+    return index, (B, H, Hkv, Nq, Nk, d, window, wp.sinks, wp.scale, flags), (B, Hkv, Nk, d)
 
 
 def window_workspace_bytes(wp: WindowParams, q, k, op: int) -> int:
-    return int(lib().mosaic_bsa_window_workspace_bytes(ctypes.byref(_WindowParams(*_window_params(wp, q, k)[1])), op))
+    return int(lib().mosaic_bsa_window_workspace_bytes(_pack(_window_pack[0], *_window_params(wp, q, k)[1]), op))
 
 
 def _window_ws(at, op, index, ws, stream):
@@ -612,9 +617,7 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _like(q, stream) if o is None else o
     lse = _rows_like(q, stream) if lse is None else lse
-    block = _block
-    a = block.at
-    _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    a = _pack(_window_pack[4], *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
     ws = _window_ws(a, OP_FWD, index, ws, stream)
     _call("mosaic_bsa_window_fwd", index, stream, a, a + 40, a + 72, a + 104, _len("q_len", q_len, sq[0], index),
           _len("k_len", k_len, sq[0], index), a + 136, _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
@@ -632,10 +635,8 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
     dq = _like(q, stream) if dq is None else dq
     dk = _like(k, stream) if dk is None else dk
     dv = _like(v, stream) if dv is None else dv
-    block = _block
-    a = block.at
-    _window_pack[8](block.buf, 0, *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
-                    *_out("dv", dv, sk, t, index))
+    a = _pack(_window_pack[8], *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
+              *_out("dv", dv, sk, t, index))
     ws = _window_ws(a, OP_BWD, index, ws, stream)
     _call("mosaic_bsa_window_bwd", index, stream, a, a + 40, a + 72, a + 104, a + 136, _flat("lse", lse, sq[:3], torch.float32, index),
           a + 168, _len("q_len", q_len, sq[0], index), _len("k_len", k_len, sq[0], index), a + 200, a + 232, a + 264, ws.data_ptr(),
@@ -652,9 +653,7 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _like(q, stream) if o is None else o
     lse = _rows_like(q, stream) if lse is None else lse
-    block = _block
-    a = block.at
-    _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    a = _pack(_window_pack[4], *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
     _call("mosaic_bsa_window_decode", index, stream, a, a + 40, a + 72, a + 104, _len("k_len", k_len, sq[0], index), a + 136,
           _flat("lse", lse, sq[:3], torch.float32, index))
     return o, lse
