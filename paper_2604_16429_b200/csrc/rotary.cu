@@ -5,8 +5,8 @@
 //
 // HBM-bound: every element is read once (x and dy in the backward) and written once.  A warp has one token and walks its
 // heads; a row of d channels is spread over P lanes (the power of two that holds d / 2V), each with two 16-byte pieces of V
-// channels: with half pairs the two pieces hold the pairs' two sides, otherwise they lie next to one another.  So a pair never
-// leaves its lane, a row's sums are shuffles among P lanes, and 32 / P rows go through a warp at a time, a few fetched ahead.
+// channels: with half pairs the two pieces hold the pairs' two sides, otherwise one lies in the first half of the head and one in the
+// second, at the same place (half a head apart).  So a pair never leaves its lane, a row's sums are shuffles among P lanes, and 32 / P rows go through a warp at a time, a few fetched ahead.
 // The token's rot_dim/2 angles are the same for all its heads: the warp's lanes share them out, take the product with the
 // position in half turns and its remainder in fp64 (an angle of 1e6 radians has 2^-33 of error there, 2^-4 in fp32), and leave
 // (cos, sin) in shared memory, from where every lane reads the V that it needs for each row.
@@ -57,24 +57,6 @@ struct HeadArgs {
 
 template <int T>
 struct Vec { static constexpr int n = T == kF32 ? 4 : 8, bytes = T == kF32 ? 4 : 2; };
-
-// two fp32 numbers in one register pair (packed arithmetic)
-__device__ __forceinline__ uint64_t two(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void one(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2f(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul2f(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 
 // 16 bytes of global memory to shared memory, or (bytes 0) zeros
 __device__ __forceinline__ void copy_async(uint32_t dst, const char* src, uint32_t bytes) {
@@ -473,25 +455,25 @@ __global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const 
     uint64_t ss2 = 0ull, dot2 = 0ull, wh[V];  // wh: the weighted gradient
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const uint64_t f0 = two(fa[2 * j], fa[2 * j + 1]), f1 = two(fb[2 * j], fb[2 * j + 1]);
-      wh[j] = mul2f(two(ha[2 * j], ha[2 * j + 1]), two(wa[2 * j], wa[2 * j + 1]));
-      wh[P + j] = mul2f(two(hb[2 * j], hb[2 * j + 1]), two(wb[2 * j], wb[2 * j + 1]));
-      ss2 = fma2f(f0, f0, fma2f(f1, f1, ss2));
-      dot2 = fma2f(wh[j], f0, fma2f(wh[P + j], f1, dot2));
+      const uint64_t f0 = pack2(fa[2 * j], fa[2 * j + 1]), f1 = pack2(fb[2 * j], fb[2 * j + 1]);
+      wh[j] = mul2(pack2(ha[2 * j], ha[2 * j + 1]), pack2(wa[2 * j], wa[2 * j + 1]));
+      wh[P + j] = mul2(pack2(hb[2 * j], hb[2 * j + 1]), pack2(wb[2 * j], wb[2 * j + 1]));
+      ss2 = fma2(f0, f0, fma2(f1, f1, ss2));
+      dot2 = fma2(wh[j], f0, fma2(wh[P + j], f1, dot2));
     }
     float s0, s1, d0, d1;
-    one(ss2, s0, s1);
-    one(dot2, d0, d1);
+    unpack2(ss2, s0, s1);
+    unpack2(dot2, d0, d1);
     const float ss = row_sum(s0 + s1, a.lanes), dot = row_sum(d0 + d1, a.lanes);
     const float rr = there ? rsqrtf(ss * a.inv_d + a.eps) : 0.f;  // (of zeros that are no row it may be infinite)
-    const uint64_t rr2 = two(rr, rr), back2 = two(-dot * rr * rr * a.inv_d, -dot * rr * rr * a.inv_d);
+    const uint64_t rr2 = pack2(rr, rr), back2 = pack2(-dot * rr * rr * a.inv_d, -dot * rr * rr * a.inv_d);
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const uint64_t t0 = mul2f(two(fa[2 * j], fa[2 * j + 1]), rr2), t1 = mul2f(two(fb[2 * j], fb[2 * j + 1]), rr2);
-      da[j] = fma2f(two(ha[2 * j], ha[2 * j + 1]), t0, da[j]);
-      db[j] = fma2f(two(hb[2 * j], hb[2 * j + 1]), t1, db[j]);
-      one(fma2f(t0, back2, mul2f(wh[j], rr2)), fa[2 * j], fa[2 * j + 1]);
-      one(fma2f(t1, back2, mul2f(wh[P + j], rr2)), fb[2 * j], fb[2 * j + 1]);
+      const uint64_t t0 = mul2(pack2(fa[2 * j], fa[2 * j + 1]), rr2), t1 = mul2(pack2(fb[2 * j], fb[2 * j + 1]), rr2);
+      da[j] = fma2(pack2(ha[2 * j], ha[2 * j + 1]), t0, da[j]);
+      db[j] = fma2(pack2(hb[2 * j], hb[2 * j + 1]), t1, db[j]);
+      unpack2(fma2(t0, back2, mul2(wh[j], rr2)), fa[2 * j], fa[2 * j + 1]);
+      unpack2(fma2(t1, back2, mul2(wh[P + j], rr2)), fb[2 * j], fb[2 * j + 1]);
     }
     if (there && pl.on) {
       *reinterpret_cast<uint4*>(out) = narrow<T>(fa);
@@ -502,9 +484,9 @@ __global__ void __launch_bounds__(kHeadThreads, kBwdCtas) head_bwd_kernel(const 
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     float u, v, lo, hi;
-    one(da[j / 2], lo, hi);
+    unpack2(da[j / 2], lo, hi);
     u = j & 1 ? hi : lo;
-    one(db[j / 2], lo, hi);
+    unpack2(db[j / 2], lo, hi);
     v = j & 1 ? hi : lo;
     for (int o = a.lanes; o < 32; o <<= 1) {
       u += __shfl_xor_sync(0xffffffffu, u, o);
@@ -575,8 +557,7 @@ HeadArgs base_args(const mosaic_rotary_params* p, const int64_t* pos, int64_t po
   return a;
 }
 
-// Few tokens: a token's rows go to several warps, until there are sixteen warps an SM or a warp has one round of rows.  (`most`: warps
-// that a token's rows keep busy.)  Then the grid: as many CTAs as there are tasks, or, one task a token, `ctas` at the most.
+// The grid: as many CTAs as there are tasks, or, one task a token, `ctas` at the most.
 int spread(HeadArgs* a, long long ctas) {
   a->tasks = a->tokens * a->parts;
   long long blocks = ((long long)a->tasks + kHeadWarps - 1) / kHeadWarps;
@@ -587,6 +568,7 @@ int spread(HeadArgs* a, long long ctas) {
   return (int)blocks;
 }
 
+// Few tokens: a token's `rows` rows go to several warps, until there are sixteen warps an SM or a warp has one round of rows.
 int plan(HeadArgs* a, int rows, int sms, long long ctas) {
   a->parts = 1;
   while ((long long)a->tokens * a->parts < 16ll * sms && a->parts * (32 / a->lanes) < rows) a->parts *= 2;
