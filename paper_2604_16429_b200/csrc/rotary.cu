@@ -6,7 +6,8 @@
 // HBM-bound: every element is read once (x and dy in the backward) and written once.  A warp has one token and walks its
 // heads; a row of d channels is spread over P lanes (the power of two that holds d / 2V), each with two 16-byte pieces of V
 // channels: with half pairs the two pieces hold the pairs' two sides, otherwise one lies in the first half of the head and one in the
-// second, at the same place (half a head apart).  So a pair never leaves its lane, a row's sums are shuffles among P lanes, and 32 / P rows go through a warp at a time, a few fetched ahead.
+// second, half a head apart.  So a pair never leaves its lane, a row's sums are shuffles among P lanes, and 32 / P rows go through a warp
+// at a time, a few fetched ahead.
 // The token's rot_dim/2 angles are the same for all its heads: the warp's lanes share them out, take the product with the
 // position in half turns and its remainder in fp64 (an angle of 1e6 radians has 2^-33 of error there, 2^-4 in fp32), and leave
 // (cos, sin) in shared memory, from where every lane reads the V that it needs for each row.
@@ -350,13 +351,11 @@ __global__ void __launch_bounds__(kHeadThreads, kCtas) head_kernel(const __grid_
       turn_part<T, HALF>(va, vb, angles[warp], a, pl);
     } else {
       turn<V, HALF, PART>(fa, fb, angles[warp], a, pl);
-      va = narrow<T>(fa);
-      vb = narrow<T>(fb);
     }
     if (there && pl.on) {
       char* y = h < heads ? yq + h * a.t[0].y.sh : yk + h * a.t[1].y.sh;
-      *reinterpret_cast<uint4*>(y) = va;
-      *reinterpret_cast<uint4*>(y + ba) = vb;
+      *reinterpret_cast<uint4*>(y) = PART && !NORM ? va : narrow<T>(fa);
+      *reinterpret_cast<uint4*>(y + ba) = PART && !NORM ? vb : narrow<T>(fb);
     }
   }
 }
