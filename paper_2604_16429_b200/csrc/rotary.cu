@@ -144,16 +144,15 @@ __device__ __forceinline__ void read_floats(const float* p, float* out) {
   }
 }
 
-// Whether pair j of the lane's two pieces turns
-template <int V, bool HALF>
-__device__ __forceinline__ bool turns(const HeadArgs& args, const Place& pl, int j) {
-  return HALF ? pl.ca < args.rot / 2 : (j < V / 2 ? pl.ca : pl.cb - V) + 2 * j < args.rot;
+// Turns the pairs of a row's two pieces.  (The angles are read anew for every row: kept over a token's rows they cost sixteen registers,
+// which are worth a second CTA on the SM.)
+__device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) {
+  const float u = x * c - y * s;
+  y = x * s + y * c;
+  x = u;
 }
-// Turns the pairs of a row's two pieces.  PART: some channels do not turn; they stay as they are, whatever they hold (a product with
-// (1, 0) makes no number of an infinite one's partner).  (The angles are read anew for every row: kept over a token's rows they cost
-// sixteen registers, which are worth a second CTA on the SM.)
-template <int V, bool HALF, bool PART>
-__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const HeadArgs& args, const Place& pl) {
+template <int V, bool HALF>
+__device__ __forceinline__ void turn_all(float (&a)[V], float (&b)[V], const Angles& t, const HeadArgs& args, const Place& pl) {
   constexpr int N = HALF ? V : V / 2;  // pairs of one piece that lie side by side
   float c[V], s[V];
   const int i0 = HALF ? min(pl.ca, args.rot / 2) : pl.ca / 2;
@@ -165,50 +164,80 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles&
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    float& x = HALF ? a[j] : j < V / 2 ? a[2 * j] : b[2 * j - V];
-    float& y = HALF ? b[j] : j < V / 2 ? a[2 * j + 1] : b[2 * j - V + 1];
-    const float u = x * c[j] - y * s[j], v = x * s[j] + y * c[j];
-    if (!PART || turns<V, HALF>(args, pl, j)) {
-      x = u;
-      y = v;
+    if constexpr (HALF) turn_pair(a[j], b[j], c[j], s[j]);
+    else if (j < N) turn_pair(a[2 * j], a[2 * j + 1], c[j], s[j]);
+    else turn_pair(b[2 * j - V], b[2 * j - V + 1], c[j], s[j]);
+  }
+}
+// Neighbouring pairs of one piece, from channel `first` on
+template <int V>
+__device__ __forceinline__ void turn_piece(float (&f)[V], int first, const Angles& t) {
+  float c[V / 2], s[V / 2];
+  read_floats<V / 2>(t.cosine + first / 2, c);
+  read_floats<V / 2>(t.sine + first / 2, s);
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) turn_pair(f[2 * j], f[2 * j + 1], c[j], s[j]);
+}
+
+// PART: some channels do not turn and stay as they are, whatever they hold.  (As pairs multiplied with (1, 0) an infinite one would
+// make no number of its partner.)  With half pairs a lane's pairs turn, all of them, or none does; otherwise the border lies among the
+// second pieces, or among the first and no second one turns.
+template <int V, bool HALF, bool PART>
+__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const HeadArgs& args, const Place& pl) {
+  if constexpr (!PART) {
+    turn_all<V, HALF>(a, b, t, args, pl);
+  } else if constexpr (HALF) {
+    if (pl.ca < args.rot / 2) turn_all<V, true>(a, b, t, args, pl);
+  } else {
+    auto border = [&](float (&f)[V], int first) {
+      float g[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) g[j] = f[j];
+      turn_piece<V>(g, first, t);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = first + j < args.rot ? g[j] : f[j];
+    };
+    if (args.rot > args.d / 2) {
+      turn_piece<V>(a, pl.ca, t);
+      border(b, pl.cb);
+    } else {
+      border(a, pl.ca);
     }
   }
 }
-// Turns what turns of a row's two pieces as they lie in memory; the rest keeps its bits (narrowing would change those of what is no
-// number), and a piece without a turning pair is not looked at.
+// The same on the two pieces as they lie in memory: what does not turn keeps its bits (narrowing would change those of what is no number).
 template <int T, bool HALF>
 __device__ __forceinline__ void turn_part(uint4& va, uint4& vb, const Angles& t, const HeadArgs& args, const Place& pl) {
-  constexpr int V = Vec<T>::n, N = V / 2;
+  constexpr int V = Vec<T>::n;
   if constexpr (HALF) {
     if (pl.ca >= args.rot / 2) return;
     float a[V], b[V];
     widen<T>(va, a);
     widen<T>(vb, b);
-    turn<V, true, false>(a, b, t, args, pl);
+    turn_all<V, true>(a, b, t, args, pl);
     va = narrow<T>(a);
     vb = narrow<T>(b);
   } else {
-    auto piece = [&](uint4& v, int first) {
-      if (first >= args.rot) return;
-      float f[V], c[N], s[N];
+    auto turned = [&](const uint4& v, int first) {
+      float f[V];
       widen<T>(v, f);
-      read_floats<N>(t.cosine + first / 2, c);
-      read_floats<N>(t.sine + first / 2, s);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float x = f[2 * j], y = f[2 * j + 1];
-        f[2 * j] = x * c[j] - y * s[j];
-        f[2 * j + 1] = x * s[j] + y * c[j];
-      }
-      const uint4 u = narrow<T>(f);
-      const int words = (args.rot - first) * Vec<T>::bytes / 4;  // that turn
-      v.x = u.x;  // (a pair is one word or two)
-      if (T == kF32 || words > 1) v.y = u.y;
-      if (words > 2) v.z = u.z;
-      if (words > (T == kF32 ? 2 : 3)) v.w = u.w;
+      turn_piece<V>(f, first, t);
+      return narrow<T>(f);
     };
-    piece(va, pl.ca);
-    piece(vb, pl.cb);
+    auto border = [&](uint4& v, int first) {
+      const uint4 u = turned(v, first);
+      const int words = (args.rot - first) * Vec<T>::bytes / 4;  // that turn (a pair is one word or two)
+      if (words > 0) v.x = u.x;
+      if (words > 1) v.y = u.y;
+      if (words > 2) v.z = u.z;
+      if (words > 3) v.w = u.w;
+    };
+    if (args.rot > args.d / 2) {
+      va = turned(va, pl.ca);
+      border(vb, pl.cb);
+    } else {
+      border(va, pl.ca);
+    }
   }
 }
 

@@ -5,10 +5,10 @@
 //
 // A tile is 128 query rows of one head.  The tiles of a key/value head are numbered with the heads of its group fastest, and a
 // CTA takes two neighbours: heads of a group read the same keys, so a staged key tile serves 256 rows.  The two tiles walk a
-// common sequence of steps of at most 64 keys: the sinks (as many columns as there are, rounded up to 32) unless the window
-// still holds them, then the union of the two windows; a step that a tile sees nothing of it leaves out.  All steps of a batch
-// member are cells of one grid of 64 keys, so that what a step holds of a row's keys, and with it the bits of the row's results, does
-// not depend on the tile beside it.  Only steps at the window's edges are masked element by element.
+// common sequence of steps of at most 64 keys: the sinks (as many columns as there are, rounded up to 32), then what else there is in
+// the union of the two windows; a step that a tile sees nothing of it leaves out.  The windows' steps of a batch member are cells of
+// one grid, so that what a step holds of a row's keys, and with it the bits of the row's results, does not depend on the tile beside
+// it.  Only steps at the window's edges are masked element by element.
 //
 // Warps (384 threads, persistent, one CTA per SM): 0-3 and 4-7 softmax of tile 0 and 1 (thread = row = TMEM lane), 8 TMA, 9 and 10
 // the products of tile 0 and 1.  TMEM (512 columns): two score buffers of a tile at 128 t + 64 b (fp32), P over a buffer's first
@@ -63,9 +63,8 @@ struct Item {
   int kl, off, ql;
   int row0[2], head[2], tiles;  // tiles: how many of the two there are
   int lo[2], hi[2];  // keys of the tile's window (sinks aside); hi <= 0: nothing to compute
-  int base, end;     // union of the windows, from the cell on that holds its first key (cells start U apart; the first may be negative)
-  int sinks, ns;     // all sinks; those in front of base, which have steps of their own (the others lie in the first of the union)
-  int cell0;         // start of the cell that holds key 0, -U < cell0 <= 0
+  int base, end;     // union of the windows behind the sinks, from the start of its first cell on (which may be less than 0)
+  int sinks, ns;     // sinks (none where every window holds them); those that there are
   int front, steps;  // steps of the sinks, of all
   // UNIFORM: by a whole warp, all of it uniform
   template <bool UNIFORM = false>
@@ -83,6 +82,7 @@ struct Item {
     kl = s.kl; off = s.off; ql = s.ql;
     base = 0x7fffffff;
     end = 0;
+    sinks = kl > g.window ? g.sinks : 0;
     tiles = min(2, g.G * ((g.Nq + kRows - 1) / kRows) - 2 * pair);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -93,20 +93,20 @@ struct Item {
       hi[t] = last >= row0[t] && t < tiles ? off + last + 1 : 0;
       lo[t] = max(0, off + row0[t] - g.window + 1);
       if (hi[t] > 0) {
-        base = min(base, lo[t]);
+        base = min(base, max(lo[t], sinks));
         end = max(end, hi[t]);
       }
     }
-    // A tile's window is window + 127 keys from a key that is `from` modulo U on.  Cells at multiples of U cover it with as many steps
-    // as cells from its first key on if its last one has `from` keys to spare (in a whole sequence it has); if not, cells start at the
-    // tiles' first keys (a chunk of 1021 rows with window 509: 30.6 us, with multiples of U 33.2).
-    const int from = (off + 1 - g.window) & (U - 1), spare = (1 - g.window) & (U - 1);
-    cell0 = kl > g.window && from > spare ? from - U : 0;
-    base -= (base - cell0) & (U - 1);
-    sinks = g.sinks;
-    ns = end > 0 ? max(min(sinks, base), 0) : 0;
-    front = ns > 0 ? (ns - cell0 + U - 1) / U : 0;
-    steps = end > 0 ? front + (end - base + U - 1) / U : 0;
+    // A full tile's window is window + rows - 1 keys from a key that is `from` modulo U on, and leaves `spare` columns of its last step.
+    // Cells at multiples of U cover it with as many steps unless it starts more than that behind one; then, and where more than half of
+    // the last step would be left, cells start at the tiles' first keys.  (us with multiples and with first keys, 4 heads a key head:
+    // 8192 tokens of 16 heads of 128, window 1024, 94.8 and 95.8; 2 x 8192 tokens of 12 heads of 64, window 100, 49.3 and 50.0; 4 x 4096
+    // of 16 of 64, window 16, 48.7 and 47.2; chunks of 4 x 1000 rows, 12 heads of 64, window 1000, 50.3 and 48.0.)
+    const int from = (off + 1 - g.window) & (U - 1), spare = (1 - g.window - min(ql, kRows)) & (U - 1);
+    base -= (base - (kl > g.window && (from > spare || spare >= U / 2) ? from : 0)) & (U - 1);
+    ns = min(sinks, end);
+    front = (ns + U - 1) / U;
+    steps = front + (end > sinks ? (end - base + U - 1) / U : 0);
   }
   // (selections, so that an item stays in registers)
   __device__ __forceinline__ int lo_of(int t) const { return t ? lo[1] : lo[0]; }
@@ -115,13 +115,14 @@ struct Item {
   __device__ __forceinline__ int head_of(int t) const { return t ? head[1] : head[0]; }
   // keys start .. start + cols - 1 of step n
   __device__ __forceinline__ void step(int n, int& start, int& cols) const {
-    const int cell = n < front ? cell0 + n * U : base + (n - front) * U;
-    start = max(cell, 0);
-    cols = min(cell + U, n < front ? ns : end) - start;
+    start = n < front ? n * U : base + (n - front) * U;
+    cols = min(U, (n < front ? ns : end) - start);
   }
   // The steps that tile t takes part in: the sinks' in front, and those from first_of(t) to last_of(t)
-  __device__ __forceinline__ int first_of(int t) const { return front + (base < sinks ? 0 : (lo_of(t) - base) / U); }
-  __device__ __forceinline__ int last_of(int t) const { return hi_of(t) > 0 ? front + (hi_of(t) - 1 - base) / U : -1; }
+  __device__ __forceinline__ int first_of(int t) const { return front + (max(lo_of(t), sinks) - base) / U; }
+  __device__ __forceinline__ int last_of(int t) const {
+    return hi_of(t) > sinks ? front + (hi_of(t) - 1 - base) / U : hi_of(t) > 0 ? front - 1 : -1;
+  }
 };
 
 // All steps of a CTA's items, one after the other
@@ -346,12 +347,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       it.make(g, per, index);
       const int i = it.row0_of(t) + row, p0 = it.off + it.row0_of(t), p = p0 + row;
       // every row of the tile sees all of a step's U keys if it starts at one of whole0 .. whole1
-      const int whole0 = p0 + kRows - g.window, whole1 = p0 + 1 - U;
+      const int whole0 = max(p0 + kRows - g.window, it.sinks), whole1 = p0 + 1 - U;
+      const int window = max(p + 1 - g.window, it.sinks);  // the row's first key behind the sinks
       float m_ref = -INFINITY, l = 0.f;
       const int last = it.last_of(t), first = it.first_of(t);
-      const int front = it.front, steps = last < 0 ? 0 : front + last + 1 - first, window0 = it.base + (first - 2 * front) * U;  // cell of step n: window0 + n U
+      const int front = it.front, steps = last < 0 ? 0 : front + max(last + 1 - first, 0), window0 = it.base + (first - 2 * front) * U;
       for (int n = 0; n < steps; ++n) {
-        const int cell = (n < front ? it.cell0 : window0) + n * U, start = max(cell, 0), cols = min(cell + U, n < front ? it.ns : it.end) - start;
+        const int start = n < front ? n * U : window0 + n * U, cols = min(U, (n < front ? it.ns : it.end) - start);
         const uint32_t b = u % 2, ts = mine + score_col(t, b);
         ok = warp_wait_here(s32(&sm.s_full[t][b]), (u / 2) & 1, abort, status);
         if (!ok) break;
@@ -407,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // What the row does not see becomes -inf.  On an edge most groups of 32 keys are seen by all rows of the warp.
         auto mask = [&](int c, uint32_t (&sc)[32]) {
           const int at = start + 32 * c;
-          const uint32_t see = low_bits(min(p + 1 - at, cols - 32 * c)) & (~low_bits(p + 1 - g.window - at) | low_bits(g.sinks - at));
+          const uint32_t see = low_bits(min(p + 1 - at, cols - 32 * c)) & ~low_bits((n < front ? 0 : window) - at);
           if (__all_sync(0xffffffffu, see == 0xffffffffu)) return;
 #pragma unroll
           for (int x = 0; x < 32; ++x) sc[x] = (see >> x) & 1u ? sc[x] : 0xff800000u;
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld32(ts, s0);
           tmem_ld32(ts + 32, s1);
           tmem_wait_ld();
-          if (start < whole0 || start > whole1 || cols < U) {
+          if (start < whole0 || start > whole1) {
             mask(0, s0);
             mask(1, s1);
           }
