@@ -99,7 +99,7 @@ struct Item {
     }
     // A full tile's window is window + rows - 1 keys from a key that is `from` modulo U on, and leaves `spare` columns of its last step.
     // Cells at multiples of U cover it with as many steps unless it starts more than that behind one; then, and where more than half of
-    // the last step would be left, cells start at the tiles' first keys.  (us with multiples and with first keys, 4 heads a key head:
+    // the last step would be left, cells start at the tiles' first keys.  (us with multiples and with first keys, on 4 key heads:
     // 8192 tokens of 16 heads of 128, window 1024, 94.8 and 95.8; 2 x 8192 tokens of 12 heads of 64, window 100, 49.3 and 50.0; 4 x 4096
     // of 16 of 64, window 16, 48.7 and 47.2; chunks of 4 x 1000 rows, 12 heads of 64, window 1000, 50.3 and 48.0.)
     const int from = (off + 1 - g.window) & (U - 1), spare = (1 - g.window - min(ql, kRows)) & (U - 1);

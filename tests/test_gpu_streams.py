@@ -125,6 +125,33 @@ def check_results_last_as_long_as_the_caller_needs_them(call):
     assert all(torch.equal(a, b) for a, b in zip(want, kept)) and len(others) == 3 * len(kept)
 
 
+def check_captured_on_a_forked_stream(call):
+    """A capture that forks to the named stream and joins it: what the call makes lives in the graph's memory."""
+    want = call()
+    want = [t.clone() for t in ((want,) if torch.is_tensor(want) else want)]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    call(stream=side)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = call(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    out = (out,) if torch.is_tensor(out) else out
+    others = [torch.full_like(t, 5) for t in want for _ in range(3)]
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out))
+        for t in out:
+            t.zero_()
+    assert all((t == 5).all() for t in others)
+
+
+@pytest.mark.parametrize("name", SEQUENCE)
+def test_sequence_operators_captured_on_a_forked_stream(name):
+    check_captured_on_a_forked_stream(sequence_calls()[name])
+
+
 @pytest.mark.parametrize("name", SEQUENCE)
 def test_sequence_operators_take_the_memory_of_their_stream(name):
     check_memory_of_the_stream(sequence_calls()[name])
@@ -153,3 +180,8 @@ def test_block_sparse_calls_leave_queued_work_alone(name):
 @pytest.mark.parametrize("name", BLOCK)
 def test_results_of_block_sparse_calls_last(name):
     check_results_last_as_long_as_the_caller_needs_them(block_calls()[name])
+
+
+@pytest.mark.parametrize("name", BLOCK)
+def test_block_sparse_calls_captured_on_a_forked_stream(name):
+    check_captured_on_a_forked_stream(block_calls()[name])
