@@ -406,14 +406,20 @@ _window_pack = {n: struct.Struct("=8ifI%dq" % (4 * n)).pack_into for n in (0, 4,
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _pack(layout, *values):
-    """Writes a call's parameters and views into the thread's buffer; its address."""
-    block = _block
+_RANGE = (struct.error, OverflowError)
+
+
+def _out_of_range(e):
+    return ValueError(f"a parameter is out of range: {e}")
+
+
+def _params_block(layout, p):
+    """Address of a parameter block alone."""
     try:
-        layout(block.buf, 0, *values)
-    except (struct.error, OverflowError) as e:
-        raise ValueError(f"a parameter is out of range: {e}") from None
-    return block.at
+        layout(_block.buf, 0, *p)
+    except _RANGE as e:
+        raise _out_of_range(e) from None
+    return _block.at
 
 
 def _bad(name, t, what):
@@ -521,7 +527,12 @@ def mosaic_bsa_rotary(rp: RotaryParams, q, k, pos, freqs, inverse=False, q_out=N
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _like(q, stream) if q_out is None else q_out
     k_out = _like(k, stream) if k_out is None else k_out
-    a = _pack(_rotary_pack[4], *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    block = _block
+    a = block.at
+    try:
+        _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     _call("mosaic_bsa_rotary", index, stream, a, a + 40, a + 72, at, step, fr, a + 104, a + 136)
     return q_out, k_out
 
@@ -535,14 +546,19 @@ def mosaic_bsa_qk_norm(rp: RotaryParams, q, k, wq, wk, pos=None, freqs=None, eps
     at, step, fr = _positions(rp, pos, freqs, sq, index)
     q_out = _like(q, stream) if q_out is None else q_out
     k_out = _like(k, stream) if k_out is None else k_out
-    a = _pack(_rotary_pack[4], *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    block = _block
+    a = block.at
+    try:
+        _rotary_pack[4](block.buf, 0, *p, *vq, *vk, *_out("q_out", q_out, sq, t, index), *_out("k_out", k_out, sk, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     _call("mosaic_bsa_qk_norm", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index), at,
           step, fr, a + 104, a + 136)
     return q_out, k_out
 
 
 def qk_norm_workspace_bytes(rp: RotaryParams, q, k) -> int:
-    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_pack(_rotary_pack[0], *_rotary_params(rp, q, k, 0, 0.0)[1])))
+    return int(lib().mosaic_bsa_qk_norm_workspace_bytes(_params_block(_rotary_pack[0], _rotary_params(rp, q, k, 0, 0.0)[1])))
 
 
 def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, d_k_out, eps=1e-6, dq=None, dk=None, dwq=None,
@@ -558,7 +574,12 @@ def mosaic_bsa_qk_norm_bwd(rp: RotaryParams, q, k, wq, wk, pos, freqs, d_q_out, 
     dk = _like(k, stream) if dk is None else dk
     dwq = _floats(rp.d, index, stream) if dwq is None else dwq
     dwk = _floats(rp.d, index, stream) if dwk is None else dwk
-    a = _pack(_rotary_pack[6], *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
+    block = _block
+    a = block.at
+    try:
+        _rotary_pack[6](block.buf, 0, *p, *vq, *vk, *gq, *gk, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     name = "mosaic_bsa_qk_norm_workspace_bytes"
     ws = _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(a)), name, index, ws, stream)
     _call("mosaic_bsa_qk_norm_bwd", index, stream, a, a + 40, a + 72, _flat("wq", wq, w, f32, index), _flat("wk", wk, w, f32, index),
@@ -589,7 +610,7 @@ def _window_params(wp, q, k):
 
 
 def window_workspace_bytes(wp: WindowParams, q, k, op: int) -> int:
-    return int(lib().mosaic_bsa_window_workspace_bytes(_pack(_window_pack[0], *_window_params(wp, q, k)[1]), op))
+    return int(lib().mosaic_bsa_window_workspace_bytes(_params_block(_window_pack[0], _window_params(wp, q, k)[1]), op))
 
 
 def _window_ws(at, op, index, ws, stream):
@@ -617,7 +638,12 @@ def mosaic_bsa_window_fwd(wp: WindowParams, q, k, v, q_len=None, k_len=None, o=N
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _like(q, stream) if o is None else o
     lse = _rows_like(q, stream) if lse is None else lse
-    a = _pack(_window_pack[4], *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    block = _block
+    a = block.at
+    try:
+        _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     ws = _window_ws(a, OP_FWD, index, ws, stream)
     _call("mosaic_bsa_window_fwd", index, stream, a, a + 40, a + 72, a + 104, _len("q_len", q_len, sq[0], index),
           _len("k_len", k_len, sq[0], index), a + 136, _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
@@ -635,8 +661,13 @@ def mosaic_bsa_window_bwd(wp: WindowParams, q, k, v, o, lse, d_o, q_len=None, k_
     dq = _like(q, stream) if dq is None else dq
     dk = _like(k, stream) if dk is None else dk
     dv = _like(v, stream) if dv is None else dv
-    a = _pack(_window_pack[8], *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
-              *_out("dv", dv, sk, t, index))
+    block = _block
+    a = block.at
+    try:
+        _window_pack[8](block.buf, 0, *p, *vq, *vk, *vv, *vo, *vd, *_out("dq", dq, sq, t, index), *_out("dk", dk, sk, t, index),
+                        *_out("dv", dv, sk, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     ws = _window_ws(a, OP_BWD, index, ws, stream)
     _call("mosaic_bsa_window_bwd", index, stream, a, a + 40, a + 72, a + 104, a + 136, _flat("lse", lse, sq[:3], torch.float32, index),
           a + 168, _len("q_len", q_len, sq[0], index), _len("k_len", k_len, sq[0], index), a + 200, a + 232, a + 264, ws.data_ptr(),
@@ -653,7 +684,12 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     vq, vk, vv = _view("q", q, sq, t, index), _view("k", k, sk, t, index), _view("v", v, sk, t, index)
     o = _like(q, stream) if o is None else o
     lse = _rows_like(q, stream) if lse is None else lse
-    a = _pack(_window_pack[4], *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    block = _block
+    a = block.at
+    try:
+        _window_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
     _call("mosaic_bsa_window_decode", index, stream, a, a + 40, a + 72, a + 104, _len("k_len", k_len, sq[0], index), a + 136,
           _flat("lse", lse, sq[:3], torch.float32, index))
     return o, lse
