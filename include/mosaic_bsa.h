@@ -257,7 +257,9 @@ typedef struct mosaic_view {
  *   rotation   channels c < rot_dim of a row turn in rot_dim/2 pairs; pair i of the token at position p by the angle
  *              p * freqs[i]: (x, y) -> amplitude * (x cos - y sin, x sin + y cos); channels from rot_dim on pass through
  *   norm       y_c = x_c * w_c / sqrt(mean(x^2) + eps) over the d channels of a row, before the rotation
- * Angles are taken and reduced in fp64, cosines, sums and products in fp32, one rounding to the storage type at the end.
+ * Angles are taken and reduced in fp64, cosines, sines, sums and products in fp32 (squares too: a row's sum of them has to stay
+ * below 3.4e38), one rounding to the storage type at the end.  The rotation alone leaves the channels that do not turn bit for bit as
+ * they are; in no call does what one of them holds reach another channel by way of the rotation.
  * Any position whose angle fp64 holds; negative ones too.
  */
 typedef struct mosaic_rotary_params {
@@ -272,12 +274,14 @@ typedef struct mosaic_rotary_params {
 
 /* Frequencies of the turned pairs, radians per position, on the HOST (a program makes them once and copies them over):
  * kind MOSAIC_ROTARY_PLAIN   f_i = theta^(-2i/rot_dim)
- *      MOSAIC_ROTARY_LINEAR  f_i / factor (positions interpolated)
+ *      MOSAIC_ROTARY_LINEAR  f_i / factor (position interpolation)
  *      MOSAIC_ROTARY_BASE    theta * factor^(rot_dim/(rot_dim-2)) in theta's place: the slowest pair is slowed by the factor
+ *                            ("NTK-aware" scaling)
  *      MOSAIC_ROTARY_PARTS   f_i (1 - t) + f_i/factor t, t a ramp over the pair index from the pair that turns `fast` times
- *                            in `length` positions (rounded down) to the one that turns `slow` times (rounded up)
+ *                            in `length` positions (rounded down) to the one that turns `slow` times (rounded up);
+ *                            YaRN's interpolation by parts, whose scaling of the scores is the caller's to put into `amplitude`
  *      MOSAIC_ROTARY_BANDS   f_i t + f_i/factor (1 - t), t a ramp over the number of turns in `length` positions, 0 at
- *                            `slow` and 1 at `fast`
+ *                            `slow` and 1 at `fast` (scaling by bands of wavelengths)
  * Returns MOSAIC_E_INVALID_ARG where a number is out of its range (rot_dim odd or < 2, theta <= 1, factor < 1; for the
  * last two kinds length <= 0 or not 0 < slow < fast). */
 enum { MOSAIC_ROTARY_PLAIN = 0, MOSAIC_ROTARY_LINEAR = 1, MOSAIC_ROTARY_BASE = 2, MOSAIC_ROTARY_PARTS = 3,
@@ -323,6 +327,8 @@ int mosaic_bsa_qk_norm_bwd(const mosaic_rotary_params *p, const mosaic_view *q, 
  *               k_len is a whole sequence and q_len < k_len a chunk behind what a cache holds.  Lengths outside
  *               [0, Nq], [0, Nk] are clamped to it.
  *   A row that sees nothing (k_len 0, or more queries than keys) gives o = 0, lse = -inf and no gradient.
+ *   Scores, softmax statistics and sums are fp32.  Weights (forward, decode, backward) and dS (backward) are rounded to the 16-bit type
+ *   once, as operands of the tensor core; over the sinks' keys the backward adds what that rounding left off.
  *   Rows of o, lse, dq from q_len[b] on and of dk, dv from k_len[b] on are left as they were, and what q, k, v, o, lse, d_o
  *   hold there is never used.  Rows below are expected finite: a value that is not spreads to the rows that see it, and may
  *   spread to rows near them that do not.

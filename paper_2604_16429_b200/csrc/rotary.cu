@@ -13,9 +13,10 @@
 // (cos, sin) in shared memory, from where every lane reads the V that it needs for each row.
 //
 // Measured (us on the device, beside the bytes at 6543 GB/s): rotation of [2, 16 + 4 heads, 8192, 128] fp16 with 32 channels turning
-// 30.5 (25.7); norm and rotation of [1, 16 + 16, 12288, 64] bf16 22.3 (15.4); its backward for [2, 16 + 4, 8192, 128] bf16 60.7 (38.5).
-// The forward is bound by HBM and a start and end of 5 us (batches of 1 KB a warp, two ahead), the norms besides by
-// instructions, the backward by instructions (four streams of rows, two row sums, three products an element) as much as by HBM.
+// 30.6 (25.7); norm and rotation of [1, 16 + 16, 12288, 64] bf16 22.3 (15.4); its backward for [2, 16 + 4, 8192, 128] bf16 60.8 (38.5).
+// The rotation is bound by HBM and a start and end of 5 us (batches of 1 KB a warp, two ahead).  The norms and their backward are at
+// no limit: counters of 2 x 8192 tokens of 16 + 4 heads of 128, caches cold, show 59 and 52 % of the issue slots and 37 and 42 % of the
+// DRAM's rate used, with 24 and 16 warps an SM; what is left is latency, of copies, row sums (shuffles one after the other) and stores.
 // Chosen by measurement, those three in order: CTAs an SM of the forward 3 (2: 31.2, 23.7; 4: 31.2, 23.1; 6: 38.6, 35.8), batches ahead
 // 2 (1: 31.2, 24.2; 3: 31.8, 24.2); CTAs an SM of the backward 2 (1: 80.2; 3: 103), batches ahead 1 (2: 61.8; 3: 64.3; held in
 // registers instead of shared memory: 84).

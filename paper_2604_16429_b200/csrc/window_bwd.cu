@@ -18,7 +18,8 @@
 // Rounded to 16 bits: P and dS as operands (the tensor core takes no wider ones; it makes the gradients' error 1.4 times that of
 // results rounded once), the results.  Items with the sinks' keys add what those roundings left off in a second product, so that the
 // few largest gradients, sums over all rows, are as exact as results rounded once (error over the sinks' keys 0.0023 -> 0.0017 of their
-// size in bf16; 4 % of a training pass of 49152 tokens with window 2048, 7 % of 4096 with window 1024).  Every wait is bounded.
+// size in bf16; 4 % of a training pass of 49152 tokens with window 2048, 7 % of 4096 with window 1024, in which is what the operands'
+// registers cost: the key-stationary kernel of d = 64 spills 84 bytes a thread in bf16 instead of 28).  Every wait is bounded.
 //
 // Bound by the way round a chunk's buffer (products, row threads, sums, and their hand-offs) and by the issuing warps: a chunk takes
 // about 900 cycles at d = 64 where MUFU needs 512 and the tensor core 540 (query-stationary) or 680, and of that an issuing warp's

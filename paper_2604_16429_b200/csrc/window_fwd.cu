@@ -19,7 +19,8 @@
 //
 // Bound by the softmax warps and the way round (scores, softmax, P V, the buffer's next scores): a step of 64 keys for both tiles
 // takes 1760 cycles at d = 64 and 1970 at d = 128, of which MUFU is busy 1024 (two warps a scheduler), the tensor core 680 and 1310.
-// Measured for 8192 tokens, 16 heads of 128 on 4, window 1024 (us): this form 95; the issuing warps finding a step's slots and limits
+// Measured for 8192 tokens, 16 heads of 128 on 4, window 1024 (us): 96, and, before the first rows too had the sinks in a step of their
+// own, 95; beside that: the issuing warps finding a step's slots and limits
 // anew each time 99; P in columns of its own beside one score buffer, so that no product has to end before the next scores, 101;
 // the two tiles taking turns at the exponentials 96 (at d = 64: 6 % slower).  Beside a form of 91 that left out the wait for the
 // buffer's earlier product: one warp for both tiles' products 111, 128 keys a step 102, a quarter or an eighth of the exponentials
