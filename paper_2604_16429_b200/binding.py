@@ -207,10 +207,15 @@ def _on(stream, make, *args, **kw):
 
 def _new(stream, make, *args, **kw):
     """The same for a tensor that the call returns: once freed, not handed out again before the caller's stream has passed that."""
+    if stream is None:
+        return make(*args, **kw)
     t = _on(stream, make, *args, **kw)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream(t.device))
+    t.record_stream(torch.cuda.current_stream(t.device))
     return t
+
+
+def _like(t, stream):
+    return torch.empty_like(t) if stream is None else _new(stream, torch.empty_like, t)
 
 
 def mosaic_bsa_select(p: Params, q, k, block_idx=None, ws=None, stream=None):
@@ -246,7 +251,7 @@ def mosaic_bsa_fwd(p: Params, q, k, v, block_idx, o=None, lse=None, ws=None, str
     _chk_qkv(p, q)
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if o is None:
-        o = _new(stream, torch.empty_like, q)
+        o = _like(q, stream)
     if lse is None:
         lse = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device)
     if ws is None:
@@ -266,7 +271,7 @@ def mosaic_bsa_fwd_branches(p: Params, q, k, v, block_idx, gates, o=None, lse_fg
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if gates.dtype != torch.float32 or not gates.is_contiguous() or tuple(gates.shape) != (p.B, p.H, p.N, 3):
         raise ValueError(f"expected contiguous cuda fp32 gates [{p.B},{p.H},{p.N},3]")
-    o = _new(stream, torch.empty_like, q) if o is None else o
+    o = _like(q, stream) if o is None else o
     lse_fg = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_fg is None else lse_fg
     lse_l = _new(stream, torch.empty, (p.B, p.H, p.N), dtype=torch.float32, device=q.device) if lse_l is None else lse_l
     if ws is None:
@@ -282,9 +287,9 @@ def mosaic_bsa_fwd_branches(p: Params, q, k, v, block_idx, gates, o=None, lse_fg
 def mosaic_bsa_bwd(p: Params, q, k, v, o, lse, d_o, block_idx, dq=None, dk=None, dv=None, ws=None, stream=None):
     _chk_qkv(p, q, o, d_o)
     _chk_qkv(p, k, v, heads=p.kv_heads)
-    dq = _new(stream, torch.empty_like, q) if dq is None else dq
-    dk = _new(stream, torch.empty_like, k) if dk is None else dk
-    dv = _new(stream, torch.empty_like, k) if dv is None else dv
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(k, stream) if dk is None else dk
+    dv = _like(k, stream) if dv is None else dv
     if ws is None:
         ws = _on(stream, alloc_workspace, p, OP_BWD, q.device)
     pc = p.c()
@@ -302,10 +307,10 @@ def mosaic_bsa_bwd_branches(p: Params, q, k, v, block_idx, gates, d_o, dq=None, 
     _chk_qkv(p, k, v, heads=p.kv_heads)
     if gates.dtype != torch.float32 or not gates.is_contiguous() or tuple(gates.shape) != (p.B, p.H, p.N, 3):
         raise ValueError(f"expected contiguous cuda fp32 gates [{p.B},{p.H},{p.N},3]")
-    dq = _new(stream, torch.empty_like, q) if dq is None else dq
-    dk = _new(stream, torch.empty_like, k) if dk is None else dk
-    dv = _new(stream, torch.empty_like, k) if dv is None else dv
-    dgates = _new(stream, torch.empty_like, gates) if dgates is None else dgates
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(k, stream) if dk is None else dk
+    dv = _like(k, stream) if dv is None else dv
+    dgates = _like(gates, stream) if dgates is None else dgates
     if ws is None:
         ws = _on(stream, alloc_workspace, p, OP_BWD_BRANCHES, q.device)
     pc = p.c()
@@ -323,8 +328,8 @@ def mosaic_bsa_rope(p: Params, q, k, pos, theta=10000.0, q_out=None, k_out=None,
     _chk_qkv(p, k, heads=p.kv_heads)
     if pos.dtype != torch.float32 or not pos.is_cuda or not pos.is_contiguous() or tuple(pos.shape) != (p.N, 2):
         raise ValueError(f"expected contiguous cuda fp32 positions [{p.N},2]")
-    q_out = _new(stream, torch.empty_like, q) if q_out is None else q_out
-    k_out = _new(stream, torch.empty_like, k) if k_out is None else k_out
+    q_out = _like(q, stream) if q_out is None else q_out
+    k_out = _like(k, stream) if k_out is None else k_out
     pc = p.c()
     rc = lib().mosaic_bsa_rope(ctypes.byref(pc), _ptr(q), _ptr(k), _ptr(pos), float(theta), _ptr(q_out), _ptr(k_out),
                                _stream(stream))
@@ -456,10 +461,6 @@ def _chk_seq(q, k):
         raise ValueError(f"expected cuda tensors [B, heads, tokens, d] in bf16, fp16 or fp32, got {q.dtype} {tuple(q.shape)} on "
                          f"{q.device} and {tuple(k.shape)}")
     return index
-
-
-def _like(t, stream):
-    return torch.empty_like(t) if stream is None else _new(stream, torch.empty_like, t)
 
 
 def _floats(n, index, stream):
