@@ -366,6 +366,44 @@ int mosaic_bsa_window_bwd(const mosaic_window_params *p, const mosaic_view *q, c
 int mosaic_bsa_window_decode(const mosaic_window_params *p, const mosaic_view *q, const mosaic_view *k, const mosaic_view *v,
                              const int32_t *k_len, const mosaic_view *o, float *lse, void *cuda_stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------
+ * A paged cache of keys and values, and attention over it: what a server of many sequences keeps, whose lengths it does not know.
+ *
+ * The cache is two pools [pages, Hkv, page, d] (views: either order of heads and slots in memory, and slices) and a table [B, width]
+ * of page numbers, int32 on the device, rows table_stride entries apart: token j of member b lies in slot j % page of page
+ * table[b][j / page].
+ *   - An entry outside [0, pages) is a page that is not there: nothing is written to it, its keys are seen by no row.  So any table
+ *     is safe, and entries that no token needs may hold anything; -1 is customary.
+ *   - A page may stand in the tables of several members, and more than once in one.  Pages that a call writes must be one member's,
+ *     once.
+ *   - k_len [B] int32 on the device: tokens that a member's pages hold, the new ones among them; the new ones are its last.  q_len [B]
+ *     (NULL: Nq for all): how many there are.  Row i of q has position k_len[b] - q_len[b] + i.  Lengths outside [0, width * page] and
+ *     [0, Nq] are clamped to it.  Rows from q_len[b] on are left as they were, and never read into a result.
+ */
+typedef struct mosaic_paged_params {
+  int64_t table_stride;  /* entries from one member's table row to the next, >= 0 (0: all members share one)  */
+  int64_t start;         /* append: position of a cache's first token (behind a shared prefix: its length)    */
+  int32_t B, H, Hkv, Nq; /* members, query heads, key heads, new tokens a member                              */
+  int32_t d;             /* 64 or 128                                                                         */
+  int32_t page;          /* slots of a page: a power of two, 16 or more                                       */
+  int32_t pages, width;  /* pages of a pool, entries of a table row; width * page at most 2^30                */
+  int32_t window, sinks; /* attention: as in mosaic_window_params, window 0: none; 0 behind a prefix           */
+  int32_t prefix_len;    /* attention behind a prefix: its tokens, > 0; otherwise 0                           */
+  int32_t rot_dim;       /* append: channels that turn, as in mosaic_rotary_params; 0: none                   */
+  float scale;           /* softmax scale; <= 0 means 1/sqrt(d)                                               */
+  float amplitude;       /* append: factor of the turned channels; 0 means 1                                  */
+  uint32_t flags;        /* MOSAIC_FLAG_FP16; append also MOSAIC_FLAG_HALF_PAIRS                              */
+} mosaic_paged_params;
+
+/* New tokens to the cache: k, v [B,Hkv,Nq,d] in; their places in the pools out, keys turned to position start + j on the way (formula and
+ * roundings of mosaic_bsa_rotary, freqs [rot_dim/2] as there; not read with rot_dim 0).  With q [B,H,Nq,d] (NULL: none, and H is not
+ * looked at) the queries are turned too, to q_out (may be q itself).  Values, and channels that do not turn, keep their bits.  No
+ * workspace. */
+int mosaic_bsa_paged_append(const mosaic_paged_params *p, const mosaic_view *k, const mosaic_view *v, const mosaic_view *k_pages,
+                            const mosaic_view *v_pages, const int32_t *table, const int32_t *k_len, const int32_t *q_len,
+                            const double *freqs, const mosaic_view *q, const mosaic_view *q_out, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.
  * Every op resets the word when it starts. */

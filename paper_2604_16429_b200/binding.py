@@ -25,7 +25,7 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
            "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd",
-           "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode")
+           "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode", "mosaic_bsa_paged_append")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
@@ -66,6 +66,14 @@ class _WindowParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Nq", ctypes.c_int32),
                 ("Nk", ctypes.c_int32), ("d", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class _PagedParams(ctypes.Structure):
+    _fields_ = [("table_stride", ctypes.c_int64), ("start", ctypes.c_int64), ("B", ctypes.c_int32), ("H", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("Nq", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("width", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("prefix_len", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("amplitude", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 @dataclass(frozen=True)
@@ -153,6 +161,9 @@ def lib():
         L.mosaic_bsa_window_bwd.argtypes = [wp, vw, vw, vw, vw, fp, vw, i32p, i32p, vw, vw, vw, vp, ctypes.c_size_t, vp]
         L.mosaic_bsa_window_decode.restype = ctypes.c_int
         L.mosaic_bsa_window_decode.argtypes = [wp, vw, vw, vw, i32p, vw, fp, vp]
+        ap = vp
+        L.mosaic_bsa_paged_append.restype = ctypes.c_int
+        L.mosaic_bsa_paged_append.argtypes = [ap, vw, vw, vw, vw, i32p, i32p, i32p, vp, vw, vw, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -408,6 +419,7 @@ _block = _Block()
 # (both parameter blocks are 40 bytes long with their padding, a view is 32)
 _rotary_pack = {n: struct.Struct("=6iI2f4x%dq" % (4 * n)).pack_into for n in (0, 4, 6)}
 _window_pack = {n: struct.Struct("=8ifI%dq" % (4 * n)).pack_into for n in (0, 4, 8)}
+_paged_pack = {n: struct.Struct("=2q12i2fI4x%dq" % (4 * n)).pack_into for n in (0, 4, 6)}  # (80 bytes in front)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
@@ -694,3 +706,63 @@ def mosaic_bsa_window_decode(wp: WindowParams, q, k, v, k_len=None, o=None, lse=
     _call("mosaic_bsa_window_decode", index, stream, a, a + 40, a + 72, a + 104, _len("k_len", k_len, sq[0], index), a + 136,
           _flat("lse", lse, sq[:3], torch.float32, index))
     return o, lse
+
+
+@dataclass(frozen=True)
+class PagedParams:
+    """Attention over a paged cache: the row at position p sees the keys j <= p with p - j < window or j < sinks."""
+    window: int = 0          # 0: no window
+    sinks: int = 0
+    scale: float = 0.0       # <= 0: 1/sqrt(d)
+
+
+def _pools(x, k_pages, v_pages, heads, d, index):
+    """(pages, page, packed views) of the pools [pages, Hkv, page, d] that go with x"""
+    if k_pages.dim() != 4:
+        raise ValueError(f"k_pages: expected [pages, Hkv, page, d], got {tuple(k_pages.shape)}")
+    shape = (k_pages.shape[0], heads, k_pages.shape[2], d)
+    return shape[0], shape[2], _out("k_pages", k_pages, shape, x.dtype, index) + _out("v_pages", v_pages, shape, x.dtype, index)
+
+
+def _page_table(name, t, B, index):
+    """(pointer, row stride, width) of a table [B, width] of page numbers"""
+    if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise _bad(name, t, f"int32 [{B}, width] on cuda:{index} with contiguous rows")
+    return t.data_ptr(), t.stride(0) if B > 1 else 0, t.shape[1]
+
+
+def mosaic_bsa_paged_append(rp: RotaryParams, k, v, k_pages, v_pages, table, k_len, freqs=None, start=0, q=None, q_len=None, q_out=None,
+                            stream=None):
+    """New tokens k, v [B,Hkv,N,d] to their places in the pools [pages, Hkv, page, d]: token i of member b to position
+    j = k_len[b] - q_len[b] + i (q_len None: N for all), slot j % page of page table[b, j // page].  Keys turn to position
+    start + j on the way (`freqs` from `rotary_freqs`; rp.rot_dim 0: they stay), and so do the new tokens' queries q [B,H,N,d], if
+    given.  Returns the turned queries, or None."""
+    index = _chk_seq(k, k if q is None else q)
+    t, sk = k.dtype, k.shape
+    if t is torch.float32:
+        raise ValueError("a paged cache takes bf16 or fp16 tensors")
+    B, Hkv, N, _ = sk
+    d, rot = rp.d, rp.rot
+    sk, sq = (B, Hkv, N, d), (B, 0 if q is None else q.shape[1], N, d)
+    vk, vv = _view("k", k, sk, t, index), _view("v", v, sk, t, index)
+    pages, page, pools = _pools(k, k_pages, v_pages, Hkv, d, index)
+    at, step, width = _page_table("table", table, B, index)
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        vq = ()
+    else:
+        vq = _view("q", q, sq, t, index)
+        q_out = _like(q, stream) if q_out is None else q_out
+        vq += _out("q_out", q_out, sq, t, index)
+    fr = _flat("freqs", freqs, (rot // 2,), torch.float64, index) if rot else 0
+    block = _block
+    a = block.at
+    try:
+        _paged_pack[4 if q is None else 6](block.buf, 0, step, start, B, sq[1], Hkv, N, d, page, pages, width, 0, 0, 0, rot, 0.0,
+                                           rp.amplitude, _STORAGE[t] | (FLAG_HALF_PAIRS if rp.half else 0), *vk, *vv, *pools, *vq)
+    except _RANGE as e:
+        raise _out_of_range(e) from None
+    _call("mosaic_bsa_paged_append", index, stream, a, a + 80, a + 112, a + 144, a + 176, at, _flat("k_len", k_len, (B,), torch.int32, index),
+          _len("q_len", q_len, B, index), fr, 0 if q is None else a + 208, 0 if q is None else a + 240)
+    return q_out

@@ -1,0 +1,78 @@
+// C ABI of the paged cache: argument checks, workspace, launches.
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace mosaic {
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+int log2_of(int n) {
+  int s = 0;
+  while ((1 << s) < n) ++s;
+  return s;
+}
+
+// What all calls have in common
+int check(const mosaic_paged_params* p, uint32_t flags) {
+  if (!p || p->B <= 0 || p->Hkv <= 0 || p->Nq <= 0 || p->pages <= 0 || p->width <= 0 || p->page <= 0 || p->table_stride < 0)
+    return MOSAIC_E_INVALID_ARG;
+  if (p->flags & ~flags) return MOSAIC_E_INVALID_ARG;
+  if (p->d != 64 && p->d != 128) return MOSAIC_E_UNSUPPORTED;
+  if (p->page < kMinPage || (p->page & (p->page - 1)) || (long long)p->width * p->page > (1 << 30)) return MOSAIC_E_UNSUPPORTED;
+  if (p->table_stride > (1ll << 40)) return MOSAIC_E_UNSUPPORTED;
+  return MOSAIC_OK;
+}
+
+int make_geo(const mosaic_paged_params* p, const int32_t* table, const int32_t* k_len, const int32_t* q_len, PagedGeo* g) {
+  *g = {};
+  g->B = p->B; g->H = p->H; g->Hkv = p->Hkv; g->T = p->Nq; g->d = p->d;
+  g->shift = log2_of(p->page); g->pages = p->pages; g->width = p->width;
+  g->window = p->window; g->sinks = p->sinks;
+  g->table_stride = p->table_stride;
+  g->table = table; g->k_len = k_len; g->q_len = q_len;
+  if (!table || !k_len) return MOSAIC_E_INVALID_ARG;
+  return aligned(table, 4) && aligned(k_len, 4) && aligned(q_len, 4) ? MOSAIC_OK : MOSAIC_E_MISALIGNED;
+}
+
+}  // namespace
+
+int check_pool(const mosaic_view* v, const mosaic_paged_params* p, View* out) {
+  if (const int rc = check_view(v, p->pages, p->Hkv, p->page, 2, out)) return rc;
+  // (a place of its own for every row)
+  return out->sn == 0 || (p->Hkv > 1 && out->sh == 0) || (p->pages > 1 && out->sb == 0) ? MOSAIC_E_UNSUPPORTED : MOSAIC_OK;
+}
+
+}  // namespace mosaic
+
+using namespace mosaic;
+
+extern "C" {
+
+int mosaic_bsa_paged_append(const mosaic_paged_params* p, const mosaic_view* k, const mosaic_view* v, const mosaic_view* k_pages,
+                            const mosaic_view* v_pages, const int32_t* table, const int32_t* k_len, const int32_t* q_len,
+                            const double* freqs, const mosaic_view* q, const mosaic_view* q_out, void* cuda_stream) {
+  int rc = check(p, MOSAIC_FLAG_FP16 | MOSAIC_FLAG_HALF_PAIRS);
+  if (rc) return rc;
+  if (p->rot_dim < 0 || p->rot_dim % 2 || p->rot_dim > p->d || !(p->amplitude >= 0.f) || isinf(p->amplitude)) return MOSAIC_E_INVALID_ARG;
+  if ((p->flags & MOSAIC_FLAG_HALF_PAIRS) && p->rot_dim % 16) return MOSAIC_E_UNSUPPORTED;
+  if ((q != nullptr) != (q_out != nullptr) || (q && p->H <= 0) || (p->rot_dim && !freqs)) return MOSAIC_E_INVALID_ARG;
+  if (p->start > (1ll << 52) || p->start < -(1ll << 52)) return MOSAIC_E_UNSUPPORTED;
+  const int heads = q ? p->H : 0;
+  if ((long long)p->B * p->Nq > (1 << 30) || (long long)heads + 2ll * p->Hkv > (1 << 16)) return MOSAIC_E_UNSUPPORTED;
+  AppendTensors t = {};
+  if ((rc = check_view(k, p->B, p->Hkv, p->Nq, 2, &t.k)) || (rc = check_view(v, p->B, p->Hkv, p->Nq, 2, &t.v)) ||
+      (rc = check_pool(k_pages, p, &t.k_pages)) || (rc = check_pool(v_pages, p, &t.v_pages)))
+    return rc;
+  if (q && ((rc = check_view(q, p->B, heads, p->Nq, 2, &t.q)) || (rc = check_view(q_out, p->B, heads, p->Nq, 2, &t.q_out)))) return rc;
+  PagedGeo g;
+  if ((rc = make_geo(p, table, k_len, q_len, &g))) return rc;
+  if (!aligned(freqs, 8)) return MOSAIC_E_MISALIGNED;
+  if ((rc = device_ok())) return rc;
+  HostCtx c = {};
+  c.stream = (cudaStream_t)cuda_stream;
+  return launch_paged_append(c, g, p, freqs, t);
+}
+
+}  // extern "C"

@@ -1,0 +1,61 @@
+"""Refusals and workspace sizes of the paged cache's calls (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2604_16429_b200 import binding as mb
+from paper_2604_16429_b200 import build as mbuild
+
+BASE = dict(table_stride=32, start=0, B=2, H=4, Hkv=2, Nq=3, d=64, page=16, pages=100, width=32, window=0, sinks=0, prefix_len=0, rot_dim=64,
+            scale=0.0, amplitude=0.0, flags=0)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    mbuild.build()
+
+
+def params(**kw):
+    v = {**BASE, **kw}
+    return ctypes.byref(mb._PagedParams(*(v[k] for k, _ in mb._PagedParams._fields_)))
+
+
+def view(ptr=256, sb=1 << 20, sh=1 << 16, sn=64):
+    return ctypes.byref(mb._View(ptr, sb, sh, sn))
+
+
+def append(p=None, k=None, v=None, k_pages=None, v_pages=None, table=256, k_len=256, q_len=None, freqs=256, q=None, q_out=None):
+    g = view()
+    return mb.lib().mosaic_bsa_paged_append(p or params(), k or g, v or g, k_pages or g, v_pages or g, table, k_len, q_len, freqs, q, q_out, None)
+
+
+ANY = [(dict(B=0), -1), (dict(Hkv=0), -1), (dict(Nq=0), -1), (dict(pages=0), -1), (dict(width=0), -1), (dict(page=0), -1),
+       (dict(page=-16), -1), (dict(table_stride=-1), -1), (dict(flags=1), -1), (dict(flags=4), -1), (dict(flags=64), -1), (dict(d=32), -2),
+       (dict(d=256), -2), (dict(page=8), -2), (dict(page=24), -2), (dict(page=1 << 20, width=1 << 11), -2), (dict(table_stride=1 << 41), -2)]
+
+
+@pytest.mark.parametrize("kw,code", ANY + [
+    (dict(rot_dim=-2), -1), (dict(rot_dim=3), -1), (dict(rot_dim=66), -1), (dict(rot_dim=24, flags=8), -2), (dict(flags=16), -1),
+    (dict(amplitude=-1.0), -1), (dict(amplitude=float("nan")), -1), (dict(amplitude=float("inf")), -1), (dict(start=1 << 53), -2),
+    (dict(start=-(1 << 53)), -2), (dict(B=1 << 20, Nq=1 << 11), -2), (dict(Hkv=1 << 16), -2)])
+def test_bad_params_of_append_are_refused(kw, code):
+    assert append(params(**kw)) == code
+
+
+POOLS = [(view(0), -1), (view(256 + 8), -4), (view(sn=68), -4), (view(sh=4), -4), (view(sb=-64), -1), (view(sb=1 << 40), -2),
+         (view(sn=0), -2), (view(sh=0), -2), (view(sb=0), -2)]
+
+
+def test_bad_tensors_of_append_are_refused():
+    for x, code in POOLS:
+        for at in ("k_pages", "v_pages"):
+            assert append(**{at: x}) == code, at
+    for x, code in POOLS[:6]:
+        for at in ("k", "v"):
+            assert append(**{at: x}) == code, at
+        assert append(q=x, q_out=view()) == code and append(q=view(), q_out=x) == code
+    assert append(q=view()) == -1 and append(q_out=view()) == -1 and append(params(H=0), q=view(), q_out=view()) == -1
+    assert append(table=None) == -1 and append(k_len=None) == -1 and append(freqs=None) == -1
+    assert append(table=258) == -4 and append(k_len=257) == -4 and append(q_len=254) == -4 and append(freqs=252) == -4
+    assert mb.lib().mosaic_bsa_paged_append(None, view(), view(), view(), view(), 256, 256, None, 256, None, None, None) == -1
+    assert mb.lib().mosaic_bsa_paged_append(params(), None, view(), view(), view(), 256, 256, None, 256, None, None, None) == -1
