@@ -404,6 +404,20 @@ int mosaic_bsa_paged_append(const mosaic_paged_params *p, const mosaic_view *k, 
                             const mosaic_view *v_pages, const int32_t *table, const int32_t *k_len, const int32_t *q_len,
                             const double *freqs, const mosaic_view *q, const mosaic_view *q_out, void *cuda_stream);
 
+/* Attention of the new tokens (Nq at most 16: the next one, or drafts that are checked at once) over their members' pages: the row at
+ * position p sees the keys j <= p with p - j < window (window 0: all) or j < sinks, under one softmax.
+ *   q [B,H,Nq,d] in (the new tokens' own keys and values are in the pools); o like q, lse [B,H,Nq] fp32 (natural log, contiguous) out.
+ *   A row that sees nothing gives o = 0, lse = -inf.
+ *   Scores, softmax statistics and sums are fp32; weights round to the 16-bit type once, as operands of the tensor core.
+ *   Slots that none of a member's rows sees may hold anything; others are expected finite (a value that is not spreads to the rows
+ *   that see it, and may spread to the member's other rows).
+ *   ws: mosaic_bsa_paged_workspace_bytes(p) bytes (0 on invalid params), 256-byte aligned, the status block first.  It grows with
+ *   B * H * Nq times the chunks of 512 keys that a member can have: those of its table row, or of its window. */
+size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params *p);
+int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
+                            const int32_t *table, const int32_t *k_len, const int32_t *q_len, const mosaic_view *o, float *lse, void *ws,
+                            size_t ws_bytes, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.
  * Every op resets the word when it starts. */

@@ -25,7 +25,8 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_descriptor_encodes", "mosaic_bsa_fwd_branches", "mosaic_bsa_bwd_branches", "mosaic_bsa_rope",
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
            "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd",
-           "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode", "mosaic_bsa_paged_append")
+           "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode", "mosaic_bsa_paged_append",
+           "mosaic_bsa_paged_workspace_bytes", "mosaic_bsa_paged_decode")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
@@ -164,6 +165,10 @@ def lib():
         ap = vp
         L.mosaic_bsa_paged_append.restype = ctypes.c_int
         L.mosaic_bsa_paged_append.argtypes = [ap, vw, vw, vw, vw, i32p, i32p, i32p, vp, vw, vw, vp]
+        L.mosaic_bsa_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.mosaic_bsa_paged_workspace_bytes.argtypes = [ap]
+        L.mosaic_bsa_paged_decode.restype = ctypes.c_int
+        L.mosaic_bsa_paged_decode.argtypes = [ap, vw, vw, vw, i32p, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -766,3 +771,47 @@ def mosaic_bsa_paged_append(rp: RotaryParams, k, v, k_pages, v_pages, table, k_l
     _call("mosaic_bsa_paged_append", index, stream, a, a + 80, a + 112, a + 144, a + 176, at, _flat("k_len", k_len, (B,), torch.int32, index),
           _len("q_len", q_len, B, index), fr, 0 if q is None else a + 208, 0 if q is None else a + 240)
     return q_out
+
+
+def _paged_params(pp, q, k_pages, table, prefix_len, index):
+    """(parameters, shape of the pools) of the attention of q [B,H,Nq,d]"""
+    if q.dtype is torch.float32:
+        raise ValueError("attention over a paged cache takes bf16 or fp16 tensors")
+    B, H, T, d = q.shape
+    pages, Hkv, page, _ = k_pages.shape
+    _, step, width = _page_table("table", table, B, index)
+    window = pp.window if pp.window < width * page else 0  # (one that holds every token is none)
+    return (step, 0, B, H, Hkv, T, d, page, pages, width, window, pp.sinks, prefix_len, 0, pp.scale, 0.0, _STORAGE[q.dtype]), (pages, Hkv, page, d)
+
+
+def paged_workspace_bytes(pp: PagedParams, q, k_pages, table, prefix_len=0) -> int:
+    """Bytes of workspace of mosaic_bsa_paged_decode."""
+    p = _paged_params(pp, q, k_pages, table, prefix_len, _chk_seq(q, k_pages))[0]
+    return int(lib().mosaic_bsa_paged_workspace_bytes(_params_block(_paged_pack[0], p)))
+
+
+def _paged_ws(at, index, ws, stream):
+    name = "mosaic_bsa_paged_workspace_bytes"
+    return _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(at)), name, index, ws, stream)
+
+
+def mosaic_bsa_paged_decode(pp: PagedParams, q, k_pages, v_pages, table, k_len, q_len=None, o=None, lse=None, ws=None, stream=None):
+    """Attention of new tokens q [B,H,Nq,d], Nq at most 16, over their members' pages: a member's q_len[b] new tokens (None: Nq for
+    all) are the last of the k_len[b] that its pages hold.  Returns (o, lse)."""
+    index = _chk_seq(q, k_pages)
+    p, sk = _paged_params(pp, q, k_pages, table, 0, index)
+    t, sq = q.dtype, q.shape
+    vq, vk, vv = _view("q", q, sq, t, index), _out("k_pages", k_pages, sk, t, index), _out("v_pages", v_pages, sk, t, index)
+    o = _like(q, stream) if o is None else o
+    lse = _rows_like(q, stream) if lse is None else lse
+    block = _block
+    a = block.at
+    try:
+        _paged_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
+    ws = _paged_ws(a, index, ws, stream)
+    _call("mosaic_bsa_paged_decode", index, stream, a, a + 80, a + 112, a + 144, table.data_ptr(),
+          _flat("k_len", k_len, (sq[0],), torch.int32, index), _len("q_len", q_len, sq[0], index), a + 176,
+          _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
+    return o, lse

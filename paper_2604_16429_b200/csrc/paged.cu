@@ -27,6 +27,8 @@ int check(const mosaic_paged_params* p, uint32_t flags) {
 
 int make_geo(const mosaic_paged_params* p, const int32_t* table, const int32_t* k_len, const int32_t* q_len, PagedGeo* g) {
   *g = {};
+  g->G = p->H / p->Hkv;
+  g->scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->d)) * 1.4426950408889634f;
   g->B = p->B; g->H = p->H; g->Hkv = p->Hkv; g->T = p->Nq; g->d = p->d;
   g->shift = log2_of(p->page); g->pages = p->pages; g->width = p->width;
   g->window = p->window; g->sinks = p->sinks;
@@ -35,6 +37,37 @@ int make_geo(const mosaic_paged_params* p, const int32_t* table, const int32_t* 
   if (!table || !k_len) return MOSAIC_E_INVALID_ARG;
   return aligned(table, 4) && aligned(k_len, 4) && aligned(q_len, 4) ? MOSAIC_OK : MOSAIC_E_MISALIGNED;
 }
+
+// The attention's own
+int check_attention(const mosaic_paged_params* p) {
+  if (const int rc = check(p, MOSAIC_FLAG_FP16)) return rc;
+  if (p->H <= 0 || p->H % p->Hkv || p->window < 0 || p->sinks < 0 || p->prefix_len < 0) return MOSAIC_E_INVALID_ARG;
+  if (!(p->scale == p->scale) || isinf(p->scale)) return MOSAIC_E_INVALID_ARG;
+  if (p->Nq > kMaxNew || p->sinks > kMaxSinks || (long long)p->B * p->H > (1 << 24)) return MOSAIC_E_UNSUPPORTED;
+  return MOSAIC_OK;
+}
+
+// Most parts that a member's own keys can have: all chunks of its pages, or those that a window and its first rows' ends touch
+int most_parts(const mosaic_paged_params* p) {
+  const long long all = ((long long)p->width * p->page + kChunkKeys - 1) / kChunkKeys;
+  if (!p->window) return (int)all;
+  const long long some = ((long long)p->window + p->Nq - 2 + kChunkKeys - 1) / kChunkKeys + 1 + (p->sinks > 0);
+  return (int)(some < all ? some : all);
+}
+
+// Behind the status block the parts: sums [part][row][d], then maximum and sum of weights [part][row]
+struct Layout {
+  size_t o, ml, total;
+};
+Layout layout(const mosaic_paged_params* p, int parts) {
+  const size_t rows = (size_t)p->B * p->H * p->Nq;
+  Layout w;
+  w.o = kStatusBytes;
+  w.ml = w.o + align256((size_t)parts * rows * p->d * sizeof(float));
+  w.total = w.ml + align256((size_t)parts * rows * sizeof(float2));
+  return w;
+}
+bool is_direct(const mosaic_paged_params* p) { return most_parts(p) == 1; }  // the part is the result
 
 }  // namespace
 
@@ -73,6 +106,38 @@ int mosaic_bsa_paged_append(const mosaic_paged_params* p, const mosaic_view* k, 
   HostCtx c = {};
   c.stream = (cudaStream_t)cuda_stream;
   return launch_paged_append(c, g, p, freqs, t);
+}
+
+size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params* p) {
+  if (check_attention(p) || p->prefix_len) return 0;
+  return is_direct(p) ? kStatusBytes : layout(p, most_parts(p)).total;
+}
+
+int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages,
+                            const int32_t* table, const int32_t* k_len, const int32_t* q_len, const mosaic_view* o, float* lse, void* ws,
+                            size_t ws_bytes, void* cuda_stream) {
+  int rc = check_attention(p);
+  if (rc) return rc;
+  if (p->prefix_len) return MOSAIC_E_INVALID_ARG;
+  View vq, vk, vv, vo;
+  if ((rc = check_view(q, p->B, p->H, p->Nq, 2, &vq)) || (rc = check_pool(k_pages, p, &vk)) || (rc = check_pool(v_pages, p, &vv)) ||
+      (rc = check_view(o, p->B, p->H, p->Nq, 2, &vo)))
+    return rc;
+  PagedGeo g;
+  if ((rc = make_geo(p, table, k_len, q_len, &g))) return rc;
+  if (!lse || !ws) return MOSAIC_E_INVALID_ARG;
+  if (!aligned(lse, 4) || !aligned(ws, 256)) return MOSAIC_E_MISALIGNED;
+  if (ws_bytes < mosaic_bsa_paged_workspace_bytes(p)) return MOSAIC_E_WORKSPACE_TOO_SMALL;
+  if ((rc = device_ok())) return rc;
+  HostCtx c = {};
+  c.stream = (cudaStream_t)cuda_stream;
+  c.status = (int*)ws;
+  const bool f16 = (p->flags & MOSAIC_FLAG_FP16) != 0, direct = is_direct(p);
+  const int most = most_parts(p);
+  const Layout w = layout(p, most);
+  const PartsOut parts = {(float*)((char*)ws + w.o), (float2*)((char*)ws + w.ml), (long long)p->B * p->H * p->Nq, 0};
+  if ((rc = launch_paged_parts(c, g, f16, vq, vk, vv, parts, most, direct, true, vo, lse)) || direct) return rc;
+  return launch_paged_join(c, g, f16, parts, most, vo, lse);
 }
 
 }  // extern "C"

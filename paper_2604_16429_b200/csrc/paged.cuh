@@ -28,6 +28,37 @@ __device__ __forceinline__ Span span_of(const PagedGeo& g, int b) {
   return s;
 }
 
+// The keys that member b's rows see, cut into parts: the chunks of kChunkKeys positions that hold some of them.  So what a part is
+// follows from positions alone, and a row's bits do not depend on what else is in the call.
+struct Parts {
+  int kl, ql, p0;   // tokens, new ones, position of the first row
+  int from, sinks;  // the rows see keys of [0, sinks) and of [from, kl) only
+  int first, front; // chunk of `from`; 1: the sinks lie in a chunk ahead of it, the first part
+  int n;            // parts
+};
+__device__ __forceinline__ Parts parts_of(const PagedGeo& g, int b) {
+  const Span s = span_of(g, b);
+  Parts p;
+  p.kl = s.kl; p.ql = s.ql; p.p0 = s.off;
+  p.from = g.window ? max(0, s.off - g.window + 1) : 0;
+  p.sinks = g.window ? min(g.sinks, s.kl) : 0;
+  p.first = p.from / kChunkKeys;
+  p.front = p.sinks > 0 && p.first > 0;
+  p.n = s.kl > 0 && s.ql > 0 ? (s.kl - 1) / kChunkKeys - p.first + 1 + p.front : 0;
+  return p;
+}
+// Chunk of part o
+__device__ __forceinline__ int chunk_of(const Parts& p, int o) { return p.front ? (o ? p.first + o - 1 : 0) : p.first + o; }
+
+// What parts leave for the join, in the workspace: the rows' weighted sums of values [part][row][d], their maximum (base 2, scaled) and
+// sum of weights [part][row], fp32; rows are [B, H, T].  The prefix' parts come first, then the member's own.
+struct PartsOut {
+  float* o;
+  float2* ml;
+  long long rows;
+  int shared;  // parts of the prefix
+};
+
 // A pool as a tensor [pages, Hkv, page, d], strides in bytes
 int check_pool(const mosaic_view* v, const mosaic_paged_params* p, View* out);
 
@@ -35,5 +66,17 @@ struct AppendTensors {
   View q, q_out, k, v, k_pages, v_pages;
 };
 int launch_paged_append(const HostCtx& c, const PagedGeo& g, const mosaic_paged_params* p, const double* freqs, const AppendTensors& t);
+
+
+// Attention over the members' own pages: parts to the workspace, or, where a member can have but one and there is no prefix (`direct`),
+// results.  `clear`: the call's first kernel, which clears the status word.
+int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
+                       const PartsOut& parts, int most_parts, bool direct, bool clear, const View& o, float* lse);
+// Joins all parts of every row
+int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const PartsOut& parts, int most_parts, const View& o, float* lse);
+// A map of a pool in boxes of 64 channels by `rows` slots
+inline bool make_map_pool(CUtensorMap* map, const View& v, const PagedGeo& g, int rows) {
+  return make_map_view(map, v, g.d, 1 << g.shift, g.Hkv, g.pages, rows);
+}
 
 }  // namespace mosaic

@@ -59,3 +59,39 @@ def test_bad_tensors_of_append_are_refused():
     assert append(table=258) == -4 and append(k_len=257) == -4 and append(q_len=254) == -4 and append(freqs=252) == -4
     assert mb.lib().mosaic_bsa_paged_append(None, view(), view(), view(), view(), 256, 256, None, 256, None, None, None) == -1
     assert mb.lib().mosaic_bsa_paged_append(params(), None, view(), view(), view(), 256, 256, None, 256, None, None, None) == -1
+
+
+def decode(p=None, q=None, k_pages=None, v_pages=None, o=None, table=256, k_len=256, q_len=None, lse=256, ws=256, n=1 << 40):
+    g = view()
+    return mb.lib().mosaic_bsa_paged_decode(p or params(), q or g, k_pages or g, v_pages or g, table, k_len, q_len, o or g, lse, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", ANY + [
+    (dict(H=3), -1), (dict(H=0), -1), (dict(window=-1), -1), (dict(sinks=-1), -1), (dict(sinks=129), -2), (dict(prefix_len=1), -1),
+    (dict(prefix_len=-1), -1), (dict(Nq=17), -2), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(flags=8), -1),
+    (dict(B=1 << 23), -2)])
+def test_bad_params_of_decode_are_refused(kw, code):
+    assert decode(params(**kw)) == code
+    assert mb.lib().mosaic_bsa_paged_workspace_bytes(params(**kw)) == 0
+
+
+def test_bad_tensors_of_decode_are_refused():
+    for x, code in POOLS:
+        for at in ("k_pages", "v_pages"):
+            assert decode(**{at: x}) == code, at
+    for x, code in POOLS[:6]:
+        for at in ("q", "o"):
+            assert decode(**{at: x}) == code, at
+    assert decode(table=None) == -1 and decode(k_len=None) == -1 and decode(lse=None) == -1 and decode(ws=None) == -1
+    assert decode(table=258) == -4 and decode(k_len=257) == -4 and decode(q_len=254) == -4 and decode(lse=258) == -4 and decode(ws=272) == -4
+    assert decode(n=255) == -3 and decode(params(width=33), n=256) == -3
+
+
+def test_workspaces():
+    ws = mb.lib().mosaic_bsa_paged_workspace_bytes
+    rows = 2 * 4 * 3
+    assert ws(None) == 0 and ws(params()) == 256  # 512 tokens at most: one part, which is the result
+    part = lambda n: 256 + n * rows * 64 * 4 + -(-n * rows * 8 // 256) * 256  # noqa: E731
+    assert ws(params(width=33)) == part(2) and ws(params(width=320)) == part(10)
+    assert ws(params(width=320, window=1)) == part(2) and ws(params(width=320, window=512)) == part(3)   # 514 keys end to end: three chunks
+    assert ws(params(width=320, window=512, sinks=1)) == part(4) and ws(params(width=33, window=512, sinks=1)) == part(2)
