@@ -386,7 +386,7 @@ typedef struct mosaic_paged_params {
   int64_t start;         /* append: position of a cache's first token (behind a shared prefix: its length)    */
   int32_t B, H, Hkv, Nq; /* members, query heads, key heads, new tokens a member                              */
   int32_t d;             /* 64 or 128                                                                         */
-  int32_t page;          /* slots of a page: a power of two, 16 or more                                       */
+  int32_t page;          /* slots of a page: a power of two from 16 to 2^20                                   */
   int32_t pages, width;  /* pages of a pool, entries of a table row; width * page at most 2^30                */
   int32_t window, sinks; /* attention: as in mosaic_window_params, window 0: none; 0 behind a prefix           */
   int32_t prefix_len;    /* attention behind a prefix: its tokens, > 0; otherwise 0                           */
@@ -417,6 +417,17 @@ size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params *p);
 int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
                             const int32_t *table, const int32_t *k_len, const int32_t *q_len, const mosaic_view *o, float *lse, void *ws,
                             size_t ws_bytes, void *cuda_stream);
+
+/* The same for a batch whose members all begin with one prefix, which lies in the pools once: prefix_table [ceil(prefix_len / page)] int32
+ * on the device holds its pages (by the same rule, entries outside the pool are not there).  Every row sees the whole prefix and its
+ * member's own keys as above (window 0); table, k_len and q_len count the member's own tokens alone, and k_len may be 0.  The prefix is
+ * read once for the whole batch.
+ *   ws as above (p with prefix_len): B * H * Nq times the parts of the prefix more, of which there are 2 * 148 / Hkv or fewer.
+ *   How the prefix is cut into parts follows from its length, Hkv and B * Nq * H / Hkv, so a member's bits depend on the shape of the
+ *   call, but on nothing that another member holds, nor on its place. */
+int mosaic_bsa_prefix_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
+                             const int32_t *prefix_table, const int32_t *table, const int32_t *k_len, const int32_t *q_len,
+                             const mosaic_view *o, float *lse, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /* Synchronises `cuda_stream`, then returns the device status word of `ws`
  * (MOSAIC_OK, MOSAIC_E_DEVICE_*) or MOSAIC_E_CUDA if the stream reports an error.

@@ -26,7 +26,7 @@ EXPORTS = ("mosaic_bsa_workspace_bytes", "mosaic_bsa_select", "mosaic_bsa_fwd", 
            "mosaic_bsa_rotary_freqs", "mosaic_bsa_rotary", "mosaic_bsa_qk_norm", "mosaic_bsa_qk_norm_workspace_bytes",
            "mosaic_bsa_qk_norm_bwd", "mosaic_bsa_window_workspace_bytes", "mosaic_bsa_window_fwd",
            "mosaic_bsa_window_bwd", "mosaic_bsa_window_decode", "mosaic_bsa_paged_append",
-           "mosaic_bsa_paged_workspace_bytes", "mosaic_bsa_paged_decode")
+           "mosaic_bsa_paged_workspace_bytes", "mosaic_bsa_paged_decode", "mosaic_bsa_prefix_decode")
 STATIC_SCRATCH_BYTES = 4 << 20
 FLAG_LOCAL_GROUPS = 1
 FLAG_FP16 = 2
@@ -169,6 +169,8 @@ def lib():
         L.mosaic_bsa_paged_workspace_bytes.argtypes = [ap]
         L.mosaic_bsa_paged_decode.restype = ctypes.c_int
         L.mosaic_bsa_paged_decode.argtypes = [ap, vw, vw, vw, i32p, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
+        L.mosaic_bsa_prefix_decode.restype = ctypes.c_int
+        L.mosaic_bsa_prefix_decode.argtypes = [ap, vw, vw, vw, i32p, i32p, i32p, i32p, vw, fp, vp, ctypes.c_size_t, vp]
         L.mosaic_bsa_last_status.restype = ctypes.c_int
         L.mosaic_bsa_last_status.argtypes = [vp, vp]
         L.mosaic_bsa_descriptor_encodes.restype = ctypes.c_longlong
@@ -780,12 +782,12 @@ def _paged_params(pp, q, k_pages, table, prefix_len, index):
     B, H, T, d = q.shape
     pages, Hkv, page, _ = k_pages.shape
     _, step, width = _page_table("table", table, B, index)
-    window = pp.window if pp.window < width * page else 0  # (one that holds every token is none)
+    window = pp.window if prefix_len or pp.window < width * page else 0  # (one that holds every token is none)
     return (step, 0, B, H, Hkv, T, d, page, pages, width, window, pp.sinks, prefix_len, 0, pp.scale, 0.0, _STORAGE[q.dtype]), (pages, Hkv, page, d)
 
 
 def paged_workspace_bytes(pp: PagedParams, q, k_pages, table, prefix_len=0) -> int:
-    """Bytes of workspace of mosaic_bsa_paged_decode."""
+    """Bytes of workspace of mosaic_bsa_paged_decode, or with `prefix_len` of mosaic_bsa_prefix_decode."""
     p = _paged_params(pp, q, k_pages, table, prefix_len, _chk_seq(q, k_pages))[0]
     return int(lib().mosaic_bsa_paged_workspace_bytes(_params_block(_paged_pack[0], p)))
 
@@ -812,6 +814,34 @@ def mosaic_bsa_paged_decode(pp: PagedParams, q, k_pages, v_pages, table, k_len, 
         raise _out_of_range(e) from None
     ws = _paged_ws(a, index, ws, stream)
     _call("mosaic_bsa_paged_decode", index, stream, a, a + 80, a + 112, a + 144, table.data_ptr(),
+          _flat("k_len", k_len, (sq[0],), torch.int32, index), _len("q_len", q_len, sq[0], index), a + 176,
+          _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
+    return o, lse
+
+
+def mosaic_bsa_prefix_decode(pp: PagedParams, q, k_pages, v_pages, prefix_table, prefix_len, table, k_len, q_len=None, o=None, lse=None,
+                             ws=None, stream=None):
+    """mosaic_bsa_paged_decode for a batch whose members all begin with the first `prefix_len` tokens of the pages that prefix_table
+    [>= prefix_len / page] int32 names; table, k_len and q_len count the members' own tokens.  No window.  Returns (o, lse)."""
+    index = _chk_seq(q, k_pages)
+    if prefix_len <= 0:
+        raise ValueError(f"prefix_len: expected at least one token, got {prefix_len}")
+    p, sk = _paged_params(pp, q, k_pages, table, prefix_len, index)
+    t, sq = q.dtype, q.shape
+    if prefix_table.dim() != 1 or prefix_table.shape[0] * sk[2] < prefix_len:
+        raise _bad("prefix_table", prefix_table, f"int32 [{-(-prefix_len // max(sk[2], 1))}] or more")
+    vq, vk, vv = _view("q", q, sq, t, index), _out("k_pages", k_pages, sk, t, index), _out("v_pages", v_pages, sk, t, index)
+    o = _like(q, stream) if o is None else o
+    lse = _rows_like(q, stream) if lse is None else lse
+    block = _block
+    a = block.at
+    try:
+        _paged_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
+    except _RANGE as e:
+        raise _out_of_range(e) from None
+    ws = _paged_ws(a, index, ws, stream)
+    _call("mosaic_bsa_prefix_decode", index, stream, a, a + 80, a + 112, a + 144,
+          _flat("prefix_table", prefix_table, prefix_table.shape, torch.int32, index), table.data_ptr(),
           _flat("k_len", k_len, (sq[0],), torch.int32, index), _len("q_len", q_len, sq[0], index), a + 176,
           _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
     return o, lse

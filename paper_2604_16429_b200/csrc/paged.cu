@@ -20,7 +20,7 @@ int check(const mosaic_paged_params* p, uint32_t flags) {
     return MOSAIC_E_INVALID_ARG;
   if (p->flags & ~flags) return MOSAIC_E_INVALID_ARG;
   if (p->d != 64 && p->d != 128) return MOSAIC_E_UNSUPPORTED;
-  if (p->page < kMinPage || (p->page & (p->page - 1)) || (long long)p->width * p->page > (1 << 30)) return MOSAIC_E_UNSUPPORTED;
+  if (p->page < kMinPage || p->page > kMaxPage || (p->page & (p->page - 1)) || (long long)p->width * p->page > (1 << 30)) return MOSAIC_E_UNSUPPORTED;
   if (p->table_stride > (1ll << 40)) return MOSAIC_E_UNSUPPORTED;
   return MOSAIC_OK;
 }
@@ -67,6 +67,15 @@ Layout layout(const mosaic_paged_params* p, int parts) {
   w.total = w.ml + align256((size_t)parts * rows * sizeof(float2));
   return w;
 }
+// The prefix' own
+int check_prefix(const mosaic_paged_params* p) {
+  if (p->prefix_len <= 0 || p->window || p->sinks) return MOSAIC_E_INVALID_ARG;
+  return p->prefix_len > (1 << 30) || (long long)p->B * p->H * p->Nq > (1 << 28) ? MOSAIC_E_UNSUPPORTED : MOSAIC_OK;
+}
+int shared_parts(const mosaic_paged_params* p, int* chunk) {
+  int keys;
+  return prefix_parts(p->prefix_len, p->Hkv, (long long)p->B * p->Nq * (p->H / p->Hkv), chunk ? chunk : &keys);
+}
 bool is_direct(const mosaic_paged_params* p) { return most_parts(p) == 1; }  // the part is the result
 
 }  // namespace
@@ -76,6 +85,36 @@ int check_pool(const mosaic_view* v, const mosaic_paged_params* p, View* out) {
   // (a place of its own for every row)
   return out->sn == 0 || (p->Hkv > 1 && out->sh == 0) || (p->pages > 1 && out->sb == 0) ? MOSAIC_E_UNSUPPORTED : MOSAIC_OK;
 }
+
+namespace {
+PartsOut parts_out(const mosaic_paged_params* p, void* ws, int shared, int all) {
+  const Layout w = layout(p, all);
+  return {(float*)((char*)ws + w.o), (float2*)((char*)ws + w.ml), (long long)p->B * p->H * p->Nq, shared};
+}
+// Tensors, buffers and device of an attention call, whose parameters have been checked
+struct Call {
+  HostCtx c;
+  PagedGeo g;
+  View q, k, v, o;
+  bool f16;
+};
+int make_call(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages, const int32_t* table,
+              const int32_t* k_len, const int32_t* q_len, const mosaic_view* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream,
+              Call* t) {
+  int rc;
+  if ((rc = check_view(q, p->B, p->H, p->Nq, 2, &t->q)) || (rc = check_pool(k_pages, p, &t->k)) || (rc = check_pool(v_pages, p, &t->v)) ||
+      (rc = check_view(o, p->B, p->H, p->Nq, 2, &t->o)) || (rc = make_geo(p, table, k_len, q_len, &t->g)))
+    return rc;
+  if (!lse || !ws) return MOSAIC_E_INVALID_ARG;
+  if (!aligned(lse, 4) || !aligned(ws, 256)) return MOSAIC_E_MISALIGNED;
+  if (ws_bytes < mosaic_bsa_paged_workspace_bytes(p)) return MOSAIC_E_WORKSPACE_TOO_SMALL;
+  t->c = {};
+  t->c.stream = (cudaStream_t)cuda_stream;
+  t->c.status = (int*)ws;
+  t->f16 = (p->flags & MOSAIC_FLAG_FP16) != 0;
+  return device_ok();
+}
+}  // namespace
 
 }  // namespace mosaic
 
@@ -109,8 +148,9 @@ int mosaic_bsa_paged_append(const mosaic_paged_params* p, const mosaic_view* k, 
 }
 
 size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params* p) {
-  if (check_attention(p) || p->prefix_len) return 0;
-  return is_direct(p) ? kStatusBytes : layout(p, most_parts(p)).total;
+  if (check_attention(p)) return 0;
+  if (!p->prefix_len) return is_direct(p) ? kStatusBytes : layout(p, most_parts(p)).total;
+  return check_prefix(p) ? 0 : layout(p, shared_parts(p, nullptr) + most_parts(p)).total;
 }
 
 int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages,
@@ -119,25 +159,30 @@ int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, 
   int rc = check_attention(p);
   if (rc) return rc;
   if (p->prefix_len) return MOSAIC_E_INVALID_ARG;
-  View vq, vk, vv, vo;
-  if ((rc = check_view(q, p->B, p->H, p->Nq, 2, &vq)) || (rc = check_pool(k_pages, p, &vk)) || (rc = check_pool(v_pages, p, &vv)) ||
-      (rc = check_view(o, p->B, p->H, p->Nq, 2, &vo)))
-    return rc;
-  PagedGeo g;
-  if ((rc = make_geo(p, table, k_len, q_len, &g))) return rc;
-  if (!lse || !ws) return MOSAIC_E_INVALID_ARG;
-  if (!aligned(lse, 4) || !aligned(ws, 256)) return MOSAIC_E_MISALIGNED;
-  if (ws_bytes < mosaic_bsa_paged_workspace_bytes(p)) return MOSAIC_E_WORKSPACE_TOO_SMALL;
-  if ((rc = device_ok())) return rc;
-  HostCtx c = {};
-  c.stream = (cudaStream_t)cuda_stream;
-  c.status = (int*)ws;
-  const bool f16 = (p->flags & MOSAIC_FLAG_FP16) != 0, direct = is_direct(p);
+  Call t;
+  if ((rc = make_call(p, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
+  const bool direct = is_direct(p);
   const int most = most_parts(p);
-  const Layout w = layout(p, most);
-  const PartsOut parts = {(float*)((char*)ws + w.o), (float2*)((char*)ws + w.ml), (long long)p->B * p->H * p->Nq, 0};
-  if ((rc = launch_paged_parts(c, g, f16, vq, vk, vv, parts, most, direct, true, vo, lse)) || direct) return rc;
-  return launch_paged_join(c, g, f16, parts, most, vo, lse);
+  const PartsOut parts = parts_out(p, ws, 0, most);
+  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.k, t.v, parts, most, direct, true, t.o, lse)) || direct) return rc;
+  return launch_paged_join(t.c, t.g, t.f16, parts, most, t.o, lse);
+}
+
+int mosaic_bsa_prefix_decode(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages,
+                             const int32_t* prefix_table, const int32_t* table, const int32_t* k_len, const int32_t* q_len,
+                             const mosaic_view* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream) {
+  int rc = check_attention(p);
+  if (rc || (rc = check_prefix(p))) return rc;
+  if (!prefix_table) return MOSAIC_E_INVALID_ARG;
+  if (!aligned(prefix_table, 4)) return MOSAIC_E_MISALIGNED;
+  Call t;
+  if ((rc = make_call(p, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
+  int chunk = 0;
+  const int shared = shared_parts(p, &chunk), most = most_parts(p);
+  const PartsOut parts = parts_out(p, ws, shared, shared + most);
+  if ((rc = launch_prefix_fwd(t.c, t.g, t.f16, t.q, t.k, t.v, prefix_table, p->prefix_len, chunk, parts))) return rc;
+  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.k, t.v, parts, most, false, false, t.o, lse))) return rc;
+  return launch_paged_join(t.c, t.g, t.f16, parts, shared + most, t.o, lse);
 }
 
 }  // extern "C"

@@ -5,8 +5,10 @@
 namespace mosaic {
 
 constexpr int kMinPage = 16;    // slots of a page at least: a step of the attention never leaves one
+constexpr int kMaxPage = 1 << 20;
 constexpr int kMaxNew = 16;     // new tokens a sequence that the attention takes
 constexpr int kChunkKeys = 512; // keys whose attention is one part, joined with the others at the end
+constexpr int kSms = 148;       // of the device that the kernels are built for
 
 // A pool of pages and the table that says which of them hold a member's tokens: token j lies in slot j % page of page
 // table[b][j / page].
@@ -72,6 +74,11 @@ int launch_paged_append(const HostCtx& c, const PagedGeo& g, const mosaic_paged_
 // results.  `clear`: the call's first kernel, which clears the status word.
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
                        const PartsOut& parts, int most_parts, bool direct, bool clear, const View& o, float* lse);
+// Attention over a prefix that all members share: its parts are the first of every row.  How it is cut follows from its length, the
+// key/value heads and the rows of a head; `chunk`: keys of a part.
+int prefix_parts(int len, int kv_heads, long long rows, int* chunk);
+int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
+                      const int32_t* prefix_table, int prefix_len, int chunk, const PartsOut& parts);
 // Joins all parts of every row
 int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const PartsOut& parts, int most_parts, const View& o, float* lse);
 // A map of a pool in boxes of 64 channels by `rows` slots

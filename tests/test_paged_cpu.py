@@ -31,7 +31,7 @@ def append(p=None, k=None, v=None, k_pages=None, v_pages=None, table=256, k_len=
 
 ANY = [(dict(B=0), -1), (dict(Hkv=0), -1), (dict(Nq=0), -1), (dict(pages=0), -1), (dict(width=0), -1), (dict(page=0), -1),
        (dict(page=-16), -1), (dict(table_stride=-1), -1), (dict(flags=1), -1), (dict(flags=4), -1), (dict(flags=64), -1), (dict(d=32), -2),
-       (dict(d=256), -2), (dict(page=8), -2), (dict(page=24), -2), (dict(page=1 << 20, width=1 << 11), -2), (dict(table_stride=1 << 41), -2)]
+       (dict(d=256), -2), (dict(page=8), -2), (dict(page=24), -2), (dict(page=1 << 20, width=1 << 11), -2), (dict(page=1 << 21, width=1), -2), (dict(table_stride=1 << 41), -2)]
 
 
 @pytest.mark.parametrize("kw,code", ANY + [
@@ -72,7 +72,8 @@ def decode(p=None, q=None, k_pages=None, v_pages=None, o=None, table=256, k_len=
     (dict(B=1 << 23), -2)])
 def test_bad_params_of_decode_are_refused(kw, code):
     assert decode(params(**kw)) == code
-    assert mb.lib().mosaic_bsa_paged_workspace_bytes(params(**kw)) == 0
+    if kw.get("prefix_len", 0) <= 0:  # (with one it is the size for a call behind a prefix)
+        assert mb.lib().mosaic_bsa_paged_workspace_bytes(params(**kw)) == 0
 
 
 def test_bad_tensors_of_decode_are_refused():
@@ -95,3 +96,36 @@ def test_workspaces():
     assert ws(params(width=33)) == part(2) and ws(params(width=320)) == part(10)
     assert ws(params(width=320, window=1)) == part(2) and ws(params(width=320, window=512)) == part(3)   # 514 keys end to end: three chunks
     assert ws(params(width=320, window=512, sinks=1)) == part(4) and ws(params(width=33, window=512, sinks=1)) == part(2)
+
+
+def prefix(p=None, table=256, prefix_table=256, k_len=256, lse=256, ws=256, n=1 << 40, q=None):
+    g = view()
+    return mb.lib().mosaic_bsa_prefix_decode(p or params(prefix_len=1000), q or g, g, g, prefix_table, table, k_len, None, g, lse, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", ANY + [
+    (dict(H=3), -1), (dict(window=5), -1), (dict(sinks=1), -1), (dict(prefix_len=0), -1), (dict(prefix_len=-1), -1), (dict(Nq=17), -2),
+    (dict(prefix_len=(1 << 30) + 1), -2), (dict(scale=float("nan")), -1), (dict(flags=32), -1)])
+def test_bad_params_behind_a_prefix_are_refused(kw, code):
+    kw = {"prefix_len": 1000, **kw}
+    assert prefix(params(**kw)) == code
+    if kw["prefix_len"]:
+        assert mb.lib().mosaic_bsa_paged_workspace_bytes(params(**kw)) == 0
+
+
+def test_bad_tensors_behind_a_prefix_are_refused():
+    assert prefix(prefix_table=None) == -1 and prefix(prefix_table=258) == -4 and prefix(table=None) == -1 and prefix(k_len=None) == -1
+    assert prefix(lse=None) == -1 and prefix(ws=None) == -1 and prefix(ws=272) == -4 and prefix(n=4096) == -3
+    assert prefix(q=view(256 + 8)) == -4 and prefix(q=view(0)) == -1
+
+
+def test_parts_of_a_prefix():
+    """The workspace holds the prefix' parts in front of the members' own: at least one, no more than steps of 64 keys or twice the SMs."""
+    ws = mb.lib().mosaic_bsa_paged_workspace_bytes
+    for B, H, Hkv, Nq, d in ((1, 1, 1, 1, 64), (64, 16, 4, 1, 128), (256, 16, 4, 4, 128), (33, 24, 3, 16, 64)):
+        for n in (1, 64, 65, 1000, 8191, 32768, 1 << 20, 1 << 30):
+            kw = dict(B=B, H=H, Hkv=Hkv, Nq=Nq, d=d, prefix_len=n)
+            rows = B * H * Nq
+            parts = (ws(params(**kw)) - 256) // (rows * (d * 4 + 8)) - 1  # (one part of the member's own: 512 tokens)
+            assert 1 <= parts <= min(-(-n // 64), 2 * 148 // Hkv + 2), (kw, parts)
+    assert ws(params(prefix_len=64)) == 256 + 2 * 24 * 64 * 4 + -(-2 * 24 * 8 // 256) * 256
