@@ -1,17 +1,18 @@
 // Attention of one or a few new tokens per sequence over a paged cache, and the join of its parts.
 //
 //   o_i = sum_j exp(scale q_i . k_j - m_i) v_j / l_i  over the keys that row i sees: j <= p_i, and p_i - j < window or j < sinks
-// HBM-bound: the visible keys and values of a key/value head are read once for all rows (new tokens x query heads of the group, up to
-// 16 at a time).  The keys of a member are cut into chunks of 512; a chunk of a head is an item.  Persistent CTAs, one an SM, take
-// equal shares of the list of all items, which each works out from the lengths; a CTA's items lie one after the other, so that a member's
-// queries stay in registers.
+// HBM-bound: the visible keys and values of a key/value head are read once for all rows (new tokens x query heads of the group, a
+// block of them at a time).  The keys of a member are cut into chunks of 512; a chunk of a head is an item.  Persistent CTAs, one an SM,
+// take equal shares of the list of all items, which each works out from the lengths; a CTA's items lie one after the other, so that a
+// member's queries stay in registers.
 //
-// A warp takes every eighth step of 16 keys of the chunk.  It asks for its own steps by TMA (pages are multiples of 16 slots, so a step
-// lies in one; the page numbers of an item's steps are looked up an item ahead) into a ring of its own, and goes on asking into
-// the next items, so that the memory never waits for a chunk's end.  Products of 16 x 8 x 16 are enough:
-//   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose
-// Weights round to 16 bits once, as operands; everything else is fp32.  The warps' maxima, sums and accumulators are joined through
-// shared memory at the chunk's end, and leave as a part; a second kernel joins a row's parts in their order.
+// One warp asks for steps of 64 keys by TMA, page by page (the page numbers of a chunk are looked up an item ahead), into a ring that
+// all warps share, and goes on asking into the next items, so that the memory never waits for a chunk's end.  The others take the
+// chunk's steps in turn, a step each: products of 16 x 8 x 16 are enough,
+//   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose,
+// and the step's 64 keys give every lane four of them that do not wait for one another.  Weights round to 16 bits once, as operands;
+// everything else is fp32.  The warps' maxima, sums and accumulators are joined through shared memory at the chunk's end, and leave as a
+// part; a second kernel joins a row's parts in their order.
 #include <type_traits>
 
 #include "mma16.cuh"
@@ -21,19 +22,25 @@ namespace mosaic {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kStep = 16, kWarpSteps = kChunkKeys / (kStep * kWarps);
+constexpr int kStep = 64, kSteps = kChunkKeys / kStep;
+// Barriers on which steps land, in turn.  A warp looks at its own steps only, and a wait on a phase's parity is exact only if the
+// barrier's phase before has completed: that is sure if it belongs to an earlier chunk, whose steps have all been taken.
+constexpr int kBars = 16;
+static_assert(kBars >= kSteps, "a step's barrier has been used by an earlier one of the chunk");
+constexpr int kMaxSmem = 232448;
 
 // NT: tiles of 8 rows that a CTA takes
 template <int D, int NT>
 struct Smem {
+  static constexpr int kWarps = 8 * NT * D > 1024 ? 4 : 8;  // that take steps: what they leave for one another has to fit
+  static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kHalf = kStep * D * 2, kStepBytes = 2 * kHalf;  // a step's keys, then its values
-  static constexpr int kStages = (NT == 1 ? 196608 : 131072) / (kWarps * kStepBytes);
+  static constexpr int kStages = D == 64 ? 10 : 6;
   static constexpr int kPitch = D + 4;  // of a row of part_o: lanes that store side by side meet different banks
-  unsigned char ring[kWarps][kStages][kStepBytes];
+  unsigned char ring[kStages][kStepBytes];
   float part_o[kWarps][8 * NT][kPitch], part_m[kWarps][8 * NT], part_l[kWarps][8 * NT];
-  unsigned long long full[kWarps][kStages];
-  int hole[kWarps][kStages];  // the step's page is not there
+  unsigned long long full[kBars], empty[kStages];
+  unsigned hole[kStages];  // the step's boxes whose page is not there, or which no row sees
   int scan[kWarps + 1], start[2];
   int abort;
 };
@@ -42,7 +49,8 @@ struct DecArgs {
   View q, o;
   float* lse;
   PartsOut parts;
-  int blocks;  // of rows
+  int blocks;     // of rows
+  int box_shift;  // log2 of the slots that a copy brings: a page, at most a step
   bool direct, clear;
   int* status;
 };
@@ -67,9 +75,13 @@ struct Walk {
       member(g, a);
     } while (p.n == 0);
   }
-  __device__ __forceinline__ int step(int warp, int i) const { return chunk_of(p, o) * kChunkKeys + (warp + kWarps * i) * kStep; }
-  // any row sees some of the step's keys
-  __device__ __forceinline__ bool seen(int j0) const { return j0 < p.kl && (j0 + kStep > p.from || j0 < p.sinks); }
+  __device__ __forceinline__ int key0() const { return chunk_of(p, o) * kChunkKeys; }
+  // any row sees some of the n keys from j on
+  __device__ __forceinline__ bool seen(int j, int n) const { return j < p.kl && (j + n > p.from || j < p.sinks); }
+  // the chunk's steps that are, by the whole warp
+  __device__ __forceinline__ unsigned steps(int lane) const {
+    return __ballot_sync(0xffffffffu, lane < kSteps && seen(key0() + lane * kStep, kStep));
+  }
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
@@ -80,6 +92,7 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
 }
 
 // Sum of v over the threads before this one, and over all
+template <int WARPS>
 __device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int x = v;
@@ -93,7 +106,7 @@ __device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < WARPS; ++w) {
     before += w < warp ? scan[w] : 0;
     total += scan[w];
   }
@@ -102,17 +115,17 @@ __device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
 }
 
 template <int D, bool F16, int NT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     paged_parts_kernel(const PagedGeo g, const __grid_constant__ DecArgs a, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v) {
   using S = Smem<D, NT>;
-  constexpr int kRowsCta = 8 * NT, kStages = S::kStages;
+  constexpr int kRowsCta = 8 * NT, kStages = S::kStages, kWarps = S::kWarps, kThreads = S::kThreads;
   extern __shared__ unsigned char smem_raw[];
   S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
   if (tid == 0) {
-    for (int w = 0; w < kWarps; ++w)
-      for (int s = 0; s < kStages; ++s) mbar_init(s32(&sm.full[w][s]), 1);
+    for (int s = 0; s < kBars; ++s) mbar_init(s32(&sm.full[s]), 1);
+    for (int s = 0; s < kStages; ++s) mbar_init(s32(&sm.empty[s]), 1);
     sm.abort = 0;
     cta_publish_barriers();
   }
@@ -120,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int zero = await_stream();
   // A code is written no earlier than a wait's bound of seconds after its CTA began; the first CTA has cleared the word by then.
   if (a.clear && blockIdx.x == 0 && tid == 0) a.status[zero] = 0;
+  volatile int* abort = &sm.abort;
 
   // ---- this CTA's share of the list
   const int per = g.Hkv * a.blocks;
@@ -134,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     for (int b0 = 0; b0 < g.B; b0 += kThreads) {
       int all;
-      before = block_scan(items(b0 + tid + zero), sm.scan, all);
+      before = block_scan<kWarps + 1>(items(b0 + tid + zero), sm.scan, all);
       total += all;
     }
     const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
@@ -143,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int base = 0;
     for (int b0 = 0; b0 < g.B; b0 += kThreads) {
       int all = 0;
-      if (g.B > kThreads) before = block_scan(items(b0 + tid + zero), sm.scan, all);
+      if (g.B > kThreads) before = block_scan<kWarps + 1>(items(b0 + tid + zero), sm.scan, all);
       const int n = w.b < g.B ? w.p.n * per : 0, at = lo - base - before;
       if (at >= 0 && at < n) {
         sm.start[0] = w.b;
@@ -159,62 +173,66 @@ __global__ void __launch_bounds__(kThreads, 1)
     w.o = r / a.blocks;
     w.rb = r % a.blocks;
   }
+  bool ok = true;
 
-  // ---- the warp's steps on their way: an item is looked up while the one before is asked for
-  Walk look = w;
-  int looked = left, f_hk = 0, f_at = 0, f_id = 0, n_hk = 0, n_at = 0, n_id = 0, slot_in = 0;
-  unsigned f_mask = 0, n_mask = 0;
-  bool more = true, ok = true;
-  uint32_t issued = 0, taken = 0;
-  auto look_up = [&]() {
-    more = looked > 0;
-    if (!more) return;
-    const int j0 = look.step(warp, lane & (kWarpSteps - 1));
-    const bool seen = lane < kWarpSteps && look.seen(j0);
-    n_mask = __ballot_sync(0xffffffffu, seen);
-    n_id = seen ? __ldg(g.table + look.b * g.table_stride + (j0 >> g.shift)) : -1;
-    n_hk = look.hk;
-    n_at = look.step(warp, 0);
-    --looked;
-    if (looked > 0) look.next(g, a);
-  };
-  look_up();
-  auto fetch = [&]() {
+  if (warp == kWarps) {
+    // ------------------------------------------------------------- copies
 #ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
-    return;  // test build only: nothing is ever loaded, so that every wait for it runs out
+    left = 0;  // test build only: nothing is ever loaded, so that every wait for it runs out
 #endif
-    while (f_mask == 0) {
-      if (!more) return;
-      f_mask = n_mask;
-      f_hk = n_hk;
-      f_at = n_at;
-      f_id = n_id;
-      look_up();
-    }
-    const int i = __ffs(f_mask) - 1;
-    f_mask &= f_mask - 1;
-    const int id = __shfl_sync(0xffffffffu, f_id, i);
-    if (lane == 0) {
-      const bool hole = (unsigned)id >= (unsigned)g.pages;
-      const int page = hole ? g.pages : id;  // (rows behind the last page arrive as zeros)
-      const int slot = (f_at + kWarps * kStep * i) & ((1 << g.shift) - 1);
-      const uint32_t bar = s32(&sm.full[warp][slot_in]), dst = s32(sm.ring[warp][slot_in]);
-      sm.hole[warp][slot_in] = hole;
-      mbar_expect_tx(bar, S::kStepBytes);
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kStep * 128, &map_k, bar, 64 * c, slot, f_hk, page);
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + S::kHalf + c * kStep * 128, &map_v, bar, 64 * c, slot, f_hk, page);
-    }
-    __syncwarp();
-    slot_in = slot_in + 1 == kStages ? 0 : slot_in + 1;
-    ++issued;
-  };
+    const int box = 1 << a.box_shift, boxes = kStep >> a.box_shift;  // a lane has one of the chunk's boxes
+    const uint32_t box_bytes = (uint32_t)box * 128;
+    int id = 0;
+    // the page of this lane's box, or g.pages: rows behind the last page arrive as zeros
+    auto look_up = [&]() {
+      const int key = w.key0() + (lane << a.box_shift);
+      int t = -1;
+      if (lane < kSteps * boxes && w.seen(key, box)) t = __ldg(g.table + w.b * g.table_stride + (key >> g.shift));
+      return t;
+    };
+    uint32_t stage = 0, phase = 0, issued = 0;
+    if (left > 0) id = look_up();
 #pragma unroll 1
-  for (int s = 0; s < kStages; ++s) fetch();
+    for (; left > 0 && ok; --left) {
+      const unsigned steps = w.steps(lane);
+      const int hk = w.hk, slot = (w.key0() + (lane << a.box_shift)) & ((1 << g.shift) - 1);
+      const bool hole = (unsigned)id >= (unsigned)g.pages;
+      const int page = hole ? g.pages : id;
+      const unsigned holes = __ballot_sync(0xffffffffu, hole);
+      if (left > 1) {
+        w.next(g, a);
+        id = look_up();
+      }
+      for (unsigned todo = steps; todo; todo &= todo - 1) {
+        const int s = __ffs(todo) - 1, first = s * boxes;
+        ok = warp_wait(s32(&sm.empty[stage]), phase ^ 1, abort, a.status);
+        if (!ok) break;
+        const uint32_t bar = s32(&sm.full[issued % kBars]), dst = s32(sm.ring[stage]) + (lane - first) * box_bytes;
+        if (lane == 0) {
+          sm.hole[stage] = (holes >> first) & low_bits(boxes);
+          mbar_expect_tx(bar, S::kStepBytes);
+        }
+        __syncwarp();
+        if (lane >= first && lane < first + boxes) {
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kStep * 128, &map_k, bar, 64 * c, slot, hk, page);
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + S::kHalf + c * kStep * 128, &map_v, bar, 64 * c, slot, hk, page);
+        }
+        __syncwarp();
+        ++issued;
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+    }
+    // copies must have landed before the CTA's memory is released (their readers have waited for them, unless a wait ran out)
+    if (*abort && lane == 0)
+      for (uint32_t n = issued > kStages ? issued - kStages : 0; n < issued; ++n) mbar_drain(s32(&sm.full[n % kBars]), (n / kBars) & 1);
+    return;
+  }
 
-  // ---- items
-  int slot_out = 0, phase = 0, have_b = -1, have_hk = -1, have_rb = -1;
+  // ------------------------------------------------------------- items
+  uint32_t taken = 0;  // steps of the items so far, all warps'
+  int have_b = -1, have_hk = -1, have_rb = -1;
   uint32_t qf[NT][D / 16][2];
   const int rows = g.G * g.T;
   const uint32_t ka = (uint32_t)((lane & 15) * 128), kx = (uint32_t)(lane & 7), kh = (uint32_t)(lane >> 4);           // keys as they lie
@@ -250,87 +268,98 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) acc[nt][c][0] = acc[nt][c][1] = acc[nt][c][2] = acc[nt][c][3] = 0.f;
     }
+    const unsigned steps = w.steps(lane);
 #pragma unroll 1
-    for (int i = 0; i < kWarpSteps; ++i) {
-      const int j0 = w.step(warp, i);
-      if (!ok || !w.seen(j0)) continue;
-      ok = warp_wait(s32(&sm.full[warp][slot_out]), phase, &sm.abort, a.status);
+    for (int s = warp; s < kSteps; s += kWarps) {
+      if (!ok || !((steps >> s) & 1u)) continue;
+      const int j0 = w.key0() + s * kStep;
+      const uint32_t at = taken + __popc(steps & low_bits(s)), stage = at % kStages;
+      ok = warp_wait(s32(&sm.full[at % kBars]), (at / kBars) & 1, abort, a.status);
       if (!ok) continue;
-      const uint32_t kt = s32(sm.ring[warp][slot_out]), vt = kt + S::kHalf;
-      if (!sm.hole[warp][slot_out]) {
-        // all rows see all of the step
-        const bool whole = j0 + kStep - 1 <= w.p.p0 && (!g.window || j0 >= w.p.kl - g.window || j0 + kStep <= w.p.sinks);
-        if (!whole) {  // a weight of zero does not silence what is no number: values that no row sees become zeros
-          for (int r = 0; r < kStep; ++r) {
-            const int j = j0 + r;
-            if ((j >= w.p.kl || (j < w.p.from && j >= w.p.sinks)) && lane < D / 8)
-              *reinterpret_cast<uint4*>(sm.ring[warp][slot_out] + S::kHalf + (lane >> 3) * kStep * 128 + r * 128 + (lane & 7) * 16) =
-                  make_uint4(0u, 0u, 0u, 0u);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the next copy into the slot comes after these stores)
-          __syncwarp();
+      const uint32_t kt = s32(sm.ring[stage]), vt = kt + S::kHalf;
+      const unsigned hole = sm.hole[stage];
+      // all rows see all of the step
+      const bool whole = !hole && j0 + kStep - 1 <= w.p.p0 && (!g.window || j0 >= w.p.kl - g.window || j0 + kStep <= w.p.sinks);
+      if (!whole) {  // a weight of zero does not silence what is no number: values that no row sees become zeros
+        for (int e = lane; e < kStep * D / 8; e += 32) {
+          const int r = e / (D / 8), c = e - r * (D / 8), j = j0 + r;
+          if (j >= w.p.kl || (j < w.p.from && j >= w.p.sinks))
+            *reinterpret_cast<uint4*>(sm.ring[stage] + S::kHalf + (c >> 3) * kStep * 128 + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
-        float s[NT][2][4];  // in two chains
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the next copy into the stage comes after these stores)
+        __syncwarp();
+      }
+      float z[NT][4][4];  // [keys 16 k ..]: (key gq, row 2 tq), (gq, 2 tq + 1), (gq + 8, 2 tq), (gq + 8, 2 tq + 1)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) s[nt][x][0] = s[nt][x][1] = s[nt][x][2] = s[nt][x][3] = 0.f;
+        for (int k = 0; k < 4; ++k) z[nt][k][0] = z[nt][k][1] = z[nt][k][2] = z[nt][k][3] = 0.f;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
           uint32_t f[4];
-          ldsm4(f, kt + (c >> 2) * kStep * 128 + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
+          ldsm4(f, kt + (c >> 2) * kStep * 128 + k * 2048 + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(s[nt][c & 1], f[0], f[1], f[2], f[3], qf[nt][c][0], qf[nt][c][1]);
+          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(z[nt][k], f[0], f[1], f[2], f[3], qf[nt][c][0], qf[nt][c][1]);
         }
-        uint32_t pt[NT][2];
+      uint32_t pt[NT][4][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float z[4];  // (key gq, row 2 tq), (gq, 2 tq + 1), (gq + 8, 2 tq), (gq + 8, 2 tq + 1)
+      for (int nt = 0; nt < NT; ++nt) {
+        if (!whole) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            z[x] = (s[nt][0][x] + s[nt][1][x]) * g.scale_log2;
-            if (!whole) {
-              const int j = j0 + gq + 4 * (x & 2), p = last[nt][x & 1];
-              if (j > p || (g.window && p - j >= g.window && j >= w.p.sinks)) z[x] = -INFINITY;
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int j = j0 + 16 * k + gq + 4 * (x & 2), p = last[nt][x & 1];
+              if (j > p || (g.window && p - j >= g.window && j >= w.p.sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u)) z[nt][k][x] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float mx = fmaxf(z[nt][0][x], z[nt][0][x + 2]);
+#pragma unroll
+          for (int k = 1; k < 4; ++k) mx = max3(mx, z[nt][k][x], z[nt][k][x + 2]);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16)) * g.scale_log2;  // scale > 0 commutes with max
+          if (mx > m[nt][x]) {  // (the same in the eight lanes of the row)
+            const float alpha = ex2(m[nt][x] - mx);
+            m[nt][x] = mx;
+            l[nt][x] *= alpha;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              acc[nt][c][x] *= alpha;
+              acc[nt][c][x + 2] *= alpha;
             }
           }
+          const float ref = m[nt][x] == -INFINITY ? 0.f : -m[nt][x];  // (nothing seen so far)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            float mx = fmaxf(z[x], z[x + 2]);
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            if (mx > m[nt][x]) {  // (the same in the eight lanes of the row)
-              const float alpha = ex2(m[nt][x] - mx);
-              m[nt][x] = mx;
-              l[nt][x] *= alpha;
-#pragma unroll
-              for (int c = 0; c < D / 16; ++c) {
-                acc[nt][c][x] *= alpha;
-                acc[nt][c][x + 2] *= alpha;
-              }
-            }
-            const float ref = m[nt][x] == -INFINITY ? 0.f : m[nt][x];  // (nothing seen so far)
-            z[x] = ex2(z[x] - ref);
-            z[x + 2] = ex2(z[x + 2] - ref);
-            l[nt][x] += z[x] + z[x + 2];
+          for (int k = 0; k < 4; ++k) {
+            z[nt][k][x] = ex2(fmaf(z[nt][k][x], g.scale_log2, ref));
+            z[nt][k][x + 2] = ex2(fmaf(z[nt][k][x + 2], g.scale_log2, ref));
+            l[nt][x] += z[nt][k][x] + z[nt][k][x + 2];
           }
-          pt[nt][0] = transpose8(pack2<F16>(z[0], z[1]));
-          pt[nt][1] = transpose8(pack2<F16>(z[2], z[3]));
         }
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          uint32_t f[4];
-          ldsm4t(f, vt + (c >> 2) * kStep * 128 + va + (((2 * (c & 3) + vh) ^ kx) << 4));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(acc[nt][c], f[0], f[1], f[2], f[3], pt[nt][0], pt[nt][1]);
+        for (int k = 0; k < 4; ++k) {
+          pt[nt][k][0] = transpose8(pack2<F16>(z[nt][k][0], z[nt][k][1]));
+          pt[nt][k][1] = transpose8(pack2<F16>(z[nt][k][2], z[nt][k][3]));
         }
       }
-      __syncwarp();  // the slot has been read
-      ++taken;
-      if (++slot_out == kStages) { slot_out = 0; phase ^= 1; }
-      fetch();
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t f[4];
+          ldsm4t(f, vt + (c >> 2) * kStep * 128 + k * 2048 + va + (((2 * (c & 3) + vh) ^ kx) << 4));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(acc[nt][c], f[0], f[1], f[2], f[3], pt[nt][k][0], pt[nt][k][1]);
+        }
+      __syncwarp();  // the stage has been read
+      if (lane == 0) mbar_arrive(s32(&sm.empty[stage]));
     }
+    taken += __popc(steps);
 
     // the warps' parts
 #pragma unroll
@@ -352,8 +381,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           sm.part_o[warp][h][16 * c + gq + 8] = acc[nt][c][x + 2];
         }
       }
-    __syncthreads();
-    for (int e = tid; e < kRowsCta * D / 4; e += kThreads) {
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
+    for (int e = tid; e < kRowsCta * D / 4; e += 32 * kWarps) {
       const int h = e / (D / 4), c = 4 * (e - h * (D / 4)), r = w.rb * kRowsCta + h, i = r / g.G;
       if (r >= rows || i >= w.p.ql) continue;
       float mx = -INFINITY, sum = 0.f;
@@ -384,24 +413,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (c == 0) a.parts.ml[at] = make_float2(mx, sum);
       }
     }
-    __syncthreads();  // the parts have been read
-    w.next(g, a);
-  }
-  // copies must have landed before the CTA's memory is released
-  if (!ok && lane == 0)
-    for (; taken < issued; ++taken) {
-      mbar_drain(s32(&sm.full[warp][slot_out]), phase);
-      if (++slot_out == kStages) { slot_out = 0; phase ^= 1; }
+    if (left > 1) {
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");  // the parts have been read
+      w.next(g, a);
     }
+  }
 }
+
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
 // A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.
 template <int D, bool F16, int W>
-__global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
   constexpr int V = D / 32;  // channels of a lane
-  __shared__ float part_o[kWarps][D], part_l[kWarps];
+  __shared__ float part_o[kJoinWarps][D], part_l[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
-  const long long row = (long long)blockIdx.x * (kWarps / W) + warp / W + await_stream();
+  const long long row = (long long)blockIdx.x * (kJoinWarps / W) + warp / W + await_stream();
   bool live = row < in.rows;
   const int i = (int)(row % g.T), head = (int)(row / g.T % g.H), b = live ? (int)(row / g.T / g.H) : 0;
   const Parts p = parts_of(g, b);
@@ -456,22 +483,23 @@ __global__ void __launch_bounds__(kThreads) paged_join_kernel(const PagedGeo g, 
 template <int D, bool F16, int NT>
 int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const View& k_pages, const View& v_pages, int most_parts) {
   CUtensorMap mk, mv;
-  if (!make_map_pool(&mk, k_pages, g, kStep) || !make_map_pool(&mv, v_pages, g, kStep)) return MOSAIC_E_CUDA;
-  const size_t smem = sizeof(Smem<D, NT>) + 1024;
-  static_assert(sizeof(Smem<D, NT>) + 1024 <= 232448, "more shared memory than a CTA can have");
+  a.box_shift = g.shift < 6 ? g.shift : 6;
+  if (!make_map_pool(&mk, k_pages, g, 1 << a.box_shift) || !make_map_pool(&mv, v_pages, g, 1 << a.box_shift)) return MOSAIC_E_CUDA;
+  constexpr size_t smem = sizeof(Smem<D, NT>) + 1024;
+  static_assert(smem <= kMaxSmem, "more shared memory than a CTA can have");
   static unsigned long long configured = 0;
   int sms = 0;
   if (const int rc = launch_setup(reinterpret_cast<const void*>(paged_parts_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
   a.blocks = (g.G * g.T + 8 * NT - 1) / (8 * NT);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
   if (most > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
-  return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), kThreads, smem, c.stream, true, 0, g, a, mk, mv);
+  return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, mk, mv);
 }
 
 template <int D, bool F16, int W>
 int launch_join(const HostCtx& c, const PagedGeo& g, const PartsOut& parts, const View& o, float* lse) {
-  constexpr int per = kWarps / W;
-  return launch_kernel(paged_join_kernel<D, F16, W>, dim3((unsigned)((parts.rows + per - 1) / per)), kThreads, 0, c.stream, true, 0, g, parts, o, lse);
+  constexpr int per = kJoinWarps / W;
+  return launch_kernel(paged_join_kernel<D, F16, W>, dim3((unsigned)((parts.rows + per - 1) / per)), kJoinThreads, 0, c.stream, true, 0, g, parts, o, lse);
 }
 
 // f(head dimension, type) as constants
@@ -486,10 +514,12 @@ int by_type(int d, bool f16, F&& f) {
 
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
                        const PartsOut& parts, int most_parts, bool direct, bool clear, const View& o, float* lse) {
-  const DecArgs a = {q, o, lse, parts, 0, direct, clear, c.status};
+  const DecArgs a = {q, o, lse, parts, 0, 0, direct, clear, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
+    if constexpr (D == 64)
+      if (g.G * g.T > 16) return launch_parts<D, F16, 4>(c, g, a, k_pages, v_pages, most_parts);
     return g.G * g.T > 8 ? launch_parts<D, F16, 2>(c, g, a, k_pages, v_pages, most_parts)
                          : launch_parts<D, F16, 1>(c, g, a, k_pages, v_pages, most_parts);
   });
@@ -499,7 +529,7 @@ int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const Parts
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
-    return most_parts > 8 ? launch_join<D, F16, kWarps>(c, g, parts, o, lse) : launch_join<D, F16, 1>(c, g, parts, o, lse);
+    return most_parts > 8 ? launch_join<D, F16, kJoinWarps>(c, g, parts, o, lse) : launch_join<D, F16, 1>(c, g, parts, o, lse);
   });
 }
 
