@@ -71,9 +71,9 @@ int launch_paged_append(const HostCtx& c, const PagedGeo& g, const mosaic_paged_
 
 
 // Attention over the members' own pages: parts to the workspace, or, where a member can have but one and there is no prefix (`direct`),
-// results.  `clear`: the call's first kernel, which clears the status word.
+// results.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                       const PartsOut& parts, int most_parts, bool direct, bool clear, const View& o, float* lse);
+                       const PartsOut& parts, int most_parts, bool direct, bool first, const View& o, float* lse);
 // Attention over a prefix that all members share: its parts are the first of every row.  How it is cut follows from its length, the
 // key/value heads and the rows of a head; `chunk`: keys of a part.
 int prefix_parts(int len, int kv_heads, long long rows, int* chunk);

@@ -6,9 +6,10 @@
 // take equal shares of the list of all items, which each works out from the lengths; a CTA's items lie one after the other, so that a
 // member's queries stay in registers.
 //
-// One warp asks for steps of 64 keys by TMA, page by page (the page numbers of a chunk are looked up an item ahead), into a ring that
-// all warps share, and goes on asking into the next items, so that the memory never waits for a chunk's end.  The others take the
-// chunk's steps in turn, a step each: products of 16 x 8 x 16 are enough,
+// One warp finds the items, and for each leaves a note of what the others need to know of it, copies its queries, and asks for its steps of
+// 64 keys by TMA, page by page (the page numbers of a chunk are looked up an item ahead), into a ring that all warps share; it goes on
+// into the next items, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a step each:
+// products of 16 x 8 x 16 are enough,
 //   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose,
 // and the step's 64 keys give every lane four of them that do not wait for one another.  Weights round to 16 bits once, as operands;
 // everything else is fp32.  The warps' maxima, sums and accumulators are joined through shared memory at the chunk's end, and leave as a
@@ -29,17 +30,32 @@ constexpr int kBars = 16;
 static_assert(kBars >= kSteps, "a step's barrier has been used by an earlier one of the chunk");
 constexpr int kMaxSmem = 232448;
 
+constexpr int kJobs = 3;  // items that the first warp may be ahead
+
+// What the others need to know of an item
+struct alignas(16) Job {
+  int b, head0, rb, part;            // member, first query head of the group, block of rows, place among all parts
+  int kl, ql, p0, from;              // as in Parts
+  int sinks, key0;                   // first position of the chunk
+  unsigned steps;                    // of the chunk, that any row sees something of
+  int more;                          // 0: no item, and none will come
+};
+
 // NT: tiles of 8 rows that a CTA takes
 template <int D, int NT>
 struct Smem {
-  static constexpr int kWarps = 8 * NT * D > 1024 ? 4 : 8;  // that take steps: what they leave for one another has to fit
+  static constexpr int kWarps = 8;  // that take steps
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kHalf = kStep * D * 2, kStepBytes = 2 * kHalf;  // a step's keys, then its values
-  static constexpr int kStages = D == 64 ? 10 : 6;
   static constexpr int kPitch = D + 4;  // of a row of part_o: lanes that store side by side meet different banks
+  static constexpr int kRowBytes = D * 2;
+  static constexpr int kOther = 4 * kWarps * 8 * NT * (kPitch + 2) + kJobs * (8 * NT * kRowBytes + (int)sizeof(Job)) + 1024;
+  static constexpr int kRoom = (kMaxSmem - 1024 - kOther) / kStepBytes, kStages = kRoom < 12 ? kRoom : 12;
   unsigned char ring[kStages][kStepBytes];
+  unsigned char q[kJobs][8 * NT * kRowBytes];  // 16-byte pieces of a row swizzled by its number
   float part_o[kWarps][8 * NT][kPitch], part_m[kWarps][8 * NT], part_l[kWarps][8 * NT];
-  unsigned long long full[kBars], empty[kStages];
+  Job job[kJobs];
+  unsigned long long full[kBars], empty[kStages], job_full[kJobs], job_empty[kJobs], parts_full, parts_read;
   unsigned hole[kStages];  // the step's boxes whose page is not there, or which no row sees
   int scan[kWarps + 1], start[2];
   int abort;
@@ -51,19 +67,49 @@ struct DecArgs {
   PartsOut parts;
   int blocks;     // of rows
   int box_shift;  // log2 of the slots that a copy brings: a page, at most a step
-  bool direct, clear;
+  bool direct, first;
   int* status;
 };
 
-// A place in the list of all items: members, their heads, their parts, blocks of rows
+// A place in the list of all items: members, their heads, their parts, blocks of rows.  Items weigh their steps and kTurn for what comes
+// with every one; `pos` is the weight of all items before.
+constexpr int kTurn = 2, kFull = kSteps + kTurn;
 struct Walk {
   Parts p;
-  int b, hk, o, rb;
+  int b, hk, o, rb, pos;
   __device__ __forceinline__ void member(const PagedGeo& g, const DecArgs& a) {
     p = parts_of(g, b);
     if (a.direct) p.n = p.ql > 0 ? 1 : 0;  // (a member without keys has results too)
   }
+  __device__ __forceinline__ int weight(int part) const {
+    if (p.front && part == 0) return (p.sinks + kStep - 1) / kStep + kTurn;
+    const int s = chunk_of(p, part) * kSteps;
+    return min(s + kSteps - 1, (p.kl - 1) >> 6) - max(s, p.from >> 6) + 1 + kTurn;
+  }
+  // of the parts before `part`: only the first two and the last may be short
+  __device__ __forceinline__ int weight_before(int part) const {
+    return part == 0 ? 0 : part == 1 ? weight(0) : weight(0) + weight(1) + (part - 2) * kFull;
+  }
+  __device__ __forceinline__ int weight_of_head(const DecArgs& a) const { return p.n ? a.blocks * (weight_before(p.n - 1) + weight(p.n - 1)) : 0; }
+  // To the first item of the member (of weight `base` before it) that does not begin before weight `to`, or behind the member
+  __device__ __forceinline__ void seek(const PagedGeo& g, const DecArgs& a, int base, int to) {
+    const int head = weight_of_head(a), at = max(to - base, 0);
+    hk = at / head;
+    const int y = at - hk * head;
+    o = 0;
+    if (p.n > 2 && y >= a.blocks * weight_before(2)) o = min(p.n - 1, 2 + (y - a.blocks * weight_before(2)) / (a.blocks * kFull));
+    else if (p.n > 1 && y >= a.blocks * weight_before(1)) o = 1;
+    const int rest = y - a.blocks * weight_before(o), each = weight(o);
+    rb = (rest + each - 1) / each;
+    pos = base + hk * head + a.blocks * weight_before(o) + rb * each;
+    if (rb == a.blocks) {
+      rb = a.blocks - 1;
+      pos -= each;
+      next(g, a);
+    }
+  }
   __device__ __forceinline__ void next(const PagedGeo& g, const DecArgs& a) {
+    pos += weight(o);
     if (++rb < a.blocks) return;
     rb = 0;
     if (++o < p.n) return;
@@ -83,6 +129,7 @@ struct Walk {
     return __ballot_sync(0xffffffffu, lane < kSteps && seen(key0() + lane * kStep, kStep));
   }
 };
+static_assert(kStep == 64, "weights count steps by shifts");
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -126,83 +173,123 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < kBars; ++s) mbar_init(s32(&sm.full[s]), 1);
     for (int s = 0; s < kStages; ++s) mbar_init(s32(&sm.empty[s]), 1);
+    for (int s = 0; s < kJobs; ++s) {
+      mbar_init(s32(&sm.job_full[s]), 33);  // the note, and every lane's copies
+      mbar_init(s32(&sm.job_empty[s]), kWarps);
+    }
+    mbar_init(s32(&sm.parts_full), kWarps);
+    mbar_init(s32(&sm.parts_read), kWarps);
     sm.abort = 0;
     cta_publish_barriers();
   }
   __syncthreads();
-  const int zero = await_stream();
+  // (behind a prefix the kernel ahead is the prefix', whose results only the join reads)
+  const int zero = a.first ? await_stream() : pass_stream();
   // A code is written no earlier than a wait's bound of seconds after its CTA began; the first CTA has cleared the word by then.
-  if (a.clear && blockIdx.x == 0 && tid == 0) a.status[zero] = 0;
+  if (a.first && blockIdx.x == 0 && tid == 0) a.status[zero] = 0;
   volatile int* abort = &sm.abort;
 
-  // ---- this CTA's share of the list
-  const int per = g.Hkv * a.blocks;
-  Walk w;
-  int left, total = 0, before = 0;
+  // ---- this CTA's share of the list: the items that begin in its share of the weight
+  int begin, end;
   {
-    auto items = [&](int b) {
+    Walk w;
+    int total = 0, before = 0;
+    auto weight = [&](int b) {
       w.b = b;
       if (b >= g.B) return 0;
       w.member(g, a);
-      return w.p.n * per;
+      return w.weight_of_head(a) * g.Hkv;
     };
     for (int b0 = 0; b0 < g.B; b0 += kThreads) {
       int all;
-      before = block_scan<kWarps + 1>(items(b0 + tid + zero), sm.scan, all);
+      before = block_scan<kWarps + 1>(weight(b0 + tid + zero), sm.scan, all);
       total += all;
     }
-    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
-    left = hi - lo;
-    if (left == 0) return;
+    begin = (int)((long long)total * blockIdx.x / gridDim.x);
+    end = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
     int base = 0;
     for (int b0 = 0; b0 < g.B; b0 += kThreads) {
       int all = 0;
-      if (g.B > kThreads) before = block_scan<kWarps + 1>(items(b0 + tid + zero), sm.scan, all);
-      const int n = w.b < g.B ? w.p.n * per : 0, at = lo - base - before;
+      if (g.B > kThreads) before = block_scan<kWarps + 1>(weight(b0 + tid + zero), sm.scan, all);
+      const int n = w.b < g.B ? w.weight_of_head(a) * g.Hkv : 0, at = begin - base - before;
       if (at >= 0 && at < n) {
         sm.start[0] = w.b;
-        sm.start[1] = at;
+        sm.start[1] = base + before;
       }
       base += all;
     }
     __syncthreads();
-    w.b = sm.start[0];
-    w.member(g, a);
-    const int at = sm.start[1], r = at % (w.p.n * a.blocks);
-    w.hk = at / (w.p.n * a.blocks);
-    w.o = r / a.blocks;
-    w.rb = r % a.blocks;
   }
-  bool ok = true;
+  const int rows = g.G * g.T;
 
   if (warp == kWarps) {
-    // ------------------------------------------------------------- copies
-#ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
-    left = 0;  // test build only: nothing is ever loaded, so that every wait for it runs out
-#endif
+    // ------------------------------------------------------------- items and copies
     const int box = 1 << a.box_shift, boxes = kStep >> a.box_shift;  // a lane has one of the chunk's boxes
     const uint32_t box_bytes = (uint32_t)box * 128;
-    int id = 0;
-    // the page of this lane's box, or g.pages: rows behind the last page arrive as zeros
+    Walk w;
+    bool more = begin < end;
+    if (more) {
+      w.b = sm.start[0];
+      w.member(g, a);
+      w.seek(g, a, sm.start[1], begin);
+      more = w.pos < end;
+    }
+#ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
+    bool ok = false;  // test build only: nothing is ever handed out or loaded, so that every wait for it runs out
+#else
+    bool ok = true;
+#endif
+    // the page number of this lane's box, or none if no row sees anything of it
     auto look_up = [&]() {
       const int key = w.key0() + (lane << a.box_shift);
       int t = -1;
       if (lane < kSteps * boxes && w.seen(key, box)) t = __ldg(g.table + w.b * g.table_stride + (key >> g.shift));
       return t;
     };
-    uint32_t stage = 0, phase = 0, issued = 0;
-    if (left > 0) id = look_up();
+    uint32_t stage = 0, phase = 0, issued = 0, slot = 0, round = 0;
+    int id = more ? look_up() : 0;
 #pragma unroll 1
-    for (; left > 0 && ok; --left) {
-      const unsigned steps = w.steps(lane);
-      const int hk = w.hk, slot = (w.key0() + (lane << a.box_shift)) & ((1 << g.shift) - 1);
-      const bool hole = (unsigned)id >= (unsigned)g.pages;
-      const int page = hole ? g.pages : id;
-      const unsigned holes = __ballot_sync(0xffffffffu, hole);
-      if (left > 1) {
-        w.next(g, a);
-        id = look_up();
+    while (ok) {
+      ok = warp_wait(s32(&sm.job_empty[slot]), round ^ 1, abort, a.status);
+      if (!ok) break;
+      const uint32_t job_bar = s32(&sm.job_full[slot]);
+      if (!more) {
+        if (lane == 0) sm.job[slot].more = 0;
+        mbar_arrive(job_bar);
+        if (lane == 0) mbar_arrive(job_bar);
+        break;
       }
+      const unsigned steps = w.steps(lane);
+      const int key0 = w.key0(), hk = w.hk;
+      {  // the queries: row by row, whatever their strides
+        const uint32_t dst = s32(sm.q[slot]);
+        const char* src = a.q.data + w.b * a.q.sb + hk * g.G * a.q.sh;
+#pragma unroll
+        for (int e0 = 0; e0 < kRowsCta * D / 8; e0 += 32) {
+          const int e = e0 + lane, row = e / (D / 8), c = e % (D / 8), r = min(w.rb * kRowsCta + row, rows - 1);
+          const int i = g.T == 1 ? 0 : r / g.G;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + row * S::kRowBytes + ((c ^ (row & 7)) << 4)),
+                       "l"(src + (r - i * g.G) * a.q.sh + i * a.q.sn + 16 * c)
+                       : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(job_bar) : "memory");
+      }
+      if (lane == 0) {
+        Job j;
+        j.b = w.b; j.head0 = hk * g.G; j.rb = w.rb; j.part = a.parts.shared + w.o;
+        j.kl = w.p.kl; j.ql = w.p.ql; j.p0 = w.p.p0; j.from = w.p.from;
+        j.sinks = w.p.sinks; j.key0 = key0; j.steps = steps; j.more = 1;
+        sm.job[slot] = j;
+        mbar_arrive(job_bar);
+      }
+      if (++slot == kJobs) { slot = 0; round ^= 1; }
+      const int at = (key0 + (lane << a.box_shift)) & ((1 << g.shift) - 1);
+      const bool hole = (unsigned)id >= (unsigned)g.pages;
+      const int page = hole ? g.pages : id;  // (rows behind the last page arrive as zeros)
+      const unsigned holes = __ballot_sync(0xffffffffu, hole);
+      w.next(g, a);
+      more = w.pos < end;
+      if (more) id = look_up();
       for (unsigned todo = steps; todo; todo &= todo - 1) {
         const int s = __ffs(todo) - 1, first = s * boxes;
         ok = warp_wait(s32(&sm.empty[stage]), phase ^ 1, abort, a.status);
@@ -215,9 +302,9 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         __syncwarp();
         if (lane >= first && lane < first + boxes) {
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kStep * 128, &map_k, bar, 64 * c, slot, hk, page);
+          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kStep * 128, &map_k, bar, 64 * c, at, hk, page);
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + S::kHalf + c * kStep * 128, &map_v, bar, 64 * c, slot, hk, page);
+          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + S::kHalf + c * kStep * 128, &map_v, bar, 64 * c, at, hk, page);
         }
         __syncwarp();
         ++issued;
@@ -225,65 +312,37 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
       }
     }
     // copies must have landed before the CTA's memory is released (their readers have waited for them, unless a wait ran out)
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (*abort && lane == 0)
       for (uint32_t n = issued > kStages ? issued - kStages : 0; n < issued; ++n) mbar_drain(s32(&sm.full[n % kBars]), (n / kBars) & 1);
+    if (!a.first) settle_stream();
     return;
   }
 
-  // ------------------------------------------------------------- items
-  uint32_t taken = 0;  // steps of the items so far, all warps'
-  int have_b = -1, have_hk = -1, have_rb = -1;
-  uint32_t qf[NT][D / 16][2];
-  const int rows = g.G * g.T;
+  // ------------------------------------------------------------- steps
+  uint32_t taken = 0, slot = 0, round = 0, joins = 0;  // steps of the items so far, all warps'; items
   const uint32_t ka = (uint32_t)((lane & 15) * 128), kx = (uint32_t)(lane & 7), kh = (uint32_t)(lane >> 4);           // keys as they lie
   const uint32_t va = (uint32_t)(((lane & 7) + 8 * (lane >> 4)) * 128), vh = (uint32_t)((lane >> 3) & 1);             // values transposed
+  const uint32_t qa = (uint32_t)((lane & 7) * S::kRowBytes), qh = (uint32_t)(lane >> 3);                              // four pieces of 8 rows
 #pragma unroll 1
-  for (; left > 0; --left) {
-    if (w.b != have_b || w.hk != have_hk || w.rb != have_rb) {
-      have_b = w.b; have_hk = w.hk; have_rb = w.rb;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int r = w.rb * kRowsCta + 8 * nt + gq, i = r / g.G, h = r - i * g.G;
-        const char* src = a.q.data + w.b * a.q.sb + (w.hk * g.G + h) * a.q.sh + i * a.q.sn + 4 * tq;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) qf[nt][c][x] = r < rows ? __ldg(reinterpret_cast<const unsigned*>(src + 32 * c + 16 * x)) : 0u;
-      }
-    }
-    // the last key that the lane's rows see (8 nt + 2 tq + x), -1 where there is no such row
-    int last[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int r = w.rb * kRowsCta + 8 * nt + 2 * tq + x, i = r / g.G;
-        last[nt][x] = r < rows && i < w.p.ql ? w.p.p0 + i : -1;
-      }
+  for (;; ++joins) {
+    if (!warp_wait(s32(&sm.job_full[slot]), round, abort, a.status)) break;
+    const Job job = sm.job[slot];
+    if (!job.more) break;
+    const unsigned steps = job.steps;
     float m[NT][2], l[NT][2], acc[NT][D / 16][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -INFINITY;
-      l[nt][0] = l[nt][1] = 0.f;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) acc[nt][c][0] = acc[nt][c][1] = acc[nt][c][2] = acc[nt][c][3] = 0.f;
-    }
-    const unsigned steps = w.steps(lane);
-#pragma unroll 1
-    for (int s = warp; s < kSteps; s += kWarps) {
-      if (!ok || !((steps >> s) & 1u)) continue;
-      const int j0 = w.key0() + s * kStep;
-      const uint32_t at = taken + __popc(steps & low_bits(s)), stage = at % kStages;
-      ok = warp_wait(s32(&sm.full[at % kBars]), (at / kBars) & 1, abort, a.status);
-      if (!ok) continue;
-      const uint32_t kt = s32(sm.ring[stage]), vt = kt + S::kHalf;
+    if ((steps >> warp) & 1u) {
+      const int j0 = job.key0 + warp * kStep;
+      const uint32_t at = taken + __popc(steps & low_bits(warp)), stage = at % kStages;
+      if (!warp_wait(s32(&sm.full[at % kBars]), (at / kBars) & 1, abort, a.status)) break;
+      const uint32_t kt = s32(sm.ring[stage]), vt = kt + S::kHalf, qt = s32(sm.q[slot]);
       const unsigned hole = sm.hole[stage];
       // all rows see all of the step
-      const bool whole = !hole && j0 + kStep - 1 <= w.p.p0 && (!g.window || j0 >= w.p.kl - g.window || j0 + kStep <= w.p.sinks);
+      const bool whole = !hole && j0 + kStep - 1 <= job.p0 && (!g.window || j0 >= job.kl - g.window || j0 + kStep <= job.sinks);
       if (!whole) {  // a weight of zero does not silence what is no number: values that no row sees become zeros
         for (int e = lane; e < kStep * D / 8; e += 32) {
           const int r = e / (D / 8), c = e - r * (D / 8), j = j0 + r;
-          if (j >= w.p.kl || (j < w.p.from && j >= w.p.sinks))
+          if (j >= job.kl || (j < job.from && j >= job.sinks))
             *reinterpret_cast<uint4*>(sm.ring[stage] + S::kHalf + (c >> 3) * kStep * 128 + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the next copy into the stage comes after these stores)
@@ -295,25 +354,39 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
         for (int k = 0; k < 4; ++k) z[nt][k][0] = z[nt][k][1] = z[nt][k][2] = z[nt][k][3] = 0.f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c)
+      for (int c2 = 0; c2 < D / 32; ++c2) {
+        uint32_t qf[NT][4];  // 32 channels of 8 rows
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t f[4];
-          ldsm4(f, kt + (c >> 2) * kStep * 128 + k * 2048 + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
+        for (int nt = 0; nt < NT; ++nt) ldsm4(qf[nt], qt + nt * 8 * S::kRowBytes + qa + (((4 * c2 + qh) ^ kx) << 4));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(z[nt][k], f[0], f[1], f[2], f[3], qf[nt][c][0], qf[nt][c][1]);
+        for (int y = 0; y < 2; ++y) {
+          const int c = 2 * c2 + y;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t f[4];
+            ldsm4(f, kt + (c >> 2) * kStep * 128 + k * 2048 + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816<F16>(z[nt][k], f[0], f[1], f[2], f[3], qf[nt][2 * y], qf[nt][2 * y + 1]);
+          }
         }
+      }
       uint32_t pt[NT][4][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (!whole) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int x = 0; x < 2; ++x) {
+            // the last key that the row sees, -1 where there is no such row
+            const int r = job.rb * kRowsCta + 8 * nt + 2 * tq + x, i = g.T == 1 ? 0 : r / g.G, p = r < rows && i < job.ql ? job.p0 + i : -1;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int j = j0 + 16 * k + gq + 4 * (x & 2), p = last[nt][x & 1];
-              if (j > p || (g.window && p - j >= g.window && j >= w.p.sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u)) z[nt][k][x] = -INFINITY;
-            }
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int j = j0 + 16 * k + gq + 8 * y;
+                if (j > p || (g.window && p - j >= g.window && j >= job.sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u))
+                  z[nt][k][x + 2 * y] = -INFINITY;
+              }
+          }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -323,29 +396,24 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16)) * g.scale_log2;  // scale > 0 commutes with max
-          if (mx > m[nt][x]) {  // (the same in the eight lanes of the row)
-            const float alpha = ex2(m[nt][x] - mx);
-            m[nt][x] = mx;
-            l[nt][x] *= alpha;
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-              acc[nt][c][x] *= alpha;
-              acc[nt][c][x + 2] *= alpha;
-            }
-          }
-          const float ref = m[nt][x] == -INFINITY ? 0.f : -m[nt][x];  // (nothing seen so far)
+          m[nt][x] = mx;
+          const float ref = mx == -INFINITY ? 0.f : -mx;  // (nothing seen)
+          float sum = 0.f;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             z[nt][k][x] = ex2(fmaf(z[nt][k][x], g.scale_log2, ref));
             z[nt][k][x + 2] = ex2(fmaf(z[nt][k][x + 2], g.scale_log2, ref));
-            l[nt][x] += z[nt][k][x] + z[nt][k][x + 2];
+            sum += z[nt][k][x] + z[nt][k][x + 2];
           }
+          l[nt][x] = sum;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           pt[nt][k][0] = transpose8(pack2<F16>(z[nt][k][0], z[nt][k][1]));
           pt[nt][k][1] = transpose8(pack2<F16>(z[nt][k][2], z[nt][k][3]));
         }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) acc[nt][c][0] = acc[nt][c][1] = acc[nt][c][2] = acc[nt][c][3] = 0.f;
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -358,39 +426,48 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         }
       __syncwarp();  // the stage has been read
       if (lane == 0) mbar_arrive(s32(&sm.empty[stage]));
+
+      // what the step leaves for the join, once all warps have read the item before's
+      if (!warp_wait(s32(&sm.parts_read), (joins & 1) ^ 1, abort, a.status)) break;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float sum = l[nt][x];
+          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+          const int h = 8 * nt + 2 * tq + x;
+          if (gq == 0) {
+            sm.part_m[warp][h] = m[nt][x];
+            sm.part_l[warp][h] = sum;
+          }
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            sm.part_o[warp][h][16 * c + gq] = acc[nt][c][x];
+            sm.part_o[warp][h][16 * c + gq + 8] = acc[nt][c][x + 2];
+          }
+        }
     }
     taken += __popc(steps);
-
-    // the warps' parts
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float sum = l[nt][x];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-        const int h = 8 * nt + 2 * tq + x;
-        if (gq == 0) {
-          sm.part_m[warp][h] = m[nt][x];
-          sm.part_l[warp][h] = sum;
-        }
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          sm.part_o[warp][h][16 * c + gq] = acc[nt][c][x];
-          sm.part_o[warp][h][16 * c + gq + 8] = acc[nt][c][x + 2];
-        }
-      }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(s32(&sm.parts_full));
+      mbar_arrive(s32(&sm.job_empty[slot]));
+    }
+    if (++slot == kJobs) { slot = 0; round ^= 1; }
+    if (!warp_wait(s32(&sm.parts_full), joins & 1, abort, a.status)) break;
     for (int e = tid; e < kRowsCta * D / 4; e += 32 * kWarps) {
-      const int h = e / (D / 4), c = 4 * (e - h * (D / 4)), r = w.rb * kRowsCta + h, i = r / g.G;
-      if (r >= rows || i >= w.p.ql) continue;
+      const int h = e / (D / 4), c = 4 * (e - h * (D / 4)), r = job.rb * kRowsCta + h, i = g.T == 1 ? 0 : r / g.G;
+      if (r >= rows || i >= job.ql) continue;
       float mx = -INFINITY, sum = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int y = 0; y < kWarps; ++y) mx = fmaxf(mx, sm.part_m[y][h]);
+      for (int y = 0; y < kWarps; ++y)
+        if ((steps >> y) & 1u) mx = fmaxf(mx, sm.part_m[y][h]);
 #pragma unroll
       for (int y = 0; y < kWarps; ++y) {
+        if (!((steps >> y) & 1u)) continue;
         const float f = sm.part_m[y][h] == -INFINITY ? 0.f : ex2(sm.part_m[y][h] - mx);
         const float4 u = *reinterpret_cast<const float4*>(&sm.part_o[y][h][c]);
         sum = fmaf(sm.part_l[y][h], f, sum);
@@ -399,77 +476,88 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         v.z = fmaf(u.z, f, v.z);
         v.w = fmaf(u.w, f, v.w);
       }
-      const int head = w.hk * g.G + r - i * g.G;
-      const long long row = ((long long)w.b * g.H + head) * g.T + i;
+      const int head = job.head0 + r - i * g.G;
+      const long long row = ((long long)job.b * g.H + head) * g.T + i;
       if (a.direct) {
         const bool some = !(sum <= 0.f);  // (a sum that is not a number stays one)
         const float inv = some ? 1.f / sum : 0.f;
-        *reinterpret_cast<uint2*>(a.o.data + w.b * a.o.sb + head * a.o.sh + i * a.o.sn + 2 * c) =
+        *reinterpret_cast<uint2*>(a.o.data + job.b * a.o.sb + head * a.o.sh + i * a.o.sn + 2 * c) =
             make_uint2(pack2<F16>(v.x * inv, v.y * inv), pack2<F16>(v.z * inv, v.w * inv));
         if (c == 0) a.lse[row] = some ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
       } else {
-        const long long at = (long long)(a.parts.shared + w.o) * a.parts.rows + row;
+        const long long at = (long long)job.part * a.parts.rows + row;
         *reinterpret_cast<float4*>(a.parts.o + at * D + c) = v;
         if (c == 0) a.parts.ml[at] = make_float2(mx, sum);
       }
     }
-    if (left > 1) {
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");  // the parts have been read
-      w.next(g, a);
-    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(s32(&sm.parts_read));
   }
+  if (!a.first) settle_stream();
 }
 
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
-// A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.
+// A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.  The lanes work out 32 parts' factors
+// at a time.
 template <int D, bool F16, int W>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
-  constexpr int V = D / 32;  // channels of a lane
-  __shared__ float part_o[kJoinWarps][D], part_l[kJoinWarps];
+  constexpr int V = D / 32, A = 8;  // channels of a lane; parts that a warp asks for at a time
+  __shared__ float part_o[W > 1 ? kJoinWarps : 1][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
-  const long long row = (long long)blockIdx.x * (kJoinWarps / W) + warp / W + await_stream();
+  const long long row = (long long)blockIdx.x * (kJoinWarps / W) + warp / W;
   bool live = row < in.rows;
   const int i = (int)(row % g.T), head = (int)(row / g.T % g.H), b = live ? (int)(row / g.T / g.H) : 0;
-  const Parts p = parts_of(g, b);
+  const int zero = await_stream();
+  const Parts p = parts_of(g, b + zero);
   live = live && i < p.ql;
   const int n = live ? in.shared + p.n : 0;
+  const float2* ml = in.ml + zero + row;
   float mx = -INFINITY, sum = 0.f, v[V];
 #pragma unroll
   for (int x = 0; x < V; ++x) v[x] = 0.f;
-  for (int y = lane; y < n; y += 32) mx = fmaxf(mx, __ldcg(&in.ml[y * in.rows + row].x));
+  for (int y = lane; y < n; y += 32) mx = fmaxf(mx, __ldcg(&ml[y * in.rows].x));
 #pragma unroll
   for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-#pragma unroll 4
-  for (int y = w; y < n; y += W) {
-    const long long at = y * in.rows + row;
-    const float2 ml = __ldcg(in.ml + at);
-    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
-    const float* src = in.o + at * D + V * lane;
-    float u[V];
-    if constexpr (V == 4) {
-      const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
-      u[0] = t.x; u[1] = t.y; u[2] = t.z; u[3] = t.w;
-    } else {
-      const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
-      u[0] = t.x; u[1] = t.y;
-    }
-    sum = fmaf(ml.y, f, sum);
+  for (int y0 = 0; y0 < n; y0 += 32) {
+    const float2 part = y0 + lane < n ? __ldcg(&ml[(y0 + lane) * in.rows]) : make_float2(-INFINITY, 0.f);
+    const float f = part.x == -INFINITY ? 0.f : ex2(part.x - mx);
+    sum += part.y * f;
+    const int m = min(32, n - y0);
+    for (int z0 = w; z0 < m; z0 += A * W) {
+      float u[A][V];
 #pragma unroll
-    for (int x = 0; x < V; ++x) v[x] = fmaf(u[x], f, v[x]);
+      for (int z = 0; z < A; ++z) {
+        const float* src = in.o + ((y0 + min(z0 + z * W, m - 1)) * in.rows + row) * D + V * lane;
+        if constexpr (V == 4) {
+          const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
+          u[z][0] = t.x; u[z][1] = t.y; u[z][2] = t.z; u[z][3] = t.w;
+        } else {
+          const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
+          u[z][0] = t.x; u[z][1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int z = 0; z < A; ++z) {
+        const float fz = __shfl_sync(0xffffffffu, f, (z0 + z * W) & 31);
+        if (z0 + z * W < m) {
+#pragma unroll
+          for (int x = 0; x < V; ++x) v[x] = fmaf(u[z][x], fz, v[x]);
+        }
+      }
+    }
   }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if constexpr (W > 1) {
 #pragma unroll
     for (int x = 0; x < V; ++x) part_o[warp][V * lane + x] = v[x];
-    if (lane == 0) part_l[warp] = sum;
     __syncthreads();
     if (w) return;
 #pragma unroll
-    for (int y = 1; y < W; ++y) {
-      sum += part_l[warp + y];
+    for (int y = 1; y < W; ++y)
 #pragma unroll
       for (int x = 0; x < V; ++x) v[x] += part_o[warp + y][V * lane + x];
-    }
   }
   if (!live) return;
   const bool some = !(sum <= 0.f);
@@ -492,7 +580,7 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const View& k_p
   if (const int rc = launch_setup(reinterpret_cast<const void*>(paged_parts_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
   a.blocks = (g.G * g.T + 8 * NT - 1) / (8 * NT);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
-  if (most > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
+  if (most * kFull > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
   return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, mk, mv);
 }
 
@@ -513,13 +601,15 @@ int by_type(int d, bool f16, F&& f) {
 }  // namespace
 
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                       const PartsOut& parts, int most_parts, bool direct, bool clear, const View& o, float* lse) {
-  const DecArgs a = {q, o, lse, parts, 0, 0, direct, clear, c.status};
+                       const PartsOut& parts, int most_parts, bool direct, bool first, const View& o, float* lse) {
+  const DecArgs a = {q, o, lse, parts, 0, 0, direct, first, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
-    if constexpr (D == 64)
-      if (g.G * g.T > 16) return launch_parts<D, F16, 4>(c, g, a, k_pages, v_pages, most_parts);
+    if constexpr (D == 64) {
+      if (g.G * g.T > 24) return launch_parts<D, F16, 4>(c, g, a, k_pages, v_pages, most_parts);
+      if (g.G * g.T > 16) return launch_parts<D, F16, 3>(c, g, a, k_pages, v_pages, most_parts);
+    }
     return g.G * g.T > 8 ? launch_parts<D, F16, 2>(c, g, a, k_pages, v_pages, most_parts)
                          : launch_parts<D, F16, 1>(c, g, a, k_pages, v_pages, most_parts);
   });
@@ -529,7 +619,9 @@ int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const Parts
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
-    return most_parts > 8 ? launch_join<D, F16, kJoinWarps>(c, g, parts, o, lse) : launch_join<D, F16, 1>(c, g, parts, o, lse);
+    // (by the parts alone, not by the rows: the order of a row's sums must not depend on the others)
+    if (most_parts <= 16) return launch_join<D, F16, 1>(c, g, parts, o, lse);
+    return most_parts <= 64 ? launch_join<D, F16, 4>(c, g, parts, o, lse) : launch_join<D, F16, 8>(c, g, parts, o, lse);
   });
 }
 

@@ -190,8 +190,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) return;
       tc_fence_after();
       if (elect_one()) {
+        if (kks == U / 16) {
+#pragma unroll
+          for (int kk = 0; kk < U / 16; ++kk) umma_ts(tco, tcp + 8 * kk, vd + (uint64_t)((2048 * kk) >> 4), idesc_pv, !fresh || kk > 0);
+        } else {
 #pragma unroll 1
-        for (int kk = 0; kk < kks; ++kk) umma_ts(tco, tcp + 8 * kk, vd + (uint64_t)((2048 * kk) >> 4), idesc_pv, !fresh || kk > 0);
+          for (int kk = 0; kk < kks; ++kk) umma_ts(tco, tcp + 8 * kk, vd + (uint64_t)((2048 * kk) >> 4), idesc_pv, !fresh || kk > 0);
+        }
         tc_commit(s32(&sm.pv_done[t][b]));
         tc_commit(s32(&sm.kv_empty[2 * v_pair + 1]));
       }
