@@ -31,7 +31,8 @@ int make_geo(const mosaic_paged_params* p, const int32_t* table, const int32_t* 
   g->scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->d)) * 1.4426950408889634f;
   g->B = p->B; g->H = p->H; g->Hkv = p->Hkv; g->T = p->Nq; g->d = p->d;
   g->shift = log2_of(p->page); g->pages = p->pages; g->width = p->width;
-  g->window = p->window; g->sinks = p->sinks;
+  g->window = p->window < p->width * p->page ? p->window : 0;  // (one that holds every token is none)
+  g->sinks = p->sinks;
   g->table_stride = p->table_stride;
   g->table = table; g->k_len = k_len; g->q_len = q_len;
   if (!table || !k_len) return MOSAIC_E_INVALID_ARG;

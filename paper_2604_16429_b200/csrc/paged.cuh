@@ -38,8 +38,7 @@ struct Parts {
   int first, front; // chunk of `from`; 1: the sinks lie in a chunk ahead of it, the first part
   int n;            // parts
 };
-__device__ __forceinline__ Parts parts_of(const PagedGeo& g, int b) {
-  const Span s = span_of(g, b);
+__device__ __forceinline__ Parts parts_of(const PagedGeo& g, const Span& s) {
   Parts p;
   p.kl = s.kl; p.ql = s.ql; p.p0 = s.off;
   p.from = g.window ? max(0, s.off - g.window + 1) : 0;
@@ -81,9 +80,13 @@ int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View&
                       const int32_t* prefix_table, int prefix_len, int chunk, const PartsOut& parts);
 // Joins all parts of every row
 int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const PartsOut& parts, int most_parts, const View& o, float* lse);
-// A map of a pool in boxes of 64 channels by `rows` slots
-inline bool make_map_pool(CUtensorMap* map, const View& v, const PagedGeo& g, int rows) {
-  return make_map_view(map, v, g.d, 1 << g.shift, g.Hkv, g.pages, rows);
+// A map of a pool in boxes of `rows` slots by `parts` times 64 channels, and the copy of one from 64 * part on
+bool make_map_pool(CUtensorMap* map, const View& v, int d, int page, int heads, int pages, int rows, int parts);
+__device__ __forceinline__ void load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int part, int head, int page) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(slot), "r"(part), "r"(head), "r"(page)
+      : "memory");
 }
 
 }  // namespace mosaic

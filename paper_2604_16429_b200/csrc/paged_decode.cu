@@ -6,9 +6,9 @@
 // take equal shares of the list of all items, which each works out from the lengths; a CTA's items lie one after the other, so that a
 // member's queries stay in registers.
 //
-// One warp finds the items, and for each leaves a note of what the others need to know of it, copies its queries, and asks for its steps of
-// 64 keys by TMA, page by page (the page numbers of a chunk are looked up an item ahead), into a ring that all warps share; it goes on
-// into the next items, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a step each:
+// One warp finds the items, and for each leaves a note of what the others need to know of it, with the numbers of its pages, and copies its
+// queries.  One asks for the items' steps of 64 keys by TMA, page by page, into a ring that all warps share; both run ahead of the
+// others, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a step each:
 // products of 16 x 8 x 16 are enough,
 //   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose,
 // and the step's 64 keys give every lane four of them that do not wait for one another.  Weights round to 16 bits once, as operands;
@@ -27,25 +27,30 @@ constexpr int kStep = 64, kSteps = kChunkKeys / kStep;
 // Barriers on which steps land, in turn.  A warp looks at its own steps only, and a wait on a phase's parity is exact only if the
 // barrier's phase before has completed: that is sure if it belongs to an earlier chunk, whose steps have all been taken.
 constexpr int kBars = 16;
+static_assert(kChunkKeys / kMinPage == 32, "a lane has a box");
 static_assert(kBars >= kSteps, "a step's barrier has been used by an earlier one of the chunk");
 constexpr int kMaxSmem = 232448;
 
-constexpr int kJobs = 3;  // items that the first warp may be ahead
+constexpr int kJobs = 4;  // items that the first warp may be ahead
 
 // What the others need to know of an item
-struct alignas(16) Job {
-  int b, head0, rb, part;            // member, first query head of the group, block of rows, place among all parts
-  int kl, ql, p0, from;              // as in Parts
-  int sinks, key0;                   // first position of the chunk
-  unsigned steps;                    // of the chunk, that any row sees something of
-  int more;                          // 0: no item, and none will come
+struct alignas(16) Note {
+  int b, head0, rb, part;  // member, first query head of the group, block of rows, place among all parts
+  int kl, ql, p0, from;    // as in Parts
+  int sinks, key0;         // first position of the chunk
+  unsigned steps;          // of the chunk, that any row sees something of
+  int more;                // 0: no item, and none will come
+};
+struct Job {
+  Note note;
+  int page[kChunkKeys / kMinPage];  // of the chunk's boxes; g.pages, behind the last: none, or no row sees anything of it
 };
 
 // NT: tiles of 8 rows that a CTA takes
 template <int D, int NT>
 struct Smem {
   static constexpr int kWarps = 8;  // that take steps
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kThreads = 32 * (kWarps + 2);
   static constexpr int kHalf = kStep * D * 2, kStepBytes = 2 * kHalf;  // a step's keys, then its values
   static constexpr int kPitch = D + 4;  // of a row of part_o: lanes that store side by side meet different banks
   static constexpr int kRowBytes = D * 2;
@@ -55,9 +60,10 @@ struct Smem {
   unsigned char q[kJobs][8 * NT * kRowBytes];  // 16-byte pieces of a row swizzled by its number
   float part_o[kWarps][8 * NT][kPitch], part_m[kWarps][8 * NT], part_l[kWarps][8 * NT];
   Job job[kJobs];
-  unsigned long long full[kBars], empty[kStages], job_full[kJobs], job_empty[kJobs], parts_full, parts_read;
-  unsigned hole[kStages];  // the step's boxes whose page is not there, or which no row sees
-  int scan[kWarps + 1], start[2];
+  unsigned long long full[kBars], empty[kStages], note_full[kJobs], job_full[kJobs], job_empty[kJobs], parts_full, parts_read;
+  unsigned hole[kStages];  // the step's boxes that have no page
+  int scan[kWarps + 2];
+  int4 start;              // the member that this CTA's share begins in, the weight before it, its lengths
   int abort;
 };
 
@@ -68,18 +74,35 @@ struct DecArgs {
   int blocks;     // of rows
   int box_shift;  // log2 of the slots that a copy brings: a page, at most a step
   bool direct, first;
+  float inv_g;    // 1 / G
   int* status;
 };
 
 // A place in the list of all items: members, their heads, their parts, blocks of rows.  Items weigh their steps and kTurn for what comes
 // with every one; `pos` is the weight of all items before.
 constexpr int kTurn = 2, kFull = kSteps + kTurn;
+__device__ __forceinline__ Parts parts_of(const PagedGeo& g, const DecArgs& a, const Span& s) {
+  Parts p = parts_of(g, s);
+  if (a.direct) p.n = p.ql > 0 ? 1 : 0;  // (a member without keys has results too)
+  return p;
+}
 struct Walk {
   Parts p;
   int b, hk, o, rb, pos;
+  int held, kl, ql;  // lengths of the 32 members from `held` on, in the lanes
+  __device__ __forceinline__ void hold(const PagedGeo& g) {
+    held = b;
+    const Span s = span_of(g, min(b + (int)(threadIdx.x & 31), g.B - 1));
+    kl = s.kl;
+    ql = s.ql;
+  }
   __device__ __forceinline__ void member(const PagedGeo& g, const DecArgs& a) {
-    p = parts_of(g, b);
-    if (a.direct) p.n = p.ql > 0 ? 1 : 0;  // (a member without keys has results too)
+    if (b - held >= 32) hold(g);
+    Span s;
+    s.kl = __shfl_sync(0xffffffffu, kl, b - held);
+    s.ql = __shfl_sync(0xffffffffu, ql, b - held);
+    s.off = s.kl - s.ql;
+    p = parts_of(g, a, s);
   }
   __device__ __forceinline__ int weight(int part) const {
     if (p.front && part == 0) return (p.sinks + kStep - 1) / kStep + kTurn;
@@ -157,7 +180,6 @@ __device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
     before += w < warp ? scan[w] : 0;
     total += scan[w];
   }
-  __syncthreads();
   return before + x - v;
 }
 
@@ -166,7 +188,7 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     paged_parts_kernel(const PagedGeo g, const __grid_constant__ DecArgs a, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v) {
   using S = Smem<D, NT>;
-  constexpr int kRowsCta = 8 * NT, kStages = S::kStages, kWarps = S::kWarps, kThreads = S::kThreads;
+  constexpr int kRowsCta = 8 * NT, kStages = S::kStages, kWarps = S::kWarps;
   extern __shared__ unsigned char smem_raw[];
   S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
@@ -174,8 +196,9 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     for (int s = 0; s < kBars; ++s) mbar_init(s32(&sm.full[s]), 1);
     for (int s = 0; s < kStages; ++s) mbar_init(s32(&sm.empty[s]), 1);
     for (int s = 0; s < kJobs; ++s) {
+      mbar_init(s32(&sm.note_full[s]), 1);
       mbar_init(s32(&sm.job_full[s]), 33);  // the note, and every lane's copies
-      mbar_init(s32(&sm.job_empty[s]), kWarps);
+      mbar_init(s32(&sm.job_empty[s]), kWarps + 1);
     }
     mbar_init(s32(&sm.parts_full), kWarps);
     mbar_init(s32(&sm.parts_read), kWarps);
@@ -189,108 +212,128 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
   if (a.first && blockIdx.x == 0 && tid == 0) a.status[zero] = 0;
   volatile int* abort = &sm.abort;
 
+  const int rows = g.G * g.T;
+
   // ---- this CTA's share of the list: the items that begin in its share of the weight
   int begin, end;
   {
-    Walk w;
-    int total = 0, before = 0;
-    auto weight = [&](int b) {
-      w.b = b;
-      if (b >= g.B) return 0;
-      w.member(g, a);
-      return w.weight_of_head(a) * g.Hkv;
+    Span s = {};
+    int total = 0, before = 0, mine = 0;
+    auto weigh = [&](int b) {
+      mine = 0;
+      if (b < g.B) {
+        Walk w;
+        s = span_of(g, b);
+        w.p = parts_of(g, a, s);
+        mine = w.weight_of_head(a) * g.Hkv;
+      }
     };
-    for (int b0 = 0; b0 < g.B; b0 += kThreads) {
+#pragma unroll 1
+    for (int b0 = 0; b0 < g.B; b0 += S::kThreads) {
       int all;
-      before = block_scan<kWarps + 1>(weight(b0 + tid + zero), sm.scan, all);
+      weigh(b0 + tid + zero);
+      if (b0) __syncthreads();
+      before = block_scan<kWarps + 2>(mine, sm.scan, all);
       total += all;
     }
     begin = (int)((long long)total * blockIdx.x / gridDim.x);
     end = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
     int base = 0;
-    for (int b0 = 0; b0 < g.B; b0 += kThreads) {
+#pragma unroll 1
+    for (int b0 = 0; b0 < g.B; b0 += S::kThreads) {
       int all = 0;
-      if (g.B > kThreads) before = block_scan<kWarps + 1>(weight(b0 + tid + zero), sm.scan, all);
-      const int n = w.b < g.B ? w.weight_of_head(a) * g.Hkv : 0, at = begin - base - before;
-      if (at >= 0 && at < n) {
-        sm.start[0] = w.b;
-        sm.start[1] = base + before;
+      if (g.B > S::kThreads) {
+        weigh(b0 + tid + zero);
+        __syncthreads();
+        before = block_scan<kWarps + 2>(mine, sm.scan, all);
       }
+      const int at = begin - base - before;
+      if (at >= 0 && at < mine) sm.start = make_int4(b0 + tid, base + before, s.kl, s.ql);
       base += all;
     }
     __syncthreads();
   }
-  const int rows = g.G * g.T;
 
   if (warp == kWarps) {
-    // ------------------------------------------------------------- items and copies
-    const int box = 1 << a.box_shift, boxes = kStep >> a.box_shift;  // a lane has one of the chunk's boxes
-    const uint32_t box_bytes = (uint32_t)box * 128;
+    // ------------------------------------------------------------- items
+    const int box = 1 << a.box_shift, boxes = kChunkKeys >> a.box_shift;  // a lane has one of the chunk's boxes
     Walk w;
-    bool more = begin < end;
-    if (more) {
-      w.b = sm.start[0];
-      w.member(g, a);
-      w.seek(g, a, sm.start[1], begin);
-      more = w.pos < end;
+    w.pos = end;
+    if (begin < end) {
+      const int4 at = sm.start;
+      w.b = at.x;
+      w.p = parts_of(g, a, Span{at.w, at.z, at.z - at.w});
+      w.hold(g);
+      w.seek(g, a, at.y, begin);
     }
 #ifdef MOSAIC_TEST_WITHHOLD_FIRST_LIST
     bool ok = false;  // test build only: nothing is ever handed out or loaded, so that every wait for it runs out
 #else
     bool ok = true;
 #endif
-    // the page number of this lane's box, or none if no row sees anything of it
+    // the page of this lane's box
     auto look_up = [&]() {
       const int key = w.key0() + (lane << a.box_shift);
-      int t = -1;
-      if (lane < kSteps * boxes && w.seen(key, box)) t = __ldg(g.table + w.b * g.table_stride + (key >> g.shift));
-      return t;
+      return lane < boxes && w.seen(key, box) ? __ldg(g.table + w.b * g.table_stride + (key >> g.shift)) : -1;
     };
-    uint32_t stage = 0, phase = 0, issued = 0, slot = 0, round = 0;
+    uint32_t slot = 0, round = 0;
+    bool more = w.pos < end;
     int id = more ? look_up() : 0;
 #pragma unroll 1
     while (ok) {
       ok = warp_wait(s32(&sm.job_empty[slot]), round ^ 1, abort, a.status);
       if (!ok) break;
       const uint32_t job_bar = s32(&sm.job_full[slot]);
-      if (!more) {
-        if (lane == 0) sm.job[slot].more = 0;
-        mbar_arrive(job_bar);
-        if (lane == 0) mbar_arrive(job_bar);
-        break;
+      const unsigned steps = more ? w.steps(lane) : 0u;
+      sm.job[slot].page[lane] = (unsigned)id < (unsigned)g.pages ? id : g.pages;
+      if (lane == 0) {
+        Note n;
+        n.b = w.b; n.head0 = w.hk * g.G; n.rb = w.rb; n.part = a.parts.shared + w.o;
+        n.kl = w.p.kl; n.ql = w.p.ql; n.p0 = w.p.p0; n.from = w.p.from;
+        n.sinks = w.p.sinks; n.key0 = w.key0(); n.steps = steps; n.more = more;
+        sm.job[slot].note = n;
       }
-      const unsigned steps = w.steps(lane);
-      const int key0 = w.key0(), hk = w.hk;
-      {  // the queries: row by row, whatever their strides
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s32(&sm.note_full[slot]));
+      if (more) {  // the queries: row by row, whatever their strides
         const uint32_t dst = s32(sm.q[slot]);
-        const char* src = a.q.data + w.b * a.q.sb + hk * g.G * a.q.sh;
+        const char* src = a.q.data + w.b * a.q.sb + w.hk * g.G * a.q.sh;
 #pragma unroll
         for (int e0 = 0; e0 < kRowsCta * D / 8; e0 += 32) {
           const int e = e0 + lane, row = e / (D / 8), c = e % (D / 8), r = min(w.rb * kRowsCta + row, rows - 1);
-          const int i = g.T == 1 ? 0 : r / g.G;
+          const int i = g.T == 1 ? 0 : quick_div(r, g.G, a.inv_g);
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + row * S::kRowBytes + ((c ^ (row & 7)) << 4)),
                        "l"(src + (r - i * g.G) * a.q.sh + i * a.q.sn + 16 * c)
                        : "memory");
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(job_bar) : "memory");
       }
-      if (lane == 0) {
-        Job j;
-        j.b = w.b; j.head0 = hk * g.G; j.rb = w.rb; j.part = a.parts.shared + w.o;
-        j.kl = w.p.kl; j.ql = w.p.ql; j.p0 = w.p.p0; j.from = w.p.from;
-        j.sinks = w.p.sinks; j.key0 = key0; j.steps = steps; j.more = 1;
-        sm.job[slot] = j;
-        mbar_arrive(job_bar);
-      }
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(job_bar) : "memory");
+      if (lane == 0) mbar_arrive(job_bar);
+      if (!more) break;
       if (++slot == kJobs) { slot = 0; round ^= 1; }
-      const int at = (key0 + (lane << a.box_shift)) & ((1 << g.shift) - 1);
-      const bool hole = (unsigned)id >= (unsigned)g.pages;
-      const int page = hole ? g.pages : id;  // (rows behind the last page arrive as zeros)
-      const unsigned holes = __ballot_sync(0xffffffffu, hole);
       w.next(g, a);
       more = w.pos < end;
       if (more) id = look_up();
-      for (unsigned todo = steps; todo; todo &= todo - 1) {
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");  // copies must have landed before the CTA's memory is released
+    if (!a.first) settle_stream();
+    return;
+  }
+  if (warp == kWarps + 1) {
+    // ------------------------------------------------------------- copies of keys and values
+    const int boxes = kStep >> a.box_shift, in_page = (1 << g.shift) - 1;
+    const uint32_t box_bytes = (uint32_t)(D * 2) << a.box_shift;
+    uint32_t stage = 0, phase = 0, issued = 0, slot = 0, round = 0;
+    bool ok = true;
+#pragma unroll 1
+    while (ok) {
+      ok = warp_wait(s32(&sm.note_full[slot]), round, abort, a.status);
+      if (!ok) break;
+      const Note& job = sm.job[slot].note;
+      if (!job.more) break;
+      const int page = sm.job[slot].page[lane], hk = quick_div(job.head0, g.G, a.inv_g), at = (job.key0 + (lane << a.box_shift)) & in_page;
+      const unsigned holes = __ballot_sync(0xffffffffu, page >= g.pages);
+      for (unsigned todo = job.steps; todo; todo &= todo - 1) {
         const int s = __ffs(todo) - 1, first = s * boxes;
         ok = warp_wait(s32(&sm.empty[stage]), phase ^ 1, abort, a.status);
         if (!ok) break;
@@ -300,19 +343,18 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
           mbar_expect_tx(bar, S::kStepBytes);
         }
         __syncwarp();
-        if (lane >= first && lane < first + boxes) {
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kStep * 128, &map_k, bar, 64 * c, at, hk, page);
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + S::kHalf + c * kStep * 128, &map_v, bar, 64 * c, at, hk, page);
+        if (lane >= first && lane < first + boxes) {  // (rows behind the last page arrive as zeros)
+          load_slots(dst, &map_k, bar, at, 0, hk, page);
+          load_slots(dst + S::kHalf, &map_v, bar, at, 0, hk, page);
         }
-        __syncwarp();
         ++issued;
         if (++stage == kStages) { stage = 0; phase ^= 1; }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s32(&sm.job_empty[slot]));
+      if (++slot == kJobs) { slot = 0; round ^= 1; }
     }
     // copies must have landed before the CTA's memory is released (their readers have waited for them, unless a wait ran out)
-    asm volatile("cp.async.wait_all;" ::: "memory");
     if (*abort && lane == 0)
       for (uint32_t n = issued > kStages ? issued - kStages : 0; n < issued; ++n) mbar_drain(s32(&sm.full[n % kBars]), (n / kBars) & 1);
     if (!a.first) settle_stream();
@@ -321,13 +363,14 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 
   // ------------------------------------------------------------- steps
   uint32_t taken = 0, slot = 0, round = 0, joins = 0;  // steps of the items so far, all warps'; items
+  const int box = 1 << a.box_shift;
   const uint32_t ka = (uint32_t)((lane & 15) * 128), kx = (uint32_t)(lane & 7), kh = (uint32_t)(lane >> 4);           // keys as they lie
   const uint32_t va = (uint32_t)(((lane & 7) + 8 * (lane >> 4)) * 128), vh = (uint32_t)((lane >> 3) & 1);             // values transposed
   const uint32_t qa = (uint32_t)((lane & 7) * S::kRowBytes), qh = (uint32_t)(lane >> 3);                              // four pieces of 8 rows
 #pragma unroll 1
   for (;; ++joins) {
     if (!warp_wait(s32(&sm.job_full[slot]), round, abort, a.status)) break;
-    const Job job = sm.job[slot];
+    const Note job = sm.job[slot].note;
     if (!job.more) break;
     const unsigned steps = job.steps;
     float m[NT][2], l[NT][2], acc[NT][D / 16][4];
@@ -339,11 +382,17 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
       const unsigned hole = sm.hole[stage];
       // all rows see all of the step
       const bool whole = !hole && j0 + kStep - 1 <= job.p0 && (!g.window || j0 >= job.kl - g.window || j0 + kStep <= job.sinks);
+      // a step's rows lie box by box, a box's 64-channel parts one behind the other
+      uint32_t tile[4];  // of 16 keys
+#pragma unroll
+      for (int k = 0; k < 4; ++k) tile[k] = D == 64 ? 2048u * k : ((16u * k) >> a.box_shift) * ((uint32_t)(D * 2) << a.box_shift) + ((16u * k) & (box - 1)) * 128u;
+      const uint32_t part = box * 128u;
       if (!whole) {  // a weight of zero does not silence what is no number: values that no row sees become zeros
-        for (int e = lane; e < kStep * D / 8; e += 32) {
-          const int r = e / (D / 8), c = e - r * (D / 8), j = j0 + r;
+        for (int r = 0; r < kStep; r += 32 / (D / 8)) {
+          const int rr = r + lane / (D / 8), c = lane % (D / 8), j = j0 + rr;
           if (j >= job.kl || (j < job.from && j >= job.sinks))
-            *reinterpret_cast<uint4*>(sm.ring[stage] + S::kHalf + (c >> 3) * kStep * 128 + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(sm.ring[stage] + S::kHalf + ((unsigned)rr >> a.box_shift) * ((D * 2) << a.box_shift) +
+                                      (c >> 3) * part + (rr & (box - 1)) * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the next copy into the stage comes after these stores)
         __syncwarp();
@@ -364,7 +413,7 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             uint32_t f[4];
-            ldsm4(f, kt + (c >> 2) * kStep * 128 + k * 2048 + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
+            ldsm4(f, kt + (c >> 2) * part + tile[k] + ka + (((2 * (c & 3) + kh) ^ kx) << 4));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma16816<F16>(z[nt][k], f[0], f[1], f[2], f[3], qf[nt][2 * y], qf[nt][2 * y + 1]);
           }
@@ -376,15 +425,15 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         if (!whole) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            // the last key that the row sees, -1 where there is no such row
-            const int r = job.rb * kRowsCta + 8 * nt + 2 * tq + x, i = g.T == 1 ? 0 : r / g.G, p = r < rows && i < job.ql ? job.p0 + i : -1;
+            // the row sees the lane's keys j0 + gq + n for n <= to, and n > to - window or n < sinks
+            const int r = job.rb * kRowsCta + 8 * nt + 2 * tq + x, i = g.T == 1 ? 0 : quick_div(r, g.G, a.inv_g);
+            const int to = (r < rows && i < job.ql ? job.p0 + i : -1) - j0 - gq, from = g.window ? to - g.window : -1, sinks = job.sinks - j0 - gq;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const int j = j0 + 16 * k + gq + 8 * y;
-                if (j > p || (g.window && p - j >= g.window && j >= job.sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u))
-                  z[nt][k][x + 2 * y] = -INFINITY;
+                const int n = 16 * k + 8 * y;
+                if (n > to || (n <= from && n >= sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u)) z[nt][k][x + 2 * y] = -INFINITY;
               }
           }
         }
@@ -420,7 +469,7 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           uint32_t f[4];
-          ldsm4t(f, vt + (c >> 2) * kStep * 128 + k * 2048 + va + (((2 * (c & 3) + vh) ^ kx) << 4));
+          ldsm4t(f, vt + (c >> 2) * part + tile[k] + va + (((2 * (c & 3) + vh) ^ kx) << 4));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma16816<F16>(acc[nt][c], f[0], f[1], f[2], f[3], pt[nt][k][0], pt[nt][k][1]);
         }
@@ -457,25 +506,31 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     }
     if (++slot == kJobs) { slot = 0; round ^= 1; }
     if (!warp_wait(s32(&sm.parts_full), joins & 1, abort, a.status)) break;
-    for (int e = tid; e < kRowsCta * D / 4; e += 32 * kWarps) {
-      const int h = e / (D / 4), c = 4 * (e - h * (D / 4)), r = job.rb * kRowsCta + h, i = g.T == 1 ? 0 : r / g.G;
-      if (r >= rows || i >= job.ql) continue;
-      float mx = -INFINITY, sum = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    // D / 4 lanes have a row; the eight lanes of a group work out the warps' factors, one each
 #pragma unroll
-      for (int y = 0; y < kWarps; ++y)
-        if ((steps >> y) & 1u) mx = fmaxf(mx, sm.part_m[y][h]);
+    for (int e = tid; e < kRowsCta * D / 4; e += 32 * kWarps) {
+      const int h = e / (D / 4), c = 4 * (e - h * (D / 4)), r = job.rb * kRowsCta + h, i = g.T == 1 ? 0 : quick_div(r, g.G, a.inv_g);
+      const bool there = (steps >> (lane & 7)) & 1u;
+      const float my = there ? sm.part_m[lane & 7][h] : -INFINITY;
+      float mx = my;
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+      const float factor = my == -INFINITY ? 0.f : ex2(my - mx);
+      float sum = there ? sm.part_l[lane & 7][h] * factor : 0.f;
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int y = 0; y < kWarps; ++y) {
         if (!((steps >> y) & 1u)) continue;
-        const float f = sm.part_m[y][h] == -INFINITY ? 0.f : ex2(sm.part_m[y][h] - mx);
+        const float f = __shfl_sync(0xffffffffu, factor, (lane & 24) | y);
         const float4 u = *reinterpret_cast<const float4*>(&sm.part_o[y][h][c]);
-        sum = fmaf(sm.part_l[y][h], f, sum);
         v.x = fmaf(u.x, f, v.x);
         v.y = fmaf(u.y, f, v.y);
         v.z = fmaf(u.z, f, v.z);
         v.w = fmaf(u.w, f, v.w);
       }
+      if (r >= rows || i >= job.ql) continue;
       const int head = job.head0 + r - i * g.G;
       const long long row = ((long long)job.b * g.H + head) * g.T + i;
       if (a.direct) {
@@ -509,7 +564,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedGeo
   bool live = row < in.rows;
   const int i = (int)(row % g.T), head = (int)(row / g.T % g.H), b = live ? (int)(row / g.T / g.H) : 0;
   const int zero = await_stream();
-  const Parts p = parts_of(g, b + zero);
+  const Parts p = parts_of(g, span_of(g, b + zero));
   live = live && i < p.ql;
   const int n = live ? in.shared + p.n : 0;
   const float2* ml = in.ml + zero + row;
@@ -572,7 +627,10 @@ template <int D, bool F16, int NT>
 int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const View& k_pages, const View& v_pages, int most_parts) {
   CUtensorMap mk, mv;
   a.box_shift = g.shift < 6 ? g.shift : 6;
-  if (!make_map_pool(&mk, k_pages, g, 1 << a.box_shift) || !make_map_pool(&mv, v_pages, g, 1 << a.box_shift)) return MOSAIC_E_CUDA;
+  a.inv_g = 1.f / (float)g.G;
+  if (!make_map_pool(&mk, k_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, D / 64) ||
+      !make_map_pool(&mv, v_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, D / 64))
+    return MOSAIC_E_CUDA;
   constexpr size_t smem = sizeof(Smem<D, NT>) + 1024;
   static_assert(smem <= kMaxSmem, "more shared memory than a CTA can have");
   static unsigned long long configured = 0;
@@ -602,7 +660,7 @@ int by_type(int d, bool f16, F&& f) {
 
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
                        const PartsOut& parts, int most_parts, bool direct, bool first, const View& o, float* lse) {
-  const DecArgs a = {q, o, lse, parts, 0, 0, direct, first, c.status};
+  const DecArgs a = {q, o, lse, parts, 0, 0, direct, first, 0.f, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;

@@ -34,7 +34,7 @@ struct Smem {
   static constexpr int kTileBytes = kRows * D * 2, kSlotBytes = U * D * 2;
   unsigned char q[2][kTileBytes];
   unsigned char kv[kSlots][kSlotBytes];
-  uint4 rows[8][32 * 4];  // a softmax warp's 32 rows of 16 results on their way out
+  uint4 rows[8][32 * 8];  // a softmax warp's 32 rows of 32 results on their way out
   unsigned long long q_full[2], q_empty[2], kv_full[kSlots], kv_empty[kSlots];
   unsigned long long s_full[2][2], p_full[2][2], pv_done[2][2], drain[2];
   uint32_t tmem_base;
@@ -48,6 +48,7 @@ struct PrefixArgs {
   int len, chunk;        // keys of the prefix, of a part (a multiple of U)
   int rows, pairs;       // rows of a key/value head; pairs of tiles
   int box_shift;         // log2 of the rows of a box: a page, at most U
+  int box_loads;         // copies that bring a box's channels: with all of a step's rows in one box, one
   int total;             // items
   int* status;
 };
@@ -78,7 +79,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   using S = Smem<D>;
   S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr uint32_t kPart = kRows * 128, kSlotPart = U * 128;  // bytes of a tile's 64 channels
-  constexpr int kParts = D / 64;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int* status = a.status;
 
@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t box_bytes = (uint32_t)box * 128;
     // Page numbers of the step's boxes in the lanes (the last page number of all where there is none: its rows arrive as zeros)
     auto look_up = [&](const Item& it, int n) {
-      const int key = it.k0 + n * U + (lane << a.box_shift);
+      const int key = it.k0 + n * U + (lane % boxes << a.box_shift);
       int id = -1;
-      if (lane < boxes && key < a.len) id = __ldg(a.table + (key >> g.shift));
+      if (lane < boxes * a.box_loads && key < a.len) id = __ldg(a.table + (key >> g.shift));
       return (unsigned)id < (unsigned)g.pages ? id : g.pages;
     };
     auto load = [&](const CUtensorMap* map, int ids, int slot, int hk) {
@@ -124,10 +124,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) return;
       if (lane == 0) mbar_expect_tx(bar, S::kSlotBytes);
       __syncwarp();
-      if (lane < boxes) {
-#pragma unroll
-        for (int c = 0; c < kParts; ++c)
-          tma_load_4d(s32(sm.kv[s]) + c * kSlotPart + lane * box_bytes, map, bar, 64 * c, (slot + (lane << a.box_shift)) & in_page, hk, ids);
+      if (lane < boxes * a.box_loads) {  // a lane has a box, or (pages smaller than a step) the half of one
+        const int c = lane / boxes, n = lane - c * boxes;
+        load_slots(s32(sm.kv[s]) + c * kSlotPart + n * box_bytes, map, bar, (slot + (n << a.box_shift)) & in_page, c, hk, ids);
       }
       __syncwarp();
       ++slot_no;
@@ -278,9 +277,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (it.row0 + t * kRows >= a.rows) continue;  // (the whole tile)
       // the row's place: member, token, head
       const int bt = r / g.G, b = bt / g.T, i = bt - b * g.T, head = it.hk * g.G + r - bt * g.G;
-      const bool live = r < a.rows && i < span_of(g, min(b, g.B - 1)).ql;
+      const bool live = r < a.rows && (!g.q_len || i < __ldg(g.q_len + min(b, g.B - 1)));
       const int at = live ? (b * g.H + head) * g.T + i : -1;
       const bool idle = !__any_sync(0xffffffffu, live);
+      ok = warp_wait_here(s32(&sm.q_empty[t]), (n_q & 1) ^ 1, abort, status);
+      ++n_q;
+      if (!ok) break;
+      {  // the warp's rows of q, a row or two at a time, whatever their strides; rows that do not exist are zeros
+        constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+        const long long src = (long long)b * a.q.sb + head * a.q.sh + i * a.q.sn;
+        const uint32_t dst = s32(sm.q[t]);
+#pragma unroll
+        for (int x = 0; x < kLanes; ++x) {
+          const int rr = x * kAtOnce + lane / kLanes, c = lane % kLanes, row_at = (warp & 3) * 32 + rr;
+          const long long from = __shfl_sync(0xffffffffu, src, rr);
+          const uint32_t bytes = __shfl_sync(0xffffffffu, at, rr) >= 0 ? 16u : 0u;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (c >> 3) * kPart + row_at * 128 + (((c & 7) ^ (row_at & 7)) << 4)),
+                       "l"(a.q.data + (bytes ? from + 16 * c : 0)), "r"(bytes)
+                       : "memory");
+        }
+      }
       bool holes = false;  // some page of the part is not there
       for (int key = it.k0 + (lane << g.shift); key < it.k1; key += 32 << g.shift) {
         const int k = max(key & ~((1 << g.shift) - 1), it.k0);
@@ -288,20 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if ((it.k1 - 1) >> g.shift != (it.k0 >> g.shift)) holes |= (unsigned)__ldg(a.table + ((it.k1 - 1) >> g.shift)) >= (unsigned)g.pages;
       holes = __any_sync(0xffffffffu, holes);
-      ok = warp_wait_here(s32(&sm.q_empty[t]), (n_q & 1) ^ 1, abort, status);
-      ++n_q;
-      if (!ok) break;
-      {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q.data + b * a.q.sb + head * a.q.sh + i * a.q.sn);
-        uint4 x[D / 8];
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) x[c] = live ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c)
-          *reinterpret_cast<uint4*>(sm.q[t] + (c >> 3) * kPart + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x[c];
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(s32(&sm.q_full[t]));
-      }
+      asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(s32(&sm.q_full[t]));
       float m_ref = -INFINITY, l = 0.f;
       for (int n = 0; n < it.steps; ++n) {
         const int start = it.k0 + n * U, cols = min(U, it.k1 - start);
@@ -430,23 +434,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       if (idle) continue;
       tc_fence_after();
-      // The rows leave by way of shared memory: a warp stores eight rows of 64 bytes at a time.
+      // The rows leave by way of shared memory: a warp stores four rows of 128 bytes at a time.
       const long long base = (long long)it.part * a.parts.rows;
       uint4* stage = sm.rows[warp];
-#pragma unroll 1
-      for (int part = 0; part < D / 16; ++part) {
-        uint32_t ov[16];
-        tmem_ld16(to + 16 * part, ov);
+#pragma unroll
+      for (int part = 0; part < D / 32; ++part) {
+        uint32_t ov[32];
+        tmem_ld32(to + 32 * part, ov);
         tmem_wait_ld();
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          stage[4 * lane + (x ^ ((lane >> 1) & 3))] = make_uint4(ov[4 * x], ov[4 * x + 1], ov[4 * x + 2], ov[4 * x + 3]);
+        for (int x = 0; x < 8; ++x) stage[8 * lane + (x ^ (lane & 7))] = make_uint4(ov[4 * x], ov[4 * x + 1], ov[4 * x + 2], ov[4 * x + 3]);
         __syncwarp();
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int rr = 8 * x + (lane >> 2), c = lane & 3, dst = __shfl_sync(0xffffffffu, at, rr);
-          const uint4 val = stage[4 * rr + (c ^ ((rr >> 1) & 3))];
-          if (dst >= 0) *reinterpret_cast<uint4*>(a.parts.o + (base + dst) * D + 16 * part + 4 * c) = val;
+        for (int x = 0; x < 8; ++x) {
+          const int rr = 4 * x + (lane >> 3), c = lane & 7, dst = __shfl_sync(0xffffffffu, at, rr);
+          const uint4 val = stage[8 * rr + (c ^ (rr & 7))];
+          if (dst >= 0) *reinterpret_cast<uint4*>(a.parts.o + (base + dst) * D + 32 * part + 4 * c) = val;
         }
         __syncwarp();
       }
@@ -461,7 +464,10 @@ namespace {
 template <int D, bool F16>
 int launch(const HostCtx& c, const PagedGeo& g, PrefixArgs a, const View& k_pages, const View& v_pages) {
   CUtensorMap mk, mv;
-  if (!make_map_pool(&mk, k_pages, g, 1 << a.box_shift) || !make_map_pool(&mv, v_pages, g, 1 << a.box_shift)) return MOSAIC_E_CUDA;
+  const int box = 1 << a.box_shift, parts = D / 64 / a.box_loads;
+  if (!make_map_pool(&mk, k_pages, D, 1 << g.shift, g.Hkv, g.pages, box, parts) ||
+      !make_map_pool(&mv, v_pages, D, 1 << g.shift, g.Hkv, g.pages, box, parts))
+    return MOSAIC_E_CUDA;
   const size_t smem = sizeof(Smem<D>) + 1024;
   static unsigned long long configured = 0;
   int sms = 0;
@@ -504,6 +510,7 @@ int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View&
   a.rows = (int)rows;
   a.pairs = pairs_of(rows);
   a.box_shift = g.shift < 6 ? g.shift : 6;
+  a.box_loads = g.shift < 6 ? g.d / 64 : 1;
   const long long total = (long long)g.Hkv * parts.shared * a.pairs;
   if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
   a.total = (int)total;

@@ -99,6 +99,19 @@ bool encode_view(CUtensorMap* map, const void* base, int d, int N, int heads, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A pool of pages [pages, heads, page, d]: one box is `rows` slots of `parts` times 64 channels, which arrive one behind the other.
+bool encode_pool(CUtensorMap* map, const View& v, int d, int page, int heads, int pages, int rows, int parts) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  g_encodes.fetch_add(1, std::memory_order_relaxed);
+  cuuint64_t dims[5] = {64u, (cuuint64_t)page, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)pages};
+  cuuint64_t strides[4] = {(cuuint64_t)v.sn, 128u, (cuuint64_t)(heads > 1 ? v.sh : 2 * d), (cuuint64_t)(pages > 1 ? v.sb : 2 * d)};
+  cuuint32_t box[5] = {64u, (cuuint32_t)rows, (cuuint32_t)parts, 1u, 1u};
+  cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, v.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr int kMaxDevices = 64;
 std::atomic<int> g_sms[kMaxDevices];
 
@@ -107,6 +120,9 @@ std::atomic<int> g_sms[kMaxDevices];
 bool make_map(CUtensorMap* map, const void* base, const Geo& g, int units) { return cached_map(map, base, g, 0, units); }
 bool make_map_view(CUtensorMap* map, const View& v, int d, int N, int heads, int B, int rows) {
   return encode_view(map, v.data, d, N, v.sh ? heads : 1, v.sb ? B : 1, v.sn, v.sh, v.sb, rows);
+}
+bool make_map_pool(CUtensorMap* map, const View& v, int d, int page, int heads, int pages, int rows, int parts) {
+  return encode_pool(map, v, d, page, heads, pages, rows, parts);
 }
 bool make_map_rows(CUtensorMap* map, const void* base, const Geo& g, int units) { return cached_map(map, base, g, 1, units); }
 
