@@ -7,8 +7,9 @@
 // member's queries stay in registers.
 //
 // One warp finds the items, and for each leaves a note of what the others need to know of it, with the numbers of its pages, and copies its
-// queries.  One asks for the items' steps of 64 keys by TMA, page by page, into a ring that all warps share; both run ahead of the
-// others, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a step each:
+// queries.  Two ask for the items' steps of 64 keys by TMA, page by page, into a ring that all warps share, one for keys and one for
+// values; they run ahead of the others, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a
+// step each:
 // products of 16 x 8 x 16 are enough,
 //   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose,
 // and the step's 64 keys give every lane four of them that do not wait for one another.  Weights round to 16 bits once, as operands;
@@ -50,7 +51,7 @@ struct Job {
 template <int D, int NT>
 struct Smem {
   static constexpr int kWarps = 8;  // that take steps
-  static constexpr int kThreads = 32 * (kWarps + 2);
+  static constexpr int kThreads = 32 * (kWarps + 3);
   static constexpr int kHalf = kStep * D * 2, kStepBytes = 2 * kHalf;  // a step's keys, then its values
   static constexpr int kPitch = D + 4;  // of a row of part_o: lanes that store side by side meet different banks
   static constexpr int kRowBytes = D * 2;
@@ -62,7 +63,7 @@ struct Smem {
   Job job[kJobs];
   unsigned long long full[kBars], empty[kStages], note_full[kJobs], job_full[kJobs], job_empty[kJobs], parts_full, parts_read;
   unsigned hole[kStages];  // the step's boxes that have no page
-  int scan[kWarps + 2];
+  int scan[kWarps + 3];
   int4 start;              // the member that this CTA's share begins in, the weight before it, its lengths
   int abort;
 };
@@ -193,12 +194,12 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
   S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gq = lane >> 2, tq = lane & 3;
   if (tid == 0) {
-    for (int s = 0; s < kBars; ++s) mbar_init(s32(&sm.full[s]), 1);
+    for (int s = 0; s < kBars; ++s) mbar_init(s32(&sm.full[s]), 2);  // keys and values
     for (int s = 0; s < kStages; ++s) mbar_init(s32(&sm.empty[s]), 1);
     for (int s = 0; s < kJobs; ++s) {
       mbar_init(s32(&sm.note_full[s]), 1);
       mbar_init(s32(&sm.job_full[s]), 33);  // the note, and every lane's copies
-      mbar_init(s32(&sm.job_empty[s]), kWarps + 1);
+      mbar_init(s32(&sm.job_empty[s]), kWarps + 2);
     }
     mbar_init(s32(&sm.parts_full), kWarps);
     mbar_init(s32(&sm.parts_read), kWarps);
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
       int all;
       weigh(b0 + tid + zero);
       if (b0) __syncthreads();
-      before = block_scan<kWarps + 2>(mine, sm.scan, all);
+      before = block_scan<kWarps + 3>(mine, sm.scan, all);
       total += all;
     }
     begin = (int)((long long)total * blockIdx.x / gridDim.x);
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
       if (g.B > S::kThreads) {
         weigh(b0 + tid + zero);
         __syncthreads();
-        before = block_scan<kWarps + 2>(mine, sm.scan, all);
+        before = block_scan<kWarps + 3>(mine, sm.scan, all);
       }
       const int at = begin - base - before;
       if (at >= 0 && at < mine) sm.start = make_int4(b0 + tid, base + before, s.kl, s.ql);
@@ -319,8 +320,10 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     if (!a.first) settle_stream();
     return;
   }
-  if (warp == kWarps + 1) {
-    // ------------------------------------------------------------- copies of keys and values
+  if (warp > kWarps) {
+    // ------------------------------------------------------------- copies: of keys the first warp, of values the second
+    const bool values = warp == kWarps + 2;
+    const CUtensorMap* map = values ? &map_v : &map_k;
     const int boxes = kStep >> a.box_shift, in_page = (1 << g.shift) - 1;
     const uint32_t box_bytes = (uint32_t)(D * 2) << a.box_shift;
     uint32_t stage = 0, phase = 0, issued = 0, slot = 0, round = 0;
@@ -337,16 +340,13 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         const int s = __ffs(todo) - 1, first = s * boxes;
         ok = warp_wait(s32(&sm.empty[stage]), phase ^ 1, abort, a.status);
         if (!ok) break;
-        const uint32_t bar = s32(&sm.full[issued % kBars]), dst = s32(sm.ring[stage]) + (lane - first) * box_bytes;
+        const uint32_t bar = s32(&sm.full[issued % kBars]), dst = s32(sm.ring[stage]) + (values ? S::kHalf : 0) + (lane - first) * box_bytes;
         if (lane == 0) {
-          sm.hole[stage] = (holes >> first) & low_bits(boxes);
-          mbar_expect_tx(bar, S::kStepBytes);
+          if (!values) sm.hole[stage] = (holes >> first) & low_bits(boxes);
+          mbar_expect_tx(bar, S::kHalf);
         }
         __syncwarp();
-        if (lane >= first && lane < first + boxes) {  // (rows behind the last page arrive as zeros)
-          load_slots(dst, &map_k, bar, at, 0, hk, page);
-          load_slots(dst + S::kHalf, &map_v, bar, at, 0, hk, page);
-        }
+        if (lane >= first && lane < first + boxes) load_slots(dst, map, bar, at, 0, hk, page);  // (rows behind the last page arrive as zeros)
         ++issued;
         if (++stage == kStages) { stage = 0; phase ^= 1; }
       }
@@ -387,16 +387,6 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
       for (int k = 0; k < 4; ++k) tile[k] = D == 64 ? 2048u * k : ((16u * k) >> a.box_shift) * ((uint32_t)(D * 2) << a.box_shift) + ((16u * k) & (box - 1)) * 128u;
       const uint32_t part = box * 128u;
-      if (!whole) {  // a weight of zero does not silence what is no number: values that no row sees become zeros
-        for (int r = 0; r < kStep; r += 32 / (D / 8)) {
-          const int rr = r + lane / (D / 8), c = lane % (D / 8), j = j0 + rr;
-          if (j >= job.kl || (j < job.from && j >= job.sinks))
-            *reinterpret_cast<uint4*>(sm.ring[stage] + S::kHalf + ((unsigned)rr >> a.box_shift) * ((D * 2) << a.box_shift) +
-                                      (c >> 3) * part + (rr & (box - 1)) * 128 + (((c & 7) ^ (rr & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the next copy into the stage comes after these stores)
-        __syncwarp();
-      }
       float z[NT][4][4];  // [keys 16 k ..]: (key gq, row 2 tq), (gq, 2 tq + 1), (gq + 8, 2 tq), (gq + 8, 2 tq + 1)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -433,7 +423,8 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
                 const int n = 16 * k + 8 * y;
-                if (n > to || (n <= from && n >= sinks) || ((hole >> (16 * k >> a.box_shift)) & 1u)) z[nt][k][x + 2 * y] = -INFINITY;
+                const bool hidden = (n > to) | ((n <= from) & (n >= sinks)) | (bool)((hole >> (16 * k >> a.box_shift)) & 1u);
+                z[nt][k][x + 2 * y] = hidden ? -INFINITY : z[nt][k][x + 2 * y];
               }
           }
         }
@@ -464,15 +455,34 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) acc[nt][c][0] = acc[nt][c][1] = acc[nt][c][2] = acc[nt][c][3] = 0.f;
       }
+      auto sums = [&](auto edge) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
+          // A weight of zero does not silence what is no number: on an edge, values that no row sees become zeros.  A lane has the
+          // neighbouring keys 16 k + 2 tq and 8 more.
+          uint32_t keep[2] = {};
+          if constexpr (decltype(edge)::value) {
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          uint32_t f[4];
-          ldsm4t(f, vt + (c >> 2) * part + tile[k] + va + (((2 * (c & 3) + vh) ^ kx) << 4));
+            for (int y = 0; y < 4; ++y) {
+              const int j = j0 + 16 * k + 2 * tq + (y & 1) + 4 * (y & 2);
+              keep[y >> 1] |= (j < job.kl) & ((j >= job.from) | (j < job.sinks)) ? 0xffffu << (16 * (y & 1)) : 0u;
+            }
+          }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma16816<F16>(acc[nt][c], f[0], f[1], f[2], f[3], pt[nt][k][0], pt[nt][k][1]);
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t f[4];
+            ldsm4t(f, vt + (c >> 2) * part + tile[k] + va + (((2 * (c & 3) + vh) ^ kx) << 4));
+            if constexpr (decltype(edge)::value) {
+              f[0] &= keep[0]; f[1] &= keep[0];
+              f[2] &= keep[1]; f[3] &= keep[1];
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816<F16>(acc[nt][c], f[0], f[1], f[2], f[3], pt[nt][k][0], pt[nt][k][1]);
+          }
         }
+      };
+      if (whole) sums(std::false_type{});
+      else sums(std::true_type{});
       __syncwarp();  // the stage has been read
       if (lane == 0) mbar_arrive(s32(&sm.empty[stage]));
 
@@ -553,45 +563,58 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
-// A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.  The lanes work out 32 parts' factors
-// at a time.
+// A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.  The lanes hold the parts' maxima and
+// sums, 32 at a time, and work out their factors.
 template <int D, bool F16, int W>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
+__global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
   constexpr int V = D / 32, A = 8;  // channels of a lane; parts that a warp asks for at a time
+  constexpr int kHeld = 2;          // times 32 parts whose maxima stay in registers
   __shared__ float part_o[W > 1 ? kJoinWarps : 1][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
-  const long long row = (long long)blockIdx.x * (kJoinWarps / W) + warp / W;
-  bool live = row < in.rows;
-  const int i = (int)(row % g.T), head = (int)(row / g.T % g.H), b = live ? (int)(row / g.T / g.H) : 0;
+  const int row = (int)blockIdx.x * (kJoinWarps / W) + warp / W;
+  bool live = row < (int)in.rows;
+  const int i = row % g.T, bh = row / g.T, b = live ? bh / g.H : 0, head = bh - b * g.H;
   const int zero = await_stream();
   const Parts p = parts_of(g, span_of(g, b + zero));
   live = live && i < p.ql;
   const int n = live ? in.shared + p.n : 0;
-  const float2* ml = in.ml + zero + row;
+  const float2* ml = in.ml + row;
+  const float* src = in.o + (long long)row * D + V * lane;
+  const long long step = in.rows * D;
+  float u[A][V];
+  auto ask = [&](int first) {  // parts first, first + W, ...
+#pragma unroll
+    for (int z = 0; z < A; ++z) {
+      const float* at = src + min(first + z * W, n - 1) * step;
+      if constexpr (V == 4) {
+        const float4 t = __ldcg(reinterpret_cast<const float4*>(at));
+        u[z][0] = t.x; u[z][1] = t.y; u[z][2] = t.z; u[z][3] = t.w;
+      } else {
+        const float2 t = __ldcg(reinterpret_cast<const float2*>(at));
+        u[z][0] = t.x; u[z][1] = t.y;
+      }
+    }
+  };
+  auto read = [&](int y) { return y < n ? __ldcg(ml + y * in.rows) : make_float2(-INFINITY, 0.f); };
+  float2 held[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) held[k] = read(32 * k + lane);
+  if (n > 0) ask(w);
   float mx = -INFINITY, sum = 0.f, v[V];
 #pragma unroll
   for (int x = 0; x < V; ++x) v[x] = 0.f;
-  for (int y = lane; y < n; y += 32) mx = fmaxf(mx, __ldcg(&ml[y * in.rows].x));
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) mx = fmaxf(mx, held[k].x);
+  for (int y = 32 * kHeld + lane; y < n; y += 32) mx = fmaxf(mx, read(y).x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
   for (int y0 = 0; y0 < n; y0 += 32) {
-    const float2 part = y0 + lane < n ? __ldcg(&ml[(y0 + lane) * in.rows]) : make_float2(-INFINITY, 0.f);
+    const float2 part = y0 == 0 ? held[0] : y0 == 32 ? held[1] : read(y0 + lane);
     const float f = part.x == -INFINITY ? 0.f : ex2(part.x - mx);
     sum += part.y * f;
     const int m = min(32, n - y0);
     for (int z0 = w; z0 < m; z0 += A * W) {
-      float u[A][V];
-#pragma unroll
-      for (int z = 0; z < A; ++z) {
-        const float* src = in.o + ((y0 + min(z0 + z * W, m - 1)) * in.rows + row) * D + V * lane;
-        if constexpr (V == 4) {
-          const float4 t = __ldcg(reinterpret_cast<const float4*>(src));
-          u[z][0] = t.x; u[z][1] = t.y; u[z][2] = t.z; u[z][3] = t.w;
-        } else {
-          const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
-          u[z][0] = t.x; u[z][1] = t.y;
-        }
-      }
+      if (y0 + z0 > w) ask(y0 + z0);
 #pragma unroll
       for (int z = 0; z < A; ++z) {
         const float fz = __shfl_sync(0xffffffffu, f, (z0 + z * W) & 31);
@@ -615,7 +638,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const PagedGeo
       for (int x = 0; x < V; ++x) v[x] += part_o[warp + y][V * lane + x];
   }
   if (!live) return;
-  const bool some = !(sum <= 0.f);
+  const bool some = !(sum <= 0.f);  // (a sum that is not a number stays one)
   const float inv = some ? 1.f / sum : 0.f;
   char* dst = o.data + b * o.sb + head * o.sh + i * o.sn + 2 * V * lane;
   if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<F16>(v[0] * inv, v[1] * inv), pack2<F16>(v[2] * inv, v[3] * inv));

@@ -111,12 +111,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     const int boxes = U >> a.box_shift, box = 1 << a.box_shift, in_page = (1 << g.shift) - 1;
     const uint32_t box_bytes = (uint32_t)box * 128;
-    // Page numbers of the step's boxes in the lanes (the last page number of all where there is none: its rows arrive as zeros)
+    // Page numbers of the step's boxes in the lanes, -1 where there is none
     auto look_up = [&](const Item& it, int n) {
       const int key = it.k0 + n * U + (lane % boxes << a.box_shift);
       int id = -1;
       if (lane < boxes * a.box_loads && key < a.len) id = __ldg(a.table + (key >> g.shift));
-      return (unsigned)id < (unsigned)g.pages ? id : g.pages;
+      return id;
     };
     auto load = [&](const CUtensorMap* map, int ids, int slot, int hk) {
       const uint32_t s = slot_no % kSlots, bar = s32(&sm.kv_full[s]);
@@ -126,7 +126,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane < boxes * a.box_loads) {  // a lane has a box, or (pages smaller than a step) the half of one
         const int c = lane / boxes, n = lane - c * boxes;
-        load_slots(s32(sm.kv[s]) + c * kSlotPart + n * box_bytes, map, bar, (slot + (n << a.box_shift)) & in_page, c, hk, ids);
+        load_slots(s32(sm.kv[s]) + c * kSlotPart + n * box_bytes, map, bar, (slot + (n << a.box_shift)) & in_page, c, hk,
+                   (unsigned)ids < (unsigned)g.pages ? ids : g.pages);  // (rows behind the last page arrive as zeros)
       }
       __syncwarp();
       ++slot_no;
