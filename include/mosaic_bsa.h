@@ -412,7 +412,8 @@ int mosaic_bsa_paged_append(const mosaic_paged_params *p, const mosaic_view *k, 
  *   Slots that none of a member's rows sees may hold anything; others are expected finite (a value that is not spreads to the rows
  *   that see it, and may spread to the member's other rows).
  *   ws: mosaic_bsa_paged_workspace_bytes(p) bytes (0 on invalid params), 256-byte aligned, the status block first.  It grows with
- *   B * H * Nq times the chunks of 512 keys that a member can have: those of its table row, or of its window. */
+ *   B * H * Nq times the chunks of 512 keys that a member can have: those of its table row, or of its window.
+ *   (MOSAIC_E_UNSUPPORTED where B * Hkv * chunks times the blocks of Nq * H / Hkv rows reach 2^31 / 10.) */
 size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params *p);
 int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
                             const int32_t *table, const int32_t *k_len, const int32_t *q_len, const mosaic_view *o, float *lse, void *ws,
@@ -422,7 +423,7 @@ int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, 
  * on the device holds its pages (by the same rule, entries outside the pool are not there).  Every row sees the whole prefix and its
  * member's own keys as above (window 0); table, k_len and q_len count the member's own tokens alone, and k_len may be 0.  The prefix is
  * read once for the whole batch.
- *   ws as above (p with prefix_len): B * H * Nq times the parts of the prefix more, of which there are 2 * 148 / Hkv or fewer.
+ *   ws as above (p with prefix_len): B * H * Nq times the parts of the prefix more, of which there are at most 2 * 148 / Hkv + 1.
  *   How the prefix is cut into parts follows from its length, Hkv and B * Nq * H / Hkv, so a member's bits depend on the shape of the
  *   call, but on nothing that another member holds, nor on its place. */
 int mosaic_bsa_prefix_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,

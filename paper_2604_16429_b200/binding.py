@@ -466,6 +466,12 @@ def _out(name, t, shape, dtype, index):
     return v
 
 
+def _made(t):
+    """The same for an output that was made here"""
+    st = t.stride()
+    return t.data_ptr(), st[0], st[1], st[2]
+
+
 def _flat(name, t, shape, dtype, index):
     """Pointer of a contiguous tensor."""
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
@@ -724,11 +730,12 @@ class PagedParams:
 
 
 def _pools(x, k_pages, v_pages, heads, d, index):
-    """(pages, page, packed views) of the pools [pages, Hkv, page, d] that go with x"""
+    """(pages, page, packed views) of the pools [pages, Hkv, page, d] that go with x (the library refuses rows that overlap)"""
     if k_pages.dim() != 4:
         raise ValueError(f"k_pages: expected [pages, Hkv, page, d], got {tuple(k_pages.shape)}")
-    shape = (k_pages.shape[0], heads, k_pages.shape[2], d)
-    return shape[0], shape[2], _out("k_pages", k_pages, shape, x.dtype, index) + _out("v_pages", v_pages, shape, x.dtype, index)
+    pages, _, page, _ = k_pages.shape
+    shape, t = (pages, heads, page, d), x.dtype
+    return pages, page, _view("k_pages", k_pages, shape, t, index) + _view("v_pages", v_pages, shape, t, index)
 
 
 def _page_table(name, t, B, index):
@@ -760,8 +767,11 @@ def mosaic_bsa_paged_append(rp: RotaryParams, k, v, k_pages, v_pages, table, k_l
         vq = ()
     else:
         vq = _view("q", q, sq, t, index)
-        q_out = _like(q, stream) if q_out is None else q_out
-        vq += _out("q_out", q_out, sq, t, index)
+        if q_out is None:
+            q_out = _like(q, stream)
+            vq += _made(q_out)
+        else:
+            vq += _out("q_out", q_out, sq, t, index)
     fr = _flat("freqs", freqs, (rot // 2,), torch.float64, index) if rot else 0
     block = _block
     a = block.at
@@ -776,14 +786,14 @@ def mosaic_bsa_paged_append(rp: RotaryParams, k, v, k_pages, v_pages, table, k_l
 
 
 def _paged_params(pp, q, k_pages, table, prefix_len, index):
-    """(parameters, shape of the pools) of the attention of q [B,H,Nq,d]"""
+    """(parameters, pointer of the table) of the attention of q [B,H,Nq,d]"""
     if q.dtype is torch.float32:
         raise ValueError("attention over a paged cache takes bf16 or fp16 tensors")
     B, H, T, d = q.shape
     pages, Hkv, page, _ = k_pages.shape
-    _, step, width = _page_table("table", table, B, index)
+    at, step, width = _page_table("table", table, B, index)
     window = pp.window if prefix_len or pp.window < width * page else 0  # (one that holds every token is none)
-    return (step, 0, B, H, Hkv, T, d, page, pages, width, window, pp.sinks, prefix_len, 0, pp.scale, 0.0, _STORAGE[q.dtype]), (pages, Hkv, page, d)
+    return (step, 0, B, H, Hkv, T, d, page, pages, width, window, pp.sinks, prefix_len, 0, pp.scale, 0.0, _STORAGE[q.dtype]), at
 
 
 def paged_workspace_bytes(pp: PagedParams, q, k_pages, table, prefix_len=0) -> int:
@@ -792,56 +802,59 @@ def paged_workspace_bytes(pp: PagedParams, q, k_pages, table, prefix_len=0) -> i
     return int(lib().mosaic_bsa_paged_workspace_bytes(_params_block(_paged_pack[0], p)))
 
 
+def _paged_attention(name, pp, q, k_pages, v_pages, prefix, table, k_len, q_len, o, lse, ws, stream):
+    """`prefix`: (its table, its tokens), or None"""
+    index = _chk_seq(q, k_pages)
+    p, at = _paged_params(pp, q, k_pages, table, prefix[1] if prefix else 0, index)
+    t, sq = q.dtype, q.shape
+    B = sq[0]
+    vq, pools = _view("q", q, sq, t, index), _pools(q, k_pages, v_pages, p[4], p[6], index)[2]
+    tables = (at,)
+    if prefix:
+        first, n = prefix
+        if first.dim() != 1 or first.shape[0] * p[7] < n:
+            raise _bad("prefix_table", first, f"int32 [{-(-n // max(p[7], 1))}] or more")
+        tables = (_flat("prefix_table", first, first.shape, torch.int32, index), at)
+    lens = _flat("k_len", k_len, (B,), torch.int32, index), _len("q_len", q_len, B, index)
+    if o is None:
+        o = _like(q, stream)
+        vo = _made(o)
+    else:
+        vo = _out("o", o, sq, t, index)
+    if lse is None:
+        lse = _rows_like(q, stream)
+        rows = lse.data_ptr()
+    else:
+        rows = _flat("lse", lse, sq[:3], torch.float32, index)
+    block = _block
+    a = block.at
+    try:
+        _paged_pack[4](block.buf, 0, *p, *vq, *pools, *vo)
+    except _RANGE as e:
+        raise _out_of_range(e) from None
+    ws = _paged_ws(a, index, ws, stream)
+    _call(name, index, stream, a, a + 80, a + 112, a + 144, *tables, *lens, a + 176, rows, ws.data_ptr(), ws.numel())
+    return o, lse
+
+
 def _paged_ws(at, index, ws, stream):
+    if ws is not None:
+        return _scratch(0, "", index, ws, stream)
     name = "mosaic_bsa_paged_workspace_bytes"
-    return _scratch(0 if ws is not None else int(getattr(_lib or lib(), name)(at)), name, index, ws, stream)
+    return _scratch((_lib or lib()).mosaic_bsa_paged_workspace_bytes(at), name, index, None, stream)
 
 
 def mosaic_bsa_paged_decode(pp: PagedParams, q, k_pages, v_pages, table, k_len, q_len=None, o=None, lse=None, ws=None, stream=None):
     """Attention of new tokens q [B,H,Nq,d], Nq at most 16, over their members' pages: a member's q_len[b] new tokens (None: Nq for
     all) are the last of the k_len[b] that its pages hold.  Returns (o, lse)."""
-    index = _chk_seq(q, k_pages)
-    p, sk = _paged_params(pp, q, k_pages, table, 0, index)
-    t, sq = q.dtype, q.shape
-    vq, vk, vv = _view("q", q, sq, t, index), _out("k_pages", k_pages, sk, t, index), _out("v_pages", v_pages, sk, t, index)
-    o = _like(q, stream) if o is None else o
-    lse = _rows_like(q, stream) if lse is None else lse
-    block = _block
-    a = block.at
-    try:
-        _paged_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
-    except _RANGE as e:
-        raise _out_of_range(e) from None
-    ws = _paged_ws(a, index, ws, stream)
-    _call("mosaic_bsa_paged_decode", index, stream, a, a + 80, a + 112, a + 144, table.data_ptr(),
-          _flat("k_len", k_len, (sq[0],), torch.int32, index), _len("q_len", q_len, sq[0], index), a + 176,
-          _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
-    return o, lse
+    return _paged_attention("mosaic_bsa_paged_decode", pp, q, k_pages, v_pages, None, table, k_len, q_len, o, lse, ws, stream)
 
 
 def mosaic_bsa_prefix_decode(pp: PagedParams, q, k_pages, v_pages, prefix_table, prefix_len, table, k_len, q_len=None, o=None, lse=None,
                              ws=None, stream=None):
     """mosaic_bsa_paged_decode for a batch whose members all begin with the first `prefix_len` tokens of the pages that prefix_table
     [>= prefix_len / page] int32 names; table, k_len and q_len count the members' own tokens.  No window.  Returns (o, lse)."""
-    index = _chk_seq(q, k_pages)
     if prefix_len <= 0:
         raise ValueError(f"prefix_len: expected at least one token, got {prefix_len}")
-    p, sk = _paged_params(pp, q, k_pages, table, prefix_len, index)
-    t, sq = q.dtype, q.shape
-    if prefix_table.dim() != 1 or prefix_table.shape[0] * sk[2] < prefix_len:
-        raise _bad("prefix_table", prefix_table, f"int32 [{-(-prefix_len // max(sk[2], 1))}] or more")
-    vq, vk, vv = _view("q", q, sq, t, index), _out("k_pages", k_pages, sk, t, index), _out("v_pages", v_pages, sk, t, index)
-    o = _like(q, stream) if o is None else o
-    lse = _rows_like(q, stream) if lse is None else lse
-    block = _block
-    a = block.at
-    try:
-        _paged_pack[4](block.buf, 0, *p, *vq, *vk, *vv, *_out("o", o, sq, t, index))
-    except _RANGE as e:
-        raise _out_of_range(e) from None
-    ws = _paged_ws(a, index, ws, stream)
-    _call("mosaic_bsa_prefix_decode", index, stream, a, a + 80, a + 112, a + 144,
-          _flat("prefix_table", prefix_table, prefix_table.shape, torch.int32, index), table.data_ptr(),
-          _flat("k_len", k_len, (sq[0],), torch.int32, index), _len("q_len", q_len, sq[0], index), a + 176,
-          _flat("lse", lse, sq[:3], torch.float32, index), ws.data_ptr(), ws.numel())
-    return o, lse
+    return _paged_attention("mosaic_bsa_prefix_decode", pp, q, k_pages, v_pages, (prefix_table, prefix_len), table, k_len, q_len, o, lse, ws,
+                            stream)

@@ -92,28 +92,34 @@ PartsOut parts_out(const mosaic_paged_params* p, void* ws, int shared, int all) 
   const Layout w = layout(p, all);
   return {(float*)((char*)ws + w.o), (float2*)((char*)ws + w.ml), (long long)p->B * p->H * p->Nq, shared};
 }
+size_t workspace(const mosaic_paged_params* p, int shared) {
+  return !shared && is_direct(p) ? kStatusBytes : layout(p, shared + most_parts(p)).total;
+}
 // Tensors, buffers and device of an attention call, whose parameters have been checked
 struct Call {
   HostCtx c;
   PagedGeo g;
-  View q, k, v, o;
+  View q, o;
+  PoolMaps maps;
   bool f16;
 };
-int make_call(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages, const int32_t* table,
-              const int32_t* k_len, const int32_t* q_len, const mosaic_view* o, float* lse, void* ws, size_t ws_bytes, void* cuda_stream,
-              Call* t) {
+int make_call(const mosaic_paged_params* p, int shared, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages,
+              const int32_t* table, const int32_t* k_len, const int32_t* q_len, const mosaic_view* o, float* lse, void* ws, size_t ws_bytes,
+              void* cuda_stream, Call* t) {
   int rc;
-  if ((rc = check_view(q, p->B, p->H, p->Nq, 2, &t->q)) || (rc = check_pool(k_pages, p, &t->k)) || (rc = check_pool(v_pages, p, &t->v)) ||
-      (rc = check_view(o, p->B, p->H, p->Nq, 2, &t->o)) || (rc = make_geo(p, table, k_len, q_len, &t->g)))
+  if ((rc = check_view(q, p->B, p->H, p->Nq, 2, &t->q)) || (rc = check_pool(k_pages, p, &t->maps.k_pages)) ||
+      (rc = check_pool(v_pages, p, &t->maps.v_pages)) || (rc = check_view(o, p->B, p->H, p->Nq, 2, &t->o)) ||
+      (rc = make_geo(p, table, k_len, q_len, &t->g)))
     return rc;
   if (!lse || !ws) return MOSAIC_E_INVALID_ARG;
   if (!aligned(lse, 4) || !aligned(ws, 256)) return MOSAIC_E_MISALIGNED;
-  if (ws_bytes < mosaic_bsa_paged_workspace_bytes(p)) return MOSAIC_E_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < workspace(p, shared)) return MOSAIC_E_WORKSPACE_TOO_SMALL;
   t->c = {};
   t->c.stream = (cudaStream_t)cuda_stream;
   t->c.status = (int*)ws;
   t->f16 = (p->flags & MOSAIC_FLAG_FP16) != 0;
-  return device_ok();
+  if ((rc = device_ok())) return rc;
+  return t->maps.make(t->g) ? MOSAIC_OK : MOSAIC_E_CUDA;
 }
 }  // namespace
 
@@ -150,8 +156,8 @@ int mosaic_bsa_paged_append(const mosaic_paged_params* p, const mosaic_view* k, 
 
 size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params* p) {
   if (check_attention(p)) return 0;
-  if (!p->prefix_len) return is_direct(p) ? kStatusBytes : layout(p, most_parts(p)).total;
-  return check_prefix(p) ? 0 : layout(p, shared_parts(p, nullptr) + most_parts(p)).total;
+  if (!p->prefix_len) return workspace(p, 0);
+  return check_prefix(p) ? 0 : workspace(p, shared_parts(p, nullptr));
 }
 
 int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, const mosaic_view* k_pages, const mosaic_view* v_pages,
@@ -161,11 +167,11 @@ int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, 
   if (rc) return rc;
   if (p->prefix_len) return MOSAIC_E_INVALID_ARG;
   Call t;
-  if ((rc = make_call(p, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
+  if ((rc = make_call(p, 0, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
   const bool direct = is_direct(p);
   const int most = most_parts(p);
   const PartsOut parts = parts_out(p, ws, 0, most);
-  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.k, t.v, parts, most, direct, true, t.o, lse)) || direct) return rc;
+  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.maps, parts, most, direct, true, t.o, lse)) || direct) return rc;
   return launch_paged_join(t.c, t.g, t.f16, parts, most, t.o, lse);
 }
 
@@ -176,13 +182,13 @@ int mosaic_bsa_prefix_decode(const mosaic_paged_params* p, const mosaic_view* q,
   if (rc || (rc = check_prefix(p))) return rc;
   if (!prefix_table) return MOSAIC_E_INVALID_ARG;
   if (!aligned(prefix_table, 4)) return MOSAIC_E_MISALIGNED;
-  Call t;
-  if ((rc = make_call(p, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
   int chunk = 0;
   const int shared = shared_parts(p, &chunk), most = most_parts(p);
+  Call t;
+  if ((rc = make_call(p, shared, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
   const PartsOut parts = parts_out(p, ws, shared, shared + most);
-  if ((rc = launch_prefix_fwd(t.c, t.g, t.f16, t.q, t.k, t.v, prefix_table, p->prefix_len, chunk, parts))) return rc;
-  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.k, t.v, parts, most, false, false, t.o, lse))) return rc;
+  if ((rc = launch_prefix_fwd(t.c, t.g, t.f16, t.q, t.maps, prefix_table, p->prefix_len, chunk, parts))) return rc;
+  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.maps, parts, most, false, false, t.o, lse))) return rc;
   return launch_paged_join(t.c, t.g, t.f16, parts, shared + most, t.o, lse);
 }
 

@@ -69,17 +69,6 @@ struct AppendTensors {
 int launch_paged_append(const HostCtx& c, const PagedGeo& g, const mosaic_paged_params* p, const double* freqs, const AppendTensors& t);
 
 
-// Attention over the members' own pages: parts to the workspace, or, where a member can have but one and there is no prefix (`direct`),
-// results.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
-int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                       const PartsOut& parts, int most_parts, bool direct, bool first, const View& o, float* lse);
-// Attention over a prefix that all members share: its parts are the first of every row.  How it is cut follows from its length, the
-// key/value heads and the rows of a head; `chunk`: keys of a part.
-int prefix_parts(int len, int kv_heads, long long rows, int* chunk);
-int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                      const int32_t* prefix_table, int prefix_len, int chunk, const PartsOut& parts);
-// Joins all parts of every row
-int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const PartsOut& parts, int most_parts, const View& o, float* lse);
 // A map of a pool in boxes of `rows` slots by `parts` times 64 channels, and the copy of one from 64 * part on
 bool make_map_pool(CUtensorMap* map, const View& v, int d, int page, int heads, int pages, int rows, int parts);
 __device__ __forceinline__ void load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int part, int head, int page) {
@@ -88,5 +77,30 @@ __device__ __forceinline__ void load_slots(uint32_t dst, const CUtensorMap* map,
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(slot), "r"(part), "r"(head), "r"(page)
       : "memory");
 }
+constexpr int kBoxShift = 6;  // log2 of the slots that a box has at the most: the keys of a step
+
+// The pools and their maps in boxes of a page, or of a step's slots, and all channels
+struct PoolMaps {
+  View k_pages, v_pages;
+  CUtensorMap k, v;
+  int box_shift;  // log2 of a box's slots
+  bool make(const PagedGeo& g) {
+    box_shift = g.shift < kBoxShift ? g.shift : kBoxShift;
+    return make_map_pool(&k, k_pages, g.d, 1 << g.shift, g.Hkv, g.pages, 1 << box_shift, g.d / 64) &&
+           make_map_pool(&v, v_pages, g.d, 1 << g.shift, g.Hkv, g.pages, 1 << box_shift, g.d / 64);
+  }
+};
+
+// Attention over the members' own pages: parts to the workspace, or, where a member can have but one and there is no prefix (`direct`),
+// results.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
+int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
+                       int most_parts, bool direct, bool first, const View& o, float* lse);
+// Attention over a prefix that all members share: its parts are the first of every row.  How it is cut follows from its length, the
+// key/value heads and the rows of a head; `chunk`: keys of a part.
+int prefix_parts(int len, int kv_heads, long long rows, int* chunk);
+int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const int32_t* prefix_table,
+                      int prefix_len, int chunk, const PartsOut& parts);
+// Joins all parts of every row
+int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const PartsOut& parts, int most_parts, const View& o, float* lse);
 
 }  // namespace mosaic

@@ -153,7 +153,7 @@ struct Walk {
     return __ballot_sync(0xffffffffu, lane < kSteps && seen(key0() + lane * kStep, kStep));
   }
 };
-static_assert(kStep == 64, "weights count steps by shifts");
+static_assert(kStep == 64 && kBoxShift == 6, "weights count steps by shifts");
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -531,14 +531,14 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
       for (int d = 1; d < 8; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int y = 0; y < kWarps; ++y) {
-        if (!((steps >> y) & 1u)) continue;
+      for (int y = 0; y < kWarps; ++y) {  // (without branches, so that the loads overlap; what a warp has not left is not looked at)
+        const bool on = (steps >> y) & 1u;
         const float f = __shfl_sync(0xffffffffu, factor, (lane & 24) | y);
         const float4 u = *reinterpret_cast<const float4*>(&sm.part_o[y][h][c]);
-        v.x = fmaf(u.x, f, v.x);
-        v.y = fmaf(u.y, f, v.y);
-        v.z = fmaf(u.z, f, v.z);
-        v.w = fmaf(u.w, f, v.w);
+        v.x = on ? fmaf(u.x, f, v.x) : v.x;
+        v.y = on ? fmaf(u.y, f, v.y) : v.y;
+        v.z = on ? fmaf(u.z, f, v.z) : v.z;
+        v.w = on ? fmaf(u.w, f, v.w) : v.w;
       }
       if (r >= rows || i >= job.ql) continue;
       const int head = job.head0 + r - i * g.G;
@@ -647,13 +647,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
 }
 
 template <int D, bool F16, int NT>
-int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const View& k_pages, const View& v_pages, int most_parts) {
-  CUtensorMap mk, mv;
-  a.box_shift = g.shift < 6 ? g.shift : 6;
-  a.inv_g = 1.f / (float)g.G;
-  if (!make_map_pool(&mk, k_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, D / 64) ||
-      !make_map_pool(&mv, v_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, D / 64))
-    return MOSAIC_E_CUDA;
+int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps& maps, int most_parts) {
   constexpr size_t smem = sizeof(Smem<D, NT>) + 1024;
   static_assert(smem <= kMaxSmem, "more shared memory than a CTA can have");
   static unsigned long long configured = 0;
@@ -662,7 +656,7 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const View& k_p
   a.blocks = (g.G * g.T + 8 * NT - 1) / (8 * NT);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
   if (most * kFull > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
-  return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, mk, mv);
+  return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, maps.k, maps.v);
 }
 
 template <int D, bool F16, int W>
@@ -681,18 +675,18 @@ int by_type(int d, bool f16, F&& f) {
 
 }  // namespace
 
-int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                       const PartsOut& parts, int most_parts, bool direct, bool first, const View& o, float* lse) {
-  const DecArgs a = {q, o, lse, parts, 0, 0, direct, first, 0.f, c.status};
+int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
+                       int most_parts, bool direct, bool first, const View& o, float* lse) {
+  const DecArgs a = {q, o, lse, parts, 0, maps.box_shift, direct, first, 1.f / (float)g.G, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
     if constexpr (D == 64) {
-      if (g.G * g.T > 24) return launch_parts<D, F16, 4>(c, g, a, k_pages, v_pages, most_parts);
-      if (g.G * g.T > 16) return launch_parts<D, F16, 3>(c, g, a, k_pages, v_pages, most_parts);
+      if (g.G * g.T > 24) return launch_parts<D, F16, 4>(c, g, a, maps, most_parts);
+      if (g.G * g.T > 16) return launch_parts<D, F16, 3>(c, g, a, maps, most_parts);
     }
-    return g.G * g.T > 8 ? launch_parts<D, F16, 2>(c, g, a, k_pages, v_pages, most_parts)
-                         : launch_parts<D, F16, 1>(c, g, a, k_pages, v_pages, most_parts);
+    return g.G * g.T > 8 ? launch_parts<D, F16, 2>(c, g, a, maps, most_parts)
+                         : launch_parts<D, F16, 1>(c, g, a, maps, most_parts);
   });
 }
 

@@ -25,7 +25,7 @@ constexpr int kLaunchRegs = 168, kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(2 * kSoftmaxRegs + kOtherRegs <= 3 * kLaunchRegs, "the shares exceed the launch's registers");
 constexpr uint32_t kTmemCols = 512, kColO = 256;  // scores, and weights over them, below; O of tile t at kColO + d t
 constexpr float kRescaleThreshold = 8.0f;         // log2 units: weights stay below 2^8
-constexpr int U = 64;                             // keys of a step
+constexpr int U = 1 << kBoxShift;                 // keys of a step
 constexpr int kSlots = 8;                         // ring of key and value tiles
 __host__ __device__ constexpr uint32_t score_col(int t, uint32_t b) { return 128 * t + 64 * b; }
 
@@ -463,24 +463,26 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 namespace {
 template <int D, bool F16>
-int launch(const HostCtx& c, const PagedGeo& g, PrefixArgs a, const View& k_pages, const View& v_pages) {
-  CUtensorMap mk, mv;
-  const int box = 1 << a.box_shift, parts = D / 64 / a.box_loads;
-  if (!make_map_pool(&mk, k_pages, D, 1 << g.shift, g.Hkv, g.pages, box, parts) ||
-      !make_map_pool(&mv, v_pages, D, 1 << g.shift, g.Hkv, g.pages, box, parts))
+int launch(const HostCtx& c, const PagedGeo& g, const PrefixArgs& a, const PoolMaps& maps) {
+  // pages smaller than a step come by halves of their channels, which lie a tile's rows apart
+  CUtensorMap k = maps.k, v = maps.v;
+  if (a.box_loads > 1 && (!make_map_pool(&k, maps.k_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, 1) ||
+                          !make_map_pool(&v, maps.v_pages, D, 1 << g.shift, g.Hkv, g.pages, 1 << a.box_shift, 1)))
     return MOSAIC_E_CUDA;
   const size_t smem = sizeof(Smem<D>) + 1024;
   static unsigned long long configured = 0;
   int sms = 0;
   if (const int rc = launch_setup_regs(reinterpret_cast<const void*>(prefix_fwd_kernel<D, F16>), kLaunchRegs, smem, &configured, &sms)) return rc;
-  return launch_kernel(prefix_fwd_kernel<D, F16>, dim3((unsigned)(a.total < sms ? a.total : sms)), kThreads, smem, c.stream, true, 0, g, a, mk, mv);
+  return launch_kernel(prefix_fwd_kernel<D, F16>, dim3((unsigned)(a.total < sms ? a.total : sms)), kThreads, smem, c.stream, true, 0, g, a, k, v);
 }
 
 constexpr int pairs_of(long long rows) { return (int)((rows + 2 * kRows - 1) / (2 * kRows)); }
 }  // namespace
 
-// Parts of a prefix of `len` keys: as many as make the longest SM's work shortest.  An SM takes ceil(items / SMs) items of its part's steps
-// and four steps' time for their start and end.
+// Parts of a prefix of `len` keys: as many as make the longest SM's work shortest.  An SM takes ceil(items / SMs) items, each of its part's
+// steps and kTurn steps' time for its start and end (measured: 5000 cycles to its rows of q, 2000 to its first weights, 5000 to write
+// its sums, against 1970 a step).
+constexpr int kTurn = 6;
 int prefix_parts(int len, int kv_heads, long long rows, int* chunk) {
   const long long units = (long long)kv_heads * pairs_of(rows);
   const int steps = (len + U - 1) / U;
@@ -489,7 +491,7 @@ int prefix_parts(int len, int kv_heads, long long rows, int* chunk) {
   for (int n = 1; n <= steps && (n == 1 || units * (n - 1) < 2 * kSms); ++n) {
     const int each = (steps + n - 1) / n;
     if ((steps + each - 1) / each != n) continue;
-    const long long cost = (units * n + kSms - 1) / kSms * (each + 4);
+    const long long cost = (units * n + kSms - 1) / kSms * (each + kTurn);
     if (n == 1 || cost < best) {
       best = cost;
       parts = n;
@@ -499,8 +501,8 @@ int prefix_parts(int len, int kv_heads, long long rows, int* chunk) {
   return parts;
 }
 
-int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const View& k_pages, const View& v_pages,
-                      const int32_t* prefix_table, int prefix_len, int chunk, const PartsOut& parts) {
+int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const int32_t* prefix_table,
+                      int prefix_len, int chunk, const PartsOut& parts) {
   PrefixArgs a = {};
   a.q = q;
   a.table = prefix_table;
@@ -510,14 +512,14 @@ int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View&
   const long long rows = (long long)g.B * g.T * g.G;
   a.rows = (int)rows;
   a.pairs = pairs_of(rows);
-  a.box_shift = g.shift < 6 ? g.shift : 6;
-  a.box_loads = g.shift < 6 ? g.d / 64 : 1;
+  a.box_shift = maps.box_shift;
+  a.box_loads = a.box_shift < kBoxShift ? g.d / 64 : 1;
   const long long total = (long long)g.Hkv * parts.shared * a.pairs;
   if (total > 0x7ffffff0ll) return MOSAIC_E_UNSUPPORTED;
   a.total = (int)total;
   a.status = c.status;
-  if (g.d == 64) return f16 ? launch<64, true>(c, g, a, k_pages, v_pages) : launch<64, false>(c, g, a, k_pages, v_pages);
-  return f16 ? launch<128, true>(c, g, a, k_pages, v_pages) : launch<128, false>(c, g, a, k_pages, v_pages);
+  if (g.d == 64) return f16 ? launch<64, true>(c, g, a, maps) : launch<64, false>(c, g, a, maps);
+  return f16 ? launch<128, true>(c, g, a, maps) : launch<128, false>(c, g, a, maps);
 }
 
 }  // namespace mosaic

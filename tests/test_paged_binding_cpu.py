@@ -93,10 +93,8 @@ def test_numbers_that_no_field_holds_are_refused(seen):
 
 def test_what_does_not_fit_is_refused(seen):
     f32, f16 = torch.float32, torch.float16
-    strided = Tensor(50, 2, 16, 64)
-    strided.strides = (2048, 0, 64, 1)
     for kw in (dict(q=Tensor(2, 4, 3, 64, dtype=f32)), dict(k_pages=Tensor(50, 2, 16, 64, dtype=f16)), dict(v_pages=Tensor(50, 2, 32, 64)),
-               dict(v_pages=Tensor(49, 2, 16, 64)), dict(k_pages=strided), dict(table=Tensor(3, 7, dtype=I32)), dict(table=Tensor(2, 7)),
+               dict(v_pages=Tensor(49, 2, 16, 64)), dict(table=Tensor(3, 7, dtype=I32)), dict(table=Tensor(2, 7)),
                dict(table=Tensor(14, dtype=I32)), dict(k_len=Tensor(3, dtype=I32)), dict(k_len=Tensor(2, dtype=torch.int64)),
                dict(q_len=Tensor(3, dtype=I32)), dict(o=Tensor(2, 4, 3, 128)), dict(lse=Tensor(2, 4, 3)), dict(ws=Tensor(9)),
                dict(k_pages=Tensor(50, 2, 16, 32))):
@@ -114,7 +112,7 @@ def test_what_does_not_fit_is_refused(seen):
     assert seen == []
 
 
-@pytest.mark.parametrize("name", ["mosaic_bsa_paged_append", "mosaic_bsa_paged_decode", "mosaic_bsa_prefix_decode", "_paged_ws"])
+@pytest.mark.parametrize("name", ["mosaic_bsa_paged_append", "mosaic_bsa_paged_decode", "mosaic_bsa_prefix_decode", "_paged_attention", "_paged_ws"])
 def test_no_call_allocates_past_its_stream(name):
     tree = ast.parse(inspect.getsource(getattr(mb, name)))
     for call in (n for n in ast.walk(tree) if isinstance(n, ast.Call)):
