@@ -45,6 +45,7 @@ int check_attention(const mosaic_paged_params* p) {
   if (p->H <= 0 || p->H % p->Hkv || p->window < 0 || p->sinks < 0 || p->prefix_len < 0) return MOSAIC_E_INVALID_ARG;
   if (!(p->scale == p->scale) || isinf(p->scale)) return MOSAIC_E_INVALID_ARG;
   if (p->Nq > kMaxNew || p->sinks > kMaxSinks || (long long)p->B * p->H > (1 << 24)) return MOSAIC_E_UNSUPPORTED;
+  if ((long long)p->H / p->Hkv * p->Nq > (1 << 20)) return MOSAIC_E_UNSUPPORTED;
   return MOSAIC_OK;
 }
 
@@ -77,7 +78,14 @@ int shared_parts(const mosaic_paged_params* p, int* chunk) {
   int keys;
   return prefix_parts(p->prefix_len, p->Hkv, (long long)p->B * p->Nq * (p->H / p->Hkv), chunk ? chunk : &keys);
 }
-bool is_direct(const mosaic_paged_params* p) { return most_parts(p) == 1; }  // the part is the result
+// Members that can have one part only get their results from the kernel that makes it.  Behind a prefix that is a launch less, but the
+// kernel joins a row's parts one item after the other: taken up to some 40 parts a CTA.  (us on the device, with the join's kernel and
+// without: 33 members behind 16 parts 30.6 and 28.0; 8 behind 32 16.7 and 16.5; 64 of 4 key heads behind 37, two items a CTA, 49.4 and 53.7.)
+bool is_direct(const mosaic_paged_params* p, int shared) {
+  if (most_parts(p) != 1) return false;
+  const long long items = (long long)p->B * p->Hkv * paged_row_blocks(p->d, p->H / p->Hkv * p->Nq);
+  return (items + kSms - 1) / kSms * shared <= 40;
+}
 
 }  // namespace
 
@@ -93,7 +101,8 @@ PartsOut parts_out(const mosaic_paged_params* p, void* ws, int shared, int all) 
   return {(float*)((char*)ws + w.o), (float2*)((char*)ws + w.ml), (long long)p->B * p->H * p->Nq, shared};
 }
 size_t workspace(const mosaic_paged_params* p, int shared) {
-  return !shared && is_direct(p) ? kStatusBytes : layout(p, shared + most_parts(p)).total;
+  const int own = is_direct(p, shared) ? 0 : most_parts(p);
+  return shared + own ? layout(p, shared + own).total : kStatusBytes;
 }
 // Tensors, buffers and device of an attention call, whose parameters have been checked
 struct Call {
@@ -168,7 +177,7 @@ int mosaic_bsa_paged_decode(const mosaic_paged_params* p, const mosaic_view* q, 
   if (p->prefix_len) return MOSAIC_E_INVALID_ARG;
   Call t;
   if ((rc = make_call(p, 0, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
-  const bool direct = is_direct(p);
+  const bool direct = is_direct(p, 0);
   const int most = most_parts(p);
   const PartsOut parts = parts_out(p, ws, 0, most);
   if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.maps, parts, most, direct, true, t.o, lse)) || direct) return rc;
@@ -186,9 +195,10 @@ int mosaic_bsa_prefix_decode(const mosaic_paged_params* p, const mosaic_view* q,
   const int shared = shared_parts(p, &chunk), most = most_parts(p);
   Call t;
   if ((rc = make_call(p, shared, q, k_pages, v_pages, table, k_len, q_len, o, lse, ws, ws_bytes, cuda_stream, &t))) return rc;
-  const PartsOut parts = parts_out(p, ws, shared, shared + most);
+  const bool direct = is_direct(p, shared);
+  const PartsOut parts = parts_out(p, ws, shared, direct ? shared : shared + most);
   if ((rc = launch_prefix_fwd(t.c, t.g, t.f16, t.q, t.maps, prefix_table, p->prefix_len, chunk, parts))) return rc;
-  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.maps, parts, most, false, false, t.o, lse))) return rc;
+  if ((rc = launch_paged_parts(t.c, t.g, t.f16, t.q, t.maps, parts, most, direct, false, t.o, lse)) || direct) return rc;
   return launch_paged_join(t.c, t.g, t.f16, parts, shared + most, t.o, lse);
 }
 

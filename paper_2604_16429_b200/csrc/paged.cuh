@@ -91,8 +91,10 @@ struct PoolMaps {
   }
 };
 
-// Attention over the members' own pages: parts to the workspace, or, where a member can have but one and there is no prefix (`direct`),
-// results.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
+// Blocks that the rows of a key/value head are taken in
+int paged_row_blocks(int d, int rows);
+// Attention over the members' own pages: parts to the workspace, or, where a member can have but one, results (`direct`), joined with the
+// prefix' parts if there are any.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
                        int most_parts, bool direct, bool first, const View& o, float* lse);
 // Attention over a prefix that all members share: its parts are the first of every row.  How it is cut follows from its length, the

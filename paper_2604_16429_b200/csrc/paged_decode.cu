@@ -3,18 +3,17 @@
 //   o_i = sum_j exp(scale q_i . k_j - m_i) v_j / l_i  over the keys that row i sees: j <= p_i, and p_i - j < window or j < sinks
 // HBM-bound: the visible keys and values of a key/value head are read once for all rows (new tokens x query heads of the group, a
 // block of them at a time).  The keys of a member are cut into chunks of 512; a chunk of a head is an item.  Persistent CTAs, one an SM,
-// take equal shares of the list of all items, which each works out from the lengths; a CTA's items lie one after the other, so that a
-// member's queries stay in registers.
+// take equal shares of the list of all items, which each works out from the lengths.
 //
 // One warp finds the items, and for each leaves a note of what the others need to know of it, with the numbers of its pages, and copies its
 // queries.  Two ask for the items' steps of 64 keys by TMA, page by page, into a ring that all warps share, one for keys and one for
 // values; they run ahead of the others, so that the memory never waits for a chunk's end.  The others take the chunk's steps in turn, a
-// step each:
-// products of 16 x 8 x 16 are enough,
+// step each: products of 16 x 8 x 16 are enough,
 //   S^T = K Q^T (16 keys x 8 rows), O^T += V^T P^T (16 channels x 8 rows), P^T turned from accumulator to operand by a transpose,
 // and the step's 64 keys give every lane four of them that do not wait for one another.  Weights round to 16 bits once, as operands;
 // everything else is fp32.  The warps' maxima, sums and accumulators are joined through shared memory at the chunk's end, and leave as a
-// part; a second kernel joins a row's parts in their order.
+// part; a second kernel joins a row's parts in their order.  Members that can have one part only get their results at once, joined with
+// the prefix' parts if there is a prefix.
 #include <type_traits>
 
 #include "mma16.cuh"
@@ -183,6 +182,10 @@ __device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
   }
   return before + x - v;
 }
+
+// A row's result is its sums over the sum of weights (a sum that is not a number stays one)
+__device__ __forceinline__ float inverse_of(float sum) { return sum <= 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float lse_of(float m, float sum) { return sum <= 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f; }
 
 template <int D, bool F16, int NT>
 __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
@@ -540,15 +543,60 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
         v.z = on ? fmaf(u.z, f, v.z) : v.z;
         v.w = on ? fmaf(u.w, f, v.w) : v.w;
       }
-      if (r >= rows || i >= job.ql) continue;
+      const bool live = r < rows && i < job.ql;
       const int head = job.head0 + r - i * g.G;
       const long long row = ((long long)job.b * g.H + head) * g.T + i;
+      if (a.direct && a.parts.shared) {
+        // the prefix' parts, D / 4 at a time: a lane of the row works out one's factor
+        constexpr int L = D / 4, A = 8;
+        settle_stream();
+        const int mine = lane % L, base = lane - mine;
+        const float2* ml = a.parts.ml + row;
+        const float* src = a.parts.o + row * D + c;
+#pragma unroll 1
+        for (int y0 = 0; y0 < a.parts.shared; y0 += L) {
+          const int n = min(L, a.parts.shared - y0);
+          float4 u[A];
+          auto ask = [&](int z0) {  // (behind the last: that again, with a factor of zero)
+#pragma unroll
+            for (int z = 0; z < A; ++z) {
+              u[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (live) u[z] = __ldcg(reinterpret_cast<const float4*>(src + (y0 + min(z0 + z, n - 1)) * a.parts.rows * D));
+            }
+          };
+          ask(0);
+          float2 part = make_float2(-INFINITY, 0.f);
+          if (live && mine < n) part = __ldcg(ml + (y0 + mine) * a.parts.rows);
+          float top = fmaxf(mx, part.x);
+#pragma unroll
+          for (int d = 1; d < L; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const float own = mx == -INFINITY ? 0.f : ex2(mx - top), f = part.x == -INFINITY ? 0.f : ex2(part.x - top);
+          float more = part.y * f;
+#pragma unroll
+          for (int d = 1; d < L; d *= 2) more += __shfl_xor_sync(0xffffffffu, more, d);
+          mx = top;
+          sum = fmaf(sum, own, more);
+          v.x *= own; v.y *= own; v.z *= own; v.w *= own;
+#pragma unroll 1
+          for (int z0 = 0; z0 < n; z0 += A) {
+            if (z0) ask(z0);
+#pragma unroll
+            for (int z = 0; z < A; ++z) {
+              const float fz = __shfl_sync(0xffffffffu, f, base + z0 + z);
+              v.x = fmaf(u[z].x, fz, v.x);
+              v.y = fmaf(u[z].y, fz, v.y);
+              v.z = fmaf(u[z].z, fz, v.z);
+              v.w = fmaf(u[z].w, fz, v.w);
+            }
+          }
+        }
+      }
+      if (!live) continue;
       if (a.direct) {
-        const bool some = !(sum <= 0.f);  // (a sum that is not a number stays one)
-        const float inv = some ? 1.f / sum : 0.f;
+        const float inv = inverse_of(sum);
         *reinterpret_cast<uint2*>(a.o.data + job.b * a.o.sb + head * a.o.sh + i * a.o.sn + 2 * c) =
             make_uint2(pack2<F16>(v.x * inv, v.y * inv), pack2<F16>(v.z * inv, v.w * inv));
-        if (c == 0) a.lse[row] = some ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        if (c == 0) a.lse[row] = lse_of(mx, sum);
       } else {
         const long long at = (long long)job.part * a.parts.rows + row;
         *reinterpret_cast<float4*>(a.parts.o + at * D + c) = v;
@@ -638,12 +686,11 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
       for (int x = 0; x < V; ++x) v[x] += part_o[warp + y][V * lane + x];
   }
   if (!live) return;
-  const bool some = !(sum <= 0.f);  // (a sum that is not a number stays one)
-  const float inv = some ? 1.f / sum : 0.f;
+  const float inv = inverse_of(sum);
   char* dst = o.data + b * o.sb + head * o.sh + i * o.sn + 2 * V * lane;
   if constexpr (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<F16>(v[0] * inv, v[1] * inv), pack2<F16>(v[2] * inv, v[3] * inv));
   else *reinterpret_cast<uint32_t*>(dst) = pack2<F16>(v[0] * inv, v[1] * inv);
-  if (lane == 0) lse[row] = some ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  if (lane == 0) lse[row] = lse_of(mx, sum);
 }
 
 template <int D, bool F16, int NT>
@@ -653,7 +700,7 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps&
   static unsigned long long configured = 0;
   int sms = 0;
   if (const int rc = launch_setup(reinterpret_cast<const void*>(paged_parts_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
-  a.blocks = (g.G * g.T + 8 * NT - 1) / (8 * NT);
+  a.blocks = paged_row_blocks(D, g.G * g.T);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
   if (most * kFull > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
   return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, maps.k, maps.v);
@@ -665,6 +712,9 @@ int launch_join(const HostCtx& c, const PagedGeo& g, const PartsOut& parts, cons
   return launch_kernel(paged_join_kernel<D, F16, W>, dim3((unsigned)((parts.rows + per - 1) / per)), kJoinThreads, 0, c.stream, true, 0, g, parts, o, lse);
 }
 
+// Tiles of 8 rows that a CTA takes: what a step's accumulators leave room for in registers, and its sums in shared memory
+int tiles_of(int d, int rows) { return rows <= 8 ? 1 : rows <= 16 || d == 128 ? 2 : rows <= 24 ? 3 : 4; }
+
 // f(head dimension, type) as constants
 template <class F>
 int by_type(int d, bool f16, F&& f) {
@@ -675,18 +725,23 @@ int by_type(int d, bool f16, F&& f) {
 
 }  // namespace
 
+int paged_row_blocks(int d, int rows) {
+  const int block = 8 * tiles_of(d, rows);
+  return (rows + block - 1) / block;
+}
+
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
                        int most_parts, bool direct, bool first, const View& o, float* lse) {
   const DecArgs a = {q, o, lse, parts, 0, maps.box_shift, direct, first, 1.f / (float)g.G, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
+    const int tiles = tiles_of(D, g.G * g.T);
     if constexpr (D == 64) {
-      if (g.G * g.T > 24) return launch_parts<D, F16, 4>(c, g, a, maps, most_parts);
-      if (g.G * g.T > 16) return launch_parts<D, F16, 3>(c, g, a, maps, most_parts);
+      if (tiles == 4) return launch_parts<D, F16, 4>(c, g, a, maps, most_parts);
+      if (tiles == 3) return launch_parts<D, F16, 3>(c, g, a, maps, most_parts);
     }
-    return g.G * g.T > 8 ? launch_parts<D, F16, 2>(c, g, a, maps, most_parts)
-                         : launch_parts<D, F16, 1>(c, g, a, maps, most_parts);
+    return tiles == 2 ? launch_parts<D, F16, 2>(c, g, a, maps, most_parts) : launch_parts<D, F16, 1>(c, g, a, maps, most_parts);
   });
 }
 

@@ -69,7 +69,7 @@ def decode(p=None, q=None, k_pages=None, v_pages=None, o=None, table=256, k_len=
 @pytest.mark.parametrize("kw,code", ANY + [
     (dict(H=3), -1), (dict(H=0), -1), (dict(window=-1), -1), (dict(sinks=-1), -1), (dict(sinks=129), -2), (dict(prefix_len=1), -1),
     (dict(prefix_len=-1), -1), (dict(Nq=17), -2), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(flags=8), -1),
-    (dict(B=1 << 23), -2)])
+    (dict(B=1 << 23), -2), (dict(B=1, H=1 << 20, Hkv=1), -2)])
 def test_bad_params_of_decode_are_refused(kw, code):
     assert decode(params(**kw)) == code
     if kw.get("prefix_len", 0) <= 0:  # (with one it is the size for a call behind a prefix)
@@ -126,6 +126,6 @@ def test_parts_of_a_prefix():
         for n in (1, 64, 65, 1000, 8191, 32768, 1 << 20, 1 << 30):
             kw = dict(B=B, H=H, Hkv=Hkv, Nq=Nq, d=d, prefix_len=n)
             rows = B * H * Nq
-            parts = (ws(params(**kw)) - 256) // (rows * (d * 4 + 8)) - 1  # (one part of the member's own: 512 tokens)
-            assert 1 <= parts <= min(-(-n // 64), 2 * 148 // Hkv + 2), (kw, parts)
-    assert ws(params(prefix_len=64)) == 256 + 2 * 24 * 64 * 4 + -(-2 * 24 * 8 // 256) * 256
+            parts = (ws(params(**kw)) - 256) // (rows * (d * 4 + 8))  # (a member's own 512 tokens are one part, kept if the join is apart)
+            assert 1 <= parts <= min(-(-n // 64), 2 * 148 // Hkv + 2) + 1, (kw, parts)
+    assert ws(params(prefix_len=64)) == 256 + 24 * 64 * 4 + 256 and ws(params(prefix_len=64, width=33)) == 256 + 3 * 24 * 64 * 4 + 3 * 256
