@@ -22,12 +22,15 @@ struct PagedGeo {
 };
 
 // Lengths of member b: its new tokens are the last ql of its kl
-__device__ __forceinline__ Span span_of(const PagedGeo& g, int b) {
+__device__ __forceinline__ Span clamped(const PagedGeo& g, int k_len, int q_len) {
   Span s;
-  s.ql = g.q_len ? min(max(__ldg(g.q_len + b), 0), g.T) : g.T;
-  s.kl = min(max(__ldg(g.k_len + b), 0), g.width << g.shift);
+  s.ql = min(max(q_len, 0), g.T);
+  s.kl = min(max(k_len, 0), g.width << g.shift);
   s.off = s.kl - s.ql;
   return s;
+}
+__device__ __forceinline__ Span span_of(const PagedGeo& g, int b) {
+  return clamped(g, __ldg(g.k_len + b), g.q_len ? __ldg(g.q_len + b) : g.T);
 }
 
 // The keys that member b's rows see, cut into parts: the chunks of kChunkKeys positions that hold some of them.  So what a part is

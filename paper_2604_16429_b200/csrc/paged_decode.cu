@@ -14,6 +14,14 @@
 // everything else is fp32.  The warps' maxima, sums and accumulators are joined through shared memory at the chunk's end, and leave as a
 // part; a second kernel joins a row's parts in their order.  Members that can have one part only get their results at once, joined with
 // the prefix' parts if there is a prefix.
+//
+// Measured (us on the device, 4 key/value heads of 128 unless given): 64 members of up to 8192 tokens, 16 heads, pages of 64, 106.7, and 8
+// of 65536, 32 heads, 189; in the steady state a chunk (262 KB) takes an SM 10100 cycles, 7.4 TB/s in all.  One member of 16384, 12.6:
+// 5000 cycles until the first copies are asked for, 600 a step, 2000 for the last step and the join, 4000 the second kernel.  5 new tokens of
+// 32 members, 12 heads on 3 of 64, window 2048: 30.
+// Tried on the last of these, with what it took then and what it takes without: rings and steps of 16 keys for every warp 63 (44), all
+// warps finding the items 46 (38), copies by one lane 35 (31), one more warp for the join of a chunk's steps 55 (31), conditions of the
+// masks and of the join as branches 33 (29).
 #include <type_traits>
 
 #include "mma16.cuh"
@@ -89,20 +97,16 @@ __device__ __forceinline__ Parts parts_of(const PagedGeo& g, const DecArgs& a, c
 struct Walk {
   Parts p;
   int b, hk, o, rb, pos;
-  int held, kl, ql;  // lengths of the 32 members from `held` on, in the lanes
+  int held, kl, ql;  // lengths of the 32 members from `held` on, in the lanes, as they stand in memory (nothing waits for them here)
   __device__ __forceinline__ void hold(const PagedGeo& g) {
     held = b;
-    const Span s = span_of(g, min(b + (int)(threadIdx.x & 31), g.B - 1));
-    kl = s.kl;
-    ql = s.ql;
+    const int m = min(b + (int)(threadIdx.x & 31), g.B - 1);
+    kl = __ldg(g.k_len + m);
+    ql = g.q_len ? __ldg(g.q_len + m) : g.T;
   }
   __device__ __forceinline__ void member(const PagedGeo& g, const DecArgs& a) {
     if (b - held >= 32) hold(g);
-    Span s;
-    s.kl = __shfl_sync(0xffffffffu, kl, b - held);
-    s.ql = __shfl_sync(0xffffffffu, ql, b - held);
-    s.off = s.kl - s.ql;
-    p = parts_of(g, a, s);
+    p = parts_of(g, a, clamped(g, __shfl_sync(0xffffffffu, kl, b - held), __shfl_sync(0xffffffffu, ql, b - held)));
   }
   __device__ __forceinline__ int weight(int part) const {
     if (p.front && part == 0) return (p.sinks + kStep - 1) / kStep + kTurn;
@@ -749,8 +753,11 @@ int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const Parts
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
-    // (by the parts alone, not by the rows: the order of a row's sums must not depend on the others)
-    if (most_parts <= 16) return launch_join<D, F16, 1>(c, g, parts, o, lse);
+    // By the parts alone, not by the rows: the order of a row's sums must not depend on the others.  A warp takes what it asks for at once,
+    // or twice that.  (us on the device, one and two warps for 9 to 16 parts: 1024 rows 108.8 and 106.7 a call; behind a prefix, where rows
+    // are many, 4096 rows 104.5 and 106.9.)
+    if (most_parts <= 8 || (parts.shared && most_parts <= 16)) return launch_join<D, F16, 1>(c, g, parts, o, lse);
+    if (most_parts <= 16) return launch_join<D, F16, 2>(c, g, parts, o, lse);
     return most_parts <= 64 ? launch_join<D, F16, 4>(c, g, parts, o, lse) : launch_join<D, F16, 8>(c, g, parts, o, lse);
   });
 }
