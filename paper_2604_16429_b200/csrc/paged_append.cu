@@ -6,8 +6,9 @@
 // are the query heads, the key heads and the value heads.  A row is spread over d / 16 lanes with two 16-byte pieces each, as in
 // the rotation by token index; rows are asked for before the token's angles are made (fp64 up to their remainder).
 //
-// Measured (us; two prompts of 8192 tokens, 16 + 4 heads of 128, bf16, pages of 64): 36.8, 5.5 TB/s, 85 % of the copy rate; the rest is the start
-// and end of the kernel and of its waves of CTAs.  64 single tokens: 4.2 on the device.
+// Measured (us; two prompts of 8192 tokens, 16 + 4 heads of 128, bf16, pages of 64): 35.4, 5.7 TB/s, 88 % of the copy rate (34.0 where nothing
+// turns); the rest is the start and end of the kernel and of its waves of CTAs.  Rows asked for behind the lengths and the page 37.1; batches
+// ahead and CTAs an SM 4 and 3: 36.4, 4 and 2: 40.5, 6 and 2: 38.8, 2 and 4: 35.4.  64 single tokens: 4.2 on the device.
 #include "paged.cuh"
 #include "rotary.cuh"
 
@@ -18,19 +19,20 @@ namespace {
 constexpr int kAppendThreads = 256, kAppendWarps = kAppendThreads / 32;
 constexpr int kRounds = 3;  // batches of rows that a warp has on their way
 
-struct AppendArgs : RotArgs {
+struct AppendArgs {
   View q, q_out, k, v, k_pages, v_pages;
   const double* freqs;
   long long start;
   unsigned tokens;
-  int N, heads, kv_heads, parts;
+  int N, d, rot, lanes, heads, kv_heads, parts;
+  float amplitude;
 };
 
 enum { kStill = 0, kPairs = 1, kHalves = 2 };
 
 // PART: some channels do not turn
 template <bool F16, int MODE, bool PART>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const PagedGeo g, const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const PagedGeo g, const __grid_constant__ AppendArgs a) {
   constexpr int T = F16 ? kF16 : kBf16, V = Vec<T>::n;
   constexpr bool HALF = MODE == kHalves;
   __shared__ alignas(16) Angles angles[kAppendWarps];
@@ -45,18 +47,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const PagedGeo g
   const char* xq = a.q.data + zero + b * a.q.sb + n * a.q.sn;
   const char* xk = a.k.data + zero + b * a.k.sb + n * a.k.sn - a.heads * a.k.sh;
   const char* xv = a.v.data + zero + b * a.v.sb + n * a.v.sn - (a.heads + a.kv_heads) * a.v.sh;
-  const Span s = span_of(g, b);
-  if (n >= s.ql) return;
-  const int j = s.off + n;
-  int page = j < 0 ? -1 : __ldg(g.table + b * g.table_stride + (j >> g.shift));
-  page = (unsigned)page < (unsigned)g.pages ? page : -1;  // a token without a page is not kept
-  const int slot = j & ((1 << g.shift) - 1);
-  char* yq = a.q_out.data + b * a.q_out.sb + n * a.q_out.sn;
-  char* yk = a.k_pages.data + page * a.k_pages.sb + slot * a.k_pages.sn - a.heads * a.k_pages.sh;
-  char* yv = a.v_pages.data + page * a.v_pages.sb + slot * a.v_pages.sn - (a.heads + a.kv_heads) * a.v_pages.sh;
-  bool turned = MODE == kStill;
-  for (int r0 = (int)((long long)rows * part / a.parts); r0 < end; r0 += kRounds * pl.groups) {
-    uint4 va[kRounds], vb[kRounds];
+  uint4 va[kRounds], vb[kRounds];
+  auto ask = [&](int r0) {
 #pragma unroll
     for (int u = 0; u < kRounds; ++u) {
       const int r = r0 + u * pl.groups + pl.group;
@@ -66,11 +58,23 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const PagedGeo g
         vb[u] = *reinterpret_cast<const uint4*>(x + cb);
       }
     }
-    if (!turned) {
-      still_angles(a, angles[warp], lane);
-      make_angles(a, a.freqs + zero, a.start + j, angles[warp], lane);
-      turned = true;
-    }
+  };
+  int r0 = (int)((long long)rows * part / a.parts);
+  ask(r0);  // (ahead of the lengths and the table, which come one after the other)
+  const Span s = span_of(g, b);
+  if (n >= s.ql) return;
+  const int j = s.off + n;
+  int page = j < 0 ? -1 : __ldg(g.table + b * g.table_stride + (j >> g.shift));
+  if constexpr (MODE != kStill) {
+    still_angles(a, angles[warp], lane);
+    make_angles(a, a.freqs + zero, a.start + j, angles[warp], lane);
+  }
+  page = (unsigned)page < (unsigned)g.pages ? page : -1;  // a token without a page is not kept
+  const int slot = j & ((1 << g.shift) - 1);
+  char* yq = a.q_out.data + b * a.q_out.sb + n * a.q_out.sn;
+  char* yk = a.k_pages.data + page * a.k_pages.sb + slot * a.k_pages.sn - a.heads * a.k_pages.sh;
+  char* yv = a.v_pages.data + page * a.v_pages.sb + slot * a.v_pages.sn - (a.heads + a.kv_heads) * a.v_pages.sh;
+  for (;;) {
 #pragma unroll
     for (int u = 0; u < kRounds; ++u) {
       const int r = r0 + u * pl.groups + pl.group;
@@ -92,6 +96,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const PagedGeo g
       *reinterpret_cast<uint4*>(y + ca) = va[u];
       *reinterpret_cast<uint4*>(y + cb) = vb[u];
     }
+    r0 += kRounds * pl.groups;
+    if (r0 >= end) break;
+    ask(r0);
   }
 }
 

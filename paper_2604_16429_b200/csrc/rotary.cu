@@ -41,7 +41,7 @@ struct HeadTensor {
   const float* w;
   int heads;
 };
-struct HeadArgs : RotArgs {
+struct HeadArgs {
   HeadTensor t[2];
   const int64_t* pos;
   const double* freqs;
@@ -51,8 +51,8 @@ struct HeadArgs : RotArgs {
   int step_b, step_n;            // the step in members and tokens
   unsigned k_step;               // backward: the same for the CTAs of K's rows, which come after q_ctas of Q's
   int k_step_b, k_step_n, q_ctas;
-  int N, parts;
-  float eps, inv_d;
+  int N, d, rot, lanes, parts;
+  float amplitude, eps, inv_d;
 };
 
 // 16 bytes of global memory to shared memory, or (bytes 0) zeros

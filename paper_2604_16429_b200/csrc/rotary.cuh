@@ -9,11 +9,8 @@ namespace {
 enum { kBf16 = 0, kF16 = 1, kF32 = 2 };
 constexpr int kMaxHeadDim = 256;
 
-// What the rotation needs of a call: channels of a head, those that turn, lanes that a row is spread over, factor of the turned channels
-struct RotArgs {
-  int d, rot, lanes;
-  float amplitude;
-};
+// The helpers take a kernel's arguments (A), of which they read: d, channels of a head; rot, those that turn; lanes that a row is spread
+// over; amplitude, factor of the turned channels.
 
 template <int T>
 struct Vec { static constexpr int n = T == kF32 ? 4 : 8, bytes = T == kF32 ? 4 : 2; };
@@ -46,8 +43,8 @@ struct Place {
   int group, groups;  // this lane's row of the `groups` rows that a warp takes at a time
   bool on;            // the lane has channels (d / 2V may be less than P)
 };
-template <int T, bool HALF>
-__device__ __forceinline__ Place place(const RotArgs& a, int lane) {
+template <int T, bool HALF, class A>
+__device__ __forceinline__ Place place(const A& a, int lane) {
   constexpr int V = Vec<T>::n;
   Place p;
   const int slot = lane & (a.lanes - 1), turning = HALF ? a.rot / (2 * V) : 0, from = HALF ? a.rot : 0;
@@ -64,14 +61,16 @@ constexpr int kAngles = kMaxHeadDim / 2 + 8;
 struct Angles {
   float cosine[kAngles], sine[kAngles];
 };
-__device__ __forceinline__ void still_angles(const RotArgs& a, Angles& t, int lane) {
+template <class A>
+__device__ __forceinline__ void still_angles(const A& a, Angles& t, int lane) {
   for (int i = a.rot / 2 + lane; i < kAngles; i += 32) {
     t.cosine[i] = 1.f;
     t.sine[i] = 0.f;
   }
 }
 // The token's angles, shared out over the warp.  (`freqs`: behind the wait for the stream)
-__device__ __forceinline__ void make_angles(const RotArgs& a, const double* freqs, long long pos, Angles& t, int lane) {
+template <class A>
+__device__ __forceinline__ void make_angles(const A& a, const double* freqs, long long pos, Angles& t, int lane) {
   __syncwarp();  // the token before has been read
   for (int i = lane; i < a.rot / 2; i += 32) {
     const double turns = (double)pos * (__ldg(freqs + i) * 0.31830988618379067154);  // half turns
@@ -105,8 +104,8 @@ __device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) 
   y = x * s + y * c;
   x = u;
 }
-template <int V, bool HALF>
-__device__ __forceinline__ void turn_all(float (&a)[V], float (&b)[V], const Angles& t, const RotArgs& args, const Place& pl) {
+template <int V, bool HALF, class A>
+__device__ __forceinline__ void turn_all(float (&a)[V], float (&b)[V], const Angles& t, const A& args, const Place& pl) {
   constexpr int N = HALF ? V : V / 2;  // pairs of one piece that lie side by side
   float c[V], s[V];
   const int i0 = HALF ? min(pl.ca, args.rot / 2) : pl.ca / 2;
@@ -136,8 +135,8 @@ __device__ __forceinline__ void turn_piece(float (&f)[V], int first, const Angle
 // PART: some channels do not turn and stay as they are, whatever they hold.  (As pairs multiplied with (1, 0) an infinite one would
 // make no number of its partner.)  With half pairs a lane's pairs turn, all of them, or none does; otherwise the border lies among the
 // second pieces, or among the first and no second one turns.
-template <int V, bool HALF, bool PART>
-__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const RotArgs& args, const Place& pl) {
+template <int V, bool HALF, bool PART, class A>
+__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles& t, const A& args, const Place& pl) {
   if constexpr (!PART) {
     turn_all<V, HALF>(a, b, t, args, pl);
   } else if constexpr (HALF) {
@@ -160,8 +159,8 @@ __device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const Angles&
   }
 }
 // The same on the two pieces as they lie in memory: what does not turn keeps its bits (narrowing would change those of what is no number).
-template <int T, bool HALF>
-__device__ __forceinline__ void turn_part(uint4& va, uint4& vb, const Angles& t, const RotArgs& args, const Place& pl) {
+template <int T, bool HALF, class A>
+__device__ __forceinline__ void turn_part(uint4& va, uint4& vb, const Angles& t, const A& args, const Place& pl) {
   constexpr int V = Vec<T>::n;
   if constexpr (HALF) {
     if (pl.ca >= args.rot / 2) return;
