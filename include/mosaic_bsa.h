@@ -413,7 +413,7 @@ int mosaic_bsa_paged_append(const mosaic_paged_params *p, const mosaic_view *k, 
  *   that see it, and may spread to the member's other rows).
  *   ws: mosaic_bsa_paged_workspace_bytes(p) bytes (0 on invalid params), 256-byte aligned, the status block first.  It grows with
  *   B * H * Nq times the chunks of 512 keys that a member can have: those of its table row, or of its window.
- *   (MOSAIC_E_UNSUPPORTED where B * Hkv * chunks times Nq * H / Hkv in blocks of 16 reach 2^31 / 10.) */
+ *   (MOSAIC_E_UNSUPPORTED where B * Hkv * chunks times Nq * H / Hkv in blocks of 16 reach 2^31 / 12.) */
 size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params *p);
 int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
                             const int32_t *table, const int32_t *k_len, const int32_t *q_len, const mosaic_view *o, float *lse, void *ws,

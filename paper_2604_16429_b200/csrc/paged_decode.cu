@@ -70,7 +70,7 @@ struct Smem {
   Job job[kJobs];
   unsigned long long full[kBars], empty[kStages], note_full[kJobs], job_full[kJobs], job_empty[kJobs], parts_full, parts_read;
   unsigned hole[kStages];  // the step's boxes that have no page
-  int scan[kWarps + 3];
+  long long scan[kWarps + 3];
   int4 start;              // the member that this CTA's share begins in, the weight before it, its lengths
   int abort;
 };
@@ -81,14 +81,14 @@ struct DecArgs {
   PartsOut parts;
   int blocks;     // of rows
   int box_shift;  // log2 of the slots that a copy brings: a page, at most a step
+  int turn;       // weight of an item beside its steps; 0: all items weigh the same
   bool direct, first;
   float inv_g;    // 1 / G
   int* status;
 };
 
-// A place in the list of all items: members, their heads, their parts, blocks of rows.  Items weigh their steps and kTurn for what comes
-// with every one; `pos` is the weight of all items before.
-constexpr int kTurn = 2, kFull = kSteps + kTurn;
+// A place in the list of all items: members, their heads, their parts, blocks of rows.  An item weighs `turn` for what comes with every one
+// and `mul` times its steps; `pos` is the weight of all items before.
 __device__ __forceinline__ Parts parts_of(const PagedGeo& g, const DecArgs& a, const Span& s) {
   Parts p = parts_of(g, s);
   if (a.direct) p.n = p.ql > 0 ? 1 : 0;  // (a member without keys has results too)
@@ -96,7 +96,7 @@ __device__ __forceinline__ Parts parts_of(const PagedGeo& g, const DecArgs& a, c
 }
 struct Walk {
   Parts p;
-  int b, hk, o, rb, pos;
+  int b, hk, o, rb, pos, mul, turn;
   int held, kl, ql;  // lengths of the 32 members from `held` on, in the lanes, as they stand in memory (nothing waits for them here)
   __device__ __forceinline__ void hold(const PagedGeo& g) {
     held = b;
@@ -109,13 +109,13 @@ struct Walk {
     p = parts_of(g, a, clamped(g, __shfl_sync(0xffffffffu, kl, b - held), __shfl_sync(0xffffffffu, ql, b - held)));
   }
   __device__ __forceinline__ int weight(int part) const {
-    if (p.front && part == 0) return (p.sinks + kStep - 1) / kStep + kTurn;
+    if (p.front && part == 0) return mul * ((p.sinks + kStep - 1) / kStep) + turn;
     const int s = chunk_of(p, part) * kSteps;
-    return min(s + kSteps - 1, (p.kl - 1) >> 6) - max(s, p.from >> 6) + 1 + kTurn;
+    return mul * (min(s + kSteps - 1, (p.kl - 1) >> 6) - max(s, p.from >> 6) + 1) + turn;
   }
   // of the parts before `part`: only the first two and the last may be short
   __device__ __forceinline__ int weight_before(int part) const {
-    return part == 0 ? 0 : part == 1 ? weight(0) : weight(0) + weight(1) + (part - 2) * kFull;
+    return part == 0 ? 0 : part == 1 ? weight(0) : weight(0) + weight(1) + (part - 2) * (mul * kSteps + turn);
   }
   __device__ __forceinline__ int weight_of_head(const DecArgs& a) const { return p.n ? a.blocks * (weight_before(p.n - 1) + weight(p.n - 1)) : 0; }
   // To the first item of the member (of weight `base` before it) that does not begin before weight `to`, or behind the member
@@ -124,7 +124,7 @@ struct Walk {
     hk = at / head;
     const int y = at - hk * head;
     o = 0;
-    if (p.n > 2 && y >= a.blocks * weight_before(2)) o = min(p.n - 1, 2 + (y - a.blocks * weight_before(2)) / (a.blocks * kFull));
+    if (p.n > 2 && y >= a.blocks * weight_before(2)) o = min(p.n - 1, 2 + (y - a.blocks * weight_before(2)) / (a.blocks * (mul * kSteps + turn)));
     else if (p.n > 1 && y >= a.blocks * weight_before(1)) o = 1;
     const int rest = y - a.blocks * weight_before(o), each = weight(o);
     rb = (rest + each - 1) / each;
@@ -167,17 +167,17 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
 
 // Sum of v over the threads before this one, and over all
 template <int WARPS>
-__device__ __forceinline__ int block_scan(int v, int* scan, int& total) {
+__device__ __forceinline__ long long block_scan(long long v, long long* scan, long long& total) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int x = v;
+  long long x = v;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
-    const int y = __shfl_up_sync(0xffffffffu, x, d);
+    const long long y = __shfl_up_sync(0xffffffffu, x, d);
     if (lane >= d) x += y;
   }
   if (lane == 31) scan[warp] = x;
   __syncthreads();
-  int before = 0;
+  long long before = 0;
   total = 0;
 #pragma unroll
   for (int w = 0; w < WARPS; ++w) {
@@ -222,42 +222,48 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 
   const int rows = g.G * g.T;
 
-  // ---- this CTA's share of the list: the items that begin in its share of the weight
-  int begin, end;
+  // ---- this CTA's share of the list: the items that begin in its share of the weight.  Where there are no more items than CTAs, each has
+  // one at most.
+  int begin, end, mul, turn;
   {
     Span s = {};
-    int total = 0, before = 0, mine = 0;
+    long long mine = 0, before = 0, total = 0;  // items in the upper half, their steps in the lower one
     auto weigh = [&](int b) {
       mine = 0;
       if (b < g.B) {
         Walk w;
         s = span_of(g, b);
         w.p = parts_of(g, a, s);
-        mine = w.weight_of_head(a) * g.Hkv;
+        w.mul = 1;
+        w.turn = 0;
+        mine = (long long)w.p.n * a.blocks * g.Hkv << 32 | (unsigned)(w.weight_of_head(a) * g.Hkv);
       }
     };
 #pragma unroll 1
     for (int b0 = 0; b0 < g.B; b0 += S::kThreads) {
-      int all;
+      long long all;
       weigh(b0 + tid + zero);
       if (b0) __syncthreads();
       before = block_scan<kWarps + 3>(mine, sm.scan, all);
       total += all;
     }
-    begin = (int)((long long)total * blockIdx.x / gridDim.x);
-    end = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    mul = a.turn && total >> 32 > gridDim.x;
+    turn = mul ? a.turn : 1;
+    auto weight = [&](long long x) { return mul * (int)(unsigned)x + turn * (int)(x >> 32); };
+    begin = (int)((long long)weight(total) * blockIdx.x / gridDim.x);
+    end = (int)((long long)weight(total) * (blockIdx.x + 1) / gridDim.x);
     int base = 0;
 #pragma unroll 1
     for (int b0 = 0; b0 < g.B; b0 += S::kThreads) {
-      int all = 0;
+      long long all = 0;
       if (g.B > S::kThreads) {
         weigh(b0 + tid + zero);
         __syncthreads();
         before = block_scan<kWarps + 3>(mine, sm.scan, all);
       }
-      const int at = begin - base - before;
-      if (at >= 0 && at < mine) sm.start = make_int4(b0 + tid, base + before, s.kl, s.ql);
-      base += all;
+      const int at = begin - base - weight(before);
+      if (at >= 0 && at < weight(mine)) sm.start = make_int4(b0 + tid, base + weight(before), s.kl, s.ql);
+      base += weight(all);
     }
     __syncthreads();
   }
@@ -267,6 +273,8 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
     const int box = 1 << a.box_shift, boxes = kChunkKeys >> a.box_shift;  // a lane has one of the chunk's boxes
     Walk w;
     w.pos = end;
+    w.mul = mul;
+    w.turn = turn;
     if (begin < end) {
       const int4 at = sm.start;
       w.b = at.x;
@@ -697,6 +705,13 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
   if (lane == 0) lse[row] = lse_of(mx, sum);
 }
 
+// An item's weight beside its steps.  It takes as long as its keys take to arrive, 1260 cycles a step at D = 128 and 630 at 64, or, if that is
+// longer, as one step takes from its keys to the end of the join: 3400 for one tile of 8 rows, 5300 for three, which is a whole chunk's
+// time at D = 64, so that all items are alike there.  (us on the device with 2, and alike: 5 new tokens of 32 members, 12 heads on 3 of 64, 30.5
+// and 26.8; 33 members with 4 behind a prefix 28.4 and 24.7.)
+template <int D, int NT>
+constexpr int kTurn = D == 128 ? 2 : NT == 1 ? 4 : 0;
+
 template <int D, bool F16, int NT>
 int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps& maps, int most_parts) {
   constexpr size_t smem = sizeof(Smem<D, NT>) + 1024;
@@ -706,7 +721,8 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps&
   if (const int rc = launch_setup(reinterpret_cast<const void*>(paged_parts_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
   a.blocks = paged_row_blocks(D, g.G * g.T);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
-  if (most * kFull > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
+  a.turn = kTurn<D, NT>;
+  if (most * (kSteps + a.turn) > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
   return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, maps.k, maps.v);
 }
 
@@ -736,7 +752,7 @@ int paged_row_blocks(int d, int rows) {
 
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
                        int most_parts, bool direct, bool first, const View& o, float* lse) {
-  const DecArgs a = {q, o, lse, parts, 0, maps.box_shift, direct, first, 1.f / (float)g.G, c.status};
+  const DecArgs a = {q, o, lse, parts, 0, maps.box_shift, 1, direct, first, 1.f / (float)g.G, c.status};
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
