@@ -18,7 +18,7 @@
 // Measured (us on the device, 4 key/value heads of 128 unless given): 64 members of up to 8192 tokens, 16 heads, pages of 64, 106.7, and 8
 // of 65536, 32 heads, 189; in the steady state a chunk (262 KB) takes an SM 10100 cycles, 7.4 TB/s in all.  One member of 16384, 12.6:
 // 5000 cycles until the first copies are asked for, 600 a step, 2000 for the last step and the join, 4000 the second kernel.  5 new tokens of
-// 32 members, 12 heads on 3 of 64, window 2048: 30.
+// 32 members, 12 heads on 3 of 64, window 2048: 27.
 // Tried on the last of these, with what it took then and what it takes without: rings and steps of 16 keys for every warp 63 (44), all
 // warps finding the items 46 (38), copies by one lane 35 (31), one more warp for the join of a chunk's steps 55 (31), conditions of the
 // masks and of the join as branches 33 (29).
