@@ -50,6 +50,8 @@ CASES = [  # B, H, Hkv, T, d, page, P, k_len, q_len
     (4, 12, 3, 5, 64, 16, 500, [5, 50, 3, 0], [5, 2, 5, 3]),                 # drafts, more new tokens than tokens
     (9, 34, 2, 16, 128, 128, 4100, [16 + i for i in range(9)], None),        # 2448 rows
     (130, 2, 2, 1, 64, 512, 65, [1] * 130, [i % 2 for i in range(130)]),     # every other member has no rows
+    (150, 2, 2, 1, 64, 16, 4000, [i % 50 for i in range(150)], None),        # one part each, but many items a CTA: joined apart
+    (80, 8, 4, 2, 128, 32, 2500, [2 + i % 90 for i in range(80)], None),
 ]
 
 
