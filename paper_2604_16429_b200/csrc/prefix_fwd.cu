@@ -54,6 +54,7 @@ struct PrefixArgs {
   int box_shift;         // log2 of the rows of a box: a page, at most U
   int box_loads;         // copies that bring a box's channels: with all of a step's rows in one box, one
   int total;             // items
+  float inv_g;           // 1 / G
   int* status;
 };
 
@@ -61,9 +62,9 @@ struct PrefixArgs {
 struct Item {
   int hk, part, row0, k0, k1, steps;
   __device__ __forceinline__ void make(const PrefixArgs& a, int index) {
-    const int pair = index % a.pairs, rest = index / a.pairs;
-    part = rest % a.parts.shared;
+    const int rest = a.pairs == 1 ? index : index / a.pairs, pair = index - rest * a.pairs;
     hk = rest / a.parts.shared;
+    part = rest - hk * a.parts.shared;
     row0 = 2 * kRows * pair;
     k0 = part * a.chunk;
     k1 = min(a.len, k0 + a.chunk);
@@ -281,10 +282,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int r = it.row0 + t * kRows + row;
       if (it.row0 + t * kRows >= a.rows) continue;  // (the whole tile)
       // the row's place: member, token, head
-      const int bt = r / g.G, b = bt / g.T, i = bt - b * g.T, head = it.hk * g.G + r - bt * g.G;
+      const int bt = a.rows < (1 << 23) ? quick_div(r, g.G, a.inv_g) : r / g.G, b = g.T == 1 ? bt : bt / g.T;
+      const int i = bt - b * g.T, head = it.hk * g.G + r - bt * g.G;
       const bool live = r < a.rows && (!g.q_len || i < __ldg(g.q_len + min(b, g.B - 1)));
       const int at = live ? (b * g.H + head) * g.T + i : -1;
       const bool idle = !__any_sync(0xffffffffu, live);
+      // some page of the part is not there: the lanes look at its pages, the first of them while the rows of q are on their way
+      const int first_page = it.k0 >> g.shift, pages = ((it.k1 - 1) >> g.shift) - first_page + 1;
+      const int probe = __ldg(a.table + first_page + min(lane, pages - 1));
       ok = warp_wait_here(s32(&sm.q_empty[t]), (n_q & 1) ^ 1, abort, status);
       ++n_q;
       if (!ok) break;
@@ -302,12 +307,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                        : "memory");
         }
       }
-      bool holes = false;  // some page of the part is not there
-      for (int key = it.k0 + (lane << g.shift); key < it.k1; key += 32 << g.shift) {
-        const int k = max(key & ~((1 << g.shift) - 1), it.k0);
-        holes |= (unsigned)__ldg(a.table + (k >> g.shift)) >= (unsigned)g.pages;
-      }
-      if ((it.k1 - 1) >> g.shift != (it.k0 >> g.shift)) holes |= (unsigned)__ldg(a.table + ((it.k1 - 1) >> g.shift)) >= (unsigned)g.pages;
+      bool holes = (unsigned)probe >= (unsigned)g.pages;
+      for (int page = lane + 32; page < pages; page += 32) holes |= (unsigned)__ldg(a.table + first_page + page) >= (unsigned)g.pages;
       holes = __any_sync(0xffffffffu, holes);
       asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
       mbar_arrive(s32(&sm.q_full[t]));
@@ -515,6 +516,7 @@ int launch_prefix_fwd(const HostCtx& c, const PagedGeo& g, bool f16, const View&
   a.chunk = chunk;
   const long long rows = (long long)g.B * g.T * g.G;
   a.rows = (int)rows;
+  a.inv_g = 1.f / (float)g.G;
   a.pairs = pairs_of(rows);
   a.box_shift = maps.box_shift;
   a.box_loads = a.box_shift < kBoxShift ? g.d / 64 : 1;
