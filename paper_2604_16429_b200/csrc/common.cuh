@@ -147,14 +147,6 @@ __device__ __forceinline__ int await_stream() {
   asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;\n\tmov.u32 %0, 0;" : "=r"(zero) : : "memory");
   return zero;
 }
-// The two halves of it, for a kernel that does not read what the one ahead of it writes: it lets the next kernel in at its start, works
-// on what was complete when the one ahead began, and waits for that one before it ends, so that the chain holds.
-__device__ __forceinline__ int pass_stream() {
-  int zero;
-  asm volatile("griddepcontrol.launch_dependents;\n\tmov.u32 %0, 0;" : "=r"(zero) : : "memory");
-  return zero;
-}
-__device__ __forceinline__ void settle_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ---- host side ---------------------------------------------------------------------------
 // Launches a kernel that calls await_stream; with `overlap` its launch and set-up overlap the kernel ahead of it.  A pass

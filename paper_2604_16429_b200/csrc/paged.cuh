@@ -63,6 +63,15 @@ struct PartsOut {
   int shared;  // parts of the prefix
 };
 
+// The two halves of await_stream, for a kernel that does not read what the one ahead of it writes: it lets the next kernel in at its
+// start, works on what was complete when the one ahead began, and waits for that one before it ends, so that the chain holds.
+__device__ __forceinline__ int pass_stream() {
+  int zero;
+  asm volatile("griddepcontrol.launch_dependents;\n\tmov.u32 %0, 0;" : "=r"(zero) : : "memory");
+  return zero;
+}
+__device__ __forceinline__ void settle_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // A pool as a tensor [pages, Hkv, page, d], strides in bytes
 int check_pool(const mosaic_view* v, const mosaic_paged_params* p, View* out);
 
