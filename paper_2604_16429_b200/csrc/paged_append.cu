@@ -39,14 +39,15 @@ __global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const PagedGe
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Place pl = place<T, HALF>(a, lane);
   const int zero = await_stream();
-  const unsigned task = blockIdx.x * kAppendWarps + warp, token = task / (unsigned)a.parts;
+  // (the token holds the wait's zero, and with it every address that follows from it: lengths, table, rows)
+  const unsigned task = blockIdx.x * kAppendWarps + warp + (unsigned)zero, token = task / (unsigned)a.parts;
   if (token >= a.tokens) return;
   const int part = (int)(task - token * a.parts), b = (int)(token / (unsigned)a.N), n = (int)(token - (unsigned)b * a.N);
   const int rows = a.heads + 2 * a.kv_heads, end = (int)((long long)rows * (part + 1) / a.parts);
   const int ca = 2 * pl.ca, cb = 2 * pl.cb;
-  const char* xq = a.q.data + zero + b * a.q.sb + n * a.q.sn;
-  const char* xk = a.k.data + zero + b * a.k.sb + n * a.k.sn - a.heads * a.k.sh;
-  const char* xv = a.v.data + zero + b * a.v.sb + n * a.v.sn - (a.heads + a.kv_heads) * a.v.sh;
+  const char* xq = a.q.data + b * a.q.sb + n * a.q.sn;
+  const char* xk = a.k.data + b * a.k.sb + n * a.k.sn - a.heads * a.k.sh;
+  const char* xv = a.v.data + b * a.v.sb + n * a.v.sn - (a.heads + a.kv_heads) * a.v.sh;
   uint4 va[kRounds], vb[kRounds];
   auto ask = [&](int r0) {
 #pragma unroll
