@@ -623,13 +623,24 @@ __global__ void __launch_bounds__(Smem<D, NT>::kThreads, 1)
 
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
-// A row's parts in their order: W warps share them out, part p to warp p % W, and are joined in turn.  The lanes hold the parts' maxima and
-// sums, 32 at a time, and work out their factors.
-template <int D, bool F16, int W>
+// A row's parts in an order that follows from the row's own parts alone, whatever the other rows hold and however many pages its table has
+// room for: part p belongs to the sum p % 8, whose parts are added up in turn, and the eight sums are joined in turn.  W warps share a row's
+// sums out, sum s to warp s % W.  The lanes hold the parts' maxima and sums of weights, 32 at a time, and work out their factors.
+//
+// W follows from the most parts that any row can have, so that a warp takes what it asks for at once, or twice that (W = 8: in rounds of 64
+// parts).  (us on the device, one and two warps for 9 to 16 parts: 1024 rows 108.8 and 106.7 a call; behind a prefix, where rows are
+// many, 4096 rows 104.5 and 106.9: there one warp takes them by pairs of a sum, PAIRS.)  With eight warps a row, four parts a batch: eight
+// spill, and where few of a wide table's pages are filled they cost 0.5 to 3 us of 13 to 103.
+constexpr int kSums = 8;
+
+template <int D, bool F16, int W, bool PAIRS>
 __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const PagedGeo g, const PartsOut in, const View o, float* __restrict__ lse) {
-  constexpr int V = D / 32, A = 8;  // channels of a lane; parts that a warp asks for at a time
-  constexpr int kHeld = 2;          // times 32 parts whose maxima stay in registers
-  __shared__ float part_o[W > 1 ? kJoinWarps : 1][D];
+  constexpr int V = D / 32, A = W == 8 ? 4 : 8;  // channels of a lane; parts that a warp asks for at a time
+  constexpr int kHeld = W <= 2 ? 1 : 2;          // times 32 parts whose maxima stay in registers, and whose factors are worked out at once
+  constexpr int kOwn = W == 1 ? 1 : kSums / W;   // sums that a warp has in registers
+  constexpr int kRound = 32 * kHeld, kBatches = PAIRS || W >= 4 ? 2 : 1;  // parts of a round; batches that a warp takes of them
+  static_assert(W == 8 ? kRound == A * W * kBatches : kRound >= A * W * kBatches, "rows of more parts have eight warps, and rounds");
+  __shared__ alignas(16) float sums[W > 1 ? kJoinWarps / W : 1][kSums][D];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % W;
   const int row = (int)blockIdx.x * (kJoinWarps / W) + warp / W;
   bool live = row < (int)in.rows;
@@ -641,11 +652,13 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
   const float2* ml = in.ml + row;
   const float* src = in.o + (long long)row * D + V * lane;
   const long long step = in.rows * D;
+  // the warp's k-th part
+  auto part_at = [&](int k) { return PAIRS ? (k >> 1) + kSums * (k & 1) : w + k * W; };
   float u[A][V];
-  auto ask = [&](int first) {  // parts first, first + W, ...
+  auto ask = [&](int k0) {
 #pragma unroll
     for (int z = 0; z < A; ++z) {
-      const float* at = src + min(first + z * W, n - 1) * step;
+      const float* at = src + min(part_at(k0 + z), n - 1) * step;
       if constexpr (V == 4) {
         const float4 t = __ldcg(reinterpret_cast<const float4*>(at));
         u[z][0] = t.x; u[z][1] = t.y; u[z][2] = t.z; u[z][3] = t.w;
@@ -656,46 +669,77 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
     }
   };
   auto read = [&](int y) { return y < n ? __ldcg(ml + y * in.rows) : make_float2(-INFINITY, 0.f); };
-  float2 held[kHeld];
+  float mx = -INFINITY, sum = 0.f, v[V], own[kOwn][V];
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) held[k] = read(32 * k + lane);
-  if (n > 0) ask(w);
-  float mx = -INFINITY, sum = 0.f, v[V];
+  for (int x = 0; x < V; ++x) {
+    v[x] = 0.f;
 #pragma unroll
-  for (int x = 0; x < V; ++x) v[x] = 0.f;
+    for (int s = 0; s < kOwn; ++s) own[s][x] = 0.f;
+  }
+  if (w < n) {  // (a warp without parts has nothing to add)
+    float2 held[kHeld];
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) mx = fmaxf(mx, held[k].x);
-  for (int y = 32 * kHeld + lane; y < n; y += 32) mx = fmaxf(mx, read(y).x);
+    for (int k = 0; k < kHeld; ++k) held[k] = read(32 * k + lane);
+    ask(0);
 #pragma unroll
-  for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-  for (int y0 = 0; y0 < n; y0 += 32) {
-    const float2 part = y0 == 0 ? held[0] : y0 == 32 ? held[1] : read(y0 + lane);
-    const float f = part.x == -INFINITY ? 0.f : ex2(part.x - mx);
-    sum += part.y * f;
-    const int m = min(32, n - y0);
-    for (int z0 = w; z0 < m; z0 += A * W) {
-      if (y0 + z0 > w) ask(y0 + z0);
+    for (int k = 0; k < kHeld; ++k) mx = fmaxf(mx, held[k].x);
+    if constexpr (W == 8)
+      for (int y = kRound + lane; y < n; y += 32) mx = fmaxf(mx, read(y).x);
 #pragma unroll
-      for (int z = 0; z < A; ++z) {
-        const float fz = __shfl_sync(0xffffffffu, f, (z0 + z * W) & 31);
-        if (z0 + z * W < m) {
+    for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    int y0 = 0;
+    do {
+      float f[kHeld];
 #pragma unroll
-          for (int x = 0; x < V; ++x) v[x] = fmaf(u[z][x], fz, v[x]);
+      for (int k = 0; k < kHeld; ++k) {
+        const float2 part = y0 == 0 ? held[k] : read(y0 + 32 * k + lane);
+        f[k] = part.x == -INFINITY ? 0.f : ex2(part.x - mx);
+        sum += part.y * f[k];
+      }
+#pragma unroll
+      for (int batch = 0; batch < kBatches; ++batch) {
+        const int k0 = y0 / W + A * batch;
+        if (batch > 0 || y0 > 0) {
+          if (part_at(k0) >= n) break;
+          ask(k0);
+        }
+#pragma unroll
+        for (int z = 0; z < A; ++z) {
+          const int at = part_at(k0 + z), in_round = part_at(A * batch + z);
+          // (whether the part is one of the first 32 of the round does not depend on the warp)
+          const float fz = __shfl_sync(0xffffffffu, f[kHeld == 1 || W * (A * batch + z) < 32 ? 0 : kHeld - 1], in_round & 31);
+          float* to = own[W == 1 ? 0 : z % kOwn];
+          if (at < n) {
+#pragma unroll
+            for (int x = 0; x < V; ++x) to[x] = fmaf(u[z][x], fz, to[x]);
+          }
+          if (W == 1 && (!PAIRS || z % 2)) {  // the sum is complete
+#pragma unroll
+            for (int x = 0; x < V; ++x) {
+              v[x] = __fadd_rn(v[x], to[x]);
+              to[x] = 0.f;
+            }
+          }
         }
       }
-    }
-  }
+      y0 += kRound;  // (one warp's eight parts are one round; as a loop its loads stay ahead of the maxima: drafts in a window 24.3 -> 23.6 us)
+    } while ((W == 8 || (W == 1 && !PAIRS)) && y0 < n);
 #pragma unroll
-  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  }
   if constexpr (W > 1) {
 #pragma unroll
-    for (int x = 0; x < V; ++x) part_o[warp][V * lane + x] = v[x];
+    for (int s = 0; s < kOwn; ++s) {
+      float* to = &sums[warp / W][w + W * s][V * lane];
+      if constexpr (V == 4) *reinterpret_cast<float4*>(to) = make_float4(own[s][0], own[s][1], own[s][2], own[s][3]);
+      else *reinterpret_cast<float2*>(to) = make_float2(own[s][0], own[s][1]);
+    }
     __syncthreads();
     if (w) return;
 #pragma unroll
-    for (int y = 1; y < W; ++y)
+    for (int s = 0; s < kSums; ++s)
 #pragma unroll
-      for (int x = 0; x < V; ++x) v[x] += part_o[warp + y][V * lane + x];
+      for (int x = 0; x < V; ++x) v[x] += sums[warp / W][s][V * lane + x];
   }
   if (!live) return;
   const float inv = inverse_of(sum);
@@ -726,10 +770,10 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps&
   return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, maps.k, maps.v);
 }
 
-template <int D, bool F16, int W>
+template <int D, bool F16, int W, bool PAIRS = false>
 int launch_join(const HostCtx& c, const PagedGeo& g, const PartsOut& parts, const View& o, float* lse) {
   constexpr int per = kJoinWarps / W;
-  return launch_kernel(paged_join_kernel<D, F16, W>, dim3((unsigned)((parts.rows + per - 1) / per)), kJoinThreads, 0, c.stream, true, 0, g, parts, o, lse);
+  return launch_kernel(paged_join_kernel<D, F16, W, PAIRS>, dim3((unsigned)((parts.rows + per - 1) / per)), kJoinThreads, 0, c.stream, true, 0, g, parts, o, lse);
 }
 
 // Tiles of 8 rows that a CTA takes: what a step's accumulators leave room for in registers, and its sums in shared memory
@@ -769,11 +813,8 @@ int launch_paged_join(const HostCtx& c, const PagedGeo& g, bool f16, const Parts
   return by_type(g.d, f16, [&](auto d, auto type) {
     constexpr int D = decltype(d)::value;
     constexpr bool F16 = decltype(type)::value;
-    // By the parts alone, not by the rows: the order of a row's sums must not depend on the others.  A warp takes what it asks for at once,
-    // or twice that.  (us on the device, one and two warps for 9 to 16 parts: 1024 rows 108.8 and 106.7 a call; behind a prefix, where rows
-    // are many, 4096 rows 104.5 and 106.9.)
-    if (most_parts <= 8 || (parts.shared && most_parts <= 16)) return launch_join<D, F16, 1>(c, g, parts, o, lse);
-    if (most_parts <= 16) return launch_join<D, F16, 2>(c, g, parts, o, lse);
+    if (most_parts <= 8) return launch_join<D, F16, 1>(c, g, parts, o, lse);
+    if (most_parts <= 16) return parts.shared ? launch_join<D, F16, 1, true>(c, g, parts, o, lse) : launch_join<D, F16, 2>(c, g, parts, o, lse);
     return most_parts <= 64 ? launch_join<D, F16, 4>(c, g, parts, o, lse) : launch_join<D, F16, 8>(c, g, parts, o, lse);
   });
 }
