@@ -370,9 +370,9 @@ int mosaic_bsa_window_decode(const mosaic_window_params *p, const mosaic_view *q
  * ---------------------------------------------------------------------------------------------------------
  * A paged cache of keys and values, and attention over it: what a server of many sequences keeps, whose lengths it does not know.
  *
- * The cache is two pools [pages, Hkv, page, d] (views: either order of heads and slots in memory, and slices) and a table [B, width]
- * of page numbers, int32 on the device, rows table_stride entries apart: token j of member b lies in slot j % page of page
- * table[b][j / page].
+ * The cache is two pools [pages, Hkv, page, d] (views: any order of pages, heads and slots in memory, and slices; MOSAIC_E_UNSUPPORTED
+ * where rows overlap) and a table [B, width] of page numbers, int32 on the device, rows table_stride entries apart: token j of
+ * member b lies in slot j % page of page table[b][j / page].
  *   - An entry outside [0, pages) is a page that is not there: nothing is written to it, its keys are seen by no row.  So any table
  *     is safe, and entries that no token needs may hold anything; -1 is customary.
  *   - A page may stand in the tables of several members, and more than once in one.  Pages that a call writes must be one member's,

@@ -1,6 +1,8 @@
 // C ABI of the paged cache: argument checks, workspace, launches.
 #include <math.h>
 
+#include <utility>
+
 #include "paged.cuh"
 
 namespace mosaic {
@@ -89,10 +91,21 @@ bool is_direct(const mosaic_paged_params* p, int shared) {
 
 }  // namespace
 
+// Every row has a place of its own: from the smallest stride on, each reaches beyond all that lies within it.  (Any order of the axes, and
+// slices of them; only rows that interleave without being a slice of anything are refused beside those that overlap.)
 int check_pool(const mosaic_view* v, const mosaic_paged_params* p, View* out) {
   if (const int rc = check_view(v, p->pages, p->Hkv, p->page, 2, out)) return rc;
-  // (a place of its own for every row)
-  return out->sn == 0 || (p->Hkv > 1 && out->sh == 0) || (p->pages > 1 && out->sb == 0) ? MOSAIC_E_UNSUPPORTED : MOSAIC_OK;
+  struct { long long stride; int n; } axis[3] = {{out->sn, p->page}, {out->sh, p->Hkv}, {out->sb, p->pages}};
+  if (axis[0].stride > axis[1].stride) std::swap(axis[0], axis[1]);
+  if (axis[1].stride > axis[2].stride) std::swap(axis[1], axis[2]);
+  if (axis[0].stride > axis[1].stride) std::swap(axis[0], axis[1]);
+  long long within = 2ll * p->d;  // bytes from the first to behind the last of what the strides so far reach
+  for (const auto& x : axis) {
+    if (x.n == 1) continue;
+    if (x.stride < within || x.stride > (1ll << 61) / x.n) return MOSAIC_E_UNSUPPORTED;
+    within += (x.n - 1) * x.stride;
+  }
+  return MOSAIC_OK;
 }
 
 namespace {
