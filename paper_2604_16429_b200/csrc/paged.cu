@@ -41,6 +41,14 @@ int make_geo(const mosaic_paged_params* p, const int32_t* table, const int32_t* 
   return aligned(table, 4) && aligned(k_len, 4) && aligned(q_len, 4) ? MOSAIC_OK : MOSAIC_E_MISALIGNED;
 }
 
+// Most parts that a member's own keys can have: all chunks of its pages, or those that a window and its first rows' ends touch
+int most_parts(const mosaic_paged_params* p) {
+  const long long all = ((long long)p->width * p->page + kChunkKeys - 1) / kChunkKeys;
+  if (!p->window) return (int)all;
+  const long long some = ((long long)p->window + p->Nq - 2 + kChunkKeys - 1) / kChunkKeys + 1 + (p->sinks > 0);
+  return (int)(some < all ? some : all);
+}
+
 // The attention's own
 int check_attention(const mosaic_paged_params* p) {
   if (const int rc = check(p, MOSAIC_FLAG_FP16)) return rc;
@@ -48,15 +56,8 @@ int check_attention(const mosaic_paged_params* p) {
   if (!(p->scale == p->scale) || isinf(p->scale)) return MOSAIC_E_INVALID_ARG;
   if (p->Nq > kMaxNew || p->sinks > kMaxSinks || (long long)p->B * p->H > (1 << 24)) return MOSAIC_E_UNSUPPORTED;
   if ((long long)p->H / p->Hkv * p->Nq > (1 << 20)) return MOSAIC_E_UNSUPPORTED;
+  if (!paged_parts_fit(p->d, p->H / p->Hkv * p->Nq, (long long)p->B * p->Hkv, most_parts(p))) return MOSAIC_E_UNSUPPORTED;
   return MOSAIC_OK;
-}
-
-// Most parts that a member's own keys can have: all chunks of its pages, or those that a window and its first rows' ends touch
-int most_parts(const mosaic_paged_params* p) {
-  const long long all = ((long long)p->width * p->page + kChunkKeys - 1) / kChunkKeys;
-  if (!p->window) return (int)all;
-  const long long some = ((long long)p->window + p->Nq - 2 + kChunkKeys - 1) / kChunkKeys + 1 + (p->sinks > 0);
-  return (int)(some < all ? some : all);
 }
 
 // Behind the status block the parts: sums [part][row][d], then maximum and sum of weights [part][row]

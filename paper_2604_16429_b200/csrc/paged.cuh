@@ -105,6 +105,8 @@ struct PoolMaps {
 
 // Blocks that the rows of a key/value head are taken in
 int paged_row_blocks(int d, int rows);
+// Whether the list of all items can be counted: `units` key/value heads of all members, `rows` of each, in `most_parts` parts
+bool paged_parts_fit(int d, int rows, long long units, int most_parts);
 // Attention over the members' own pages: parts to the workspace, or, where a member can have but one, results (`direct`), joined with the
 // prefix' parts if there are any.  `first`: the call's first kernel, which clears the status word; otherwise it follows the prefix' kernel.
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,

@@ -10,7 +10,7 @@
 // Measured (us; two prompts of 8192 tokens, 16 + 4 heads of 128, bf16, pages of 64): 35.4, 5.7 TB/s, 88 % of the copy rate (34.0 where nothing
 // turns); the rest is the start and end of the kernel and of its waves of CTAs.  Rows asked for behind the lengths and the page 37.1; batches
 // ahead and CTAs an SM 4 and 3: 36.4, 4 and 2: 40.5, 6 and 2: 38.8, 2 and 4: 35.4.  64 single tokens: 4.2 on the device.
-// Eight prompts padded to 8192 tokens, with q_len: 121.6 if all are full, 68.7 if they have 512 to 8192 (36 % of the tokens; 44 without the
+// Eight prompts padded to 8192 tokens, with q_len: 121.6 if all are full, 68.7 if they have 512 to 8192 (34 % of the tokens; 42 without the
 // padding); with the lengths read ahead of the rows, 139.3 and 62.0, and two at 75 % on average 32.2 instead of 29.4.  The lines cross where
 // about half the tokens are padding, so the rows come first.
 #include "paged.cuh"

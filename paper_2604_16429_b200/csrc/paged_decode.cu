@@ -753,8 +753,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
 // longer, as one step takes from its keys to the end of the join: 3400 for one tile of 8 rows, 5300 for three, which is a whole chunk's
 // time at D = 64, so that all items are alike there.  (us on the device with 2, and alike: 5 new tokens of 32 members, 12 heads on 3 of 64, 30.5
 // and 26.8; 33 members with 4 behind a prefix 28.4 and 24.7.)
-template <int D, int NT>
-constexpr int kTurn = D == 128 ? 2 : NT == 1 ? 4 : 0;
+constexpr int turn_of(int d, int tiles) { return d == 128 ? 2 : tiles == 1 ? 4 : 0; }
 
 template <int D, bool F16, int NT>
 int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps& maps, int most_parts) {
@@ -765,8 +764,7 @@ int launch_parts(const HostCtx& c, const PagedGeo& g, DecArgs a, const PoolMaps&
   if (const int rc = launch_setup(reinterpret_cast<const void*>(paged_parts_kernel<D, F16, NT>), smem, &configured, &sms)) return rc;
   a.blocks = paged_row_blocks(D, g.G * g.T);
   const long long most = (long long)g.B * g.Hkv * a.blocks * most_parts;
-  a.turn = kTurn<D, NT>;
-  if (most * (kSteps + a.turn) > 0x7fffffffll) return MOSAIC_E_UNSUPPORTED;
+  a.turn = turn_of(D, NT);
   return launch_kernel(paged_parts_kernel<D, F16, NT>, dim3((unsigned)(most < sms ? most : sms)), Smem<D, NT>::kThreads, smem, c.stream, true, 0, g, a, maps.k, maps.v);
 }
 
@@ -792,6 +790,10 @@ int by_type(int d, bool f16, F&& f) {
 int paged_row_blocks(int d, int rows) {
   const int block = 8 * tiles_of(d, rows);
   return (rows + block - 1) / block;
+}
+
+bool paged_parts_fit(int d, int rows, long long units, int most_parts) {
+  return units * paged_row_blocks(d, rows) * most_parts <= 0x7fffffffll / (kSteps + turn_of(d, tiles_of(d, rows)));
 }
 
 int launch_paged_parts(const HostCtx& c, const PagedGeo& g, bool f16, const View& q, const PoolMaps& maps, const PartsOut& parts,
