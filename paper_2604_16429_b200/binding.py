@@ -750,7 +750,7 @@ def mosaic_bsa_paged_append(rp: RotaryParams, k, v, k_pages, v_pages, table, k_l
     """New tokens k, v [B,Hkv,N,d] to their places in the pools [pages, Hkv, page, d]: token i of member b to position
     j = k_len[b] - q_len[b] + i (q_len None: N for all), slot j % page of page table[b, j // page].  Keys turn to position
     start + j on the way (`freqs` from `rotary_freqs`; rp.rot_dim 0: they stay), and so do the new tokens' queries q [B,H,N,d], if
-    given.  Returns the turned queries, or None."""
+    given.  Returns the turned queries, or None.  Rows from q_len[b] on are not written: without `q_out` they hold anything."""
     index = _chk_seq(k, k if q is None else q)
     t, sk = k.dtype, k.shape
     if t is torch.float32:
@@ -846,14 +846,16 @@ def _paged_ws(at, index, ws, stream):
 
 def mosaic_bsa_paged_decode(pp: PagedParams, q, k_pages, v_pages, table, k_len, q_len=None, o=None, lse=None, ws=None, stream=None):
     """Attention of new tokens q [B,H,Nq,d], Nq at most 16, over their members' pages: a member's q_len[b] new tokens (None: Nq for
-    all) are the last of the k_len[b] that its pages hold.  Returns (o, lse)."""
+    all) are the last of the k_len[b] that its pages hold.  Returns (o, lse); rows from q_len[b] on are not written, and hold anything
+    where the call made the tensor."""
     return _paged_attention("mosaic_bsa_paged_decode", pp, q, k_pages, v_pages, None, table, k_len, q_len, o, lse, ws, stream)
 
 
 def mosaic_bsa_prefix_decode(pp: PagedParams, q, k_pages, v_pages, prefix_table, prefix_len, table, k_len, q_len=None, o=None, lse=None,
                              ws=None, stream=None):
     """mosaic_bsa_paged_decode for a batch whose members all begin with the first `prefix_len` tokens of the pages that prefix_table
-    [>= prefix_len / page] int32 names; table, k_len and q_len count the members' own tokens.  No window.  Returns (o, lse)."""
+    [>= prefix_len / page] int32 names; table, k_len and q_len count the members' own tokens.  No window.  Returns (o, lse), with rows
+    from q_len[b] on as there."""
     if prefix_len <= 0:
         raise ValueError(f"prefix_len: expected at least one token, got {prefix_len}")
     return _paged_attention("mosaic_bsa_prefix_decode", pp, q, k_pages, v_pages, (prefix_table, prefix_len), table, k_len, q_len, o, lse, ws,
