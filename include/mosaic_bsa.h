@@ -413,7 +413,8 @@ int mosaic_bsa_paged_append(const mosaic_paged_params *p, const mosaic_view *k, 
  *   that see it, and may spread to the member's other rows).
  *   ws: mosaic_bsa_paged_workspace_bytes(p) bytes (0 on invalid params), 256-byte aligned, the status block first.  It grows with
  *   B * H * Nq times the chunks of 512 keys that a member can have: those of its table row, or of its window.
- *   (MOSAIC_E_UNSUPPORTED where B * Hkv * chunks times Nq * H / Hkv in blocks of 16 reach 2^31 / 12.) */
+ *   (MOSAIC_E_UNSUPPORTED, and no workspace, where B * Hkv * chunks times Nq * H / Hkv in blocks of 16 reach 2^31 / 12.)
+ *   A member's bits depend neither on the other members nor on the table's width. */
 size_t mosaic_bsa_paged_workspace_bytes(const mosaic_paged_params *p);
 int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
                             const int32_t *table, const int32_t *k_len, const int32_t *q_len, const mosaic_view *o, float *lse, void *ws,
@@ -424,8 +425,9 @@ int mosaic_bsa_paged_decode(const mosaic_paged_params *p, const mosaic_view *q, 
  * member's own keys as above (window 0); table, k_len and q_len count the member's own tokens alone, and k_len may be 0.  The prefix is
  * read once for the whole batch.
  *   ws as above (p with prefix_len): B * H * Nq times the parts of the prefix more, of which there are at most 2 * 148 / Hkv + 1.
- *   How the prefix is cut into parts follows from its length, Hkv and B * Nq * H / Hkv, so a member's bits depend on the shape of the
- *   call, but on nothing that another member holds, nor on its place. */
+ *   How the prefix is cut into parts follows from its length, Hkv and B * Nq * H / Hkv, and a member's own keys are joined in another
+ *   order where the tables have room for 512 tokens at most; so a member's bits depend on the shape of the call, but on nothing that
+ *   another member holds, nor on its place. */
 int mosaic_bsa_prefix_decode(const mosaic_paged_params *p, const mosaic_view *q, const mosaic_view *k_pages, const mosaic_view *v_pages,
                              const int32_t *prefix_table, const int32_t *table, const int32_t *k_len, const int32_t *q_len,
                              const mosaic_view *o, float *lse, void *ws, size_t ws_bytes, void *cuda_stream);

@@ -4,7 +4,7 @@
 
 namespace mosaic {
 
-constexpr int kMinPage = 16;    // slots of a page at least: a step of the attention never leaves one
+constexpr int kMinPage = 16;    // slots of a page at least: 16 keys, the rows of one product, never leave one
 constexpr int kMaxPage = 1 << 20;
 constexpr int kMaxNew = 16;     // new tokens a sequence that the attention takes
 constexpr int kChunkKeys = 512; // keys whose attention is one part, joined with the others at the end
@@ -34,7 +34,8 @@ __device__ __forceinline__ Span span_of(const PagedGeo& g, int b) {
 }
 
 // The keys that member b's rows see, cut into parts: the chunks of kChunkKeys positions that hold some of them.  So what a part is
-// follows from positions alone, and a row's bits do not depend on what else is in the call.
+// follows from positions alone, and a row's bits depend neither on what else is in the call nor on its table's width (the join keeps to
+// that).
 struct Parts {
   int kl, ql, p0;   // tokens, new ones, position of the first row
   int from, sinks;  // the rows see keys of [0, sinks) and of [from, kl) only
@@ -79,7 +80,6 @@ struct AppendTensors {
   View q, q_out, k, v, k_pages, v_pages;
 };
 int launch_paged_append(const HostCtx& c, const PagedGeo& g, const mosaic_paged_params* p, const double* freqs, const AppendTensors& t);
-
 
 // A map of a pool in boxes of `rows` slots by `parts` times 64 channels, and the copy of one from 64 * part on
 bool make_map_pool(CUtensorMap* map, const View& v, int d, int page, int heads, int pages, int rows, int parts);

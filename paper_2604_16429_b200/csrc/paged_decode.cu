@@ -1,8 +1,8 @@
 // Attention of one or a few new tokens per sequence over a paged cache, and the join of its parts.
 //
 //   o_i = sum_j exp(scale q_i . k_j - m_i) v_j / l_i  over the keys that row i sees: j <= p_i, and p_i - j < window or j < sinks
-// HBM-bound: the visible keys and values of a key/value head are read once for all rows (new tokens x query heads of the group, a
-// block of them at a time).  The keys of a member are cut into chunks of 512; a chunk of a head is an item.  Persistent CTAs, one an SM,
+// HBM-bound: the visible keys and values of a key/value head are read once for each block of its rows (new tokens x query heads of the
+// group; up to 16 at D = 128 and 32 at 64 are one block), by further blocks from the L2.  The keys of a member are cut into chunks of 512; a chunk of a head is an item.  Persistent CTAs, one an SM,
 // take equal shares of the list of all items, which each works out from the lengths.
 //
 // One warp finds the items, and for each leaves a note of what the others need to know of it, with the numbers of its pages, and copies its
@@ -15,8 +15,8 @@
 // part; a second kernel joins a row's parts in their order.  Members that can have one part only get their results at once, joined with
 // the prefix' parts if there is a prefix.
 //
-// Measured (us on the device, 4 key/value heads of 128 unless given): 64 members of up to 8192 tokens, 16 heads, pages of 64, 106.7, and 8
-// of 65536, 32 heads, 189; in the steady state a chunk (262 KB) takes an SM 10100 cycles, 7.4 TB/s in all.  One member of 16384, 12.6:
+// Measured (us on the device, 4 key/value heads of 128 unless given): 64 members of up to 8192 tokens, 16 heads, pages of 64, 106.8, and 8
+// of 65536, 32 heads, 188; in the steady state a chunk (262 KB) takes an SM 10100 cycles, 7.4 TB/s in all.  One member of 16384, 12.6:
 // 5000 cycles until the first copies are asked for, 600 a step, 2000 for the last step and the join, 4000 the second kernel.  5 new tokens of
 // 32 members, 12 heads on 3 of 64, window 2048: 27.
 // Tried on the last of these, with what it took then and what it takes without: rings and steps of 16 keys for every warp 63 (44), all
